@@ -67,7 +67,10 @@ typedef enum { ADADIM_DIM_OC = 0, ADADIM_DIM_IC = 1, ADADIM_DIM_BOTH = 2, ADADIM
  * total number of working rows of a batched call (sum over its layers of out, twice for a layer
  * quantized in both dimensions). */
 typedef enum { ADADIM_WS_HESSIAN = 0, ADADIM_WS_GPTQ = 1, ADADIM_WS_SCORE = 2,
-               ADADIM_WS_FACTOR = 3, ADADIM_WS_GPTQ_ROWS = 4, ADADIM_WS_GEMV = 5 } adadim_ws_kind;
+               ADADIM_WS_FACTOR = 3, ADADIM_WS_GPTQ_ROWS = 4, ADADIM_WS_GEMV = 5,
+               ADADIM_WS_FP4 = 6 } adadim_ws_kind;
+/* 4-bit floating-point formats, see adadim_quantize_fp4. */
+typedef enum { ADADIM_MXFP4 = 0, ADADIM_NVFP4 = 1 } adadim_fp4_format;
 
 /*
  * One quantized tensor (device pointers, caller-owned).
@@ -298,6 +301,108 @@ ADADIM_API size_t adadim_static_scratch_bytes(void);
  */
 ADADIM_API int adadim_dequant_gemv(const adadim_qtensor* q, int dim, int64_t out, int64_t in, int bits, int group,
                         const void* x, void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * ---- microscaled 4-bit floating point ---------------------------------------------------------
+ * A matrix [rows][cols] held as E2M1 codes (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign) with one 8-bit
+ * scale for every block of B consecutive columns of a row:
+ *   ADADIM_MXFP4  B = 32, scale E8M0 (a power of two)
+ *   ADADIM_NVFP4  B = 16, scale E4M3 (unsigned), times one power of two t for the whole matrix
+ * the two forms that the tensor cores multiply directly.
+ *   codes   [rows][ld] bytes, two codes per byte, the even column in the low half.  16-byte
+ *           aligned, ld a multiple of 16 and >= (cols + 1) / 2; bytes from there up to
+ *           round_up((cols + 1) / 2, 8) are written as zeros, further bytes of a row are not used.
+ *   scales  tiles of 128 rows x 4 blocks, 512 bytes each: the byte of row r, block b is at
+ *               ((r / 128) * n4 + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,
+ *           n4 = ceil(cols / (4 B)).  adadim_fp4_scale_bytes() says how many; 128-byte aligned.
+ *           Scales of rows and columns beyond the matrix are written as 0 inside its tiles.
+ *   amax    NVFP4: device float with the largest magnitude the matrix is expected to hold (see
+ *           adadim_absmax), or NULL; it fixes t = 2^max(ceil(log2(amax / 2688)), -100) (2688 = 6 * 448,
+ *           the largest E2M1 times the largest E4M3).  NULL, zero, infinite or NaN: t = 1.
+ *           A power of two costs no precision (E4M3 carries its own exponent) and keeps every
+ *           decision below exact.  MXFP4: not used.
+ * Rows in groups (experts): rows offsets[e] .. offsets[e+1]-1 of the matrix belong to group e, and
+ * every group starts a scale tile of its own, so that a group's scales can be loaded as whole
+ * tiles wherever it begins: the scale tiles of group e start at tile row offsets[e] / 128 + e.
+ */
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  const float* amax;
+  int64_t ld;
+} adadim_fp4tensor;
+
+/* Bytes of `scales` for a matrix (n_groups = 0) or for rows in n_groups groups; 0 for bad arguments. */
+ADADIM_API size_t adadim_fp4_scale_bytes(int format, int64_t rows, int64_t cols, int n_groups);
+
+/*
+ * *amax = max(*amax, max |X|): the caller sets it to 0 once and may pass several chunks.
+ * xdtype any; ldx in elements; no alignment beyond the element's.  A NaN in X makes *amax NaN.
+ */
+ADADIM_API int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax,
+                        void* cuda_stream);
+
+/*
+ * Quantizer.  Per block, with m = max |x|; every decision is that of exact arithmetic, ties go to
+ * the even code:
+ *   MXFP4  scale = 2^(floor(log2 m) - 2), at least 2^-127;  element = nearest level to x / scale,
+ *          at most 6
+ *   NVFP4  s = nearest E4M3 to m / (6 t), at most 448;  element = nearest level to x / (s t), at
+ *          most 6; zero where s is 0.  The sign bit is that of x in every code, zeros included
+ *   A block that holds an infinity or a NaN gets a NaN scale (0xFF / 0x7F) and codes 0: its
+ *   values, and every product with it, are NaN.
+ *   X          [x_rows][cols], xdtype any, ldx in elements.  16-byte aligned rows take the wide
+ *              loads; any element-aligned X is accepted.
+ *   row_index  optional device int32[rows]: row r is taken from X[row_index[r]]; an index outside
+ *              0 .. x_rows-1 gives a row of zeros.  NULL: row r is X[r], x_rows >= rows.
+ *   offsets    optional device int32[n_groups + 1] (n_groups 1 .. 1024), not falling, within
+ *              0 .. rows: the groups described above.  Rows outside offsets[0] .. offsets[n_groups]-1
+ *              are not written.  NULL: n_groups must be 0.
+ *   values     optional: the quantized values, [rows][cols], vdtype ADADIM_BF16 or ADADIM_F32, ldv in
+ *              elements.  Both types hold them exactly (up to their own range).
+ */
+ADADIM_API int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows,
+                        int format, const int32_t* row_index, const int32_t* offsets, int n_groups,
+                        const adadim_fp4tensor* q, void* values, int vdtype, int64_t ldv, void* cuda_stream);
+
+/*
+ * Y = A B^T of two 4-bit matrices of one format: A [n_tokens][in] (activations), B [out][in] (a weight),
+ * Y [n_tokens][out], ydtype any, ldy in elements, element-aligned.  Products are exact, sums binary32
+ * in the tensor cores' accumulators, one rounding to ydtype at the end.
+ * Any sizes with 1 <= in <= 2^20; n_tokens and out up to 2^22, n_experts * out below 2^31.
+ */
+ADADIM_API int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,
+                        int format, void* Y, int ydtype, int64_t ldy, int* status_dev, void* cuda_stream);
+
+/*
+ * The same product for rows sorted by expert: row r of group e (offsets as in adadim_quantize_fp4,
+ * with which A was quantized; read on the device) is multiplied by expert e's weight.  B holds the
+ * experts one after the other: codes [n_experts][out][ld], scales n_experts times
+ * adadim_fp4_scale_bytes(format, out, in, 0) bytes.  Rows of no group are not written.  Offsets that
+ * fall or leave 0 .. n_rows are reported as ADADIM_ERR_SHAPE in status_dev (and clamped).
+ */
+ADADIM_API int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const int32_t* offsets, int n_experts,
+                        const adadim_fp4tensor* B, int64_t out, int64_t in, int format,
+                        void* Y, int ydtype, int64_t ldy, int* status_dev, void* cuda_stream);
+
+/*
+ * Linear layer with 4-bit weights and activations in the model's own type: X is quantized as by
+ * adadim_quantize_fp4 (x_amax: its amax) and multiplied as by adadim_fp4_matmul.
+ *   workspace  adadim_workspace_bytes(ADADIM_WS_FP4, n_tokens, in, 4, 0) bytes, 256-byte aligned.
+ */
+ADADIM_API int adadim_fp4_linear(const void* X, int xdtype, int64_t n_tokens, int64_t in, int64_t ldx, const float* x_amax,
+                        const adadim_fp4tensor* B, int64_t out, int format, void* Y, int ydtype, int64_t ldy,
+                        int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The same for expert layers: row r of Y belongs to the token row_index[r] of X [x_rows][in] (NULL: to
+ * X[r]) and to the expert whose range offsets gives it.
+ *   workspace  adadim_workspace_bytes(ADADIM_WS_FP4, n_rows, in, 4, n_experts) bytes, 256-byte aligned.
+ */
+ADADIM_API int adadim_fp4_linear_grouped(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ldx,
+                        const float* x_amax, const int32_t* row_index, const int32_t* offsets, int n_experts, int64_t n_rows,
+                        const adadim_fp4tensor* B, int64_t out, int format, void* Y, int ydtype, int64_t ldy,
+                        int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Helpers. */
 ADADIM_API size_t adadim_workspace_bytes(int kind, int64_t out, int64_t in, int bits, int group);

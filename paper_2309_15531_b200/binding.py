@@ -17,7 +17,8 @@ import torch
 OK = 0
 F32, F16, BF16 = 0, 1, 2
 DIM_OC, DIM_IC, DIM_BOTH, DIM_CHOSEN = 0, 1, 2, 3
-WS_HESSIAN, WS_GPTQ, WS_SCORE, WS_FACTOR, WS_GPTQ_ROWS, WS_GEMV = 0, 1, 2, 3, 4, 5
+WS_HESSIAN, WS_GPTQ, WS_SCORE, WS_FACTOR, WS_GPTQ_ROWS, WS_GEMV, WS_FP4 = 0, 1, 2, 3, 4, 5, 6
+MXFP4, NVFP4 = 0, 1
 DIM_NAMES = {DIM_OC: "oc", DIM_IC: "ic"}
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libadadim.so")
@@ -32,6 +33,10 @@ class AdadimError(RuntimeError):
 
 class QTensorC(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p)]
+
+
+class Fp4TensorC(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("amax", C.c_void_p), ("ld", C.c_int64)]
 
 
 class GptqLayerC(C.Structure):
@@ -77,6 +82,22 @@ def lib():
         L.adadim_static_scratch_bytes.restype = sz
         L.adadim_dequant_gemv.restype = C.c_int
         L.adadim_dequant_gemv.argtypes = [qp, C.c_int, i64, i64, C.c_int, C.c_int, vp, vp, vp, sz, vp]
+        fp, ci = C.POINTER(Fp4TensorC), C.c_int
+        L.adadim_fp4_scale_bytes.restype = sz
+        L.adadim_fp4_scale_bytes.argtypes = [ci, i64, i64, ci]
+        L.adadim_absmax.restype = ci
+        L.adadim_absmax.argtypes = [vp, ci, i64, i64, i64, vp, vp]
+        L.adadim_quantize_fp4.restype = ci
+        L.adadim_quantize_fp4.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, ci, fp, vp, ci, i64, vp]
+        L.adadim_fp4_matmul.restype = ci
+        L.adadim_fp4_matmul.argtypes = [fp, i64, fp, i64, i64, ci, vp, ci, i64, vp, vp]
+        L.adadim_fp4_matmul_grouped.restype = ci
+        L.adadim_fp4_matmul_grouped.argtypes = [fp, i64, vp, ci, fp, i64, i64, ci, vp, ci, i64, vp, vp]
+        L.adadim_fp4_linear.restype = ci
+        L.adadim_fp4_linear.argtypes = [vp, ci, i64, i64, i64, vp, fp, i64, ci, vp, ci, i64, vp, vp, sz, vp]
+        L.adadim_fp4_linear_grouped.restype = ci
+        L.adadim_fp4_linear_grouped.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, ci, i64, fp, i64, ci, vp, ci, i64,
+                                                vp, vp, sz, vp]
         L.adadim_unpack_codes.restype = C.c_int
         L.adadim_unpack_codes.argtypes = [vp, i64, i64, C.c_int, vp, vp]
         _lib = L
@@ -312,6 +333,171 @@ def dequant_gemv(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
     rc = lib().adadim_dequant_gemv(C.byref(qc), DIM_IC, out, inp, bits, group, x.data_ptr(), y.data_ptr(),
                                    workspace.data_ptr(), workspace.numel(), _stream())
     _check(rc, "adadim_dequant_gemv")
+    return y
+
+
+class Fp4Tensor:
+    """Device buffers of a matrix in microscaled 4-bit floating point (see include/adadim.h for the layout).
+    `groups` > 0: the rows are in that many groups given by an offsets tensor (activations sorted by
+    expert).  `experts` > 0: a stack of that many [rows, cols] weights; expert(e) is a view of one."""
+
+    def __init__(self, rows: int, cols: int, fmt: int, groups: int = 0, experts: int = 0, device="cuda"):
+        if rows < 0 or cols < 0 or fmt not in (MXFP4, NVFP4) or groups < 0 or experts < 0 or (groups and experts):
+            raise ValueError("Fp4Tensor: bad sizes or format")
+        self.rows, self.cols, self.fmt, self.groups, self.experts = rows, cols, fmt, groups, experts
+        n = max(experts, 1)
+        self.scale_bytes = int(lib().adadim_fp4_scale_bytes(fmt, rows, cols, groups))
+        ld = ((cols + 1) // 2 + 15) // 16 * 16
+        self.codes = torch.zeros(n * rows, ld, dtype=torch.uint8, device=device)
+        self.scales = torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device)
+        self.amax: Optional[torch.Tensor] = None
+        self._c = None
+
+    def expert(self, e: int) -> "Fp4Tensor":
+        if not 0 <= e < self.experts:
+            raise IndexError(e)
+        one = object.__new__(Fp4Tensor)
+        one.rows, one.cols, one.fmt, one.groups, one.experts = self.rows, self.cols, self.fmt, 0, 0
+        one.scale_bytes = self.scale_bytes
+        one.codes = self.codes[e * self.rows:(e + 1) * self.rows]
+        one.scales = self.scales[e * self.scale_bytes:(e + 1) * self.scale_bytes]
+        one._parent = self
+        one.amax, one._c = self.amax, None
+        return one
+
+    def set_amax(self, amax: Optional[torch.Tensor]) -> None:
+        if amax is not None:
+            assert amax.is_cuda and amax.dtype == torch.float32 and amax.numel() == 1
+        self.amax, self._c = amax, None
+        parent = getattr(self, "_parent", None)          # the experts of a stack share one amax
+        if parent is not None:
+            assert parent.amax is None or amax is None or parent.amax.data_ptr() == amax.data_ptr()
+            parent.set_amax(amax)
+
+    def c(self) -> Fp4TensorC:
+        if self._c is None:
+            self._c = Fp4TensorC(self.codes.data_ptr(), self.scales.data_ptr(),
+                                 self.amax.data_ptr() if self.amax is not None else None, self.codes.stride(0))
+        return self._c
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return t.data_ptr() if t is not None else None
+
+
+def _i32(t: torch.Tensor) -> torch.Tensor:
+    assert t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+    return t
+
+
+def _rows_of(X: torch.Tensor) -> torch.Tensor:
+    assert X.is_cuda and X.dim() == 2 and (X.shape[1] <= 1 or X.stride(1) == 1)
+    return X
+
+
+def _ld(X: torch.Tensor) -> int:
+    return X.stride(0) if X.shape[0] > 1 else max(X.stride(0), X.shape[1])
+
+
+def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """float32[1] = max(amax, max |X|); pass the same tensor for several chunks."""
+    _rows_of(X)
+    if amax is None:
+        amax = torch.zeros(1, dtype=torch.float32, device=X.device)
+    assert amax.dtype == torch.float32 and amax.is_cuda
+    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), amax.data_ptr(), _stream()),
+           "adadim_absmax")
+    return amax
+
+
+def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None, q: Optional[Fp4Tensor] = None,
+                 values: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
+                 offsets: Optional[torch.Tensor] = None) -> Fp4Tensor:
+    """Quantize X[rows, cols] (fp32, fp16 or bf16) to MXFP4 or NVFP4.  amax: float32[1], NVFP4's tensor scale is
+    taken from it (None: 1) and it is remembered in the result.  values (bf16 or fp32 [rows, cols]): receives the
+    quantized values.  row_index int32[rows]: take row r from X[row_index[r]].  offsets int32[n + 1]: the rows are in
+    n groups (see Fp4Tensor)."""
+    _rows_of(X)
+    cols = X.shape[1]
+    rows = X.shape[0] if row_index is None else _i32(row_index).numel()
+    groups = _i32(offsets).numel() - 1 if offsets is not None else 0
+    if q is None:
+        q = Fp4Tensor(rows, cols, fmt, groups=groups, device=X.device)
+    if (q.rows, q.cols, q.fmt, q.groups, q.experts) != (rows, cols, fmt, groups, 0):
+        raise ValueError("quantize_fp4: q was made for another shape or format")
+    q.set_amax(amax)
+    if values is not None:
+        _rows_of(values)
+        assert values.shape == (rows, cols)
+    _check(lib().adadim_quantize_fp4(X.data_ptr(), _DT[X.dtype], rows, cols, _ld(X), X.shape[0], fmt, _ptr(row_index),
+                                     _ptr(offsets), groups, C.byref(q.c()), _ptr(values),
+                                     _DT[values.dtype] if values is not None else BF16,
+                                     _ld(values) if values is not None else 0, _stream()), "adadim_quantize_fp4")
+    return q
+
+
+def _product_out(y, rows, out, dtype, device):
+    if y is None:
+        return torch.empty(rows, out, dtype=dtype, device=device)
+    _rows_of(y)
+    assert y.shape == (rows, out)
+    return y
+
+
+def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = Q(X) W^T for activations X[n_tokens, in] (fp32, fp16, bf16; quantized in the call with x_amax) or for an
+    Fp4Tensor X that is quantized already (y is bf16 then unless given).  y has X's type unless given."""
+    if W.experts:
+        raise ValueError("fp4_linear: W is a stack of experts")
+    if isinstance(X, Fp4Tensor):
+        if X.fmt != W.fmt or X.cols != W.cols or X.groups or X.experts:
+            raise ValueError("fp4_linear: X and W do not match")
+        y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
+        _check(lib().adadim_fp4_matmul(C.byref(X.c()), X.rows, C.byref(W.c()), W.rows, W.cols, W.fmt, y.data_ptr(),
+                                       _DT[y.dtype], _ld(y), _ptr(status), _stream()), "adadim_fp4_matmul")
+        return y
+    _rows_of(X)
+    rows, inp = X.shape
+    if inp != W.cols:
+        raise ValueError("fp4_linear: X and W do not match")
+    y = _product_out(y, rows, W.rows, X.dtype, X.device)
+    if workspace is None:
+        workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
+    _check(lib().adadim_fp4_linear(X.data_ptr(), _DT[X.dtype], rows, inp, _ld(X), _ptr(x_amax), C.byref(W.c()), W.rows,
+                                   W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
+                                   workspace.numel(), _stream()), "adadim_fp4_linear")
+    return y
+
+
+def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Optional[torch.Tensor] = None,
+                       x_amax: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The product for rows sorted by expert: rows offsets[e] .. offsets[e+1]-1 (int32 on the device) are
+    multiplied by expert e of the stack W.  Row r is X[row_index[r]] (None: X[r]); X may be an Fp4Tensor with
+    groups.  Rows of no expert are not written."""
+    n = _i32(offsets).numel() - 1
+    if W.experts != n or n < 1:
+        raise ValueError("fp4_linear_grouped: offsets do not match the stack of experts")
+    if isinstance(X, Fp4Tensor):
+        if X.fmt != W.fmt or X.cols != W.cols or X.groups != n or row_index is not None:
+            raise ValueError("fp4_linear_grouped: X and W do not match")
+        y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
+        _check(lib().adadim_fp4_matmul_grouped(C.byref(X.c()), X.rows, offsets.data_ptr(), n, C.byref(W.c()), W.rows,
+                                               W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status),
+                                               _stream()), "adadim_fp4_matmul_grouped")
+        return y
+    _rows_of(X)
+    rows, inp = X.shape[0] if row_index is None else _i32(row_index).numel(), X.shape[1]
+    if inp != W.cols:
+        raise ValueError("fp4_linear_grouped: X and W do not match")
+    y = _product_out(y, rows, W.rows, X.dtype, X.device)
+    if workspace is None:
+        workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, n), X.device)
+    _check(lib().adadim_fp4_linear_grouped(X.data_ptr(), _DT[X.dtype], X.shape[0], inp, _ld(X), _ptr(x_amax),
+                                           _ptr(row_index), offsets.data_ptr(), n, rows, C.byref(W.c()), W.rows, W.fmt,
+                                           y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
+                                           workspace.numel(), _stream()), "adadim_fp4_linear_grouped")
     return y
 
 

@@ -1,5 +1,6 @@
 // extern "C" entry points: argument validation on the host, then the kernel launchers.
 #include "common.cuh"
+#include "fp4.cuh"
 
 namespace adadim {
 int rtn_launch(const void* W, int wdtype, int64_t out, int64_t in, int64_t ldw, int bits, int group, int dim,
@@ -61,6 +62,91 @@ int check_qtensor(const adadim_qtensor* q) {
   return ADADIM_OK;
 }
 
+bool known_dtype(int dtype) { return dtype == ADADIM_F32 || dtype == ADADIM_F16 || dtype == ADADIM_BF16; }
+int64_t dtype_size(int dtype) { return dtype == ADADIM_F32 ? 4 : 2; }
+
+constexpr int64_t kFp4MaxIn = 1 << 20, kFp4MaxRows = 1 << 22;
+
+// A matrix of 16- or 32-bit elements: any row pitch, element-aligned.
+int check_matrix(const void* X, int dtype, int64_t cols, int64_t ld) {
+  if (!known_dtype(dtype)) return ADADIM_ERR_DTYPE;
+  if (ld < cols || ld > (int64_t{1} << 40)) return ADADIM_ERR_SHAPE;
+  if (X == nullptr) return ADADIM_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(X) % dtype_size(dtype) != 0) return ADADIM_ERR_ALIGN;
+  return ADADIM_OK;
+}
+int check_fp4(const adadim_fp4tensor* q, int64_t cols) {
+  if (q == nullptr || q->codes == nullptr || q->scales == nullptr) return ADADIM_ERR_NULL;
+  if (q->ld < (cols + 1) / 2 || q->ld > (int64_t{1} << 30)) return ADADIM_ERR_SHAPE;
+  if (!aligned16(q->codes) || q->ld % 16 != 0 || (reinterpret_cast<uintptr_t>(q->scales) & 127u) != 0) return ADADIM_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(q->amax) & 3u) != 0) return ADADIM_ERR_ALIGN;
+  return ADADIM_OK;
+}
+int check_fp4_shape(int format, int64_t rows, int64_t cols) {
+  if (format != ADADIM_MXFP4 && format != ADADIM_NVFP4) return ADADIM_ERR_PARAM;
+  if (rows < 0 || cols < 0 || rows > kFp4MaxRows || cols > kFp4MaxIn) return ADADIM_ERR_SHAPE;
+  return ADADIM_OK;
+}
+int check_groups(const int32_t* offsets, int n_groups) {
+  if (n_groups < 0 || n_groups > fp4::kMaxGroups) return ADADIM_ERR_PARAM;
+  if (n_groups == 0) return offsets == nullptr ? ADADIM_OK : ADADIM_ERR_PARAM;
+  if (offsets == nullptr) return ADADIM_ERR_NULL;
+  return (reinterpret_cast<uintptr_t>(offsets) & 3u) != 0 ? ADADIM_ERR_ALIGN : ADADIM_OK;
+}
+// The rules of a product's weight and result, shared by the four product entry points.  Returns
+// ADADIM_OK with *empty set where there is nothing to compute.
+int check_fp4_product(int64_t rows, int64_t out, int64_t in, int format, const int32_t* offsets, int n_experts,
+                      const adadim_fp4tensor* B, const void* Y, int ydtype, int64_t ldy, bool* empty) {
+  int rc = check_fp4_shape(format, rows, in);
+  if (rc != ADADIM_OK) return rc;
+  if (out < 0 || out > kFp4MaxRows) return ADADIM_ERR_SHAPE;
+  if ((rc = check_groups(offsets, n_experts)) != ADADIM_OK) return rc;
+  if (n_experts > 0 && out * n_experts > 0x7fffffff) return ADADIM_ERR_SHAPE;
+  *empty = rows == 0 || out == 0;
+  if (*empty) return ADADIM_OK;
+  if (in == 0) return ADADIM_ERR_SHAPE;
+  // tile numbers and scale rows are 32-bit in the kernel
+  const int64_t tiles = ((rows + 15) / 16 + n_experts) * ((out + 127) / 128);
+  const int64_t weights = n_experts > 0 ? n_experts : 1;
+  const int64_t sf_rows = weights * static_cast<int64_t>(fp4::scale_bytes(format, out, in, 0)) / 128;
+  const int64_t a_sf_rows = static_cast<int64_t>(fp4::scale_bytes(format, rows, in, n_experts)) / 128;
+  if (tiles > 0x7fffffff || sf_rows > 0x7fffffff || a_sf_rows > 0x7fffffff) return ADADIM_ERR_SHAPE;
+  if ((rc = check_fp4(B, in)) != ADADIM_OK) return rc;
+  return check_matrix(Y, ydtype, out, ldy);
+}
+
+// Workspace of the linear entry points: codes, then scale tiles, of the quantized activations.
+size_t fp4_code_bytes(int64_t rows, int64_t in) { return round_up(static_cast<size_t>(rows) * fp4::code_pitch(in), 256); }
+size_t fp4_workspace_bytes(int64_t rows, int64_t in, int n_groups) {
+  // the scales of the finer format; the coarser one needs less
+  return fp4_code_bytes(rows, in) + round_up(fp4::scale_bytes(ADADIM_NVFP4, rows, in, n_groups), 256);
+}
+int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ldx, const float* x_amax,
+               const int32_t* row_index, const int32_t* offsets, int n_experts, int64_t rows, const adadim_fp4tensor* B,
+               int64_t out, int format, void* Y, int ydtype, int64_t ldy, int* status_dev, void* workspace,
+               size_t workspace_bytes, cudaStream_t st) {
+  bool empty = false;
+  int rc = check_fp4_product(rows, out, in, format, offsets, n_experts, B, Y, ydtype, ldy, &empty);
+  if (rc != ADADIM_OK || empty) return rc;
+  if (x_rows < 0 || (row_index == nullptr && x_rows < rows)) return ADADIM_ERR_SHAPE;
+  if (row_index == nullptr || x_rows > 0) {
+    if ((rc = check_matrix(X, xdtype, in, ldx)) != ADADIM_OK) return rc;
+  }
+  if ((reinterpret_cast<uintptr_t>(row_index) & 3u) != 0 || (reinterpret_cast<uintptr_t>(x_amax) & 3u) != 0) return ADADIM_ERR_ALIGN;
+  if (workspace == nullptr) return ADADIM_ERR_NULL;
+  if (!aligned256(workspace)) return ADADIM_ERR_ALIGN;
+  if (workspace_bytes < fp4_workspace_bytes(rows, in, n_experts)) return ADADIM_ERR_WORKSPACE;
+  adadim_fp4tensor A;
+  A.codes = static_cast<uint8_t*>(workspace);
+  A.scales = A.codes + fp4_code_bytes(rows, in);
+  A.amax = x_amax;
+  A.ld = fp4::code_pitch(in);
+  rc = quantize_fp4_launch(X, xdtype, rows, in, ldx, x_rows, format, row_index, offsets, n_experts, A, nullptr,
+                           ADADIM_BF16, 0, st);
+  if (rc != ADADIM_OK) return rc;
+  return fp4_matmul_launch(A, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, st);
+}
+
 }  // namespace
 
 int check_score_args(const void* W, int wdtype, int64_t out, int64_t in, int64_t ldw, const float* H, int bits,
@@ -117,6 +203,7 @@ size_t adadim_workspace_bytes(int kind, int64_t out, int64_t in, int bits, int g
     case ADADIM_WS_GEMV: return group > 0 ? gemv_workspace_bytes(out, in, group) : 0;
     case ADADIM_WS_SCORE: return score_workspace_bytes(out, in);
     case ADADIM_WS_FACTOR: return factor_workspace_bytes(in);
+    case ADADIM_WS_FP4: return group >= 0 ? fp4_workspace_bytes(out, in, group) : 0;        // out = rows, group = experts
     default: return 0;
   }
 }
@@ -297,6 +384,77 @@ int adadim_dequant_gemv(const adadim_qtensor* q, int dim, int64_t out, int64_t i
   if (!aligned16(x) || !aligned256(workspace) || (reinterpret_cast<uintptr_t>(y) & 1u) != 0) return ADADIM_ERR_ALIGN;
   if (workspace_bytes < gemv_workspace_bytes(out, in, group)) return ADADIM_ERR_WORKSPACE;
   return gemv_launch(*q, out, in, bits, group, x, y, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t adadim_fp4_scale_bytes(int format, int64_t rows, int64_t cols, int n_groups) {
+  if (check_fp4_shape(format, rows, cols) != ADADIM_OK || n_groups < 0 || n_groups > fp4::kMaxGroups) return 0;
+  return fp4::scale_bytes(format, rows, cols, n_groups);
+}
+
+int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, void* cuda_stream) {
+  if (!known_dtype(xdtype)) return ADADIM_ERR_DTYPE;
+  if (rows < 0 || cols < 0 || rows > (int64_t{1} << 40) || cols > (int64_t{1} << 40)) return ADADIM_ERR_SHAPE;
+  if (rows == 0 || cols == 0) return ADADIM_OK;
+  const int rc = check_matrix(X, xdtype, cols, ldx);
+  if (rc != ADADIM_OK) return rc;
+  if (amax == nullptr) return ADADIM_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(amax) & 3u) != 0) return ADADIM_ERR_ALIGN;
+  return absmax_launch(X, xdtype, rows, cols, ldx, amax, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
+                        const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor* q,
+                        void* values, int vdtype, int64_t ldv, void* cuda_stream) {
+  int rc = check_fp4_shape(format, rows, cols);
+  if (rc != ADADIM_OK) return rc;
+  if (!known_dtype(xdtype) || (values != nullptr && vdtype != ADADIM_BF16 && vdtype != ADADIM_F32)) return ADADIM_ERR_DTYPE;
+  if ((rc = check_groups(offsets, n_groups)) != ADADIM_OK) return rc;
+  if (rows == 0 || cols == 0) return ADADIM_OK;
+  if (x_rows < 0 || (row_index == nullptr && x_rows < rows)) return ADADIM_ERR_SHAPE;
+  if (x_rows > 0 && (rc = check_matrix(X, xdtype, cols, ldx)) != ADADIM_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(row_index) & 3u) != 0) return ADADIM_ERR_ALIGN;
+  if ((rc = check_fp4(q, cols)) != ADADIM_OK) return rc;
+  if (values != nullptr && (rc = check_matrix(values, vdtype, cols, ldv)) != ADADIM_OK) return rc;
+  return quantize_fp4_launch(X, xdtype, rows, cols, ldx, x_rows, format, row_index, offsets, n_groups, *q, values, vdtype,
+                             ldv, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,
+                      int format, void* Y, int ydtype, int64_t ldy, int* status_dev, void* cuda_stream) {
+  bool empty = false;
+  int rc = check_fp4_product(n_tokens, out, in, format, nullptr, 0, B, Y, ydtype, ldy, &empty);
+  if (rc != ADADIM_OK || empty) return rc;
+  if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
+  return fp4_matmul_launch(*A, n_tokens, nullptr, 0, *B, out, in, format, Y, ydtype, ldy, status_dev,
+                           static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const int32_t* offsets, int n_experts,
+                              const adadim_fp4tensor* B, int64_t out, int64_t in, int format, void* Y, int ydtype,
+                              int64_t ldy, int* status_dev, void* cuda_stream) {
+  if (n_experts == 0) return ADADIM_ERR_PARAM;
+  bool empty = false;
+  int rc = check_fp4_product(n_rows, out, in, format, offsets, n_experts, B, Y, ydtype, ldy, &empty);
+  if (rc != ADADIM_OK || empty) return rc;
+  if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
+  return fp4_matmul_launch(*A, n_rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
+                           static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_fp4_linear(const void* X, int xdtype, int64_t n_tokens, int64_t in, int64_t ldx, const float* x_amax,
+                      const adadim_fp4tensor* B, int64_t out, int format, void* Y, int ydtype, int64_t ldy,
+                      int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  return fp4_linear(X, xdtype, n_tokens, in, ldx, x_amax, nullptr, nullptr, 0, n_tokens, B, out, format, Y, ydtype, ldy,
+                    status_dev, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_fp4_linear_grouped(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ldx, const float* x_amax,
+                              const int32_t* row_index, const int32_t* offsets, int n_experts, int64_t n_rows,
+                              const adadim_fp4tensor* B, int64_t out, int format, void* Y, int ydtype, int64_t ldy,
+                              int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (n_experts == 0) return ADADIM_ERR_PARAM;
+  return fp4_linear(X, xdtype, x_rows, in, ldx, x_amax, row_index, offsets, n_experts, n_rows, B, out, format, Y, ydtype,
+                    ldy, status_dev, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_unpack_codes(const uint32_t* codes, int64_t out, int64_t in, int bits, uint8_t* dst, void* cuda_stream) {

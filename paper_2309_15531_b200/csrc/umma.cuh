@@ -146,6 +146,32 @@ __device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
       : "memory");
 }
+// D[tmem] (+)= A[smem] * B[smem]^T for packed 4-bit inputs with block scales in TMEM: one 64-deep step.
+// MXFP4: two E8M0 scales per row and step (bytes picked by the descriptor's scale ids); NVFP4: four E4M3.
+template <bool NV>
+__device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t sfa_tmem, uint32_t sfb_tmem, bool accumulate) {
+  if constexpr (NV) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+  }
+}
+// 32 rows x 16 bytes of shared memory into 4 TMEM columns of lanes 0..31, repeated for the other
+// three groups of 32 lanes: a tile of block scales.  Ordered with the MMAs this thread issues.
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
 // The barrier receives one arrival once every MMA issued so far by this thread has completed.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
@@ -200,6 +226,18 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn, bool 
          (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// The same without a swizzle (scale tiles: 8-row groups of 16-byte rows, 128 bytes apart).
+__host__ __device__ constexpr uint64_t smem_desc_plain(uint32_t lbo_bytes, uint32_t sbo_bytes) {
+  return (static_cast<uint64_t>((lbo_bytes >> 4) & 0x3FFFu) << 16) |
+         (static_cast<uint64_t>((sbo_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46);
+}
+// Instruction descriptor of the block-scaled 4-bit kinds: E2M1 operands, both K-major; scales E8M0 or
+// E4M3; the byte of the 32-bit scale words at which this step's scales begin (MXFP4: 0 or 2).
+__host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, bool e8m0, uint32_t sf_byte) {
+  return (sf_byte << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(e8m0) << 23) | (static_cast<uint32_t>(M >> 4) << 24) | (sf_byte << 29);
+}
+
 }  // namespace ptx
 
 // ---- host side: tensor maps -------------------------------------------------------------------
@@ -210,5 +248,10 @@ int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t 
 // The same for fp32 with box {32, box_rows} (32 floats = one 128-byte swizzle row).
 int make_tmap_f32(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
                   uint32_t box_rows);
+
+// Bytes with 128-byte swizzle (box {128, box_rows}: packed 4-bit codes) or without (scale tiles as
+// 128-byte rows).
+int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
+                 uint32_t box_rows, bool swizzle);
 
 }  // namespace adadim
