@@ -123,6 +123,11 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _raw_stream(t: torch.Tensor) -> int:
+    """The same handle for t's device without building a Stream object (3.5 us on the measured host)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 def _check(rc: int, where: str):
     if rc != OK:
         raise AdadimError(rc, where)
@@ -405,7 +410,7 @@ def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor
     if amax is None:
         amax = torch.zeros(1, dtype=torch.float32, device=X.device)
     assert amax.dtype == torch.float32 and amax.is_cuda
-    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), amax.data_ptr(), _stream()),
+    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), amax.data_ptr(), _raw_stream(X)),
            "adadim_absmax")
     return amax
 
@@ -432,7 +437,7 @@ def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None,
     _check(lib().adadim_quantize_fp4(X.data_ptr(), _DT[X.dtype], rows, cols, _ld(X), X.shape[0], fmt, _ptr(row_index),
                                      _ptr(offsets), groups, C.byref(q.c()), _ptr(values),
                                      _DT[values.dtype] if values is not None else BF16,
-                                     _ld(values) if values is not None else 0, _stream()), "adadim_quantize_fp4")
+                                     _ld(values) if values is not None else 0, _raw_stream(X)), "adadim_quantize_fp4")
     return q
 
 
@@ -455,7 +460,7 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
             raise ValueError("fp4_linear: X and W do not match")
         y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
         _check(lib().adadim_fp4_matmul(C.byref(X.c()), X.rows, C.byref(W.c()), W.rows, W.cols, W.fmt, y.data_ptr(),
-                                       _DT[y.dtype], _ld(y), _ptr(status), _stream()), "adadim_fp4_matmul")
+                                       _DT[y.dtype], _ld(y), _ptr(status), _raw_stream(X.codes)), "adadim_fp4_matmul")
         return y
     _rows_of(X)
     rows, inp = X.shape
@@ -466,7 +471,7 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
     _check(lib().adadim_fp4_linear(X.data_ptr(), _DT[X.dtype], rows, inp, _ld(X), _ptr(x_amax), C.byref(W.c()), W.rows,
                                    W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
-                                   workspace.numel(), _stream()), "adadim_fp4_linear")
+                                   workspace.numel(), _raw_stream(X)), "adadim_fp4_linear")
     return y
 
 
@@ -485,7 +490,7 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
         y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
         _check(lib().adadim_fp4_matmul_grouped(C.byref(X.c()), X.rows, offsets.data_ptr(), n, C.byref(W.c()), W.rows,
                                                W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status),
-                                               _stream()), "adadim_fp4_matmul_grouped")
+                                               _raw_stream(X.codes)), "adadim_fp4_matmul_grouped")
         return y
     _rows_of(X)
     rows, inp = X.shape[0] if row_index is None else _i32(row_index).numel(), X.shape[1]
@@ -497,7 +502,7 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
     _check(lib().adadim_fp4_linear_grouped(X.data_ptr(), _DT[X.dtype], X.shape[0], inp, _ld(X), _ptr(x_amax),
                                            _ptr(row_index), offsets.data_ptr(), n, rows, C.byref(W.c()), W.rows, W.fmt,
                                            y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
-                                           workspace.numel(), _stream()), "adadim_fp4_linear_grouped")
+                                           workspace.numel(), _raw_stream(X)), "adadim_fp4_linear_grouped")
     return y
 
 

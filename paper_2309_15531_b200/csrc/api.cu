@@ -144,7 +144,7 @@ int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ld
   rc = quantize_fp4_launch(X, xdtype, rows, in, ldx, x_rows, format, row_index, offsets, n_experts, A, nullptr,
                            ADADIM_BF16, 0, st);
   if (rc != ADADIM_OK) return rc;
-  return fp4_matmul_launch(A, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, st);
+  return fp4_matmul_launch(A, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, true, st);
 }
 
 }  // namespace
@@ -425,7 +425,7 @@ int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_
   int rc = check_fp4_product(n_tokens, out, in, format, nullptr, 0, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(*A, n_tokens, nullptr, 0, *B, out, in, format, Y, ydtype, ldy, status_dev,
+  return fp4_matmul_launch(*A, n_tokens, nullptr, 0, *B, out, in, format, Y, ydtype, ldy, status_dev, false,
                            static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -437,7 +437,7 @@ int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const i
   int rc = check_fp4_product(n_rows, out, in, format, offsets, n_experts, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(*A, n_rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
+  return fp4_matmul_launch(*A, n_rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, false,
                            static_cast<cudaStream_t>(cuda_stream));
 }
 

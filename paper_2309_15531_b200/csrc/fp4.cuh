@@ -163,6 +163,6 @@ int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, i
                         void* values, int vdtype, int64_t ldv, cudaStream_t st);
 int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* offsets, int n_experts,
                       const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype, int64_t ldy,
-                      int* status_dev, cudaStream_t st);
+                      int* status_dev, bool chained, cudaStream_t st);
 
 }  // namespace adadim

@@ -9,6 +9,7 @@
 // the block's reciprocal; MXFP4 one multiplication by a power of two), and the hardware
 // conversion of pairs to E2M1.
 #include "fp4.cuh"
+#include "umma.cuh"
 
 namespace adadim {
 namespace {
@@ -93,6 +94,7 @@ __global__ void __launch_bounds__(kThreads)
 quantize_kernel(const QuantParams p) {
   constexpr int kTiles = kCols / sf_cols(FORMAT);
   __shared__ __align__(16) uint8_t sf[kTiles * kSfTileBytes];
+  ptx::pdl_launch_dependents();                               // a product launched behind this may start on its weight
   const int col_ctas = static_cast<int>((p.cols + kCols - 1) / kCols);
   const int v = blockIdx.x / col_ctas;                        // tile row
   const int cx = blockIdx.x - v * col_ctas;
