@@ -129,13 +129,22 @@ __device__ __forceinline__ uint32_t codes8(const float* v, const BlockScale& b) 
   const uint32_t r = e2m1_pack8(q);
   return b.finite ? r : 0u;
 }
-// The value of an E2M1 code
-__device__ __forceinline__ float e2m1_value(uint32_t code) {
-  const uint32_t mag = code & 7u;
-  // 0, .5, 1, 1.5, 2, 3, 4, 6: twice the values packed as bytes
-  const uint32_t twice = static_cast<uint32_t>((0x0c08060403020100ull >> (8 * mag)) & 0xff);
-  const float v = 0.5f * static_cast<float>(twice);
-  return (code & 8u) ? -v : v;
+// The values of eight packed codes, low half first.
+__device__ __forceinline__ void e2m1_values8(uint32_t codes, float (&v)[8]) {
+  uint32_t h[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+    v[2 * k] = f.x;
+    v[2 * k + 1] = f.y;
+  }
 }
 
 // The group of a virtual tile row v (see sf_tile_rows), by bisection over the clamped offsets, and

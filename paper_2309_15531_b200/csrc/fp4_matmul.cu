@@ -28,6 +28,7 @@ using namespace fp4;
 
 constexpr int kKT = 256;                               // columns of a stage
 constexpr int kThreads = 192;                          // TMA warp, MMA warp, four epilogue warps
+constexpr int kPairThreads = 320;                      // pair kernel: eight
 constexpr int kMaxStages = 8;
 constexpr uint32_t kWBytes = 128 * 128;
 constexpr int kBand = 8;                               // weight tiles that share a sweep over the tokens
@@ -45,7 +46,6 @@ struct MmParams {
   int64_t n_sf;                                        // scale tiles of a tile row
   int64_t w_sf_rows;                                   // scale tile rows of one weight
   void* Y;
-  int ydtype;
   int64_t ldy;
   const float* a_amax;
   const float* b_amax;
@@ -119,10 +119,25 @@ __device__ __forceinline__ void tile_prefix(const MmParams& p, int lane, int* pr
   if (lane == 0) prefix[p.n_experts] = sum;
 }
 
-__device__ __forceinline__ void store_y(void* Y, int ydtype, int64_t at, float v) {
-  if (ydtype == ADADIM_BF16) static_cast<__nv_bfloat16*>(Y)[at] = __float2bfloat16_rn(v);
-  else if (ydtype == ADADIM_F16) static_cast<__half*>(Y)[at] = __float2half_rn(v);
-  else static_cast<float*>(Y)[at] = v;
+__device__ __forceinline__ void put(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put(__half* y, float v) { *y = __float2half_rn(v); }
+__device__ __forceinline__ void put(float* y, float v) { *y = v; }
+// 32 tokens of one weight row: y + j * ldy receives v[j] * scale, j < n
+template <typename T>
+__device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, float scale, const float (&v)[32]) {
+  if (n >= 32) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) { put(y, v[j] * scale); y += ldy; }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) { if (j < n) put(y, v[j] * scale); y += ldy; }
+  }
+}
+// 2^(ta + tb).  Each lies between 2^-100 and 2^117: the product is 0 or infinite only where |amax| of both
+// matrices are so far out that every result is.
+template <bool NV>
+__device__ __forceinline__ float product_scale(const MmParams& p) {
+  return NV ? exp2_int(tensor_scale_log2(p.a_amax)) * exp2_int(tensor_scale_log2(p.b_amax)) : 1.0f;
 }
 // After a wait that ran out: time for the copies already issued to land before shared memory goes away
 // (they take microseconds).
@@ -162,8 +177,8 @@ __device__ __forceinline__ int steps_of(int64_t in, int k) {
 }
 
 // ---- pair -----------------------------------------------------------------------------------------
-template <int FORMAT>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int FORMAT, typename T>
+__global__ void __launch_bounds__(kPairThreads, 1)
 fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                 const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
@@ -178,7 +193,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   __shared__ int dead_word;
   __shared__ int prefix[kMaxGroups + 1];
   volatile int* dead = &dead_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
   const uint32_t stage_size = stage_bytes(FORMAT, true, p.n_tile);
   const uint32_t a_bytes = static_cast<uint32_t>(p.n_tile) * 64;
@@ -186,8 +201,8 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.n_stages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 8); }
-    ptx::mbar_init(&part_empty, 8);
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 16); }
+    ptx::mbar_init(&part_empty, 16);
     dead_word = 0;
     ptx::fence_mbar_init();
     ptx::tma_prefetch_desc(&tmW);
@@ -209,36 +224,44 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (both CTAs)
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
-      ptx::pdl_wait();
-      for (int t = pair0; t < num_tiles && !*dead; t += pairs) {
-        const Tile x = tile_of<256>(t, p, prefix);
-        const int half = ((x.count + 15) & ~15) >> 1;  // tokens of this CTA
-        const int w_row = static_cast<int>(x.e * p.out + x.m) + static_cast<int>(rank) * 128;
-        const int64_t w_sf = (x.e * p.w_sf_rows + x.m / kSfRows + rank) * p.n_sf, a_sf = x.a_sf_row * p.n_sf;
-        for (int k = 0; k < p.num_k; ++k) {
-          if (!ptx::mbar_wait(&empty[stage], phase ^ 1u, dead, p.status_dev)) break;
-          uint8_t* w_dst = smem + stage * stage_size;
-          uint8_t* a_dst = w_dst + kWBytes;
-          uint8_t* ws_dst = a_dst + a_bytes;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    ptx::pdl_wait();
+    for (int t = pair0; t < num_tiles && ok; t += pairs) {
+      const Tile x = tile_of<256>(t, p, prefix);
+      const int half = ((x.count + 15) & ~15) >> 1;    // tokens of this CTA
+      const int w_row = static_cast<int>(x.e * p.out + x.m) + static_cast<int>(rank) * 128;
+      const int a_row = x.row + static_cast<int>(rank) * half;
+      int w_sf = static_cast<int>((x.e * p.w_sf_rows + x.m / kSfRows + rank) * p.n_sf * 4);
+      int a_sf0 = static_cast<int>(x.a_sf_row * p.n_sf * 4), a_sf1 = static_cast<int>((x.a_sf_row + 1) * p.n_sf * 4);
+      for (int k = 0; k < p.num_k; ++k) {
+        ok = ptx::mbar_wait_warp(&empty[stage], phase ^ 1u, dead, p.status_dev);
+        if (!ok) break;
+        uint8_t* w_dst = smem + stage * stage_size;
+        uint8_t* a_dst = w_dst + kWBytes;
+        uint8_t* ws_dst = a_dst + a_bytes;
+        const uint32_t bar = ptx::map_to_cta(ptx::smem_addr(&full[stage]), 0);
+        if (ptx::elect_one()) {
           // one barrier, the leader's, counts both CTAs' bytes
           if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * stage_size);
-          const uint32_t bar = ptx::map_to_cta(ptx::smem_addr(&full[stage]), 0);
           ptx::tma_load_2d_pair(w_dst, &tmW, k * (kKT / 2), w_row, bar);
-          ptx::tma_load_2d_pair(a_dst, &tmA, k * (kKT / 2), x.row + static_cast<int>(rank) * half, bar);
-          ptx::tma_load_2d_pair(ws_dst, &tmWs, 0, static_cast<int>((w_sf + k * kSfTiles) * 4), bar);
-          ptx::tma_load_2d_pair(ws_dst + kSf, &tmAs, 0, static_cast<int>((a_sf + k * kSfTiles) * 4), bar);
-          ptx::tma_load_2d_pair(ws_dst + 2 * kSf, &tmAs, 0, static_cast<int>((a_sf + p.n_sf + k * kSfTiles) * 4), bar);
-          if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
+          ptx::tma_load_2d_pair(a_dst, &tmA, k * (kKT / 2), a_row, bar);
+          ptx::tma_load_2d_pair(ws_dst, &tmWs, 0, w_sf, bar);
+          ptx::tma_load_2d_pair(ws_dst + kSf, &tmAs, 0, a_sf0, bar);
+          ptx::tma_load_2d_pair(ws_dst + 2 * kSf, &tmAs, 0, a_sf1, bar);
         }
+        __syncwarp();
+        w_sf += kSfTiles * 4;
+        a_sf0 += kSfTiles * 4;
+        a_sf1 += kSfTiles * 4;
+        if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
       }
-      if (*dead) let_copies_land();
     }
+    if (!ok) let_copies_land();
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (leader)
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, part_phase = 0;
       bool ok = true;
@@ -246,66 +269,63 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         const Tile x = tile_of<256>(t, p, prefix);
         const int n = (x.count + 15) & ~15;
         const uint32_t id0 = ptx::idesc_fp4(256, n, !NV, 0), id1 = ptx::idesc_fp4(256, n, !NV, NV ? 0 : 2);
-        ok = ptx::mbar_wait(&acc_empty[buf], acc_phase ^ 1u, dead, p.status_dev);
+        ok = ptx::mbar_wait_warp(&acc_empty[buf], acc_phase ^ 1u, dead, p.status_dev);
         if (ok && t != pair0) {                        // the tile before has left the shared columns
-          ok = ptx::mbar_wait(&part_empty, part_phase, dead, p.status_dev);
+          ok = ptx::mbar_wait_warp(&part_empty, part_phase, dead, p.status_dev);
           part_phase ^= 1u;
         }
         if (!ok) break;
         ptx::tc_fence_after_sync();
         for (int k = 0; k < p.num_k; ++k) {
-          ok = ptx::mbar_wait(&full[stage], phase, dead, p.status_dev);
+          ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
           if (!ok) break;
           ptx::tc_fence_after_sync();
           const uint32_t w_addr = ptx::smem_addr(smem + stage * stage_size);
-          issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, 0, w_addr, w_addr + kWBytes,
-                                    w_addr + kWBytes + a_bytes, id0, id1, steps_of(p.in, k), k == 0);
-          ptx::mma_commit_pair(&empty[stage]);
+          const int steps = steps_of(p.in, k);
+          if (ptx::elect_one()) {
+            issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, 0, w_addr, w_addr + kWBytes,
+                                      w_addr + kWBytes + a_bytes, id0, id1, steps, k == 0);
+            ptx::mma_commit_pair(&empty[stage]);
+            if (k == p.num_k - 1) ptx::mma_commit_pair(&acc_full[buf]);
+          }
+          __syncwarp();
           if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
         }
-        if (!ok) break;
-        ptx::mma_commit_pair(&acc_full[buf]);
         buf ^= 1;
         if (buf == 0) acc_phase ^= 1u;
       }
-      if (*dead) let_copies_land();
+      if (!ok) let_copies_land();
     }
   } else {
-    // ------------------------------------------------------------------ epilogue (warps 2..5 of both CTAs)
+    // ------------------------------------------------------------------ epilogue (warps 2..9 of both CTAs)
     const int q = warp & 3;                            // TMEM lane quadrant this warp may read
+    const int side = (warp - 2) >> 2;                  // of each 64 columns, which 32 this warp takes
     int buf = 0;
     uint32_t acc_phase = 0;
-    const float sa = exp2_int(NV ? tensor_scale_log2(p.a_amax) : 0), sb = exp2_int(NV ? tensor_scale_log2(p.b_amax) : 0);
+    const float scale = product_scale<NV>(p);
     const uint32_t part_bar = ptx::map_to_cta(ptx::smem_addr(&part_empty), 0);
     for (int t = pair0; t < num_tiles; t += pairs) {
       const Tile x = tile_of<256>(t, p, prefix);
-      if (!ptx::mbar_wait(&acc_full[buf], acc_phase, dead, p.status_dev)) break;
+      if (!ptx::mbar_wait_warp(&acc_full[buf], acc_phase, dead, p.status_dev)) break;
       ptx::tc_fence_after_sync();
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
-      const int64_t base = static_cast<int64_t>(x.row) * p.ldy + o;
+      T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
       const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + buf * kAccStep;
-      auto store = [&](int c, const float (&v)[32]) {
-        if (o >= p.out) return;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (c + j < x.count) store_y(p.Y, p.ydtype, base + (c + j) * p.ldy, v[j] * sa * sb);
-      };
       // the shared columns first: the last 64 of accumulator 0, the first 64 of accumulator 1
-      const int s0 = buf == 0 ? static_cast<int>(kAccStep) : 0;
+      const int s0 = (buf == 0 ? static_cast<int>(kAccStep) : 0) + side * 32;
       {
-        float v0[32], v1[32];
-        const bool any = s0 < x.count;
-        if (any) { ptx::tmem_ld32(acc + s0, v0); ptx::tmem_ld32(acc + s0 + 32, v1); }
+        float v[32];
+        if (s0 < x.count) ptx::tmem_ld32(acc + s0, v);
         ptx::tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_cluster(part_bar);
-        if (any) { store(s0, v0); store(s0 + 32, v1); }
+        if (s0 < x.count && o < p.out) store_tokens(y + s0 * p.ldy, p.ldy, x.count - s0, scale, v);
       }
 #pragma unroll 1
-      for (int c = buf == 0 ? 0 : static_cast<int>(kShared); c < min(x.count, buf == 0 ? static_cast<int>(kAccStep) : 256); c += 32) {
+      for (int c = (buf == 0 ? 0 : 64) + side * 32; c < min(x.count, buf == 0 ? 192 : 256); c += 64) {
         float v[32];
         ptx::tmem_ld32(acc + c, v);
-        store(c, v);
+        if (o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
       }
       ptx::tc_fence_before_sync();
       __syncwarp();
@@ -325,7 +345,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 }
 
 // ---- split ----------------------------------------------------------------------------------------
-template <int FORMAT>
+template <int FORMAT, typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                  const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
@@ -341,7 +361,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   __shared__ int dead_word;
   __shared__ int prefix[kMaxGroups + 1];
   volatile int* dead = &dead_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t stage_size = stage_bytes(FORMAT, false, p.n_tile);
   const uint32_t a_bytes = static_cast<uint32_t>(p.n_tile) * 128;
   float* red = reinterpret_cast<float*>(smem + p.n_stages * stage_size);     // [tokens of this CTA][splits][128 rows]
@@ -377,19 +397,26 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
-    if (lane == 0 && work) {
+    if (work) {
       const int w_row = static_cast<int>(x.e * p.out + x.m);
-      const int64_t w_sf = (x.e * p.w_sf_rows + x.m / kSfRows) * p.n_sf, a_sf = x.a_sf_row * p.n_sf;
+      const int w_sf = static_cast<int>((x.e * p.w_sf_rows + x.m / kSfRows) * p.n_sf * 4);
+      const int a_sf = static_cast<int>(x.a_sf_row * p.n_sf * 4);
       auto load_w = [&](int k, int stage) {
         uint8_t* w_dst = smem + stage * stage_size;
-        ptx::mbar_arrive_expect_tx(&full[stage], stage_size);
-        ptx::tma_load_2d(w_dst, &tmW, k * (kKT / 2), w_row, &full[stage]);
-        ptx::tma_load_2d(w_dst + kWBytes + a_bytes, &tmWs, 0, static_cast<int>((w_sf + k * kSfTiles) * 4), &full[stage]);
+        if (ptx::elect_one()) {
+          ptx::mbar_arrive_expect_tx(&full[stage], stage_size);
+          ptx::tma_load_2d(w_dst, &tmW, k * (kKT / 2), w_row, &full[stage]);
+          ptx::tma_load_2d(w_dst + kWBytes + a_bytes, &tmWs, 0, w_sf + k * kSfTiles * 4, &full[stage]);
+        }
+        __syncwarp();
       };
       auto load_a = [&](int k, int stage) {
         uint8_t* a_dst = smem + stage * stage_size + kWBytes;
-        ptx::tma_load_2d(a_dst, &tmA, k * (kKT / 2), x.row, &full[stage]);
-        ptx::tma_load_2d(a_dst + a_bytes + kSf, &tmAs, 0, static_cast<int>((a_sf + k * kSfTiles) * 4), &full[stage]);
+        if (ptx::elect_one()) {
+          ptx::tma_load_2d(a_dst, &tmA, k * (kKT / 2), x.row, &full[stage]);
+          ptx::tma_load_2d(a_dst + a_bytes + kSf, &tmAs, 0, a_sf + k * kSfTiles * 4, &full[stage]);
+        }
+        __syncwarp();
       };
       // the ring's first fill: the weight does not depend on the launch before this one
       const int ahead = min(k1 - k0, p.n_stages);
@@ -398,55 +425,57 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
       int stage = 0;
       uint32_t phase = 0;
-      for (int k = k0 + ahead; k < k1; ++k) {
-        if (!ptx::mbar_wait(&empty[stage], phase, dead, p.status_dev)) break;
+      bool ok = true;
+      for (int k = k0 + ahead; k < k1 && ok; ++k) {
+        ok = ptx::mbar_wait_warp(&empty[stage], phase, dead, p.status_dev);
+        if (!ok) break;
         load_w(k, stage);
         load_a(k, stage);
         if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
       }
-      if (*dead) let_copies_land();
+      if (!ok) let_copies_land();
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0 && work) {
+    if (work) {
       const int n = (x.count + 15) & ~15;
       const uint32_t id0 = ptx::idesc_fp4(128, n, !NV, 0), id1 = ptx::idesc_fp4(128, n, !NV, NV ? 0 : 2);
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (int k = k0; k < k1; ++k) {
-        ok = ptx::mbar_wait(&full[stage], phase, dead, p.status_dev);
+        ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         const uint32_t w_addr = ptx::smem_addr(smem + stage * stage_size);
-        issue_stage<FORMAT, false>(tmem, tmem + kSfCol, x.a_sf_col, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
-                                   id0, id1, steps_of(p.in, k), k == k0);
-        ptx::mma_commit(&empty[stage]);
+        const int steps = steps_of(p.in, k);
+        if (ptx::elect_one()) {
+          issue_stage<FORMAT, false>(tmem, tmem + kSfCol, x.a_sf_col, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
+                                     id0, id1, steps, k == k0);
+          ptx::mma_commit(&empty[stage]);
+          if (k == k1 - 1) ptx::mma_commit(&acc_full);
+        }
+        __syncwarp();
         if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
       }
-      if (ok) ptx::mma_commit(&acc_full);
-      else let_copies_land();
+      if (!ok) let_copies_land();
     }
   } else if (work) {
     // ------------------------------------------------------------------ epilogue (warps 2..5)
     const int q = warp & 3;                            // TMEM lane quadrant this warp may read
-    const float sa = exp2_int(NV ? tensor_scale_log2(p.a_amax) : 0), sb = exp2_int(NV ? tensor_scale_log2(p.b_amax) : 0);
+    const float scale = product_scale<NV>(p);
     const int row = q * 32 + lane;
     const int64_t o = x.m + row;
-    const int64_t base = static_cast<int64_t>(x.row) * p.ldy + o;
+    T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
     const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16);
-    bool ok = ptx::mbar_wait(&acc_full, 0, dead, p.status_dev);
+    bool ok = ptx::mbar_wait_warp(&acc_full, 0, dead, p.status_dev);
     ptx::tc_fence_after_sync();
     if (p.splits == 1) {
 #pragma unroll 1
       for (int c = 0; c < x.count && ok; c += 32) {
         float v[32];
         ptx::tmem_ld32(acc + c, v);
-        if (o < p.out) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c + j < x.count) store_y(p.Y, p.ydtype, base + (c + j) * p.ldy, v[j] * sa * sb);
-        }
+        if (o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
       }
     } else {
       // token c of the tile is finished by CTA c % splits: every CTA sends it its partial sums
@@ -464,12 +493,12 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       }
       __syncwarp();
       if (lane < p.splits) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&red_full), lane));
-      ok = ptx::mbar_wait(&red_full, 0, dead, p.status_dev) && ok;
+      ok = ptx::mbar_wait_warp(&red_full, 0, dead, p.status_dev) && ok;
       ptx::fence_acquire_cluster();
       for (int c = rank, slot = 0; c < x.count && ok; c += p.splits, ++slot) {
         float s = 0.0f;
         for (int k = 0; k < p.splits; ++k) s += red[(slot * p.splits + k) * 128 + row];
-        if (o < p.out) store_y(p.Y, p.ydtype, base + c * p.ldy, s * sa * sb);
+        if (o < p.out) put(y + c * p.ldy, s * scale);
       }
     }
   }
@@ -486,12 +515,12 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 constexpr size_t kSmemOne = 220 * 1024, kSmemTwo = 106 * 1024;       // dynamic shared memory at one and two CTAs per SM
 
 template <typename K>
-int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, unsigned grid, int cluster, size_t smem, bool chained,
-           cudaStream_t st) {
+int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, unsigned grid, int threads, int cluster, size_t smem,
+           bool chained, cudaStream_t st) {
   ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemOne)));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -512,6 +541,15 @@ int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, unsigned gri
   cfg.numAttrs = static_cast<unsigned>(n);
   ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm[0], tm[1], tm[2], tm[3], p));
   return ADADIM_OK;
+}
+
+template <typename T>
+int launch_format(bool pair, int format, const CUtensorMap (&tm)[4], const MmParams& p, unsigned grid, size_t smem, bool chained,
+                  cudaStream_t st) {
+  if (pair) return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st)
+                                          : launch(fp4_pair_kernel<ADADIM_NVFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st);
+  return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T>, tm, p, grid, kThreads, p.splits, smem, chained, st)
+                                : launch(fp4_split_kernel<ADADIM_NVFP4, T>, tm, p, grid, kThreads, p.splits, smem, chained, st);
 }
 
 }  // namespace
@@ -535,7 +573,6 @@ int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* 
   p.n_sf = sf_tiles(format, in);
   p.w_sf_rows = sf_tile_rows(out, 0);
   p.Y = Y;
-  p.ydtype = ydtype;
   p.ldy = ldy;
   p.a_amax = A.amax;
   p.b_amax = B.amax;
@@ -567,26 +604,27 @@ int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* 
   if ((rc = make_tmap_u8(&tm[3], A.scales, 128, scale_bytes(format, n_rows, in, n_experts) / 128, 128, sf_box, false)) != ADADIM_OK) return rc;
 
   const size_t per = stage_bytes(format, pair, p.n_tile);
+  unsigned grid;
+  size_t smem;
   if (pair) {
     p.n_stages = static_cast<int>((kSmemOne - 1024) / per);
     if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
-    const int64_t pairs = tiles < sm_count / 2 ? tiles : sm_count / 2;
-    const unsigned grid = static_cast<unsigned>(2 * pairs);
-    const size_t smem = p.n_stages * per + 1024;
-    return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4>, tm, p, grid, 2, smem, chained, st)
-                                  : launch(fp4_pair_kernel<ADADIM_NVFP4>, tm, p, grid, 2, smem, chained, st);
+    grid = static_cast<unsigned>(2 * (tiles < sm_count / 2 ? tiles : sm_count / 2));
+    smem = p.n_stages * per + 1024;
+  } else {
+    // split the columns until there are two CTAs for every SM
+    p.splits = 1;
+    while (p.splits < 8 && tiles * p.splits * 2 <= 2 * sm_count && p.splits * 2 <= p.num_k) p.splits *= 2;
+    const size_t red = p.splits > 1 ? static_cast<size_t>((p.n_tile + p.splits - 1) / p.splits) * p.splits * 512 : 0;
+    p.n_stages = static_cast<int>((kSmemTwo - 1024 - red) / per);
+    if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
+    if (p.n_stages < 2) p.n_stages = 2;
+    grid = static_cast<unsigned>(tiles * p.splits);
+    smem = p.n_stages * per + red + 1024;
   }
-  // split the columns until there are two CTAs for every SM
-  p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= 2 * sm_count && p.splits * 2 <= p.num_k) p.splits *= 2;
-  const size_t red = p.splits > 1 ? static_cast<size_t>((p.n_tile + p.splits - 1) / p.splits) * p.splits * 512 : 0;
-  p.n_stages = static_cast<int>((kSmemTwo - 1024 - red) / per);
-  if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
-  if (p.n_stages < 2) p.n_stages = 2;
-  const size_t smem = p.n_stages * per + red + 1024;
-  const unsigned grid = static_cast<unsigned>(tiles * p.splits);
-  return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4>, tm, p, grid, p.splits, smem, chained, st)
-                                : launch(fp4_split_kernel<ADADIM_NVFP4>, tm, p, grid, p.splits, smem, chained, st);
+  if (ydtype == ADADIM_F32) return launch_format<float>(pair, format, tm, p, grid, smem, chained, st);
+  if (ydtype == ADADIM_F16) return launch_format<__half>(pair, format, tm, p, grid, smem, chained, st);
+  return launch_format<__nv_bfloat16>(pair, format, tm, p, grid, smem, chained, st);
 }
 
 }  // namespace adadim
