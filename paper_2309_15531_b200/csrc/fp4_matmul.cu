@@ -163,12 +163,17 @@ __device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, int a_
     ptx::tmem_cp_scales<PAIR>(sf_tmem + 16 + j * kTok, ptx::with_start(sf_desc, ws_addr + kSf + j * kSfTileBytes));
     if (PAIR) ptx::tmem_cp_scales<PAIR>(sf_tmem + 16 + j * kTok + 4, ptx::with_start(sf_desc, ws_addr + 2 * kSf + j * kSfTileBytes));
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (j >= steps) break;
+  auto step = [&](int j) {
     const int tile = NV ? j : j / 2;
     ptx::mma_fp4<NV, PAIR>(d, ptx::with_start(desc, w_addr + j * 32), ptx::with_start(desc, a_addr + j * 32),
                            (j & 1) ? id1 : id0, sf_tmem + tile * 4, sf_tmem + 16 + tile * kTok + a_sf_col, !(first && j == 0));
+  };
+  if (steps == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) step(j);
+  } else {
+#pragma unroll 1
+    for (int j = 0; j < steps; ++j) step(j);
   }
 }
 __device__ __forceinline__ int steps_of(int64_t in, int k) {
@@ -184,7 +189,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
   constexpr int kSfTiles = kSf / kSfTileBytes;
-  constexpr uint32_t kAccStep = 192, kShared = 64, kSfCol = 448;     // accumulators at 0 and 192, scales at 448
+  constexpr uint32_t kAccStep = 192, kSfCol = 448;     // accumulators at 0 and 192, scales at 448
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -264,7 +269,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     if (rank == 0) {
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, part_phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;
       for (int t = pair0; t < num_tiles && ok; t += pairs) {
         const Tile x = tile_of<256>(t, p, prefix);
         const int n = (x.count + 15) & ~15;
@@ -277,19 +282,22 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         if (!ok) break;
         ptx::tc_fence_after_sync();
         for (int k = 0; k < p.num_k; ++k) {
-          ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
+          if (!ready) ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
           if (!ok) break;
           ptx::tc_fence_after_sync();
-          const uint32_t w_addr = ptx::smem_addr(smem + stage * stage_size);
+          const int cur = stage;
+          if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
+          // asked before this stage's instructions are issued: the answer is there when they are
+          const bool next = ptx::mbar_try_wait(&full[stage], phase);
+          const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
           const int steps = steps_of(p.in, k);
           if (ptx::elect_one()) {
             issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, 0, w_addr, w_addr + kWBytes,
                                       w_addr + kWBytes + a_bytes, id0, id1, steps, k == 0);
-            ptx::mma_commit_pair(&empty[stage]);
+            ptx::mma_commit_pair(&empty[cur]);
             if (k == p.num_k - 1) ptx::mma_commit_pair(&acc_full[buf]);
           }
-          __syncwarp();
-          if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
+          ready = __all_sync(0xffffffffu, next) != 0;
         }
         buf ^= 1;
         if (buf == 0) acc_phase ^= 1u;
@@ -492,7 +500,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         }
       }
       __syncwarp();
-      if (lane < p.splits) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&red_full), lane));
+      if (lane < p.splits) ptx::mbar_arrive_release_cluster(ptx::map_to_cta(ptx::smem_addr(&red_full), lane));
       ok = ptx::mbar_wait_warp(&red_full, 0, dead, p.status_dev) && ok;
       ptx::fence_acquire_cluster();
       for (int c = rank, slot = 0; c < x.count && ok; c += p.splits, ++slot) {
