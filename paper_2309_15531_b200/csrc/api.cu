@@ -109,7 +109,7 @@ int check_fp4_product(int64_t rows, int64_t out, int64_t in, int format, const i
   const int64_t tiles = ((rows + 15) / 16 + n_experts) * ((out + 127) / 128);
   const int64_t weights = n_experts > 0 ? n_experts : 1;
   const int64_t sf_rows = weights * static_cast<int64_t>(fp4::scale_bytes(format, out, in, 0)) / 128;
-  const int64_t a_sf_rows = static_cast<int64_t>(fp4::scale_bytes(format, rows, in, n_experts)) / 128;
+  const int64_t a_sf_rows = fp4_most_tile_rows(rows, n_experts) * fp4::sf_tiles(format, in) * 4;
   if (tiles > 0x7fffffff || sf_rows > 0x7fffffff || a_sf_rows > 0x7fffffff) return ADADIM_ERR_SHAPE;
   if ((rc = check_fp4(B, in)) != ADADIM_OK) return rc;
   return check_matrix(Y, ydtype, out, ldy);
@@ -119,7 +119,8 @@ int check_fp4_product(int64_t rows, int64_t out, int64_t in, int format, const i
 size_t fp4_code_bytes(int64_t rows, int64_t in) { return round_up(static_cast<size_t>(rows) * fp4::code_pitch(in), 256); }
 size_t fp4_workspace_bytes(int64_t rows, int64_t in, int n_groups) {
   // the scales of the finer format; the coarser one needs less
-  return fp4_code_bytes(rows, in) + round_up(fp4::scale_bytes(ADADIM_NVFP4, rows, in, n_groups), 256);
+  return fp4_code_bytes(rows, in) +
+         round_up(static_cast<size_t>(fp4_most_tile_rows(rows, n_groups)) * fp4::sf_tiles(ADADIM_NVFP4, in) * fp4::kSfTileBytes, 256);
 }
 int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ldx, const float* x_amax,
                const int32_t* row_index, const int32_t* offsets, int n_experts, int64_t rows, const adadim_fp4tensor* B,
@@ -141,10 +142,12 @@ int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ld
   A.scales = A.codes + fp4_code_bytes(rows, in);
   A.amax = x_amax;
   A.ld = fp4::code_pitch(in);
-  rc = quantize_fp4_launch(X, xdtype, rows, in, ldx, x_rows, format, row_index, offsets, n_experts, A, nullptr,
+  const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, true);
+  rc = quantize_fp4_launch(X, xdtype, rows, in, ldx, x_rows, format, row_index, offsets, n_experts, A, plan.n_tile, nullptr,
                            ADADIM_BF16, 0, st);
   if (rc != ADADIM_OK) return rc;
-  return fp4_matmul_launch(A, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, true, st);
+  return fp4_matmul_launch(plan, A, plan.n_tile, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
+                           true, st);
 }
 
 }  // namespace
@@ -415,8 +418,8 @@ int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, i
   if ((reinterpret_cast<uintptr_t>(row_index) & 3u) != 0) return ADADIM_ERR_ALIGN;
   if ((rc = check_fp4(q, cols)) != ADADIM_OK) return rc;
   if (values != nullptr && (rc = check_matrix(values, vdtype, cols, ldv)) != ADADIM_OK) return rc;
-  return quantize_fp4_launch(X, xdtype, rows, cols, ldx, x_rows, format, row_index, offsets, n_groups, *q, values, vdtype,
-                             ldv, static_cast<cudaStream_t>(cuda_stream));
+  return quantize_fp4_launch(X, xdtype, rows, cols, ldx, x_rows, format, row_index, offsets, n_groups, *q, fp4::kSfRows,
+                             values, vdtype, ldv, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,
@@ -425,8 +428,8 @@ int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_
   int rc = check_fp4_product(n_tokens, out, in, format, nullptr, 0, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(*A, n_tokens, nullptr, 0, *B, out, in, format, Y, ydtype, ldy, status_dev, false,
-                           static_cast<cudaStream_t>(cuda_stream));
+  return fp4_matmul_launch(fp4_plan(n_tokens, out, in, 0, format, false), *A, fp4::kSfRows, n_tokens, nullptr, 0, *B, out,
+                           in, format, Y, ydtype, ldy, status_dev, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const int32_t* offsets, int n_experts,
@@ -437,8 +440,8 @@ int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const i
   int rc = check_fp4_product(n_rows, out, in, format, offsets, n_experts, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(*A, n_rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev, false,
-                           static_cast<cudaStream_t>(cuda_stream));
+  return fp4_matmul_launch(fp4_plan(n_rows, out, in, n_experts, format, false), *A, fp4::kSfRows, n_rows, offsets, n_experts,
+                           *B, out, in, format, Y, ydtype, ldy, status_dev, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_fp4_linear(const void* X, int xdtype, int64_t n_tokens, int64_t in, int64_t ldx, const float* x_amax,

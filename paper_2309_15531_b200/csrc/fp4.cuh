@@ -22,10 +22,13 @@ __host__ __device__ constexpr int sf_cols(int format) { return 4 * block_of(form
 __host__ __device__ __forceinline__ int64_t sf_tiles(int format, int64_t cols) {
   return (cols + sf_cols(format) - 1) / sf_cols(format);
 }
-// tile rows of a matrix; of rows in groups (group e starts at tile row offsets[e] / 128 + e, and
-// floor(a / 128) + ceil(n / 128) <= floor((a + n) / 128) + 1, so groups never overlap)
-__host__ __device__ __forceinline__ int64_t sf_tile_rows(int64_t rows, int n_groups) {
-  return n_groups > 0 ? rows / kSfRows + n_groups : (rows + kSfRows - 1) / kSfRows;
+// Tile rows of a matrix; of rows in groups (group e starts at tile row offsets[e] / 128 + e, and
+// floor(a / 128) + ceil(n / 128) <= floor((a + n) / 128) + 1, so groups never overlap).
+// Inside the library activations may be laid out for token tiles of another height `lt`: the rows are
+// cut every lt (in each group), and every cut starts a tile row (TMEM holds the scales of 32 rows per
+// column, and a product's scales have to begin on a whole tile).  lt = 128 is the public layout.
+__host__ __device__ __forceinline__ int64_t sf_tile_rows(int64_t rows, int n_groups, int lt = kSfRows) {
+  return (n_groups > 0 ? rows / lt + n_groups : (rows + lt - 1) / lt) * ((lt + kSfRows - 1) / kSfRows);
 }
 inline size_t scale_bytes(int format, int64_t rows, int64_t cols, int n_groups) {
   return static_cast<size_t>(sf_tile_rows(rows, n_groups)) * sf_tiles(format, cols) * kSfTileBytes;
@@ -147,19 +150,24 @@ __device__ __forceinline__ void e2m1_values8(uint32_t codes, float (&v)[8]) {
   }
 }
 
-// The group of a virtual tile row v (see sf_tile_rows), by bisection over the clamped offsets, and
-// the rows it stands for: first row and count (0 if the tile row belongs to no group).
+// The rows that scale tile row v holds (see sf_tile_rows): first and count, 0 if it holds none.  Groups are
+// found by bisection over the clamped offsets.
 __device__ __forceinline__ int clamped(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
-__device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_groups, int rows, int v, int& first, int& count) {
-  int lo = 0, hi = n_groups - 1;                                     // last e with offsets[e] / 128 + e <= v
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (clamped(offsets[mid], rows) / kSfRows + mid <= v) lo = mid; else hi = mid - 1;
+__device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_groups, int rows, int lt, int v, int& first, int& count) {
+  const int sub = (lt + kSfRows - 1) / kSfRows, cut = v / sub, part = v - cut * sub;
+  int a = 0, z = rows, skip = cut * lt;
+  if (offsets != nullptr) {
+    int lo = 0, hi = n_groups - 1;                                   // last e with offsets[e] / lt + e <= cut
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (clamped(offsets[mid], rows) / lt + mid <= cut) lo = mid; else hi = mid - 1;
+    }
+    a = clamped(offsets[lo], rows);
+    z = clamped(offsets[lo + 1], rows);
+    skip = (cut - (a / lt + lo)) * lt;
   }
-  const int a = clamped(offsets[lo], rows), z = clamped(offsets[lo + 1], rows);
-  const int skip = (v - (a / kSfRows + lo)) * kSfRows;
-  first = a + skip;
-  count = skip < 0 ? 0 : z - first < kSfRows ? z - first : kSfRows;
+  first = a + skip + part * kSfRows;
+  count = skip < 0 ? 0 : min(min(lt - part * kSfRows, kSfRows), z - first);
   if (count < 0) count = 0;
 }
 
@@ -169,9 +177,19 @@ __device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_g
 int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, cudaStream_t st);
 int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
                         const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor& q,
-                        void* values, int vdtype, int64_t ldv, cudaStream_t st);
-int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* offsets, int n_experts,
-                      const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype, int64_t ldy,
-                      int* status_dev, bool chained, cudaStream_t st);
+                        int lt, void* values, int vdtype, int64_t ldv, cudaStream_t st);
+// How a product is laid out on the SMs.
+struct Fp4Plan {
+  bool pair;               // which kernel
+  int n_tile;              // tokens of a tile
+  int splits, per_sm;      // split kernel: CTAs of a cluster, CTAs of an SM
+};
+// own_layout: the activations' scales are laid out as the plan likes best (lt = n_tile), otherwise lt = 128
+Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout);
+int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, int64_t n_rows, const int32_t* offsets,
+                      int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
+                      int64_t ldy, int* status_dev, bool chained, cudaStream_t st);
+// the most scale tile rows that activations take in any plan's layout
+int64_t fp4_most_tile_rows(int64_t rows, int n_experts);
 
 }  // namespace adadim

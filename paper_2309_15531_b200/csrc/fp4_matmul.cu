@@ -15,8 +15,9 @@
 //          those alone.
 //   split  few tokens, bound by the weight's bytes: 128 weight rows x up to 128 tokens per cluster, the
 //          columns split over the cluster's 1 .. 8 CTAs, partial sums exchanged through distributed
-//          shared memory and added in the order of the columns; two CTAs to an SM.  Launched behind
-//          the quantizer it starts streaming the weight at once and waits only before it reads the
+//          shared memory and added in the order of the columns; up to four CTAs to an SM, so that all
+//          tiles are under way at once and share the memory's bandwidth evenly.  Launched behind the
+//          quantizer it starts streaming the weight at once and waits only before it reads the
 //          activations.
 #include "fp4.cuh"
 #include "umma.cuh"
@@ -40,9 +41,12 @@ struct MmParams {
   const int32_t* offsets;
   int m_tiles;                                         // tiles of one weight's rows
   int n_tile;                                          // tokens of a tile
+  int lt;                                              // of the layout of A's scales: n_tile is a multiple of it
+                                                       // (or there is one tile)
   int num_k;                                           // stages of a tile
   int n_stages;
   int splits;                                          // split kernel: CTAs of a cluster
+  int tmem_cols;                                       // and TMEM columns
   int64_t n_sf;                                        // scale tiles of a tile row
   int64_t w_sf_rows;                                   // scale tile rows of one weight
   void* Y;
@@ -61,14 +65,13 @@ __host__ __device__ __forceinline__ uint32_t stage_bytes(int format, bool pair, 
 // One output tile: weight rows from `m` on, the `count` (<= n_tile) rows of A from `row` on.
 struct Tile {
   int e, m, row, count;
-  int64_t a_sf_row;                                    // scale tile row of A, and where in it the tile
-  int a_sf_col;                                        // begins, in 32-row columns
+  int64_t a_sf_row;                                    // scale tile row of A
 };
 
 // Tiles are numbered expert by expert; inside one, bands of kBand weight tiles sweep over the tokens,
 // so that the CTAs at work at one time share both operands in L2.
-template <int TILE_M>
 __device__ __forceinline__ Tile tile_of(int t, const MmParams& p, const int* prefix) {
+  constexpr int TILE_M = 256;
   Tile x;
   x.e = 0;
   int first = 0, n = p.rows;
@@ -91,9 +94,28 @@ __device__ __forceinline__ Tile tile_of(int t, const MmParams& p, const int* pre
   x.m = (band * kBand + in_band - j * width) * TILE_M;
   x.row = first + j * p.n_tile;
   x.count = min(p.n_tile, n - j * p.n_tile);
-  x.a_sf_row = (p.n_experts > 0 ? first / kSfRows + x.e : 0) + j * p.n_tile / kSfRows;
-  x.a_sf_col = j * p.n_tile % kSfRows / 32;            // several tiles only where n_tile is a multiple of 32
+  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? first / p.lt + x.e : 0) + j * (p.n_tile / p.lt)) * ((p.lt + kSfRows - 1) / kSfRows);
   return x;
+}
+// The split kernel's order: the token tiles of one weight tile next to each other.  Dense: from the grid.
+__device__ __forceinline__ Tile tile_at(int j, int m, int e, int first, int n, const MmParams& p) {
+  Tile x;
+  x.e = e;
+  x.m = m * 128;
+  x.row = first + j * p.n_tile;
+  x.count = min(p.n_tile, n - j * p.n_tile);
+  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? first / p.lt + e : 0) + j * (p.n_tile / p.lt)) * ((p.lt + kSfRows - 1) / kSfRows);
+  return x;
+}
+__device__ __forceinline__ Tile tile_of_group(int t, const MmParams& p, const int* prefix) {
+  int lo = 0, hi = p.n_experts - 1;                    // last e with prefix[e] <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (prefix[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  const int first = clamped(p.offsets[lo], p.rows), n = clamped(p.offsets[lo + 1], p.rows) - first;
+  const int n_tiles = (n + p.n_tile - 1) / p.n_tile, m = (t - prefix[lo]) / n_tiles;
+  return tile_at(t - prefix[lo] - m * n_tiles, m, lo, first, n, p);
 }
 // Tiles of each expert as a running sum, by one warp; prefix[n_experts] is their number.
 __device__ __forceinline__ void tile_prefix(const MmParams& p, int lane, int* prefix) {
@@ -103,7 +125,7 @@ __device__ __forceinline__ void tile_prefix(const MmParams& p, int lane, int* pr
     int c = 0;
     if (e < p.n_experts) {
       const int a = p.offsets[e], z = p.offsets[e + 1];
-      if (blockIdx.x == 0 && (a < 0 || z > p.rows || z < a)) report(p.status_dev, ADADIM_ERR_SHAPE);
+      if (blockIdx.x + blockIdx.y == 0 && (a < 0 || z > p.rows || z < a)) report(p.status_dev, ADADIM_ERR_SHAPE);
       const int n = clamped(z, p.rows) - clamped(a, p.rows);
       c = n > 0 ? (n + p.n_tile - 1) / p.n_tile * p.m_tiles : 0;
     }
@@ -147,9 +169,9 @@ __device__ __forceinline__ void let_copies_land() {
 }
 
 // The MMAs of one stage: scale tiles to TMEM, then the 64-column steps that hold columns of the matrix
-// (beyond them scales need not exist).  SFT: TMEM columns of one scale tile of the tokens.
+// (beyond them scales need not exist).
 template <int FORMAT, bool PAIR>
-__device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, int a_sf_col, uint32_t w_addr, uint32_t a_addr,
+__device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, uint32_t w_addr, uint32_t a_addr,
                                             uint32_t ws_addr, uint32_t id0, uint32_t id1, int steps, bool first) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
@@ -166,7 +188,7 @@ __device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, int a_
   auto step = [&](int j) {
     const int tile = NV ? j : j / 2;
     ptx::mma_fp4<NV, PAIR>(d, ptx::with_start(desc, w_addr + j * 32), ptx::with_start(desc, a_addr + j * 32),
-                           (j & 1) ? id1 : id0, sf_tmem + tile * 4, sf_tmem + 16 + tile * kTok + a_sf_col, !(first && j == 0));
+                           (j & 1) ? id1 : id0, sf_tmem + tile * 4, sf_tmem + 16 + tile * kTok, !(first && j == 0));
   };
   if (steps == 4) {
 #pragma unroll
@@ -234,7 +256,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     bool ok = true;
     ptx::pdl_wait();
     for (int t = pair0; t < num_tiles && ok; t += pairs) {
-      const Tile x = tile_of<256>(t, p, prefix);
+      const Tile x = tile_of(t, p, prefix);
       const int half = ((x.count + 15) & ~15) >> 1;    // tokens of this CTA
       const int w_row = static_cast<int>(x.e * p.out + x.m) + static_cast<int>(rank) * 128;
       const int a_row = x.row + static_cast<int>(rank) * half;
@@ -271,7 +293,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       uint32_t phase = 0, acc_phase = 0, part_phase = 0;
       bool ok = true, ready = false;
       for (int t = pair0; t < num_tiles && ok; t += pairs) {
-        const Tile x = tile_of<256>(t, p, prefix);
+        const Tile x = tile_of(t, p, prefix);
         const int n = (x.count + 15) & ~15;
         const uint32_t id0 = ptx::idesc_fp4(256, n, !NV, 0), id1 = ptx::idesc_fp4(256, n, !NV, NV ? 0 : 2);
         ok = ptx::mbar_wait_warp(&acc_empty[buf], acc_phase ^ 1u, dead, p.status_dev);
@@ -288,11 +310,11 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           const int cur = stage;
           if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
           // asked before this stage's instructions are issued: the answer is there when they are
-          const bool next = ptx::mbar_try_wait(&full[stage], phase);
+          const bool next = ptx::mbar_test(&full[stage], phase);
           const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
           const int steps = steps_of(p.in, k);
           if (ptx::elect_one()) {
-            issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, 0, w_addr, w_addr + kWBytes,
+            issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, w_addr, w_addr + kWBytes,
                                       w_addr + kWBytes + a_bytes, id0, id1, steps, k == 0);
             ptx::mma_commit_pair(&empty[cur]);
             if (k == p.num_k - 1) ptx::mma_commit_pair(&acc_full[buf]);
@@ -313,7 +335,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     const float scale = product_scale<NV>(p);
     const uint32_t part_bar = ptx::map_to_cta(ptx::smem_addr(&part_empty), 0);
     for (int t = pair0; t < num_tiles; t += pairs) {
-      const Tile x = tile_of<256>(t, p, prefix);
+      const Tile x = tile_of(t, p, prefix);
       if (!ptx::mbar_wait_warp(&acc_full[buf], acc_phase, dead, p.status_dev)) break;
       ptx::tc_fence_after_sync();
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
@@ -353,96 +375,111 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 }
 
 // ---- split ----------------------------------------------------------------------------------------
+// Tokens that one CTA of a cluster of `splits` finishes: a multiple of four, the last CTAs may have none.
+__host__ __device__ __forceinline__ int tokens_of_cta(int count, int splits) {
+  return ((count + splits - 1) / splits + 3) & ~3;
+}
+// floats that a CTA receives: for each of its tokens and each CTA, 128 rows
+__host__ __device__ __forceinline__ int exchange_floats(int n_tile, int splits) {
+  return splits > 1 ? tokens_of_cta(n_tile, splits) * splits * 128 : 0;
+}
+
 template <int FORMAT, typename T>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads)
 fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                  const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
   constexpr int kSfTiles = kSf / kSfTileBytes;
-  constexpr uint32_t kSfCol = 128;                     // TMEM: one accumulator of 128 columns, then scales
 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full, red_full;
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_word;
-  __shared__ int prefix[kMaxGroups + 1];
   volatile int* dead = &dead_word;
   const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t stage_size = stage_bytes(FORMAT, false, p.n_tile);
   const uint32_t a_bytes = static_cast<uint32_t>(p.n_tile) * 128;
-  float* red = reinterpret_cast<float*>(smem + p.n_stages * stage_size);     // [tokens of this CTA][splits][128 rows]
-  const int rank = blockIdx.x % p.splits, t = blockIdx.x / p.splits;
-  const int k0 = static_cast<int>(static_cast<int64_t>(p.num_k) * rank / p.splits);
-  const int k1 = static_cast<int>(static_cast<int64_t>(p.num_k) * (rank + 1) / p.splits);
+  float4* red = reinterpret_cast<float4*>(smem + p.n_stages * stage_size);   // [CTA][4 tokens][128 rows]
+  int* prefix = reinterpret_cast<int*>(red + exchange_floats(p.n_tile, p.splits) / 4);      // [n_experts + 1], grouped only
+  // grid: x / splits is the token tile and y the weight tile (grouped: x / splits numbers both); splits is a power of two
+  const int rank = blockIdx.x & (p.splits - 1), t = static_cast<int>(blockIdx.x) >> (__ffs(p.splits) - 1);
+  const int k0 = p.num_k * rank / p.splits, k1 = p.num_k * (rank + 1) / p.splits;
+  const uint32_t sf_col = p.n_tile;                    // TMEM: an accumulator of n_tile columns, then scales
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < p.n_stages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
-    ptx::mbar_init(&acc_full, 1);
-    ptx::mbar_init(&red_full, 4 * p.splits);
-    dead_word = 0;
-    ptx::fence_mbar_init();
-    ptx::tma_prefetch_desc(&tmW);
-    ptx::tma_prefetch_desc(&tmA);
-    ptx::tma_prefetch_desc(&tmWs);
-    ptx::tma_prefetch_desc(&tmAs);
+  Tile x = {};
+  bool work = true;
+  if (p.n_experts > 0) {
+    if (warp == 2) tile_prefix(p, lane, prefix);
+    __syncthreads();
+    work = t < prefix[p.n_experts];       // the grid is an upper bound
+    if (work) x = tile_of_group(t, p, prefix);
+  } else {
+    x = tile_at(t, blockIdx.y, 0, 0, p.rows, p);
   }
+  const int mine = tokens_of_cta(x.count, p.splits);   // tokens finished here: [rank * mine, + tokens)
+  const int tokens = max(0, min(mine, x.count - rank * mine));
+
+  const int w_row = static_cast<int>(x.e * p.out + x.m);
+  const int w_sf = static_cast<int>((x.e * p.w_sf_rows + x.m / kSfRows) * p.n_sf * 4);
+  const int a_sf = static_cast<int>(x.a_sf_row * p.n_sf * 4);
+  auto load_w = [&](int k, int stage) {
+    uint8_t* w_dst = smem + stage * stage_size;
+    if (ptx::elect_one()) {
+      ptx::mbar_arrive_expect_tx(&full[stage], stage_size);
+      ptx::tma_load_2d(w_dst, &tmW, k * (kKT / 2), w_row, &full[stage]);
+      ptx::tma_load_2d(w_dst + kWBytes + a_bytes, &tmWs, 0, w_sf + k * kSfTiles * 4, &full[stage]);
+    }
+    __syncwarp();
+  };
+  auto load_a = [&](int k, int stage) {
+    uint8_t* a_dst = smem + stage * stage_size + kWBytes;
+    if (ptx::elect_one()) {
+      ptx::tma_load_2d(a_dst, &tmA, k * (kKT / 2), x.row, &full[stage]);
+      ptx::tma_load_2d(a_dst + a_bytes + kSf, &tmAs, 0, a_sf + k * kSfTiles * 4, &full[stage]);
+    }
+    __syncwarp();
+  };
+  const int ahead = work ? min(k1 - k0, p.n_stages) : 0;
+  if (warp == 0) {
+    // the ring's first fill starts before anything else: the weight does not depend on the launch ahead
+    if (ptx::elect_one()) {
+      for (int s = 0; s < p.n_stages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
+      ptx::mbar_init(&acc_full, 1);
+      ptx::mbar_init(&red_full, 1);
+      dead_word = 0;
+      ptx::fence_mbar_init();
+      if (p.splits > 1) ptx::mbar_arrive_expect_tx(&red_full, static_cast<uint32_t>(p.splits * ((tokens + 3) / 4) * 128 * 16));
+    }
+    __syncwarp();
+    for (int i = 0; i < ahead; ++i) load_w(k0 + i, i);
+  }
+  if (p.splits > 1) ptx::cluster_arrive();             // waited for before the first word goes to another CTA
   if (warp == 1) {
-    ptx::tmem_alloc(&tmem_slot, 256);
+    ptx::tmem_alloc(&tmem_slot, p.tmem_cols);
     ptx::tmem_relinquish();
   }
-  if (warp == 2 && p.n_experts > 0) tile_prefix(p, lane, prefix);
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (p.splits > 1) ptx::cluster_sync();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = tmem_slot;
-  const int num_tiles = p.n_experts > 0 ? prefix[p.n_experts] : (p.rows + p.n_tile - 1) / p.n_tile * p.m_tiles;
-  const bool work = t < num_tiles;                     // the grid is an upper bound where experts are ragged
-  Tile x = {};
-  if (work) x = tile_of<128>(t, p, prefix);
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
-    if (work) {
-      const int w_row = static_cast<int>(x.e * p.out + x.m);
-      const int w_sf = static_cast<int>((x.e * p.w_sf_rows + x.m / kSfRows) * p.n_sf * 4);
-      const int a_sf = static_cast<int>(x.a_sf_row * p.n_sf * 4);
-      auto load_w = [&](int k, int stage) {
-        uint8_t* w_dst = smem + stage * stage_size;
-        if (ptx::elect_one()) {
-          ptx::mbar_arrive_expect_tx(&full[stage], stage_size);
-          ptx::tma_load_2d(w_dst, &tmW, k * (kKT / 2), w_row, &full[stage]);
-          ptx::tma_load_2d(w_dst + kWBytes + a_bytes, &tmWs, 0, w_sf + k * kSfTiles * 4, &full[stage]);
-        }
-        __syncwarp();
-      };
-      auto load_a = [&](int k, int stage) {
-        uint8_t* a_dst = smem + stage * stage_size + kWBytes;
-        if (ptx::elect_one()) {
-          ptx::tma_load_2d(a_dst, &tmA, k * (kKT / 2), x.row, &full[stage]);
-          ptx::tma_load_2d(a_dst + a_bytes + kSf, &tmAs, 0, a_sf + k * kSfTiles * 4, &full[stage]);
-        }
-        __syncwarp();
-      };
-      // the ring's first fill: the weight does not depend on the launch before this one
-      const int ahead = min(k1 - k0, p.n_stages);
-      for (int i = 0; i < ahead; ++i) load_w(k0 + i, i);
-      ptx::pdl_wait();
-      for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int k = k0 + ahead; k < k1 && ok; ++k) {
-        ok = ptx::mbar_wait_warp(&empty[stage], phase, dead, p.status_dev);
-        if (!ok) break;
-        load_w(k, stage);
-        load_a(k, stage);
-        if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
-      }
-      if (!ok) let_copies_land();
+    ptx::pdl_wait();
+    for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int k = k0 + ahead; k < k1 && work; ++k) {
+      ok = ptx::mbar_wait_warp(&empty[stage], phase, dead, p.status_dev);
+      if (!ok) break;
+      load_w(k, stage);
+      load_a(k, stage);
+      if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
     }
+    if (!ok) let_copies_land();
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     if (work) {
@@ -450,21 +487,24 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       const uint32_t id0 = ptx::idesc_fp4(128, n, !NV, 0), id1 = ptx::idesc_fp4(128, n, !NV, NV ? 0 : 2);
       int stage = 0;
       uint32_t phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;
       for (int k = k0; k < k1; ++k) {
-        ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
+        if (!ready) ok = ptx::mbar_wait_warp(&full[stage], phase, dead, p.status_dev);
         if (!ok) break;
         ptx::tc_fence_after_sync();
-        const uint32_t w_addr = ptx::smem_addr(smem + stage * stage_size);
+        const int cur = stage;
+        if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
+        // asked before this stage's instructions are issued: the answer is there when they are
+        const bool next = ptx::mbar_test(&full[stage], phase);
+        const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
         const int steps = steps_of(p.in, k);
         if (ptx::elect_one()) {
-          issue_stage<FORMAT, false>(tmem, tmem + kSfCol, x.a_sf_col, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
+          issue_stage<FORMAT, false>(tmem, tmem + sf_col, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
                                      id0, id1, steps, k == k0);
-          ptx::mma_commit(&empty[stage]);
+          ptx::mma_commit(&empty[cur]);
           if (k == k1 - 1) ptx::mma_commit(&acc_full);
         }
-        __syncwarp();
-        if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
+        ready = __all_sync(0xffffffffu, next) != 0;
       }
       if (!ok) let_copies_land();
     }
@@ -476,6 +516,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     const int64_t o = x.m + row;
     T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
     const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16);
+    if (p.splits > 1) ptx::cluster_wait();             // the other CTAs have set up their barriers
     bool ok = ptx::mbar_wait_warp(&acc_full, 0, dead, p.status_dev);
     ptx::tc_fence_after_sync();
     if (p.splits == 1) {
@@ -486,48 +527,63 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         if (o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
       }
     } else {
-      // token c of the tile is finished by CTA c % splits: every CTA sends it its partial sums
+      // tokens in fours: CTA c / mine finishes token c, and every CTA sends it its partial sums
+      const uint32_t red_addr = ptx::smem_addr(red), bar_addr = ptx::smem_addr(&red_full);
+      const int fours = mine / 4;
 #pragma unroll 1
       for (int c = 0; c < x.count && ok; c += 32) {
         float v[32];
         ptx::tmem_ld32(acc + c, v);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          if (c + j < x.count) {
-            const int dst = (c + j) % p.splits, slot = (c + j) / p.splits;
-            ptx::st_cluster_f32(ptx::map_to_cta(ptx::smem_addr(red + (slot * p.splits + rank) * 128 + row), dst), v[j]);
+        for (int j = 0; j < 8; ++j) {
+          const int four = c / 4 + j;
+          if (four * 4 < x.count) {
+            const int dst = four / fours, slot = four - dst * fours;
+            ptx::st_async_v4(ptx::map_to_cta(red_addr + ((rank * fours + slot) * 128 + row) * 16, dst), v[4 * j], v[4 * j + 1],
+                             v[4 * j + 2], v[4 * j + 3], ptx::map_to_cta(bar_addr, dst));
           }
         }
       }
-      __syncwarp();
-      if (lane < p.splits) ptx::mbar_arrive_release_cluster(ptx::map_to_cta(ptx::smem_addr(&red_full), lane));
-      ok = ptx::mbar_wait_warp(&red_full, 0, dead, p.status_dev) && ok;
-      ptx::fence_acquire_cluster();
-      for (int c = rank, slot = 0; c < x.count && ok; c += p.splits, ++slot) {
-        float s = 0.0f;
-        for (int k = 0; k < p.splits; ++k) s += red[(slot * p.splits + k) * 128 + row];
-        if (o < p.out) put(y + c * p.ldy, s * scale);
+      ok = ptx::mbar_wait_warp<true>(&red_full, 0, dead, p.status_dev) && ok;
+      y += rank * mine * p.ldy;
+      for (int f = 0; f * 4 < tokens && ok; ++f) {
+        float4 s = red[f * 128 + row];
+        for (int k = 1; k < p.splits; ++k) {
+          const float4 v = red[(k * fours + f) * 128 + row];
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        if (o < p.out) {
+          put(y, s.x * scale);
+          if (f * 4 + 1 < tokens) put(y + p.ldy, s.y * scale);
+          if (f * 4 + 2 < tokens) put(y + 2 * p.ldy, s.z * scale);
+          if (f * 4 + 3 < tokens) put(y + 3 * p.ldy, s.w * scale);
+        }
+        y += 4 * p.ldy;
       }
     }
   }
 
+  if (p.splits > 1) {
+    if (warp < 2 || !work) ptx::cluster_wait();
+    ptx::cluster_arrive();                             // no CTA leaves while another may still write to it
+    ptx::cluster_wait();
+  }
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (p.splits > 1) ptx::cluster_sync();               // no CTA leaves while another may still write to it
   if (warp == 1) {
     ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc(tmem, 256);
+    ptx::tmem_dealloc(tmem, p.tmem_cols);
   }
 }
 
-constexpr size_t kSmemOne = 220 * 1024, kSmemTwo = 106 * 1024;       // dynamic shared memory at one and two CTAs per SM
+constexpr size_t kSmem = 220 * 1024;                   // dynamic shared memory of one SM's CTAs
 
 template <typename K>
-int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, unsigned grid, int threads, int cluster, size_t smem,
+int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem,
            bool chained, cudaStream_t st) {
-  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemOne)));
+  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -552,7 +608,7 @@ int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, unsigned gri
 }
 
 template <typename T>
-int launch_format(bool pair, int format, const CUtensorMap (&tm)[4], const MmParams& p, unsigned grid, size_t smem, bool chained,
+int launch_format(bool pair, int format, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, size_t smem, bool chained,
                   cudaStream_t st) {
   if (pair) return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st)
                                           : launch(fp4_pair_kernel<ADADIM_NVFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st);
@@ -560,23 +616,87 @@ int launch_format(bool pair, int format, const CUtensorMap (&tm)[4], const MmPar
                                 : launch(fp4_split_kernel<ADADIM_NVFP4, T>, tm, p, grid, kThreads, p.splits, smem, chained, st);
 }
 
+// Tiles of fewer tokens than 128 are cut no lower than this, and only up to so many rows (of a typical
+// expert), which bounds the scale tiles of the activations.
+constexpr int kMinCut = 32, kMaxCutRows = 512;
+
+// The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
+// kernels below (1.9 GHz, 148 SMs):
+//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256; a tile 500 on top; start and end 5000;
+//          it streams no faster than 1 / 1.7 of the split kernel
+//   split  a CTA's stage takes no less than 300 whatever its size, and the CTAs of an SM share 80 bytes a
+//          nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
+//          and in all no less than the weights' bytes at 6000 a nanosecond.
+Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout, int sms) {
+  const int64_t weights = n_experts > 0 ? (n_experts < rows ? n_experts : rows) : 1;
+  const int64_t typical = (rows + weights - 1) / weights;            // rows of one expert if they were equal
+  const int64_t num_k = (in + kKT - 1) / kKT;
+  // tiles of an expert's rows; experts are not equal, so half a tile more than an equal share would take
+  auto token_tiles = [&](int64_t n) { return n_experts > 0 ? weights * ((typical + typical / 2 + n - 1) / n) : (rows + n - 1) / n; };
+  Fp4Plan best = {true, 256, 1, 1};
+  double best_ns;
+  const double floor_ns = static_cast<double>(weights * out) * static_cast<double>(in) * (format == ADADIM_MXFP4 ? 0.53125 : 0.5625) / 6000.0;
+  {
+    const int64_t tiles = (out + 255) / 256 * token_tiles(256), waves = (tiles + sms / 2 - 1) / (sms / 2);
+    const double n = typical < 256 ? static_cast<double>((typical + 15) / 16 * 16) : 256.0;
+    const double stage = 270.0 * n / 256.0 < 200.0 ? 200.0 : 270.0 * n / 256.0;
+    best_ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + 500.0);
+    if (best_ns < 1.7 * floor_ns) best_ns = 1.7 * floor_ns;
+    best_ns += 5000.0;
+  }
+  for (int n_tile = 16; n_tile <= 128; n_tile *= 2) {
+    // lower tiles than 128 rows: only where they are the only ones, or the scales are laid out for them
+    if (n_tile < 128 && rows > n_tile && (!own_layout || n_tile < kMinCut || typical > kMaxCutRows)) continue;
+    if (n_tile > 16 && n_tile / 2 >= rows) break;
+    const int64_t tiles = (out + 127) / 128 * token_tiles(n_tile);
+    const size_t per = stage_bytes(format, false, n_tile);
+    for (int splits = 1; splits <= 8 && splits <= num_k; splits *= 2) {
+      const int64_t ctas = tiles * splits, k = (num_k + splits - 1) / splits;
+      const size_t fixed = exchange_floats(n_tile, splits) * 4 + 1024 + static_cast<size_t>(n_experts + 1) * 4;
+      const int stages = static_cast<int>(k < 3 ? k : 3);
+      int per_sm = static_cast<int>((ctas + sms - 1) / sms < 4 ? (ctas + sms - 1) / sms : 4);
+      while (per_sm > 1 && (per_sm * (stages * per + fixed + 1024) > kSmem || per_sm * 2 * n_tile > 512)) --per_sm;
+      if (stages * per + fixed + 1024 > kSmem) continue;
+      const int64_t waves = (ctas + static_cast<int64_t>(per_sm) * sms - 1) / (static_cast<int64_t>(per_sm) * sms);
+      const double shared = static_cast<double>(per_sm) * static_cast<double>(per) / 80.0;
+      const double stage = shared < 300.0 ? 300.0 : shared;
+      double ns = static_cast<double>(waves) * static_cast<double>(k) * stage;
+      if (ns < floor_ns) ns = floor_ns;
+      ns += 4000.0 + (splits > 1 ? 1500.0 + 15.0 * n_tile : 0.0);
+      if (ns < best_ns) { best_ns = ns; best = {false, n_tile, splits, per_sm}; }
+    }
+  }
+  return best;
+}
+
+constexpr int kSms = 148;
+
 }  // namespace
 
-int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* offsets, int n_experts,
-                      const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype, int64_t ldy,
-                      int* status_dev, bool chained, cudaStream_t st) {
-  static int sm_count = 0;
-  if (sm_count == 0) {
-    int dev = 0;
-    ADADIM_CUDA_TRY(cudaGetDevice(&dev));
-    ADADIM_CUDA_TRY(cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev));
-  }
+Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout) {
+  return plan_of(rows, out, in, n_experts, format, own_layout, kSms);
+}
+
+int64_t fp4_most_tile_rows(int64_t rows, int n_experts) {
+  const int64_t groups = n_experts > 0 ? n_experts : 1;
+  if (rows == 0) return 0;
+  const int lowest = rows <= kMaxCutRows * groups ? kMinCut : kSfRows;
+  return rows / lowest + 2 * groups + 2;
+}
+
+int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, int64_t n_rows, const int32_t* offsets,
+                      int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
+                      int64_t ldy, int* status_dev, bool chained, cudaStream_t st) {
+  const bool pair = plan.pair;
   MmParams p = {};
   p.out = out;
   p.in = in;
   p.rows = static_cast<int>(n_rows);
   p.n_experts = n_experts;
   p.offsets = offsets;
+  p.n_tile = plan.n_tile;
+  p.lt = lt;
+  p.splits = plan.splits;
   p.num_k = static_cast<int>((in + kKT - 1) / kKT);
   p.n_sf = sf_tiles(format, in);
   p.w_sf_rows = sf_tile_rows(out, 0);
@@ -585,22 +705,13 @@ int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* 
   p.a_amax = A.amax;
   p.b_amax = B.amax;
   p.status_dev = status_dev;
-  const int64_t weights = n_experts > 0 ? n_experts : 1;
-  const int64_t typical = (n_rows + weights - 1) / weights;          // rows of one expert if they were equal
-  const bool pair = typical > 128;
-  if (pair) {
-    p.n_tile = 256;
-  } else {
-    // several tiles of one expert begin at multiples of 32 rows (the scale tiles' columns)
-    const int64_t want = n_experts > 0 ? (2 * typical < n_rows ? 2 * typical : n_rows) : n_rows;
-    p.n_tile = want <= 16 && want == n_rows ? 16 : want <= 32 ? 32 : want <= 64 ? 64 : 128;
-  }
   p.m_tiles = static_cast<int>((out + (pair ? 255 : 127)) / (pair ? 256 : 128));
   // dense: the tiles are known here; grouped: at most one partial tile for every expert on top
-  int64_t tiles = (n_rows + p.n_tile - 1) / p.n_tile;
-  if (n_experts > 0) tiles += n_experts < n_rows ? n_experts : n_rows;
-  tiles *= p.m_tiles;
+  int64_t token_tiles = (n_rows + p.n_tile - 1) / p.n_tile;
+  if (n_experts > 0) token_tiles += n_experts < n_rows ? n_experts : n_rows;
+  const int64_t tiles = token_tiles * p.m_tiles;
 
+  const int64_t weights = n_experts > 0 ? n_experts : 1;
   const uint64_t inner = static_cast<uint64_t>((in + 1) / 2);
   const uint32_t sf_box = sf_stage_bytes(format) / 128;
   CUtensorMap tm[4];
@@ -609,27 +720,25 @@ int fp4_matmul_launch(const adadim_fp4tensor& A, int64_t n_rows, const int32_t* 
   if ((rc = make_tmap_u8(&tm[1], A.codes, inner, static_cast<uint64_t>(n_rows), static_cast<uint64_t>(A.ld),
                          static_cast<uint32_t>(pair ? p.n_tile / 2 : p.n_tile), true)) != ADADIM_OK) return rc;
   if ((rc = make_tmap_u8(&tm[2], B.scales, 128, weights * scale_bytes(format, out, in, 0) / 128, 128, sf_box, false)) != ADADIM_OK) return rc;
-  if ((rc = make_tmap_u8(&tm[3], A.scales, 128, scale_bytes(format, n_rows, in, n_experts) / 128, 128, sf_box, false)) != ADADIM_OK) return rc;
+  if ((rc = make_tmap_u8(&tm[3], A.scales, 128, static_cast<uint64_t>(sf_tile_rows(n_rows, n_experts, lt) * p.n_sf * 4), 128, sf_box, false)) != ADADIM_OK) return rc;
 
   const size_t per = stage_bytes(format, pair, p.n_tile);
-  unsigned grid;
-  size_t smem;
+  size_t fixed = 1024;                                 // alignment, and what lies behind the ring
+  dim3 grid;
   if (pair) {
-    p.n_stages = static_cast<int>((kSmemOne - 1024) / per);
-    if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
-    grid = static_cast<unsigned>(2 * (tiles < sm_count / 2 ? tiles : sm_count / 2));
-    smem = p.n_stages * per + 1024;
+    grid = dim3(static_cast<unsigned>(2 * (tiles < kSms / 2 ? tiles : kSms / 2)));
+    p.n_stages = static_cast<int>((kSmem - fixed) / per);
   } else {
-    // split the columns until there are two CTAs for every SM
-    p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= 2 * sm_count && p.splits * 2 <= p.num_k) p.splits *= 2;
-    const size_t red = p.splits > 1 ? static_cast<size_t>((p.n_tile + p.splits - 1) / p.splits) * p.splits * 512 : 0;
-    p.n_stages = static_cast<int>((kSmemTwo - 1024 - red) / per);
-    if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
-    if (p.n_stages < 2) p.n_stages = 2;
-    grid = static_cast<unsigned>(tiles * p.splits);
-    smem = p.n_stages * per + red + 1024;
+    grid = n_experts > 0 ? dim3(static_cast<unsigned>(tiles * p.splits))
+                         : dim3(static_cast<unsigned>(token_tiles * p.splits), static_cast<unsigned>(p.m_tiles));
+    p.tmem_cols = p.n_tile <= 32 ? 64 : 2 * p.n_tile;
+    fixed += exchange_floats(p.n_tile, p.splits) * 4 + static_cast<size_t>(n_experts > 0 ? n_experts + 1 : 0) * 4;
+    p.n_stages = static_cast<int>((kSmem / plan.per_sm - 1024 - fixed) / per);     // 1024: a CTA's share kept by the system
+    const int k = (p.num_k + p.splits - 1) / p.splits;
+    if (p.n_stages > k) p.n_stages = k;
   }
+  if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
+  const size_t smem = p.n_stages * per + fixed;
   if (ydtype == ADADIM_F32) return launch_format<float>(pair, format, tm, p, grid, smem, chained, st);
   if (ydtype == ADADIM_F16) return launch_format<__half>(pair, format, tm, p, grid, smem, chained, st);
   return launch_format<__nv_bfloat16>(pair, format, tm, p, grid, smem, chained, st);

@@ -102,7 +102,7 @@ __device__ __forceinline__ uint32_t widen(const Raw<T>& r, float (&v)[kPer]) {
 struct QuantParams {
   const void* X;
   int64_t cols, ldx, x_rows;
-  int rows;
+  int rows, lt;
   const int32_t* row_index;
   const int32_t* offsets;
   int n_groups;
@@ -128,8 +128,8 @@ quantize_kernel(const QuantParams p) {
   const int n_sf = static_cast<int>(p.n_sf);
   const int v = blockIdx.x / n_sf;                            // tile row
   const int cx = blockIdx.x - v * n_sf;
-  int first = v * kSfRows, count = min(kSfRows, p.rows - first);
-  if (p.offsets != nullptr) rows_of_tile_row(p.offsets, p.n_groups, p.rows, v, first, count);
+  int first, count;
+  rows_of_tile_row(p.offsets, p.n_groups, p.rows, p.lt, v, first, count);
   if (count <= 0) return;
 
   const int chunk = threadIdx.x % kChunks;
@@ -272,7 +272,7 @@ int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t
 
 int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
                         const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor& q,
-                        void* values, int vdtype, int64_t ldv, cudaStream_t st) {
+                        int lt, void* values, int vdtype, int64_t ldv, cudaStream_t st) {
   const int64_t esz = xdtype == ADADIM_F32 ? 4 : 2, vsz = vdtype == ADADIM_F32 ? 4 : 2;
   QuantParams p = {};
   p.X = X;
@@ -280,6 +280,7 @@ int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, i
   p.ldx = ldx;
   p.x_rows = x_rows;
   p.rows = static_cast<int>(rows);
+  p.lt = lt;
   p.row_index = row_index;
   p.offsets = offsets;
   p.n_groups = n_groups;
@@ -295,7 +296,7 @@ int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, i
   p.wide_v = values != nullptr && reinterpret_cast<uintptr_t>(values) % 32 == 0 && (ldv * vsz) % 32 == 0;
   p.x_begin = x0;
   p.x_end = x0 + static_cast<uintptr_t>(((x_rows - 1) * ldx + cols) * esz);
-  const dim3 grid(static_cast<unsigned>(p.n_sf * sf_tile_rows(rows, n_groups)));
+  const dim3 grid(static_cast<unsigned>(p.n_sf * sf_tile_rows(rows, n_groups, lt)));
   const int vsel = values == nullptr ? 0 : vdtype == ADADIM_BF16 ? 1 : 2;
   if (xdtype == ADADIM_F32) launch_format<float>(p, format, vsel, grid, st);
   else if (xdtype == ADADIM_F16) launch_format<__half>(p, format, vsel, grid, st);
