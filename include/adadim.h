@@ -348,7 +348,7 @@ ADADIM_API int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t co
  *   MXFP4  scale = 2^(floor(log2 m) - 2), at least 2^-127;  element = nearest level to x / scale,
  *          at most 6
  *   NVFP4  s = nearest E4M3 to m / (6 t), at most 448;  element = nearest level to x / (s t), at
- *          most 6; zero where s is 0.  The sign bit is that of x in every code, zeros included
+ *          most 6; zero where s is 0.  (The sign bit of a zero code is not specified.)
  *   A block that holds an infinity or a NaN gets a NaN scale (0xFF / 0x7F) and codes 0: its
  *   values, and every product with it, are NaN.
  *   X          [x_rows][cols], xdtype any, ldx in elements.  16-byte aligned rows take the wide

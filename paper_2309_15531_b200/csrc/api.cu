@@ -142,12 +142,14 @@ int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ld
   A.scales = A.codes + fp4_code_bytes(rows, in);
   A.amax = x_amax;
   A.ld = fp4::code_pitch(in);
-  const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, true);
-  rc = quantize_fp4_launch(X, xdtype, rows, in, ldx, x_rows, format, row_index, offsets, n_experts, A, plan.n_tile, nullptr,
-                           ADADIM_BF16, 0, st);
-  if (rc != ADADIM_OK) return rc;
-  return fp4_matmul_launch(plan, A, plan.n_tile, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
-                           true, st);
+  const fp4::Source x = fp4::source_of(X, xdtype, ldx, x_rows, in, row_index);
+  const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, false, xdtype == ydtype && x.wide != 0 && in % fp4::kPer == 0);
+  if (!plan.fused) {
+    rc = quantize_fp4_launch(x, xdtype, rows, in, format, offsets, n_experts, A, plan.n_tile, nullptr, ADADIM_BF16, 0, st);
+    if (rc != ADADIM_OK) return rc;
+  }
+  return fp4_matmul_launch(plan, A, plan.n_tile, x, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
+                           !plan.fused, st);
 }
 
 }  // namespace
@@ -418,8 +420,8 @@ int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, i
   if ((reinterpret_cast<uintptr_t>(row_index) & 3u) != 0) return ADADIM_ERR_ALIGN;
   if ((rc = check_fp4(q, cols)) != ADADIM_OK) return rc;
   if (values != nullptr && (rc = check_matrix(values, vdtype, cols, ldv)) != ADADIM_OK) return rc;
-  return quantize_fp4_launch(X, xdtype, rows, cols, ldx, x_rows, format, row_index, offsets, n_groups, *q, fp4::kSfRows,
-                             values, vdtype, ldv, static_cast<cudaStream_t>(cuda_stream));
+  return quantize_fp4_launch(fp4::source_of(X, xdtype, ldx, x_rows, cols, row_index), xdtype, rows, cols, format, offsets,
+                             n_groups, *q, fp4::kSfRows, values, vdtype, ldv, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,
@@ -428,7 +430,7 @@ int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_
   int rc = check_fp4_product(n_tokens, out, in, format, nullptr, 0, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(fp4_plan(n_tokens, out, in, 0, format, false), *A, fp4::kSfRows, n_tokens, nullptr, 0, *B, out,
+  return fp4_matmul_launch(fp4_plan(n_tokens, out, in, 0, format, true, false), *A, fp4::kSfRows, {}, n_tokens, nullptr, 0, *B, out,
                            in, format, Y, ydtype, ldy, status_dev, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -440,7 +442,7 @@ int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_rows, const i
   int rc = check_fp4_product(n_rows, out, in, format, offsets, n_experts, B, Y, ydtype, ldy, &empty);
   if (rc != ADADIM_OK || empty) return rc;
   if ((rc = check_fp4(A, in)) != ADADIM_OK) return rc;
-  return fp4_matmul_launch(fp4_plan(n_rows, out, in, n_experts, format, false), *A, fp4::kSfRows, n_rows, offsets, n_experts,
+  return fp4_matmul_launch(fp4_plan(n_rows, out, in, n_experts, format, true, false), *A, fp4::kSfRows, {}, n_rows, offsets, n_experts,
                            *B, out, in, format, Y, ydtype, ldy, status_dev, false, static_cast<cudaStream_t>(cuda_stream));
 }
 

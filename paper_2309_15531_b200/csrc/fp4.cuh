@@ -72,15 +72,39 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {
   return __half2float(__ushort_as_half(static_cast<uint16_t>(h2 & 0xffffu)));
 }
 
-// The scale of a block with largest magnitude m (NaN if the block holds one).  What is returned:
-// the byte, and the divisor of the elements as (s, 1 / s correctly rounded); s = 0 means all codes 0.
+// Two binary32 operations at once (the packed instructions of this architecture).
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// The scale of a block with largest magnitude m (NaN if the block holds one).  What is returned: the
+// byte, and the divisor of the elements as s and 1 / s (exact for MXFP4; for NVFP4 correctly rounded, or
+// with X16 within an ulp); s = 0 means that every value is 0.
 struct BlockScale {
   uint32_t byte;
   float s, rcp;
   bool finite;
   bool far;                // NVFP4: quotients of binary32 numbers may overflow (amax far below the block's m)
 };
-template <int FORMAT>
+template <int FORMAT, bool X16>
 __device__ __forceinline__ BlockScale block_scale(float m, int t_log2) {
   BlockScale b;
   const bool finite = m < INFINITY;                                  // false for NaN too
@@ -94,40 +118,52 @@ __device__ __forceinline__ BlockScale block_scale(float m, int t_log2) {
     b.s = byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(static_cast<uint32_t>(byte) << 23);
     b.rcp = __uint_as_float(static_cast<uint32_t>(254 - byte) << 23);
   } else {
-    // m / t is exact.  The binary32 quotient by 6 decides every comparison with a number of at most
-    // 5 significant bits as the exact quotient does: a number that is not the midpoint c differs from
-    // it by at least an ulp of the dividend 6 c, which is more than half an ulp of the quotient.
-    const float u = __fdiv_rn(m * exp2_int(-t_log2), 6.0f);
+    // m / t is exact (and cut where it is far beyond the largest scale anyway).  The correctly rounded
+    // quotient by 6 decides every comparison with a number of at most 5 significant bits as the exact
+    // quotient does: a number that is not the midpoint c differs from it by at least an ulp of the dividend
+    // 6 c, which is more than half an ulp of the quotient.
+    const float u = quotient(fminf(m * exp2_int(-t_log2), 1e30f), 6.0f, 1.0f / 6.0f);
     b.byte = finite ? e4m3_of(u) : 0x7fu;
     const float sf = finite ? e4m3_value(b.byte) : 0.0f;
     b.s = sf * exp2_int(t_log2);
-    b.rcp = b.s > 0.0f ? __frcp_rn(b.s) : 0.0f;
-    b.far = m * b.rcp > 1e30f;
+    if (X16) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b.rcp) : "f"(b.s));
+    else b.rcp = __frcp_rn(b.s);
+    if (!(b.s > 0.0f)) b.rcp = 0.0f;
+    if (!X16) b.far = m * b.rcp > 1e30f;
   }
   return b;
 }
-// x / s as the quantizer needs it: something that lies on the same side of (or on) every midpoint c
-// of two levels as the exact quotient, and keeps the sign of a zero.
+// The eight codes of v[0..7], elements of one block, from x / s in a form that lies on the same side of
+// (or on) every midpoint c of two levels as the exact quotient:
 //   MXFP4: exact (s is a power of two).
-//   NVFP4, x of a 16-bit type: x * (1 / s) is within 2^-23 of the quotient; a quotient that is not c
-//     differs from it by 2^-11 or more (x has at most 11 significant bits, c s at most 7), so rounding
-//     the product to 17 significant bits restores exact midpoints and moves nothing across one.
+//   NVFP4, x of a 16-bit type: x * (1 / s) is within 2^-22 of the quotient, relatively, and 5 is the largest c.
+//     A quotient that is not c differs from it by 2^-11 c or more (x has at most 11 significant bits, c s at
+//     most 7) and c is at least 1/4, so rounding to multiples of 2^-18, by adding 48 and taking it away,
+//     restores exact midpoints and moves nothing across one.
 //   NVFP4, x binary32: the correctly rounded quotient, by the argument given for the block scale.
-template <int FORMAT, bool X16>
-__device__ __forceinline__ float scaled(float x, const BlockScale& b) {
-  if (FORMAT == ADADIM_MXFP4) return x * b.rcp;
-  if (X16) return __uint_as_float((__float_as_uint(x * b.rcp) + 0x40u) & ~0x7fu);
-  return copysignf(quotient(x, b.s, b.rcp), x);
-}
-// The eight codes of v[0..7], elements of one block
+// The sign of a zero is not kept.
 template <int FORMAT, bool X16>
 __device__ __forceinline__ uint32_t codes8(const float* v, const BlockScale& b) {
   float q[8];
+  const uint64_t rcp = pack2(b.rcp, b.rcp);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    float x = v[k];
-    if (FORMAT == ADADIM_NVFP4 && !X16 && b.far) x = fminf(fmaxf(x, -8.0f * b.s), 8.0f * b.s);   // beyond 6 s all the same
-    q[k] = scaled<FORMAT, X16>(x, b);
+  for (int k = 0; k < 8; k += 2) {
+    float x0 = v[k], x1 = v[k + 1];
+    if (FORMAT == ADADIM_NVFP4 && !X16 && b.far) {                   // beyond 6 s all the same
+      x0 = fminf(fmaxf(x0, -8.0f * b.s), 8.0f * b.s);
+      x1 = fminf(fmaxf(x1, -8.0f * b.s), 8.0f * b.s);
+    }
+    const uint64_t x = pack2(x0, x1);
+    uint64_t y;
+    if (FORMAT == ADADIM_MXFP4) {
+      y = mul2(x, rcp);
+    } else if (X16) {
+      y = add2(fma2(x, rcp, pack2(48.0f, 48.0f)), pack2(-48.0f, -48.0f));
+    } else {
+      const uint64_t q0 = mul2(x, rcp);
+      y = fma2(fma2(pack2(-b.s, -b.s), q0, x), rcp, q0);
+    }
+    unpack2(y, q[k], q[k + 1]);
   }
   const uint32_t r = e2m1_pack8(q);
   return b.finite ? r : 0u;
@@ -150,21 +186,143 @@ __device__ __forceinline__ void e2m1_values8(uint32_t codes, float (&v)[8]) {
   }
 }
 
-// The rows that scale tile row v holds (see sf_tile_rows): first and count, 0 if it holds none.  Groups are
-// found by bisection over the clamped offsets.
+// ---- a matrix to be quantized: 16 consecutive elements at a time -------------------------------------
+constexpr int kPer = 16;
+struct Source {
+  const void* X;
+  int64_t ldx, x_rows;
+  const int32_t* row_index;   // row r is X[row_index[r]], zeros where that is outside; NULL: X[r]
+  uintptr_t begin, end;       // the bytes of X: no 16-byte block that leaves them is loaded whole
+  int wide;                   // every row starts on a 32-byte boundary
+};
+inline Source source_of(const void* X, int dtype, int64_t ldx, int64_t x_rows, int64_t cols, const int32_t* row_index) {
+  const int64_t esz = dtype == ADADIM_F32 ? 4 : 2;
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(X);
+  Source s = {X, ldx, x_rows, row_index, x0, x0, x0 % 32 == 0 && (ldx * esz) % 32 == 0};
+  if (x_rows > 0) s.end = x0 + static_cast<uintptr_t>(((x_rows - 1) * ldx + cols) * esz);
+  return s;
+}
+template <typename T> struct Elem;
+template <> struct Elem<__half> {
+  typedef __half2 Two;
+  static __device__ __forceinline__ float to_f32(uint16_t b) { return __half2float(__ushort_as_half(b)); }
+  static __device__ __forceinline__ Two abs2(uint32_t w) { return __habs2(*reinterpret_cast<const Two*>(&w)); }
+  static __device__ __forceinline__ float2 widen2(uint32_t w) { return __half22float2(*reinterpret_cast<const Two*>(&w)); }
+  static __device__ __forceinline__ float top_f32(Two t) { return __half2float(__hmax_nan(__low2half(t), __high2half(t))); }
+};
+template <> struct Elem<__nv_bfloat16> {
+  typedef __nv_bfloat162 Two;
+  static __device__ __forceinline__ float to_f32(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
+  static __device__ __forceinline__ Two abs2(uint32_t w) { return __habs2(*reinterpret_cast<const Two*>(&w)); }
+  static __device__ __forceinline__ float2 widen2(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+  static __device__ __forceinline__ float top_f32(Two t) { return __bfloat162float(__hmax_nan(__low2bfloat16(t), __high2bfloat16(t))); }
+};
+
+// The sixteen elements of a thread as they lie in memory, and their loads.
+template <typename T> struct Raw { uint32_t w[kPer * sizeof(T) / 4]; };
+
+__device__ __forceinline__ void load32(const void* p, uint32_t* w) {            // 32-byte aligned
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+template <typename T>
+__device__ __forceinline__ void load16_aligned(const T* p, Raw<T>& r) {
+  load32(p, r.w);
+  if constexpr (sizeof(T) == 4) load32(p + 8, r.w + 8);
+}
+// Any alignment: the 16-byte blocks that hold the elements, shifted into place.  The caller has checked
+// that the blocks lie inside the matrix.
+template <typename T>
+__device__ __forceinline__ void load16_shifted(const T* p, Raw<T>& r) {
+  constexpr int kW = kPer * sizeof(T) / 4;
+  const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u;
+  const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) - off);
+  uint32_t w[kW + 4];
+#pragma unroll
+  for (int k = 0; k <= kW / 4; ++k) {
+    const uint4 v = k < kW / 4 || off != 0 ? __ldg(q + k) : make_uint4(0, 0, 0, 0);
+    w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+  }
+#pragma unroll
+  for (int k = 0; k < kW + 2; ++k) if (off & 8u) w[k] = w[k + 2];
+#pragma unroll
+  for (int k = 0; k < kW + 1; ++k) if (off & 4u) w[k] = w[k + 1];
+#pragma unroll
+  for (int k = 0; k < kW; ++k) r.w[k] = sizeof(T) == 2 ? __funnelshift_r(w[k], w[k + 1], (off & 2u) * 8) : w[k];
+}
+// The first n elements one by one, zeros behind them.
+template <typename T>
+__device__ __forceinline__ void load16_narrow(const T* p, int n, Raw<T>& r) {
+#pragma unroll
+  for (int k = 0; k < kPer * static_cast<int>(sizeof(T)) / 4; ++k) {
+    if constexpr (sizeof(T) == 2) {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+      const uint32_t lo = 2 * k < n ? h[2 * k] : 0u, hi = 2 * k + 1 < n ? h[2 * k + 1] : 0u;
+      r.w[k] = lo | (hi << 16);
+    } else {
+      r.w[k] = k < n ? reinterpret_cast<const uint32_t*>(p)[k] : 0u;
+    }
+  }
+}
+// Widened to binary32; the largest magnitude as a binary32 pattern (patterns are ordered as integers)
+template <typename T>
+__device__ __forceinline__ uint32_t widen(const Raw<T>& r, float (&v)[kPer]) {
+  if constexpr (sizeof(T) == 2) {
+    typename Elem<T>::Two top = Elem<T>::abs2(r.w[0]);
+#pragma unroll
+    for (int k = 1; k < 8; ++k) top = __hmax2_nan(top, Elem<T>::abs2(r.w[k]));   // a NaN stays on top
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 f = Elem<T>::widen2(r.w[k]);
+      v[2 * k] = f.x;
+      v[2 * k + 1] = f.y;
+    }
+    return __float_as_uint(Elem<T>::top_f32(top)) & 0x7fffffffu;
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      v[k] = __uint_as_float(r.w[k]);
+      m = max(m, r.w[k] & 0x7fffffffu);
+    }
+    return m;
+  }
+}
+
+// Row r of the matrix in X, or -1 for a row of zeros.
+__device__ __forceinline__ int64_t source_row(const Source& s, int64_t r) {
+  if (s.row_index == nullptr) return r;
+  const int64_t src = s.row_index[r];
+  return src < 0 || src >= s.x_rows ? -1 : src;
+}
+// Elements c0 .. c0 + n - 1 of row src of X (n = 0 or src = -1: none), zeros behind them.
+template <typename T>
+__device__ __forceinline__ void load16(const Source& s, int64_t src, int64_t c0, int n, Raw<T>& r) {
+  const T* at = static_cast<const T*>(s.X) + src * s.ldx + c0;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+  if (src < 0 || n == 0) load16_narrow(at, 0, r);
+  else if (n == kPer && s.wide) load16_aligned(at, r);
+  else if (n == kPer && (a & ~uintptr_t(15)) >= s.begin && a + kPer * sizeof(T) + 15 < s.end) load16_shifted(at, r);
+  else load16_narrow(at, n, r);
+}
+
+// The rows that scale tile row v holds (see sf_tile_rows): first and count, 0 if it holds none.  For a whole
+// converged warp: the group is found by counting over the clamped offsets, all of which are loaded at once.
 __device__ __forceinline__ int clamped(int v, int rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 __device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_groups, int rows, int lt, int v, int& first, int& count) {
   const int sub = (lt + kSfRows - 1) / kSfRows, cut = v / sub, part = v - cut * sub;
   int a = 0, z = rows, skip = cut * lt;
   if (offsets != nullptr) {
-    int lo = 0, hi = n_groups - 1;                                   // last e with offsets[e] / lt + e <= cut
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (clamped(offsets[mid], rows) / lt + mid <= cut) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x & 31;
+    int n = 0;                                                       // groups with offsets[e] / lt + e <= cut
+    for (int e0 = 0; e0 < n_groups; e0 += 32) {
+      const int e = e0 + lane;
+      n += __popc(__ballot_sync(0xffffffffu, e < n_groups && clamped(offsets[e], rows) / lt + e <= cut));
     }
-    a = clamped(offsets[lo], rows);
-    z = clamped(offsets[lo + 1], rows);
-    skip = (cut - (a / lt + lo)) * lt;
+    const int e = n > 0 ? n - 1 : 0;
+    a = clamped(offsets[e], rows);
+    z = clamped(offsets[e + 1], rows);
+    skip = (cut - (a / lt + e)) * lt;
   }
   first = a + skip + part * kSfRows;
   count = skip < 0 ? 0 : min(min(lt - part * kSfRows, kSfRows), z - first);
@@ -175,19 +333,23 @@ __device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_g
 
 // implemented in fp4_quant.cu and fp4_matmul.cu
 int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, cudaStream_t st);
-int quantize_fp4_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
-                        const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor& q,
-                        int lt, void* values, int vdtype, int64_t ldv, cudaStream_t st);
+int quantize_fp4_launch(const fp4::Source& x, int xdtype, int64_t rows, int64_t cols, int format, const int32_t* offsets,
+                        int n_groups, const adadim_fp4tensor& q, int lt, void* values, int vdtype, int64_t ldv,
+                        cudaStream_t st);
 // How a product is laid out on the SMs.
 struct Fp4Plan {
   bool pair;               // which kernel
   int n_tile;              // tokens of a tile
   int splits, per_sm;      // split kernel: CTAs of a cluster, CTAs of an SM
+  bool fused;              // it quantizes the activations itself
 };
-// own_layout: the activations' scales are laid out as the plan likes best (lt = n_tile), otherwise lt = 128
-Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout);
-int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, int64_t n_rows, const int32_t* offsets,
-                      int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
+// The activations come quantized (lt = 128), or the library quantizes them: then their scales are laid out as
+// the plan likes best (lt = n_tile), and `fuse` says that the product could do it
+// (X and Y of one type, 32-byte aligned rows, whole sixteens of columns).
+Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool quantized, bool fuse);
+// A: quantized activations, or with plan.fused only their amax, and x the matrix itself.
+int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, const fp4::Source& x, int64_t n_rows,
+                      const int32_t* offsets, int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
                       int64_t ldy, int* status_dev, bool chained, cudaStream_t st);
 // the most scale tile rows that activations take in any plan's layout
 int64_t fp4_most_tile_rows(int64_t rows, int n_experts);

@@ -32,6 +32,9 @@ constexpr int kThreads = 192;                          // TMA warp, MMA warp, fo
 constexpr int kPairThreads = 320;                      // pair kernel: eight
 constexpr int kMaxStages = 8;
 constexpr uint32_t kWBytes = 128 * 128;
+constexpr int kFusedThreads = 320;                     // split kernel that quantizes: four warps more,
+constexpr int kFusedPerSm = 3;                         // CTAs of an SM (by its registers)
+constexpr int kFusedTile = 16;                         // and tokens of a tile
 constexpr int kBand = 8;                               // weight tiles that share a sweep over the tokens
 
 struct MmParams {
@@ -47,6 +50,7 @@ struct MmParams {
   int n_stages;
   int splits;                                          // split kernel: CTAs of a cluster
   int tmem_cols;                                       // and TMEM columns
+  Source x;                                            // and, where it quantizes the activations, those
   int64_t n_sf;                                        // scale tiles of a tile row
   int64_t w_sf_rows;                                   // scale tile rows of one weight
   void* Y;
@@ -384,8 +388,10 @@ __host__ __device__ __forceinline__ int exchange_floats(int n_tile, int splits) 
   return splits > 1 ? tokens_of_cta(n_tile, splits) * splits * 128 : 0;
 }
 
-template <int FORMAT, typename T>
-__global__ void __launch_bounds__(kThreads)
+// FUSED: the activations are p.x, of type T, and eight warps (the epilogue's four among them) quantize
+// them into the ring; a tile has up to 16 tokens, a warp takes two of them.
+template <int FORMAT, typename T, bool FUSED>
+__global__ void __launch_bounds__(FUSED ? kFusedThreads : kThreads, FUSED ? kFusedPerSm : 4)
 fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
                  const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
@@ -406,7 +412,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   // grid: x / splits is the token tile and y the weight tile (grouped: x / splits numbers both); splits is a power of two
   const int rank = blockIdx.x & (p.splits - 1), t = static_cast<int>(blockIdx.x) >> (__ffs(p.splits) - 1);
   const int k0 = p.num_k * rank / p.splits, k1 = p.num_k * (rank + 1) / p.splits;
-  const uint32_t sf_col = p.n_tile;                    // TMEM: an accumulator of n_tile columns, then scales
+  const uint32_t sf_col = p.n_tile;                    // TMEM: an accumulator of n_tile columns, then scales of two stages
 
   Tile x = {};
   bool work = true;
@@ -427,7 +433,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   auto load_w = [&](int k, int stage) {
     uint8_t* w_dst = smem + stage * stage_size;
     if (ptx::elect_one()) {
-      ptx::mbar_arrive_expect_tx(&full[stage], stage_size);
+      ptx::mbar_arrive_expect_tx(&full[stage], FUSED ? kWBytes + kSf : stage_size);
       ptx::tma_load_2d(w_dst, &tmW, k * (kKT / 2), w_row, &full[stage]);
       ptx::tma_load_2d(w_dst + kWBytes + a_bytes, &tmWs, 0, w_sf + k * kSfTiles * 4, &full[stage]);
     }
@@ -442,10 +448,14 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     __syncwarp();
   };
   const int ahead = work ? min(k1 - k0, p.n_stages) : 0;
+  // FUSED: warps that share a stage (two tokens each), and stages under way at once.  Not more than the ring
+  // has: a warp's wait for its next place would otherwise be two phases of that barrier ahead.
+  const int sharing = x.count > 8 ? 8 : x.count > 4 ? 4 : x.count > 2 ? 2 : 1;
+  const int in_turn = min(8 / sharing, p.n_stages);
   if (warp == 0) {
     // the ring's first fill starts before anything else: the weight does not depend on the launch ahead
     if (ptx::elect_one()) {
-      for (int s = 0; s < p.n_stages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
+      for (int s = 0; s < p.n_stages; ++s) { ptx::mbar_init(&full[s], FUSED ? 1 + sharing : 1); ptx::mbar_init(&empty[s], 1); }
       ptx::mbar_init(&acc_full, 1);
       ptx::mbar_init(&red_full, 1);
       dead_word = 0;
@@ -467,8 +477,10 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
-    ptx::pdl_wait();
-    for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
+    if (!FUSED) {
+      ptx::pdl_wait();
+      for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
+    }
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -476,7 +488,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       ok = ptx::mbar_wait_warp(&empty[stage], phase, dead, p.status_dev);
       if (!ok) break;
       load_w(k, stage);
-      load_a(k, stage);
+      if (!FUSED) load_a(k, stage);
       if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
     }
     if (!ok) let_copies_land();
@@ -499,7 +511,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
         const int steps = steps_of(p.in, k);
         if (ptx::elect_one()) {
-          issue_stage<FORMAT, false>(tmem, tmem + sf_col, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
+          issue_stage<FORMAT, false>(tmem, tmem + sf_col + (k & 1) * 32, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
                                      id0, id1, steps, k == k0);
           ptx::mma_commit(&empty[cur]);
           if (k == k1 - 1) ptx::mma_commit(&acc_full);
@@ -509,6 +521,53 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       if (!ok) let_copies_land();
     }
   } else if (work) {
+    if (FUSED) {
+      // ---------------------------------------------------------------- quantizer (warps 2..9)
+      // 16 columns of a token per lane, two tokens across the lanes; the next stage's are loaded while this
+      // one's are worked on.  Rows behind `count` are left as they are in the ring: what they give lands in
+      // columns of the accumulator that nobody reads.
+      const int group = (warp - 2) / sharing, chunk = lane & 15;
+      const int r = ((warp - 2) - group * sharing) * 2 + (lane >> 4);
+      const int64_t src = r < x.count ? source_row(p.x, static_cast<int64_t>(x.row) + r) : -1;
+      const T* at = static_cast<const T*>(p.x.X) + (src < 0 ? 0 : src * p.x.ldx);
+      const int t_log2 = NV ? tensor_scale_log2(p.a_amax) : 0;
+      const uint32_t a_at = r * 128 + (((chunk >> 1) ^ (r & 7)) << 4) + (chunk & 1) * 8;
+      const int blk = NV ? chunk : chunk >> 1;
+      const uint32_t s_at = (blk >> 2) * kSfTileBytes + r * 16 + (blk & 3);
+      Raw<T> next;
+      auto load = [&](int i) {
+        const int64_t c0 = static_cast<int64_t>(k0 + i) * kKT + chunk * kPer;
+        if (src >= 0 && c0 < p.in) load16_aligned(at + c0, next);
+        else
+#pragma unroll
+          for (uint32_t& w : next.w) w = 0;
+      };
+      if (group < in_turn) load(group);
+      int slot = group;
+      uint32_t phase = 0;
+      for (int i = group; group < in_turn && i < k1 - k0; i += in_turn) {
+        float v[kPer];
+        uint32_t top = widen(next, v);
+        load(i + in_turn);
+        if (!NV) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        const BlockScale b = block_scale<FORMAT, sizeof(T) == 2>(__uint_as_float(top), t_log2);
+        uint2 c;
+        c.x = codes8<FORMAT, sizeof(T) == 2>(v, b);
+        c.y = codes8<FORMAT, sizeof(T) == 2>(v + 8, b);
+        if (!ptx::mbar_wait_warp(&empty[slot], phase ^ 1u, dead, p.status_dev)) break;
+        uint8_t* a_dst = smem + slot * stage_size + kWBytes;
+        if (r < x.count) {
+          *reinterpret_cast<uint2*>(a_dst + a_at) = c;
+          if (NV || (chunk & 1) == 0) (a_dst + a_bytes + kSf)[s_at] = static_cast<uint8_t>(b.byte);
+        }
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&full[slot]);
+        slot += in_turn;
+        if (slot >= p.n_stages) { slot -= p.n_stages; phase ^= 1u; }
+      }
+    }
+    if (warp < 6) {
     // ------------------------------------------------------------------ epilogue (warps 2..5)
     const int q = warp & 3;                            // TMEM lane quadrant this warp may read
     const float scale = product_scale<NV>(p);
@@ -561,10 +620,11 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         y += 4 * p.ldy;
       }
     }
+    }
   }
 
   if (p.splits > 1) {
-    if (warp < 2 || !work) ptx::cluster_wait();
+    if (warp < 2 || warp >= 6 || !work) ptx::cluster_wait();
     ptx::cluster_arrive();                             // no CTA leaves while another may still write to it
     ptx::cluster_wait();
   }
@@ -608,17 +668,23 @@ int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, i
 }
 
 template <typename T>
-int launch_format(bool pair, int format, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, size_t smem, bool chained,
+int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, size_t smem, bool chained,
                   cudaStream_t st) {
   if (pair) return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st)
                                           : launch(fp4_pair_kernel<ADADIM_NVFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st);
-  return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T>, tm, p, grid, kThreads, p.splits, smem, chained, st)
-                                : launch(fp4_split_kernel<ADADIM_NVFP4, T>, tm, p, grid, kThreads, p.splits, smem, chained, st);
+  if (fused) return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T, true>, tm, p, grid, kFusedThreads, p.splits, smem, false, st)
+                                           : launch(fp4_split_kernel<ADADIM_NVFP4, T, true>, tm, p, grid, kFusedThreads, p.splits, smem, false, st);
+  return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T, false>, tm, p, grid, kThreads, p.splits, smem, chained, st)
+                                : launch(fp4_split_kernel<ADADIM_NVFP4, T, false>, tm, p, grid, kThreads, p.splits, smem, chained, st);
 }
 
 // Tiles of fewer tokens than 128 are cut no lower than this, and only up to so many rows (of a typical
 // expert), which bounds the scale tiles of the activations.
 constexpr int kMinCut = 32, kMaxCutRows = 512;
+// Rows (of a typical expert) up to which the product quantizes them itself: every weight tile's CTA repeats
+// the work, which at 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us
+// fused, 24.5 us behind the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).
+constexpr int kFusedTokens = 8;
 
 // The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
 // kernels below (1.9 GHz, 148 SMs):
@@ -627,13 +693,13 @@ constexpr int kMinCut = 32, kMaxCutRows = 512;
 //   split  a CTA's stage takes no less than 300 whatever its size, and the CTAs of an SM share 80 bytes a
 //          nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
 //          and in all no less than the weights' bytes at 6000 a nanosecond.
-Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout, int sms) {
+Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool quantized, bool fuse, int sms) {
   const int64_t weights = n_experts > 0 ? (n_experts < rows ? n_experts : rows) : 1;
   const int64_t typical = (rows + weights - 1) / weights;            // rows of one expert if they were equal
   const int64_t num_k = (in + kKT - 1) / kKT;
   // tiles of an expert's rows; experts are not equal, so half a tile more than an equal share would take
   auto token_tiles = [&](int64_t n) { return n_experts > 0 ? weights * ((typical + typical / 2 + n - 1) / n) : (rows + n - 1) / n; };
-  Fp4Plan best = {true, 256, 1, 1};
+  Fp4Plan best = {true, 256, 1, 1, false};
   double best_ns;
   const double floor_ns = static_cast<double>(weights * out) * static_cast<double>(in) * (format == ADADIM_MXFP4 ? 0.53125 : 0.5625) / 6000.0;
   {
@@ -646,7 +712,8 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
   }
   for (int n_tile = 16; n_tile <= 128; n_tile *= 2) {
     // lower tiles than 128 rows: only where they are the only ones, or the scales are laid out for them
-    if (n_tile < 128 && rows > n_tile && (!own_layout || n_tile < kMinCut || typical > kMaxCutRows)) continue;
+    const bool fused = fuse && n_tile <= kFusedTile && typical <= kFusedTokens;
+    if (n_tile < 128 && rows > n_tile && (quantized || (n_tile < kMinCut && !fused) || typical > kMaxCutRows)) continue;
     if (n_tile > 16 && n_tile / 2 >= rows) break;
     const int64_t tiles = (out + 127) / 128 * token_tiles(n_tile);
     const size_t per = stage_bytes(format, false, n_tile);
@@ -654,8 +721,9 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
       const int64_t ctas = tiles * splits, k = (num_k + splits - 1) / splits;
       const size_t fixed = exchange_floats(n_tile, splits) * 4 + 1024 + static_cast<size_t>(n_experts + 1) * 4;
       const int stages = static_cast<int>(k < 3 ? k : 3);
-      int per_sm = static_cast<int>((ctas + sms - 1) / sms < 4 ? (ctas + sms - 1) / sms : 4);
-      while (per_sm > 1 && (per_sm * (stages * per + fixed + 1024) > kSmem || per_sm * 2 * n_tile > 512)) --per_sm;
+      const int most = fused ? kFusedPerSm : 4;
+      int per_sm = static_cast<int>((ctas + sms - 1) / sms < most ? (ctas + sms - 1) / sms : most);
+      while (per_sm > 1 && (per_sm * (stages * per + fixed + 1024) > kSmem || per_sm * (n_tile <= 64 ? 128 : 256) > 512)) --per_sm;
       if (stages * per + fixed + 1024 > kSmem) continue;
       const int64_t waves = (ctas + static_cast<int64_t>(per_sm) * sms - 1) / (static_cast<int64_t>(per_sm) * sms);
       const double shared = static_cast<double>(per_sm) * static_cast<double>(per) / 80.0;
@@ -663,7 +731,7 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
       double ns = static_cast<double>(waves) * static_cast<double>(k) * stage;
       if (ns < floor_ns) ns = floor_ns;
       ns += 4000.0 + (splits > 1 ? 1500.0 + 15.0 * n_tile : 0.0);
-      if (ns < best_ns) { best_ns = ns; best = {false, n_tile, splits, per_sm}; }
+      if (ns < best_ns) { best_ns = ns; best = {false, n_tile, splits, per_sm, fused}; }
     }
   }
   return best;
@@ -673,8 +741,8 @@ constexpr int kSms = 148;
 
 }  // namespace
 
-Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool own_layout) {
-  return plan_of(rows, out, in, n_experts, format, own_layout, kSms);
+Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool quantized, bool fuse) {
+  return plan_of(rows, out, in, n_experts, format, quantized, fuse, kSms);
 }
 
 int64_t fp4_most_tile_rows(int64_t rows, int n_experts) {
@@ -684,8 +752,8 @@ int64_t fp4_most_tile_rows(int64_t rows, int n_experts) {
   return rows / lowest + 2 * groups + 2;
 }
 
-int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, int64_t n_rows, const int32_t* offsets,
-                      int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
+int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, const fp4::Source& x, int64_t n_rows,
+                      const int32_t* offsets, int n_experts, const adadim_fp4tensor& B, int64_t out, int64_t in, int format, void* Y, int ydtype,
                       int64_t ldy, int* status_dev, bool chained, cudaStream_t st) {
   const bool pair = plan.pair;
   MmParams p = {};
@@ -696,6 +764,7 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, in
   p.offsets = offsets;
   p.n_tile = plan.n_tile;
   p.lt = lt;
+  p.x = x;
   p.splits = plan.splits;
   p.num_k = static_cast<int>((in + kKT - 1) / kKT);
   p.n_sf = sf_tiles(format, in);
@@ -717,10 +786,15 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, in
   CUtensorMap tm[4];
   int rc;
   if ((rc = make_tmap_u8(&tm[0], B.codes, inner, static_cast<uint64_t>(weights * out), static_cast<uint64_t>(B.ld), 128, true)) != ADADIM_OK) return rc;
-  if ((rc = make_tmap_u8(&tm[1], A.codes, inner, static_cast<uint64_t>(n_rows), static_cast<uint64_t>(A.ld),
-                         static_cast<uint32_t>(pair ? p.n_tile / 2 : p.n_tile), true)) != ADADIM_OK) return rc;
   if ((rc = make_tmap_u8(&tm[2], B.scales, 128, weights * scale_bytes(format, out, in, 0) / 128, 128, sf_box, false)) != ADADIM_OK) return rc;
-  if ((rc = make_tmap_u8(&tm[3], A.scales, 128, static_cast<uint64_t>(sf_tile_rows(n_rows, n_experts, lt) * p.n_sf * 4), 128, sf_box, false)) != ADADIM_OK) return rc;
+  if (plan.fused) {
+    tm[1] = tm[0];                                     // not used
+    tm[3] = tm[2];
+  } else {
+    if ((rc = make_tmap_u8(&tm[1], A.codes, inner, static_cast<uint64_t>(n_rows), static_cast<uint64_t>(A.ld),
+                           static_cast<uint32_t>(pair ? p.n_tile / 2 : p.n_tile), true)) != ADADIM_OK) return rc;
+    if ((rc = make_tmap_u8(&tm[3], A.scales, 128, static_cast<uint64_t>(sf_tile_rows(n_rows, n_experts, lt) * p.n_sf * 4), 128, sf_box, false)) != ADADIM_OK) return rc;
+  }
 
   const size_t per = stage_bytes(format, pair, p.n_tile);
   size_t fixed = 1024;                                 // alignment, and what lies behind the ring
@@ -731,7 +805,7 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, in
   } else {
     grid = n_experts > 0 ? dim3(static_cast<unsigned>(tiles * p.splits))
                          : dim3(static_cast<unsigned>(token_tiles * p.splits), static_cast<unsigned>(p.m_tiles));
-    p.tmem_cols = p.n_tile <= 32 ? 64 : 2 * p.n_tile;
+    p.tmem_cols = p.n_tile <= 64 ? 128 : 256;
     fixed += exchange_floats(p.n_tile, p.splits) * 4 + static_cast<size_t>(n_experts > 0 ? n_experts + 1 : 0) * 4;
     p.n_stages = static_cast<int>((kSmem / plan.per_sm - 1024 - fixed) / per);     // 1024: a CTA's share kept by the system
     const int k = (p.num_k + p.splits - 1) / p.splits;
@@ -739,9 +813,9 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, in
   }
   if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
   const size_t smem = p.n_stages * per + fixed;
-  if (ydtype == ADADIM_F32) return launch_format<float>(pair, format, tm, p, grid, smem, chained, st);
-  if (ydtype == ADADIM_F16) return launch_format<__half>(pair, format, tm, p, grid, smem, chained, st);
-  return launch_format<__nv_bfloat16>(pair, format, tm, p, grid, smem, chained, st);
+  if (ydtype == ADADIM_F32) return launch_format<float>(pair, plan.fused, format, tm, p, grid, smem, chained, st);
+  if (ydtype == ADADIM_F16) return launch_format<__half>(pair, plan.fused, format, tm, p, grid, smem, chained, st);
+  return launch_format<__nv_bfloat16>(pair, plan.fused, format, tm, p, grid, smem, chained, st);
 }
 
 }  // namespace adadim
