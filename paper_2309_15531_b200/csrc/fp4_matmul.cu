@@ -9,10 +9,8 @@
 // that use them.  Two kernels:
 //   pair   many tokens, bound by the tensor pipe: a cluster of two CTAs works on one 256 x 256 tile
 //          (each CTA loads half of either operand, so a step's bytes per CTA are half of what one CTA
-//          on a 128 x 256 tile would need), persistent over the tiles, with two accumulators that
-//          share 64 of their 256 TMEM columns (512 columns hold two of them and the scales only that
-//          way): the epilogue drains the shared columns first, and the next tile's MMAs wait for
-//          those alone.
+//          on a 128 x 256 tile would need), persistent over the tiles, with two accumulators in TMEM,
+//          so that one is drained while the other is filled.
 //   split  few tokens, bound by the weight's bytes: 128 weight rows x up to 128 tokens per cluster, the
 //          columns split over the cluster's 1 .. 8 CTAs, partial sums exchanged through distributed
 //          shared memory and added in the order of the columns; up to four CTAs to an SM, so that all
@@ -46,6 +44,7 @@ struct MmParams {
   int n_tile;                                          // tokens of a tile
   int lt;                                              // of the layout of A's scales: n_tile is a multiple of it
                                                        // (or there is one tile)
+  int lt_per_tile, sub;                                // n_tile / lt; scale tile rows of lt rows
   int num_k;                                           // stages of a tile
   int n_stages;
   int splits;                                          // split kernel: CTAs of a cluster
@@ -72,6 +71,12 @@ struct Tile {
   int64_t a_sf_row;                                    // scale tile row of A
 };
 
+// a / b for a, b > 0.  In binary32 below 2^21, where (a + 1/2) / b is off by less than its distance 1 / (2 b) from
+// a whole number: a sixth of an integer division's latency, which a tile's first stage would wait for.
+__device__ __forceinline__ int quick_div(int a, int b) {
+  if (a >= (1 << 21)) return a / b;
+  return static_cast<int>((static_cast<float>(a) + 0.5f) * __frcp_rn(static_cast<float>(b)));
+}
 // Tiles are numbered expert by expert; inside one, bands of kBand weight tiles sweep over the tokens,
 // so that the CTAs at work at one time share both operands in L2.
 __device__ __forceinline__ Tile tile_of(int t, const MmParams& p, const int* prefix) {
@@ -90,15 +95,15 @@ __device__ __forceinline__ Tile tile_of(int t, const MmParams& p, const int* pre
     first = clamped(p.offsets[lo], p.rows);
     n = clamped(p.offsets[lo + 1], p.rows) - first;
   }
-  const int n_tiles = (n + p.n_tile - 1) / p.n_tile;
-  const int band = t / (kBand * n_tiles);
+  const int n_tiles = quick_div(n + p.n_tile - 1, p.n_tile);
+  const int band = quick_div(t, kBand * n_tiles);
   const int in_band = t - band * kBand * n_tiles;
   const int width = min(kBand, p.m_tiles - band * kBand);
-  const int j = in_band / width;
+  const int j = quick_div(in_band, width);
   x.m = (band * kBand + in_band - j * width) * TILE_M;
   x.row = first + j * p.n_tile;
   x.count = min(p.n_tile, n - j * p.n_tile);
-  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? first / p.lt + x.e : 0) + j * (p.n_tile / p.lt)) * ((p.lt + kSfRows - 1) / kSfRows);
+  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? quick_div(first, p.lt) + x.e : 0) + j * p.lt_per_tile) * p.sub;
   return x;
 }
 // The split kernel's order: the token tiles of one weight tile next to each other.  Dense: from the grid.
@@ -108,7 +113,7 @@ __device__ __forceinline__ Tile tile_at(int j, int m, int e, int first, int n, c
   x.m = m * 128;
   x.row = first + j * p.n_tile;
   x.count = min(p.n_tile, n - j * p.n_tile);
-  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? first / p.lt + e : 0) + j * (p.n_tile / p.lt)) * ((p.lt + kSfRows - 1) / kSfRows);
+  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? quick_div(first, p.lt) + e : 0) + j * p.lt_per_tile) * p.sub;
   return x;
 }
 __device__ __forceinline__ Tile tile_of_group(int t, const MmParams& p, const int* prefix) {
@@ -118,7 +123,7 @@ __device__ __forceinline__ Tile tile_of_group(int t, const MmParams& p, const in
     if (prefix[mid] <= t) lo = mid; else hi = mid - 1;
   }
   const int first = clamped(p.offsets[lo], p.rows), n = clamped(p.offsets[lo + 1], p.rows) - first;
-  const int n_tiles = (n + p.n_tile - 1) / p.n_tile, m = (t - prefix[lo]) / n_tiles;
+  const int n_tiles = quick_div(n + p.n_tile - 1, p.n_tile), m = quick_div(t - prefix[lo], n_tiles);
   return tile_at(t - prefix[lo] - m * n_tiles, m, lo, first, n, p);
 }
 // Tiles of each expert as a running sum, by one warp; prefix[n_experts] is their number.
@@ -173,33 +178,37 @@ __device__ __forceinline__ void let_copies_land() {
 }
 
 // The MMAs of one stage: scale tiles to TMEM, then the 64-column steps that hold columns of the matrix
-// (beyond them scales need not exist).
+// (beyond them scales need not exist).  Addresses are shared-memory addresses in units of 16 bytes, added to
+// constant descriptors.  PAIR and NVFP4: in two halves that use the same TMEM columns in turn (the copies and
+// MMAs of one thread execute in order), so that a stage's scales fit into 32 columns.
 template <int FORMAT, bool PAIR>
-__device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, uint32_t w_addr, uint32_t a_addr,
-                                            uint32_t ws_addr, uint32_t id0, uint32_t id1, int steps, bool first) {
+__device__ __forceinline__ void issue_stage(uint32_t d, uint32_t sf_tmem, uint32_t w, uint32_t a, uint32_t ws, uint32_t id0,
+                                            uint32_t id1, int steps, bool first) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
-  constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
-  constexpr int kSfTiles = kSf / kSfTileBytes;                       // scale tiles of a stage: 4 or 2
+  constexpr uint32_t kSf16 = sf_stage_bytes(FORMAT) / 16, kTile16 = kSfTileBytes / 16;
+  constexpr int kSfTiles = sf_stage_bytes(FORMAT) / kSfTileBytes;    // scale tiles of a stage: 4 or 2
   constexpr uint64_t desc = ptx::smem_desc_sw128(16, 1024);          // K-major: 8-row groups 1024 bytes apart
   constexpr uint64_t sf_desc = ptx::smem_desc_plain(16, 128);
   constexpr int kTok = PAIR ? 8 : 4;                                 // TMEM columns of one step's token scales
-#pragma unroll
-  for (int j = 0; j < kSfTiles; ++j) {
-    ptx::tmem_cp_scales<PAIR>(sf_tmem + j * 4, ptx::with_start(sf_desc, ws_addr + j * kSfTileBytes));
-    ptx::tmem_cp_scales<PAIR>(sf_tmem + 16 + j * kTok, ptx::with_start(sf_desc, ws_addr + kSf + j * kSfTileBytes));
-    if (PAIR) ptx::tmem_cp_scales<PAIR>(sf_tmem + 16 + j * kTok + 4, ptx::with_start(sf_desc, ws_addr + 2 * kSf + j * kSfTileBytes));
-  }
-  auto step = [&](int j) {
-    const int tile = NV ? j : j / 2;
-    ptx::mma_fp4<NV, PAIR>(d, ptx::with_start(desc, w_addr + j * 32), ptx::with_start(desc, a_addr + j * 32),
-                           (j & 1) ? id1 : id0, sf_tmem + tile * 4, sf_tmem + 16 + tile * kTok, !(first && j == 0));
+  constexpr int kHalves = PAIR && NV ? 2 : 1, kTilesPer = kSfTiles / kHalves, kTokAt = 4 * kTilesPer;
+  auto copy = [&](int j) {                                           // scale tile j of the stage
+    const int at = j % kTilesPer;
+    ptx::tmem_cp_scales<PAIR>(sf_tmem + at * 4, sf_desc + ws + j * kTile16);
+    ptx::tmem_cp_scales<PAIR>(sf_tmem + kTokAt + at * kTok, sf_desc + ws + kSf16 + j * kTile16);
+    if (PAIR) ptx::tmem_cp_scales<PAIR>(sf_tmem + kTokAt + at * kTok + 4, sf_desc + ws + 2 * kSf16 + j * kTile16);
   };
-  if (steps == 4) {
+  auto step = [&](int j) {
+    const int at = (NV ? j : j / 2) % kTilesPer;
+    ptx::mma_fp4<NV, PAIR>(d, desc + w + j * 2, desc + a + j * 2, (j & 1) ? id1 : id0, sf_tmem + at * 4,
+                           sf_tmem + kTokAt + at * kTok, !(first && j == 0));
+  };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) step(j);
-  } else {
-#pragma unroll 1
-    for (int j = 0; j < steps; ++j) step(j);
+  for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+    for (int j = 0; j < kTilesPer; ++j) copy(h * kTilesPer + j);
+#pragma unroll
+    for (int j = h * 4 / kHalves; j < (h + 1) * 4 / kHalves; ++j)
+      if (j < steps) step(j);
   }
 }
 __device__ __forceinline__ int steps_of(int64_t in, int k) {
@@ -215,10 +224,15 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
   constexpr int kSfTiles = kSf / kSfTileBytes;
-  constexpr uint32_t kAccStep = 192, kSfCol = 448;     // accumulators at 0 and 192, scales at 448
+  // TMEM: two accumulators and 32 columns of scales.  240 tokens: side by side.  256 tokens: they share 32
+  // columns, which the epilogue drains first and the next tile's MMAs wait for.
+  constexpr uint32_t kSfCol = 480;
+  const bool sharing = p.n_tile > 240;
+  const uint32_t acc_step = sharing ? 224 : 240;
 
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t smem_at = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;      // shared-memory address of the ring
+  uint8_t* smem = smem_raw + (smem_at - ptx::smem_addr(smem_raw));
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], part_empty;
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_word;
@@ -253,14 +267,17 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   const uint32_t tmem = tmem_slot;
   const int num_tiles = p.n_experts > 0 ? prefix[p.n_experts] : (p.rows + p.n_tile - 1) / p.n_tile * p.m_tiles;
 
+  const int ahead_k = min(3, p.num_k - 1);             // in this stage of a tile the next one is worked out
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (both CTAs)
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
     ptx::pdl_wait();
+    Tile x = {}, next_x = {};
+    if (pair0 < num_tiles) next_x = tile_of(pair0, p, prefix);
     for (int t = pair0; t < num_tiles && ok; t += pairs) {
-      const Tile x = tile_of(t, p, prefix);
+      x = next_x;
       const int half = ((x.count + 15) & ~15) >> 1;    // tokens of this CTA
       const int w_row = static_cast<int>(x.e * p.out + x.m) + static_cast<int>(rank) * 128;
       const int a_row = x.row + static_cast<int>(rank) * half;
@@ -283,6 +300,8 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           ptx::tma_load_2d_pair(ws_dst + 2 * kSf, &tmAs, 0, a_sf1, bar);
         }
         __syncwarp();
+        // the next tile is worked out while there is nothing to wait for
+        if (k == ahead_k && t + pairs < num_tiles) next_x = tile_of(t + pairs, p, prefix);
         w_sf += kSfTiles * 4;
         a_sf0 += kSfTiles * 4;
         a_sf1 += kSfTiles * 4;
@@ -296,12 +315,12 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, part_phase = 0;
       bool ok = true, ready = false;
+      int next_count = pair0 < num_tiles ? tile_of(pair0, p, prefix).count : 0;
       for (int t = pair0; t < num_tiles && ok; t += pairs) {
-        const Tile x = tile_of(t, p, prefix);
-        const int n = (x.count + 15) & ~15;
+        const int n = (next_count + 15) & ~15;
         const uint32_t id0 = ptx::idesc_fp4(256, n, !NV, 0), id1 = ptx::idesc_fp4(256, n, !NV, NV ? 0 : 2);
         ok = ptx::mbar_wait_warp(&acc_empty[buf], acc_phase ^ 1u, dead, p.status_dev);
-        if (ok && t != pair0) {                        // the tile before has left the shared columns
+        if (ok && sharing && t != pair0) {             // the tile before has left the shared columns
           ok = ptx::mbar_wait_warp(&part_empty, part_phase, dead, p.status_dev);
           part_phase ^= 1u;
         }
@@ -315,14 +334,15 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
           // asked before this stage's instructions are issued: the answer is there when they are
           const bool next = ptx::mbar_test(&full[stage], phase);
-          const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
+          const uint32_t w16 = (smem_at + cur * stage_size) >> 4;
           const int steps = steps_of(p.in, k);
           if (ptx::elect_one()) {
-            issue_stage<FORMAT, true>(tmem + buf * kAccStep, tmem + kSfCol, w_addr, w_addr + kWBytes,
-                                      w_addr + kWBytes + a_bytes, id0, id1, steps, k == 0);
+            issue_stage<FORMAT, true>(tmem + buf * acc_step, tmem + kSfCol, w16, w16 + kWBytes / 16,
+                                      w16 + (kWBytes + a_bytes) / 16, id0, id1, steps, k == 0);
             ptx::mma_commit_pair(&empty[cur]);
             if (k == p.num_k - 1) ptx::mma_commit_pair(&acc_full[buf]);
           }
+          if (k == ahead_k && t + pairs < num_tiles) next_count = tile_of(t + pairs, p, prefix).count;
           ready = __all_sync(0xffffffffu, next) != 0;
         }
         buf ^= 1;
@@ -333,7 +353,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   } else {
     // ------------------------------------------------------------------ epilogue (warps 2..9 of both CTAs)
     const int q = warp & 3;                            // TMEM lane quadrant this warp may read
-    const int side = (warp - 2) >> 2;                  // of each 64 columns, which 32 this warp takes
+    const int side = (warp - 2) >> 2;                  // of each 64 columns, the 32 that this warp takes
     int buf = 0;
     uint32_t acc_phase = 0;
     const float scale = product_scale<NV>(p);
@@ -344,19 +364,22 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       ptx::tc_fence_after_sync();
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
       T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
-      const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + buf * kAccStep;
-      // the shared columns first: the last 64 of accumulator 0, the first 64 of accumulator 1
-      const int s0 = (buf == 0 ? static_cast<int>(kAccStep) : 0) + side * 32;
-      {
+      const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + buf * acc_step;
+      int done = -1;                                   // the shared columns, taken first by half of the warps
+      if (sharing) {
         float v[32];
-        if (s0 < x.count) ptx::tmem_ld32(acc + s0, v);
+        const int c = buf == 0 ? 224 : 0;
+        if (side == (c >> 5 & 1)) done = c;
+        const bool any = done >= 0 && c < x.count;
+        if (any) ptx::tmem_ld32(acc + c, v);
         ptx::tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive_cluster(part_bar);
-        if (s0 < x.count && o < p.out) store_tokens(y + s0 * p.ldy, p.ldy, x.count - s0, scale, v);
+        if (any && o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
       }
 #pragma unroll 1
-      for (int c = (buf == 0 ? 0 : 64) + side * 32; c < min(x.count, buf == 0 ? 192 : 256); c += 64) {
+      for (int c = side * 32; c < x.count; c += 64) {
+        if (c == done) continue;
         float v[32];
         ptx::tmem_ld32(acc + c, v);
         if (o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
@@ -399,7 +422,8 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   constexpr int kSfTiles = kSf / kSfTileBytes;
 
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t smem_at = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;      // shared-memory address of the ring
+  uint8_t* smem = smem_raw + (smem_at - ptx::smem_addr(smem_raw));
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full, red_full;
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_word;
@@ -508,11 +532,11 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
         // asked before this stage's instructions are issued: the answer is there when they are
         const bool next = ptx::mbar_test(&full[stage], phase);
-        const uint32_t w_addr = ptx::smem_addr(smem + cur * stage_size);
+        const uint32_t w16 = (smem_at + cur * stage_size) >> 4;
         const int steps = steps_of(p.in, k);
         if (ptx::elect_one()) {
-          issue_stage<FORMAT, false>(tmem, tmem + sf_col + (k & 1) * 32, w_addr, w_addr + kWBytes, w_addr + kWBytes + a_bytes,
-                                     id0, id1, steps, k == k0);
+          issue_stage<FORMAT, false>(tmem, tmem + sf_col + (k & 1) * 32, w16, w16 + kWBytes / 16,
+                                     w16 + (kWBytes + a_bytes) / 16, id0, id1, steps, k == k0);
           ptx::mma_commit(&empty[cur]);
           if (k == k1 - 1) ptx::mma_commit(&acc_full);
         }
@@ -681,6 +705,7 @@ int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[4],
 // Tiles of fewer tokens than 128 are cut no lower than this, and only up to so many rows (of a typical
 // expert), which bounds the scale tiles of the activations.
 constexpr int kMinCut = 32, kMaxCutRows = 512;
+constexpr int kMinPairTile = 160;                      // the pair kernel's lowest token tile, two scale tile rows
 // Rows (of a typical expert) up to which the product quantizes them itself: every weight tile's CTA repeats
 // the work, which at 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us
 // fused, 24.5 us behind the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).
@@ -688,7 +713,8 @@ constexpr int kFusedTokens = 8;
 
 // The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
 // kernels below (1.9 GHz, 148 SMs):
-//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256; a tile 500 on top; start and end 5000;
+//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256, and no less than 235 (MXFP4) or 270 (its
+//          instructions have to be issued); a tile 650 on top, 100 up to 240 tokens; start and end 5000;
 //          it streams no faster than 1 / 1.7 of the split kernel
 //   split  a CTA's stage takes no less than 300 whatever its size, and the CTAs of an SM share 80 bytes a
 //          nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
@@ -700,15 +726,16 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
   // tiles of an expert's rows; experts are not equal, so half a tile more than an equal share would take
   auto token_tiles = [&](int64_t n) { return n_experts > 0 ? weights * ((typical + typical / 2 + n - 1) / n) : (rows + n - 1) / n; };
   Fp4Plan best = {true, 256, 1, 1, false};
-  double best_ns;
+  double best_ns = 1e300;
   const double floor_ns = static_cast<double>(weights * out) * static_cast<double>(in) * (format == ADADIM_MXFP4 ? 0.53125 : 0.5625) / 6000.0;
-  {
-    const int64_t tiles = (out + 255) / 256 * token_tiles(256), waves = (tiles + sms / 2 - 1) / (sms / 2);
-    const double n = typical < 256 ? static_cast<double>((typical + 15) / 16 * 16) : 256.0;
-    const double stage = 270.0 * n / 256.0 < 200.0 ? 200.0 : 270.0 * n / 256.0;
-    best_ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + 500.0);
-    if (best_ns < 1.7 * floor_ns) best_ns = 1.7 * floor_ns;
-    best_ns += 5000.0;
+  for (int n_tile = 256; n_tile >= (quantized ? 256 : kMinPairTile); n_tile -= 16) {
+    const int64_t tiles = (out + 255) / 256 * token_tiles(n_tile), waves = (tiles + sms / 2 - 1) / (sms / 2);
+    const double n = typical < n_tile ? static_cast<double>((typical + 15) / 16 * 16) : n_tile;
+    const double least = format == ADADIM_MXFP4 ? 235.0 : 270.0, stage = 1.055 * n < least ? least : 1.055 * n;
+    double ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + (n_tile > 240 ? 650.0 : 100.0));
+    if (ns < 1.7 * floor_ns) ns = 1.7 * floor_ns;
+    ns += 5000.0;
+    if (ns < best_ns) { best_ns = ns; best.n_tile = n_tile; }
   }
   for (int n_tile = 16; n_tile <= 128; n_tile *= 2) {
     // lower tiles than 128 rows: only where they are the only ones, or the scales are laid out for them
@@ -748,7 +775,7 @@ Fp4Plan fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int forma
 int64_t fp4_most_tile_rows(int64_t rows, int n_experts) {
   const int64_t groups = n_experts > 0 ? n_experts : 1;
   if (rows == 0) return 0;
-  const int lowest = rows <= kMaxCutRows * groups ? kMinCut : kSfRows;
+  const int lowest = rows <= kMaxCutRows * groups ? kMinCut : kMinPairTile / 2;      // rows a tile row has at least, but for ends
   return rows / lowest + 2 * groups + 2;
 }
 
@@ -764,6 +791,8 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, co
   p.offsets = offsets;
   p.n_tile = plan.n_tile;
   p.lt = lt;
+  p.lt_per_tile = plan.n_tile / lt;
+  p.sub = static_cast<int>((lt + kSfRows - 1) / kSfRows);
   p.x = x;
   p.splits = plan.splits;
   p.num_k = static_cast<int>((in + kKT - 1) / kKT);

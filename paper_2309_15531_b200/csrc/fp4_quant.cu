@@ -1,12 +1,12 @@
 // Microscaled 4-bit quantizer and the largest magnitude its tensor scale is taken from.
 //
 // Both are bound by memory.  Quantizer: a CTA owns one scale tile, 128 rows x 64 (NVFP4) or 128 (MXFP4)
-// columns (for token tiles of 16, 32 or 64 rows up to 128 / rows tiles side by side), so the
-// scales leave as one contiguous run although a row's scales lie 512 bytes apart.  A thread takes 16 consecutive columns (one NVFP4 block, half an MXFP4 block: the halves meet in one
-// shuffle) of 2 or 4 rows, all of whose loads are issued before the first is used; its codes are one
-// 8-byte store.  What it executes matters as much as what it moves (24 instructions an element were the
-// limit at 39 us for W[11008,4096] with its values): packed magnitude maximum, packed binary32 for the
-// quotients, hardware conversions to and from E2M1.
+// columns (for token tiles of 16, 32 or 64 rows up to 128 / rows tiles side by side), so the scales leave as
+// one contiguous run although a row's scales lie 512 bytes apart.  A thread takes 16 consecutive columns (one
+// NVFP4 block, half an MXFP4 block: the halves meet in one shuffle) of 4 or 8 rows, the loads of four of them
+// issued before the first is used; its codes are one 8-byte store.  What it executes matters as much as what
+// it moves (24 instructions an element were the limit at 39 us for W[11008,4096] with its values): packed
+// magnitude maximum, packed binary32 for the quotients, hardware conversions to and from E2M1.
 #include "fp4.cuh"
 #include "umma.cuh"
 
@@ -15,7 +15,8 @@ namespace {
 
 using namespace fp4;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kBatch = 4;                    // rows of a thread whose loads are in flight together
 
 __device__ __forceinline__ void store32(void* p, const uint32_t* w) {           // 32-byte aligned
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -39,88 +40,98 @@ struct QuantParams {
   int wide_v;                 // values: every row starts on a 32-byte boundary
 };
 
-// VALUES: 0 none, 1 bf16, 2 fp32
 // CTAs of an SM that the registers must leave room for: the loads in flight are what hides the memory's latency
 template <typename T, int FORMAT>
-constexpr int kResident = sizeof(T) == 4 ? (FORMAT == ADADIM_NVFP4 ? 4 : 2) : FORMAT == ADADIM_NVFP4 ? 5 : 4;
+constexpr int kResident = sizeof(T) == 4 ? 5 : 8;
 
+// VALUES: 0 none, 1 bf16, 2 fp32, 3 none and tiles side by side or few CTAs (see the launcher)
 template <typename T, int FORMAT, int VALUES>
 __global__ void __launch_bounds__(kThreads, kResident<T, FORMAT>)
 quantize_kernel(const QuantParams p) {
   constexpr int kChunks = sf_cols(FORMAT) / kPer;             // threads to a row of a tile: 4 or 8
-  constexpr int kRows = kSfRows * kChunks / kThreads;         // rows of a thread: 2 or 4
+  constexpr int kRows = kSfRows * kChunks / kThreads;         // rows of a thread: 4 or 8
   extern __shared__ __align__(16) uint8_t sf[];               // [side][kSfTileBytes]
   ptx::pdl_launch_dependents();                               // a product launched behind this may start on its weight
-  const int n_sf = static_cast<int>(p.n_sf), ctas = (n_sf + p.side - 1) / p.side;
+  const int side = VALUES == 3 ? p.side : 1;
+  const int n_sf = static_cast<int>(p.n_sf), ctas = VALUES == 3 ? (n_sf + side - 1) / side : n_sf;
   const int v = blockIdx.x / ctas;                            // tile row
-  const int tile0 = (blockIdx.x - v * ctas) * p.side;         // first of the tiles side by side
+  const int tile0 = (blockIdx.x - v * ctas) * side;           // first of the tiles side by side
   int first, count;
   rows_of_tile_row(p.offsets, p.n_groups, p.rows, p.lt, v, first, count);
   if (count <= 0) return;
 
-  const int wide = kChunks * p.side;                          // threads to a row
-  const int chunk = threadIdx.x & (wide - 1), row0 = threadIdx.x / wide, row_step = kThreads / wide;
+  const int wide = kChunks * side, shift = __ffs(wide) - 1;   // threads to a row, a power of two
+  const int chunk = threadIdx.x & (wide - 1), row0 = threadIdx.x >> shift, row_step = kThreads >> shift;
   const int64_t c0 = (static_cast<int64_t>(tile0) * kChunks + chunk) * kPer;
   const int n = static_cast<int>(p.cols - c0 < kPer ? (p.cols - c0 < 0 ? 0 : p.cols - c0) : kPer);   // columns here
-  Raw<T> raw[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int r = i * row_step + row0;
-    const int64_t src = r < count ? source_row(p.x, static_cast<int64_t>(first) + r) : -1;
-    load16(p.x, src, c0, r < count ? n : 0, raw[i]);
-  }
   const int t_log2 = FORMAT == ADADIM_NVFP4 ? tensor_scale_log2(p.amax) : 0;
+  const int blk = chunk * kPer / block_of(FORMAT);
+  uint8_t* sf_at = sf + (blk / 4) * kSfTileBytes + blk % 4;
+  uint8_t* codes = p.codes + static_cast<int64_t>(first) * p.ld + c0 / 2;
+#pragma unroll 1
+  for (int r1 = row0; r1 - row0 < kRows * row_step && r1 - row0 < count; r1 += kBatch * row_step) {
+    Raw<T> raw[kBatch];
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int r = i * row_step + row0;
-    const int64_t row = static_cast<int64_t>(first) + r;
-    float x[kPer];
-    uint32_t top = widen(raw[i], x);
-    if (FORMAT == ADADIM_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const BlockScale b = block_scale<FORMAT, sizeof(T) == 2>(__uint_as_float(top), t_log2);
-    uint2 c;
-    c.x = codes8<FORMAT, sizeof(T) == 2>(x, b);
-    c.y = codes8<FORMAT, sizeof(T) == 2>(x + 8, b);
-    const bool live = r < count && n > 0;
-    const int blk = chunk * kPer / block_of(FORMAT);
-    if (FORMAT == ADADIM_NVFP4 || (chunk & 1) == 0)           // 0 behind the last row and column
-      sf[(blk / 4) * kSfTileBytes + (r % 32) * 16 + (r / 32) * 4 + blk % 4] = static_cast<uint8_t>(live ? b.byte : 0u);
-    if (!live) continue;
-    *reinterpret_cast<uint2*>(p.codes + row * p.ld + c0 / 2) = c;
-    if (VALUES != 0) {
-      const float s = b.finite ? b.s : __uint_as_float(0x7fffffffu);
-      float q[kPer];
-      e2m1_values8(c.x, *reinterpret_cast<float(*)[8]>(q));
-      e2m1_values8(c.y, *reinterpret_cast<float(*)[8]>(q + 8));
-      const uint64_t s2 = pack2(s, s);
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = r1 + i * row_step;
+      const int64_t src = r < count ? source_row(p.x, static_cast<int64_t>(first) + r) : -1;
+      load16(p.x, src, c0, n, raw[i]);
+    }
 #pragma unroll
-      for (int k = 0; k < kPer; k += 2) unpack2(mul2(pack2(q[k], q[k + 1]), s2), q[k], q[k + 1]);
-      if (VALUES == 1) {
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.values) + row * p.ldv + c0;
-        if (n == kPer && p.wide_v) {
-          uint32_t w[8];
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = r1 + i * row_step;
+      float x[kPer];
+      uint32_t top = widen(raw[i], x);
+      if (FORMAT == ADADIM_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      const BlockScale b = block_scale<FORMAT, sizeof(T) == 2>(__uint_as_float(top), t_log2);
+      uint2 c;
+      c.x = codes8<FORMAT, sizeof(T) == 2>(x, b);
+      c.y = codes8<FORMAT, sizeof(T) == 2>(x + 8, b);
+      const bool live = r < count && n > 0;
+      if (FORMAT == ADADIM_NVFP4 || (chunk & 1) == 0)         // 0 behind the last row and column
+        sf_at[(r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(live ? b.byte : 0u);
+      if (!live) continue;
+      *reinterpret_cast<uint2*>(codes + r * p.ld) = c;
+      if (VALUES == 1 || VALUES == 2) {
+        const int64_t row = static_cast<int64_t>(first) + r;
+        const float s = b.finite ? b.s : __uint_as_float(0x7fffffffu);
+        float q[kPer];
+        e2m1_values8(c.x, *reinterpret_cast<float(*)[8]>(q));
+        e2m1_values8(c.y, *reinterpret_cast<float(*)[8]>(q + 8));
+        const uint64_t s2 = pack2(s, s);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(q[2 * k], q[2 * k + 1]);
-            w[k] = *reinterpret_cast<const uint32_t*>(&h);
+        for (int k = 0; k < kPer; k += 2) unpack2(mul2(pack2(q[k], q[k + 1]), s2), q[k], q[k + 1]);
+        if (VALUES == 1) {
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.values) + row * p.ldv + c0;
+          if (n == kPer && p.wide_v) {
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(q[2 * k], q[2 * k + 1]);
+              w[k] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            store32(out, w);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) if (k < n) out[k] = __float2bfloat16_rn(q[k]);
           }
-          store32(out, w);
         } else {
+          float* out = static_cast<float*>(p.values) + row * p.ldv + c0;
+          if (n == kPer && p.wide_v) {
+            store32(out, reinterpret_cast<const uint32_t*>(q));
+            store32(out + 8, reinterpret_cast<const uint32_t*>(q) + 8);
+          } else {
 #pragma unroll
-          for (int k = 0; k < kPer; ++k) if (k < n) out[k] = __float2bfloat16_rn(q[k]);
-        }
-      } else {
-        float* out = static_cast<float*>(p.values) + row * p.ldv + c0;
-        if (n == kPer && p.wide_v) {
-          store32(out, reinterpret_cast<const uint32_t*>(q));
-          store32(out + 8, reinterpret_cast<const uint32_t*>(q) + 8);
-        } else {
-#pragma unroll
-          for (int k = 0; k < kPer; ++k) if (k < n) out[k] = q[k];
+            for (int k = 0; k < kPer; ++k) if (k < n) out[k] = q[k];
+          }
         }
       }
     }
   }
+  // rows of a public (128-row) tile that no sweep reached
+  if (p.lt % kSfRows == 0)
+    for (int r = row0; r < kSfRows; r += row_step)
+      if (r >= count && (FORMAT == ADADIM_NVFP4 || (chunk & 1) == 0)) sf_at[(r & 31) * 16 + (r >> 5) * 4] = 0;
   __syncthreads();
   // (in a token tile lower than 128 the places of the rows it does not have hold anything: nobody reads them)
   const int tiles = min(p.side, n_sf - tile0);
@@ -167,8 +178,10 @@ absmax_kernel(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx, 
 template <typename T, int FORMAT, int VALUES>
 int launch(const QuantParams& p, dim3 grid, cudaStream_t st) {
   // A product behind this kernel starts while this one runs and needs nearly all of an SM's shared memory:
-  // if this kernel left the SM with a small share, the product would wait until the SM is empty.
-  if (VALUES == 0)
+  // if this kernel left the SM with a small share, the product would wait until the SM is empty.  With few
+  // CTAs (VALUES = 3) the share is therefore set to the most; with many that would cost the kernel the
+  // cache its loads in flight need (8192 x 4096 bf16: 27 us instead of 16).
+  if (VALUES == 3)
     ADADIM_CUDA_TRY(cudaFuncSetAttribute(quantize_kernel<T, FORMAT, VALUES>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                          cudaSharedmemCarveoutMaxShared));
   quantize_kernel<T, FORMAT, VALUES><<<grid, kThreads, static_cast<size_t>(p.side) * kSfTileBytes, st>>>(p);
@@ -176,7 +189,7 @@ int launch(const QuantParams& p, dim3 grid, cudaStream_t st) {
 }
 template <typename T, int FORMAT>
 int launch_values(const QuantParams& p, int vsel, dim3 grid, cudaStream_t st) {
-  if (vsel == 0) return launch<T, FORMAT, 0>(p, grid, st);
+  if (vsel == 0) return p.side > 1 || grid.x <= 4 * 148 ? launch<T, FORMAT, 3>(p, grid, st) : launch<T, FORMAT, 0>(p, grid, st);
   return vsel == 1 ? launch<T, FORMAT, 1>(p, grid, st) : launch<T, FORMAT, 2>(p, grid, st);
 }
 template <typename T>
