@@ -68,7 +68,7 @@ __host__ __device__ __forceinline__ uint32_t stage_bytes(int format, bool pair, 
 // One output tile: weight rows from `m` on, the `count` (<= n_tile) rows of A from `row` on.
 struct Tile {
   int e, m, row, count;
-  int64_t a_sf_row;                                    // scale tile row of A
+  int a_sf_row;                                        // scale tile row of A
 };
 
 // a / b for a, b > 0.  In binary32 below 2^21, where (a + 1/2) / b is off by less than its distance 1 / (2 b) from
@@ -103,9 +103,27 @@ __device__ __forceinline__ Tile tile_of(int t, const MmParams& p, const int* pre
   x.m = (band * kBand + in_band - j * width) * TILE_M;
   x.row = first + j * p.n_tile;
   x.count = min(p.n_tile, n - j * p.n_tile);
-  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? quick_div(first, p.lt) + x.e : 0) + j * p.lt_per_tile) * p.sub;
+  x.a_sf_row = ((p.n_experts > 0 ? quick_div(first, p.lt) + x.e : 0) + j * p.lt_per_tile) * p.sub;
   return x;
 }
+// The tiles of a persistent warp, first, first + step, ..: worked out for 32 of them at a time, one by each lane
+// (a tile takes several hundred cycles of dependent divisions, which would stall the loads at its start).
+struct TileWalk {
+  Tile mine;
+  int n;
+  __device__ __forceinline__ Tile next(int t, int step, int num_tiles, const MmParams& p, const int* prefix) {
+    const int lane = threadIdx.x & 31;
+    if ((n & 31) == 0) mine = t + lane * step < num_tiles ? tile_of(t + lane * step, p, prefix) : Tile{};
+    const int from = n++ & 31;
+    Tile x;
+    x.e = __shfl_sync(0xffffffffu, mine.e, from);
+    x.m = __shfl_sync(0xffffffffu, mine.m, from);
+    x.row = __shfl_sync(0xffffffffu, mine.row, from);
+    x.count = __shfl_sync(0xffffffffu, mine.count, from);
+    x.a_sf_row = __shfl_sync(0xffffffffu, mine.a_sf_row, from);
+    return x;
+  }
+};
 // The split kernel's order: the token tiles of one weight tile next to each other.  Dense: from the grid.
 __device__ __forceinline__ Tile tile_at(int j, int m, int e, int first, int n, const MmParams& p) {
   Tile x;
@@ -113,7 +131,7 @@ __device__ __forceinline__ Tile tile_at(int j, int m, int e, int first, int n, c
   x.m = m * 128;
   x.row = first + j * p.n_tile;
   x.count = min(p.n_tile, n - j * p.n_tile);
-  x.a_sf_row = static_cast<int64_t>((p.n_experts > 0 ? quick_div(first, p.lt) + e : 0) + j * p.lt_per_tile) * p.sub;
+  x.a_sf_row = ((p.n_experts > 0 ? quick_div(first, p.lt) + e : 0) + j * p.lt_per_tile) * p.sub;
   return x;
 }
 __device__ __forceinline__ Tile tile_of_group(int t, const MmParams& p, const int* prefix) {
@@ -234,6 +252,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   const uint32_t smem_at = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;      // shared-memory address of the ring
   uint8_t* smem = smem_raw + (smem_at - ptx::smem_addr(smem_raw));
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], part_empty;
+  __shared__ int stage_n[kMaxStages];                  // tokens of the tile a stage belongs to, from the producer
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_word;
   __shared__ int prefix[kMaxGroups + 1];
@@ -267,22 +286,20 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   const uint32_t tmem = tmem_slot;
   const int num_tiles = p.n_experts > 0 ? prefix[p.n_experts] : (p.rows + p.n_tile - 1) / p.n_tile * p.m_tiles;
 
-  const int ahead_k = min(3, p.num_k - 1);             // in this stage of a tile the next one is worked out
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (both CTAs)
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
     ptx::pdl_wait();
-    Tile x = {}, next_x = {};
-    if (pair0 < num_tiles) next_x = tile_of(pair0, p, prefix);
+    TileWalk walk = {};
     for (int t = pair0; t < num_tiles && ok; t += pairs) {
-      x = next_x;
+      const Tile x = walk.next(t, pairs, num_tiles, p, prefix);
       const int half = ((x.count + 15) & ~15) >> 1;    // tokens of this CTA
       const int w_row = static_cast<int>(x.e * p.out + x.m) + static_cast<int>(rank) * 128;
       const int a_row = x.row + static_cast<int>(rank) * half;
       int w_sf = static_cast<int>((x.e * p.w_sf_rows + x.m / kSfRows + rank) * p.n_sf * 4);
-      int a_sf0 = static_cast<int>(x.a_sf_row * p.n_sf * 4), a_sf1 = static_cast<int>((x.a_sf_row + 1) * p.n_sf * 4);
+      int a_sf0 = static_cast<int>(x.a_sf_row * p.n_sf * 4), a_sf1 = a_sf0 + static_cast<int>(p.n_sf * 4);
       for (int k = 0; k < p.num_k; ++k) {
         ok = ptx::mbar_wait_warp(&empty[stage], phase ^ 1u, dead, p.status_dev);
         if (!ok) break;
@@ -292,7 +309,10 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         const uint32_t bar = ptx::map_to_cta(ptx::smem_addr(&full[stage]), 0);
         if (ptx::elect_one()) {
           // one barrier, the leader's, counts both CTAs' bytes
-          if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * stage_size);
+          if (rank == 0) {
+            stage_n[stage] = 2 * half;
+            ptx::mbar_arrive_expect_tx(&full[stage], 2 * stage_size);
+          }
           ptx::tma_load_2d_pair(w_dst, &tmW, k * (kKT / 2), w_row, bar);
           ptx::tma_load_2d_pair(a_dst, &tmA, k * (kKT / 2), a_row, bar);
           ptx::tma_load_2d_pair(ws_dst, &tmWs, 0, w_sf, bar);
@@ -300,8 +320,6 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           ptx::tma_load_2d_pair(ws_dst + 2 * kSf, &tmAs, 0, a_sf1, bar);
         }
         __syncwarp();
-        // the next tile is worked out while there is nothing to wait for
-        if (k == ahead_k && t + pairs < num_tiles) next_x = tile_of(t + pairs, p, prefix);
         w_sf += kSfTiles * 4;
         a_sf0 += kSfTiles * 4;
         a_sf1 += kSfTiles * 4;
@@ -315,10 +333,8 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, part_phase = 0;
       bool ok = true, ready = false;
-      int next_count = pair0 < num_tiles ? tile_of(pair0, p, prefix).count : 0;
       for (int t = pair0; t < num_tiles && ok; t += pairs) {
-        const int n = (next_count + 15) & ~15;
-        const uint32_t id0 = ptx::idesc_fp4(256, n, !NV, 0), id1 = ptx::idesc_fp4(256, n, !NV, NV ? 0 : 2);
+        uint32_t id0 = 0, id1 = 0;
         ok = ptx::mbar_wait_warp(&acc_empty[buf], acc_phase ^ 1u, dead, p.status_dev);
         if (ok && sharing && t != pair0) {             // the tile before has left the shared columns
           ok = ptx::mbar_wait_warp(&part_empty, part_phase, dead, p.status_dev);
@@ -334,6 +350,11 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           if (++stage == p.n_stages) { stage = 0; phase ^= 1u; }
           // asked before this stage's instructions are issued: the answer is there when they are
           const bool next = ptx::mbar_test(&full[stage], phase);
+          if (k == 0) {
+            const int n = __shfl_sync(0xffffffffu, stage_n[cur], 0);
+            id0 = ptx::idesc_fp4(256, n, !NV, 0);
+            id1 = ptx::idesc_fp4(256, n, !NV, NV ? 0 : 2);
+          }
           const uint32_t w16 = (smem_at + cur * stage_size) >> 4;
           const int steps = steps_of(p.in, k);
           if (ptx::elect_one()) {
@@ -342,7 +363,6 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
             ptx::mma_commit_pair(&empty[cur]);
             if (k == p.num_k - 1) ptx::mma_commit_pair(&acc_full[buf]);
           }
-          if (k == ahead_k && t + pairs < num_tiles) next_count = tile_of(t + pairs, p, prefix).count;
           ready = __all_sync(0xffffffffu, next) != 0;
         }
         buf ^= 1;
@@ -358,8 +378,9 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     uint32_t acc_phase = 0;
     const float scale = product_scale<NV>(p);
     const uint32_t part_bar = ptx::map_to_cta(ptx::smem_addr(&part_empty), 0);
+    TileWalk walk = {};
     for (int t = pair0; t < num_tiles; t += pairs) {
-      const Tile x = tile_of(t, p, prefix);
+      const Tile x = walk.next(t, pairs, num_tiles, p, prefix);
       if (!ptx::mbar_wait_warp(&acc_full[buf], acc_phase, dead, p.status_dev)) break;
       ptx::tc_fence_after_sync();
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
