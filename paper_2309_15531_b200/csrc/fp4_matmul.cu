@@ -30,6 +30,7 @@ constexpr int kThreads = 192;                          // TMA warp, MMA warp, fo
 constexpr int kPairThreads = 320;                      // pair kernel: eight
 constexpr int kMaxStages = 8;
 constexpr uint32_t kWBytes = 128 * 128;
+constexpr uint32_t kOutBytes = 8 * 4096;               // pair kernel: tiles of Y on their way out
 constexpr int kFusedThreads = 320;                     // split kernel that quantizes: four warps more,
 constexpr int kFusedPerSm = 3;                         // CTAs of an SM (by its registers)
 constexpr int kFusedTile = 16;                         // and tokens of a tile
@@ -54,6 +55,8 @@ struct MmParams {
   int64_t w_sf_rows;                                   // scale tile rows of one weight
   void* Y;
   int64_t ldy;
+  int bulk_y;                                          // pair kernel: Y can be stored by TMA
+  unsigned pace_ns;                                    // and the pause between two stores of 32 tokens
   const float* a_amax;
   const float* b_amax;
   int* status_dev;
@@ -171,6 +174,12 @@ __device__ __forceinline__ void tile_prefix(const MmParams& p, int lane, int* pr
 __device__ __forceinline__ void put(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(__half* y, float v) { *y = __float2half_rn(v); }
 __device__ __forceinline__ void put(float* y, float v) { *y = v; }
+template <typename T>
+__device__ __forceinline__ uint32_t packed(float a, float b) {       // a in the low half
+  if constexpr (sizeof(T) == 4) return 0;
+  else if constexpr (__is_same(T, __half)) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+  else { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
+}
 // 32 tokens of one weight row: y + j * ldy receives v[j] * scale, j < n
 template <typename T>
 __device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, float scale, const float (&v)[32]) {
@@ -238,7 +247,8 @@ __device__ __forceinline__ int steps_of(int64_t in, int k) {
 template <int FORMAT, typename T>
 __global__ void __launch_bounds__(kPairThreads, 1)
 fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
+                const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs,
+                const __grid_constant__ CUtensorMap tmY, const MmParams p) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
   constexpr int kSfTiles = kSf / kSfTileBytes;
@@ -255,12 +265,13 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   __shared__ int stage_n[kMaxStages];                  // tokens of the tile a stage belongs to, from the producer
   __shared__ uint32_t tmem_slot;
   __shared__ int dead_word;
-  __shared__ int prefix[kMaxGroups + 1];
   volatile int* dead = &dead_word;
   const int warp = ptx::uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
   const uint32_t stage_size = stage_bytes(FORMAT, true, p.n_tile);
   const uint32_t a_bytes = static_cast<uint32_t>(p.n_tile) * 64;
+  const uint32_t out_at = smem_at + p.n_stages * stage_size;                  // [4 warp pairs][2][32 tokens][128 bytes]
+  int* prefix = reinterpret_cast<int*>(smem + p.n_stages * stage_size + kOutBytes);      // [n_experts + 1], grouped only
   const int pair0 = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
@@ -378,6 +389,13 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     uint32_t acc_phase = 0;
     const float scale = product_scale<NV>(p);
     const uint32_t part_bar = ptx::map_to_cta(ptx::smem_addr(&part_empty), 0);
+    auto give_back = [&]() {
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive_cluster(part_bar);
+    };
+    const bool bulk_y = sizeof(T) == 2 && p.bulk_y;
+    int out_buf = 0;
     TileWalk walk = {};
     for (int t = pair0; t < num_tiles; t += pairs) {
       const Tile x = walk.next(t, pairs, num_tiles, p, prefix);
@@ -386,31 +404,71 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
       T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
       const uint32_t acc = tmem + (static_cast<uint32_t>(q * 32) << 16) + buf * acc_step;
+      // Columns c .. c + 31 of the accumulator.  Results of 16 bits leave through shared memory, 64 weight rows of
+      // 16 tokens by a pair of warps as a bulk store: 64-byte stores from registers held up the loads of the
+      // next tile's operands (2048 tokens x W[11008,4096]: a tile of 7700 cycles took 9200).
+      auto drain = [&](int c, bool hand_back) {
+        const int left = x.count - c;
+        // the matrix's last tile may be cut anywhere (what lies behind the matrix is not written), others at 16
+        if (left > 0 && bulk_y && (left >= 32 || left == 16 || (p.n_experts == 0 && x.row + x.count == p.rows))) {
+          float lo[16], hi[16];
+          ptx::tmem_ld_rows16_nowait(acc + c, lo);
+          ptx::tmem_ld_rows16_nowait(acc + c + (16u << 16), hi);
+          ptx::tmem_ld_wait();
+          if (hand_back) give_back();
+          if (lane == 0 && (q & 1) == 0) ptx::bulk_wait_read_but_one();       // this buffer's last store has read it
+          ptx::named_sync(1 + side * 2 + (q >> 1), 64);
+          const uint32_t tile = out_at + (side * 4 + (q >> 1) * 2 + out_buf) * 4096;
+          const uint32_t unit = (q & 1) * 4 + (lane >> 3);                    // 16 bytes: eight weight rows
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int token = u * 8 + (lane & 7);
+            ptx::stmatrix_trans(tile + token * 128 + ((unit ^ (token & 7)) << 4), packed<T>(lo[4 * u] * scale, lo[4 * u + 1] * scale),
+                                packed<T>(lo[4 * u + 2] * scale, lo[4 * u + 3] * scale),
+                                packed<T>(hi[4 * u] * scale, hi[4 * u + 1] * scale),
+                                packed<T>(hi[4 * u + 2] * scale, hi[4 * u + 3] * scale));
+          }
+          ptx::fence_proxy_async();
+          ptx::named_sync(1 + side * 2 + (q >> 1), 64);
+          const int y_col = x.m + static_cast<int>(rank) * 128 + (q >> 1) * 64;
+          if (lane == 0 && (q & 1) == 0) {
+            if (y_col < p.out) {
+              ptx::tma_store_2d(&tmY, y_col, x.row + c, tile);
+              if (left > 16) ptx::tma_store_2d(&tmY, y_col, x.row + c + 16, tile + 16 * 128);
+            }
+            ptx::bulk_commit();
+          }
+          out_buf ^= 1;
+        } else {
+          float v[32];
+          if (left > 0) ptx::tmem_ld32(acc + c, v);
+          if (hand_back) give_back();
+          if (left > 0 && o < p.out) store_tokens(y + c * p.ldy, p.ldy, left, scale, v);
+        }
+      };
       int done = -1;                                   // the shared columns, taken first by half of the warps
       if (sharing) {
-        float v[32];
         const int c = buf == 0 ? 224 : 0;
-        if (side == (c >> 5 & 1)) done = c;
-        const bool any = done >= 0 && c < x.count;
-        if (any) ptx::tmem_ld32(acc + c, v);
-        ptx::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive_cluster(part_bar);
-        if (any && o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
+        if (side == (c >> 5 & 1)) {
+          done = c;
+          drain(c, true);
+        } else {
+          give_back();
+        }
       }
 #pragma unroll 1
-      for (int c = side * 32; c < x.count; c += 64) {
-        if (c == done) continue;
-        float v[32];
-        ptx::tmem_ld32(acc + c, v);
-        if (o < p.out) store_tokens(y + c * p.ldy, p.ldy, x.count - c, scale, v);
-      }
+      for (int c = side * 32; c < x.count; c += 64)
+        if (c != done) {
+          drain(c, false);
+          if (p.pace_ns > 0 && t + pairs < num_tiles) __nanosleep(p.pace_ns);
+        }
       ptx::tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(ptx::smem_addr(&acc_empty[buf]), 0));
       buf ^= 1;
       if (buf == 0) acc_phase ^= 1u;
     }
+    if (bulk_y && lane == 0) ptx::bulk_wait_all();     // every store is complete before the CTA ends
   }
 
   ptx::tc_fence_before_sync();
@@ -437,7 +495,8 @@ __host__ __device__ __forceinline__ int exchange_floats(int n_tile, int splits) 
 template <int FORMAT, typename T, bool FUSED>
 __global__ void __launch_bounds__(FUSED ? kFusedThreads : kThreads, FUSED ? kFusedPerSm : 4)
 fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
-                 const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs, const MmParams p) {
+                 const __grid_constant__ CUtensorMap tmWs, const __grid_constant__ CUtensorMap tmAs,
+                 const __grid_constant__ CUtensorMap, const MmParams p) {
   constexpr bool NV = FORMAT == ADADIM_NVFP4;
   constexpr uint32_t kSf = sf_stage_bytes(FORMAT);
   constexpr int kSfTiles = kSf / kSfTileBytes;
@@ -681,12 +740,13 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   }
 }
 
-constexpr size_t kSmem = 220 * 1024;                   // dynamic shared memory of one SM's CTAs
+constexpr size_t kSmem = 220 * 1024;                   // dynamic shared memory of one SM's split CTAs
+constexpr size_t kSmemPair = 226 * 1024 - 512;         // and of a pair CTA
 
 template <typename K>
-int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem,
+int launch(K kernel, const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem,
            bool chained, cudaStream_t st) {
-  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)));
+  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemPair)));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
@@ -708,12 +768,12 @@ int launch(K kernel, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, i
   }
   cfg.attrs = attr;
   cfg.numAttrs = static_cast<unsigned>(n);
-  ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm[0], tm[1], tm[2], tm[3], p));
+  ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm[0], tm[1], tm[2], tm[3], tm[4], p));
   return ADADIM_OK;
 }
 
 template <typename T>
-int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[4], const MmParams& p, dim3 grid, size_t smem, bool chained,
+int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, size_t smem, bool chained,
                   cudaStream_t st) {
   if (pair) return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st)
                                           : launch(fp4_pair_kernel<ADADIM_NVFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st);
@@ -833,7 +893,7 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, co
   const int64_t weights = n_experts > 0 ? n_experts : 1;
   const uint64_t inner = static_cast<uint64_t>((in + 1) / 2);
   const uint32_t sf_box = sf_stage_bytes(format) / 128;
-  CUtensorMap tm[4];
+  CUtensorMap tm[5];
   int rc;
   if ((rc = make_tmap_u8(&tm[0], B.codes, inner, static_cast<uint64_t>(weights * out), static_cast<uint64_t>(B.ld), 128, true)) != ADADIM_OK) return rc;
   if ((rc = make_tmap_u8(&tm[2], B.scales, 128, weights * scale_bytes(format, out, in, 0) / 128, 128, sf_box, false)) != ADADIM_OK) return rc;
@@ -846,12 +906,22 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, co
     if ((rc = make_tmap_u8(&tm[3], A.scales, 128, static_cast<uint64_t>(sf_tile_rows(n_rows, n_experts, lt) * p.n_sf * 4), 128, sf_box, false)) != ADADIM_OK) return rc;
   }
 
+  tm[4] = tm[0];                                       // used by the pair kernel only
   const size_t per = stage_bytes(format, pair, p.n_tile);
   size_t fixed = 1024;                                 // alignment, and what lies behind the ring
   dim3 grid;
   if (pair) {
     grid = dim3(static_cast<unsigned>(2 * (tiles < kSms / 2 ? tiles : kSms / 2)));
-    p.n_stages = static_cast<int>((kSmem - fixed) / per);
+    fixed += kOutBytes + static_cast<size_t>(n_experts > 0 ? n_experts + 1 : 0) * 4;
+    p.n_stages = static_cast<int>((kSmemPair - fixed) / per);
+    const int64_t ysz = ydtype == ADADIM_F32 ? 4 : 2;
+    // All CTAs drain at the same time, and their stores hold up each other's loads: pauses spread the stores over
+    // the next tile's time (270 ns a stage, four stores of a warp pair) where that is long enough.  2048 tokens x
+    // W[11008,4096] 42.3 -> 40.7 us, experts 177 -> 170 us; with four stages a tile (in = 1024) it lost 7 %.
+    p.pace_ns = p.num_k < 16 ? 0u : p.num_k < 32 ? 30u * static_cast<unsigned>(p.num_k) : 960u;
+    p.bulk_y = ysz == 2 && aligned16(Y) && (ldy * ysz) % 16 == 0;
+    if (p.bulk_y && (rc = make_tmap_u16(&tm[4], Y, static_cast<uint64_t>(out), static_cast<uint64_t>(n_rows),
+                                        static_cast<uint64_t>(ldy * ysz), 16)) != ADADIM_OK) return rc;
   } else {
     grid = n_experts > 0 ? dim3(static_cast<unsigned>(tiles * p.splits))
                          : dim3(static_cast<unsigned>(token_tiles * p.splits), static_cast<unsigned>(p.m_tiles));

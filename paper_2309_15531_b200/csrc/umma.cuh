@@ -146,6 +146,14 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, int
       : "memory");
 }
 
+// 2-D tile store from this CTA's shared memory, as part of the issuing thread's bulk async-group.  The part of the
+// tile outside the tensor is not written; the tile must start inside it.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(src) : "memory");
+}
+// until all but the latest committed group have finished reading shared memory
+__device__ __forceinline__ void bulk_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 // 2-D tile reduction (element-wise add) from this CTA's shared memory into global memory, as part
 // of the issuing thread's bulk async-group.  x as above; the tile must lie inside the tensor.
 __device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap* m, int x, int y, const void* src) {
@@ -286,6 +294,26 @@ __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, float (&v)[16])
 #pragma unroll
   for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
 }
+// 32 fp32 columns of 16 TMEM lanes (16 or 0 of this warp's 32): lane t of the warp gets, of every eight columns u,
+// columns 2 (t % 4) and + 1 of row t / 4 in r[4 u], r[4 u + 1] and of row t / 4 + 8 in r[4 u + 2], r[4 u + 3].
+// The caller waits (tmem_ld_wait).
+__device__ __forceinline__ void tmem_ld_rows16_nowait(uint32_t taddr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+}
+// Four 8 x 8 matrices of 16-bit elements to shared memory, transposed: lane t holds elements (2 (t % 4), t / 4) and
+// (2 (t % 4) + 1, t / 4) of each; lane 8 i + j gives the address of row j (16 bytes) of matrix i.
+__device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- descriptors ----------------------------------------------------------------------------
@@ -330,6 +358,8 @@ int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t 
 int make_tmap_f32(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
                   uint32_t box_rows);
 
+// 16-bit elements with 128-byte swizzle, box {64, box_rows}, for stores.
+int make_tmap_u16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes, uint32_t box_rows);
 // Bytes with 128-byte swizzle (box {128, box_rows}: packed 4-bit codes) or without (scale tiles as
 // 128-byte rows).
 int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
