@@ -449,6 +449,16 @@ def _product_out(y, rows, out, dtype, device):
     return y
 
 
+def _matrix_in(X: torch.Tensor):
+    """(pointer, dtype code, rows, columns, pitch, device index) of a row-major matrix; as few tensor queries as
+    possible, for the small products whose time is the caller's."""
+    rows, cols = X.shape
+    ld, step = X.stride()
+    dev = X.get_device()
+    assert dev >= 0 and (cols <= 1 or step == 1)
+    return X.data_ptr(), _DT[X.dtype], rows, cols, (ld if rows > 1 or ld > cols else cols), dev
+
+
 def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y = Q(X) W^T for activations X[n_tokens, in] (fp32, fp16, bf16; quantized in the call with x_amax) or for an
@@ -462,16 +472,21 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
         _check(lib().adadim_fp4_matmul(C.byref(X.c()), X.rows, C.byref(W.c()), W.rows, W.cols, W.fmt, y.data_ptr(),
                                        _DT[y.dtype], _ld(y), _ptr(status), _raw_stream(X.codes)), "adadim_fp4_matmul")
         return y
-    _rows_of(X)
-    rows, inp = X.shape
+    xp, xdt, rows, inp, ldx, dev = _matrix_in(X)
     if inp != W.cols:
         raise ValueError("fp4_linear: X and W do not match")
-    y = _product_out(y, rows, W.rows, X.dtype, X.device)
+    if y is None:
+        y = torch.empty(rows, W.rows, dtype=X.dtype, device=X.device)
+    yp, ydt, y_rows, y_cols, ldy, _ = _matrix_in(y)
+    assert y_rows == rows and y_cols == W.rows
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
-    _check(lib().adadim_fp4_linear(X.data_ptr(), _DT[X.dtype], rows, inp, _ld(X), _ptr(x_amax), C.byref(W.c()), W.rows,
-                                   W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
-                                   workspace.numel(), _raw_stream(X)), "adadim_fp4_linear")
+    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, x_amax.data_ptr() if x_amax is not None else None,
+                                 C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
+                                 status.data_ptr() if status is not None else None, workspace.data_ptr(),
+                                 workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check(rc, "adadim_fp4_linear")
     return y
 
 
@@ -492,17 +507,22 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
                                                W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status),
                                                _raw_stream(X.codes)), "adadim_fp4_matmul_grouped")
         return y
-    _rows_of(X)
-    rows, inp = X.shape[0] if row_index is None else _i32(row_index).numel(), X.shape[1]
+    xp, xdt, x_rows, inp, ldx, dev = _matrix_in(X)
     if inp != W.cols:
         raise ValueError("fp4_linear_grouped: X and W do not match")
-    y = _product_out(y, rows, W.rows, X.dtype, X.device)
+    rows, ip = (x_rows, None) if row_index is None else (_i32(row_index).numel(), row_index.data_ptr())
+    if y is None:
+        y = torch.empty(rows, W.rows, dtype=X.dtype, device=X.device)
+    yp, ydt, y_rows, y_cols, ldy, _ = _matrix_in(y)
+    assert y_rows == rows and y_cols == W.rows
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, n), X.device)
-    _check(lib().adadim_fp4_linear_grouped(X.data_ptr(), _DT[X.dtype], X.shape[0], inp, _ld(X), _ptr(x_amax),
-                                           _ptr(row_index), offsets.data_ptr(), n, rows, C.byref(W.c()), W.rows, W.fmt,
-                                           y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status), workspace.data_ptr(),
-                                           workspace.numel(), _raw_stream(X)), "adadim_fp4_linear_grouped")
+    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, x_amax.data_ptr() if x_amax is not None else None,
+                                         ip, offsets.data_ptr(), n, rows, C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
+                                         status.data_ptr() if status is not None else None, workspace.data_ptr(),
+                                         workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check(rc, "adadim_fp4_linear_grouped")
     return y
 
 

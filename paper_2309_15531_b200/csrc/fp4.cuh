@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace adadim {
@@ -330,6 +332,19 @@ __device__ __forceinline__ void rows_of_tile_row(const int32_t* offsets, int n_g
 }
 
 }  // namespace fp4
+
+// Sets an attribute of a kernel the first time it is launched on a device (a kernel's attributes stay as they are
+// set; asking again costs each call half a microsecond).
+template <typename K>
+int set_once(K kernel, cudaFuncAttribute attr, int value, std::atomic<uint64_t>& devices) {
+  int dev = 0;
+  ADADIM_CUDA_TRY(cudaGetDevice(&dev));
+  const uint64_t bit = uint64_t{1} << (dev & 63);
+  if (dev < 64 && (devices.load(std::memory_order_acquire) & bit) != 0) return ADADIM_OK;
+  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, attr, value));
+  if (dev < 64) devices.fetch_or(bit, std::memory_order_release);
+  return ADADIM_OK;
+}
 
 // implemented in fp4_quant.cu and fp4_matmul.cu
 int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, cudaStream_t st);

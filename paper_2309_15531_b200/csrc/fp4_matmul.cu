@@ -743,10 +743,12 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 constexpr size_t kSmem = 220 * 1024;                   // dynamic shared memory of one SM's split CTAs
 constexpr size_t kSmemPair = 226 * 1024 - 512;         // and of a pair CTA
 
-template <typename K>
-int launch(K kernel, const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem,
-           bool chained, cudaStream_t st) {
-  ADADIM_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemPair)));
+template <auto KERNEL>
+int launch(const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem, bool chained,
+           cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  const int rc = set_once(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemPair), done);
+  if (rc != ADADIM_OK) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
@@ -768,19 +770,19 @@ int launch(K kernel, const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, i
   }
   cfg.attrs = attr;
   cfg.numAttrs = static_cast<unsigned>(n);
-  ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, tm[0], tm[1], tm[2], tm[3], tm[4], p));
+  ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, KERNEL, tm[0], tm[1], tm[2], tm[3], tm[4], p));
   return ADADIM_OK;
 }
 
 template <typename T>
 int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, size_t smem, bool chained,
                   cudaStream_t st) {
-  if (pair) return format == ADADIM_MXFP4 ? launch(fp4_pair_kernel<ADADIM_MXFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st)
-                                          : launch(fp4_pair_kernel<ADADIM_NVFP4, T>, tm, p, grid, kPairThreads, 2, smem, chained, st);
-  if (fused) return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T, true>, tm, p, grid, kFusedThreads, p.splits, smem, false, st)
-                                           : launch(fp4_split_kernel<ADADIM_NVFP4, T, true>, tm, p, grid, kFusedThreads, p.splits, smem, false, st);
-  return format == ADADIM_MXFP4 ? launch(fp4_split_kernel<ADADIM_MXFP4, T, false>, tm, p, grid, kThreads, p.splits, smem, chained, st)
-                                : launch(fp4_split_kernel<ADADIM_NVFP4, T, false>, tm, p, grid, kThreads, p.splits, smem, chained, st);
+  if (pair) return format == ADADIM_MXFP4 ? launch<fp4_pair_kernel<ADADIM_MXFP4, T>>(tm, p, grid, kPairThreads, 2, smem, chained, st)
+                                          : launch<fp4_pair_kernel<ADADIM_NVFP4, T>>(tm, p, grid, kPairThreads, 2, smem, chained, st);
+  if (fused) return format == ADADIM_MXFP4 ? launch<fp4_split_kernel<ADADIM_MXFP4, T, true>>(tm, p, grid, kFusedThreads, p.splits, smem, false, st)
+                                           : launch<fp4_split_kernel<ADADIM_NVFP4, T, true>>(tm, p, grid, kFusedThreads, p.splits, smem, false, st);
+  return format == ADADIM_MXFP4 ? launch<fp4_split_kernel<ADADIM_MXFP4, T, false>>(tm, p, grid, kThreads, p.splits, smem, chained, st)
+                                : launch<fp4_split_kernel<ADADIM_NVFP4, T, false>>(tm, p, grid, kThreads, p.splits, smem, chained, st);
 }
 
 // Tiles of fewer tokens than 128 are cut no lower than this, and only up to so many rows (of a typical

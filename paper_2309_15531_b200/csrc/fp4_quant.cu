@@ -181,9 +181,12 @@ int launch(const QuantParams& p, dim3 grid, cudaStream_t st) {
   // if this kernel left the SM with a small share, the product would wait until the SM is empty.  With few
   // CTAs (VALUES = 3) the share is therefore set to the most; with many that would cost the kernel the
   // cache its loads in flight need (8192 x 4096 bf16: 27 us instead of 16).
-  if (VALUES == 3)
-    ADADIM_CUDA_TRY(cudaFuncSetAttribute(quantize_kernel<T, FORMAT, VALUES>, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                         cudaSharedmemCarveoutMaxShared));
+  if (VALUES == 3) {
+    static std::atomic<uint64_t> done{0};
+    const int rc = set_once(quantize_kernel<T, FORMAT, VALUES>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                            cudaSharedmemCarveoutMaxShared, done);
+    if (rc != ADADIM_OK) return rc;
+  }
   quantize_kernel<T, FORMAT, VALUES><<<grid, kThreads, static_cast<size_t>(p.side) * kSfTileBytes, st>>>(p);
   return cudaGetLastError() == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
 }
