@@ -632,8 +632,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       // columns of the accumulator that nobody reads.
       const int group = (warp - 2) / sharing, chunk = lane & 15;
       const int r = ((warp - 2) - group * sharing) * 2 + (lane >> 4);
-      const int64_t src = r < x.count ? source_row(p.x, static_cast<int64_t>(x.row) + r) : -1;
-      const T* at = static_cast<const T*>(p.x.X) + (src < 0 ? 0 : src * p.x.ldx);
+      const T* at = static_cast<const T*>(p.x.X) + static_cast<int64_t>(r < x.count ? x.row + r : 0) * p.x.ldx;
       const int t_log2 = NV ? tensor_scale_log2(p.a_amax) : 0;
       const uint32_t a_at = r * 128 + (((chunk >> 1) ^ (r & 7)) << 4) + (chunk & 1) * 8;
       const int blk = NV ? chunk : chunk >> 1;
@@ -641,7 +640,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       Raw<T> next;
       auto load = [&](int i) {
         const int64_t c0 = static_cast<int64_t>(k0 + i) * kKT + chunk * kPer;
-        if (src >= 0 && c0 < p.in) load16_aligned(at + c0, next);
+        if (r < x.count && c0 < p.in) load16_aligned(at + c0, next);
         else
 #pragma unroll
           for (uint32_t& w : next.w) w = 0;
@@ -789,19 +788,20 @@ int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[5],
 // expert), which bounds the scale tiles of the activations.
 constexpr int kMinCut = 32, kMaxCutRows = 512;
 constexpr int kMinPairTile = 160;                      // the pair kernel's lowest token tile, two scale tile rows
-// Rows (of a typical expert) up to which the product quantizes them itself: every weight tile's CTA repeats
-// the work, which at 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us
-// fused, 24.5 us behind the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).
+// Rows up to which a dense product quantizes them itself: every weight tile's CTA repeats the work, which at
+// 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us fused, 24.5 us behind
+// the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).  Not with experts, some of which have more rows than the
+// typical one (128 rows over 32: 27.4 us fused, 25.0 us behind the quantizer).
 constexpr int kFusedTokens = 8;
 
 // The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
 // kernels below (1.9 GHz, 148 SMs):
-//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256, and no less than 235 (MXFP4) or 270 (its
-//          instructions have to be issued); a tile 650 on top, 100 up to 240 tokens; start and end 5000;
+//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256, and a CTA takes in no more than 130 bytes a
+//          nanosecond; a tile 1000 on top; start and end 5000;
 //          it streams no faster than 1 / 1.7 of the split kernel
-//   split  a CTA's stage takes no less than 300 whatever its size, and the CTAs of an SM share 80 bytes a
-//          nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
-//          and in all no less than the weights' bytes at 6000 a nanosecond.
+//   split  a CTA's stage takes no less than 300 whatever its size, an SM takes in 80 bytes a nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
+//          and in all no less than the weights' bytes at 6000 a nanosecond
+//   and the result's bytes leave at 5000 (pair) or 2500 (split) a nanosecond, hardly beside the rest.
 Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool quantized, bool fuse, int sms) {
   const int64_t weights = n_experts > 0 ? (n_experts < rows ? n_experts : rows) : 1;
   const int64_t typical = (rows + weights - 1) / weights;            // rows of one expert if they were equal
@@ -811,18 +811,19 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
   Fp4Plan best = {true, 256, 1, 1, false};
   double best_ns = 1e300;
   const double floor_ns = static_cast<double>(weights * out) * static_cast<double>(in) * (format == ADADIM_MXFP4 ? 0.53125 : 0.5625) / 6000.0;
+  const double y_bytes = 2.0 * static_cast<double>(rows) * static_cast<double>(out);
   for (int n_tile = 256; n_tile >= (quantized ? 256 : kMinPairTile); n_tile -= 16) {
     const int64_t tiles = (out + 255) / 256 * token_tiles(n_tile), waves = (tiles + sms / 2 - 1) / (sms / 2);
     const double n = typical < n_tile ? static_cast<double>((typical + 15) / 16 * 16) : n_tile;
-    const double least = format == ADADIM_MXFP4 ? 235.0 : 270.0, stage = 1.055 * n < least ? least : 1.055 * n;
-    double ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + (n_tile > 240 ? 650.0 : 100.0));
+    const double bytes = stage_bytes(format, true, n_tile) / 130.0, stage = 1.055 * n < bytes ? bytes : 1.055 * n;
+    double ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + 1000.0);
     if (ns < 1.7 * floor_ns) ns = 1.7 * floor_ns;
-    ns += 5000.0;
+    ns += 5000.0 + y_bytes / 5000.0;
     if (ns < best_ns) { best_ns = ns; best.n_tile = n_tile; }
   }
   for (int n_tile = 16; n_tile <= 128; n_tile *= 2) {
     // lower tiles than 128 rows: only where they are the only ones, or the scales are laid out for them
-    const bool fused = fuse && n_tile <= kFusedTile && typical <= kFusedTokens;
+    const bool fused = fuse && n_experts == 0 && n_tile <= kFusedTile && rows <= kFusedTokens;
     if (n_tile < 128 && rows > n_tile && (quantized || (n_tile < kMinCut && !fused) || typical > kMaxCutRows)) continue;
     if (n_tile > 16 && n_tile / 2 >= rows) break;
     const int64_t tiles = (out + 127) / 128 * token_tiles(n_tile);
@@ -833,14 +834,16 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
       const int stages = static_cast<int>(k < 3 ? k : 3);
       const int most = fused ? kFusedPerSm : 4;
       int per_sm = static_cast<int>((ctas + sms - 1) / sms < most ? (ctas + sms - 1) / sms : most);
+      // clusters find their SMs more easily when they need not be empty (64 x W[1024,12288] over 8: 12.8 -> 8.5 us)
+      if (splits > 1 && per_sm < 2) per_sm = 2;
       while (per_sm > 1 && (per_sm * (stages * per + fixed + 1024) > kSmem || per_sm * (n_tile <= 64 ? 128 : 256) > 512)) --per_sm;
       if (stages * per + fixed + 1024 > kSmem) continue;
       const int64_t waves = (ctas + static_cast<int64_t>(per_sm) * sms - 1) / (static_cast<int64_t>(per_sm) * sms);
-      const double shared = static_cast<double>(per_sm) * static_cast<double>(per) / 80.0;
-      const double stage = shared < 300.0 ? 300.0 : shared;
-      double ns = static_cast<double>(waves) * static_cast<double>(k) * stage;
+      const double latency = static_cast<double>(waves) * static_cast<double>(k) * 300.0;
+      const double bytes = static_cast<double>(ctas) / sms * static_cast<double>(k) * static_cast<double>(per) / 80.0;
+      double ns = latency > bytes ? latency : bytes;
       if (ns < floor_ns) ns = floor_ns;
-      ns += 4000.0 + (splits > 1 ? 1500.0 + 15.0 * n_tile : 0.0);
+      ns += 4000.0 + y_bytes / 2500.0 + (splits > 1 ? 1500.0 + 15.0 * n_tile : 0.0);
       if (ns < best_ns) { best_ns = ns; best = {false, n_tile, splits, per_sm, fused}; }
     }
   }

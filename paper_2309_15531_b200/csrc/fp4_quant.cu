@@ -15,12 +15,54 @@ namespace {
 
 using namespace fp4;
 
-constexpr int kThreads = 128;
-constexpr int kBatch = 4;                    // rows of a thread whose loads are in flight together
+// How the work is laid out, by the number of CTAs (one to a scale tile):
+//   kMany  128 threads, a thread takes 4 or 8 rows, the loads of four in flight together
+//   kLow   the same for a product's low token tiles, which may lie side by side in a CTA, and for up to kLowCtas
+//          CTAs in front of a product: with the SM's shared memory left to the product (see the launcher)
+//   kFew   up to kFewCtas: 512 threads with one or two rows each, to have something to hide the latencies behind
+// (333 x 5003 fp32, 237 CTAs: 13.4 us as kMany, 7.4 us as kFew; 2048 x 4096 bf16 to MXFP4, 512 CTAs: 6.8 and 7.8 us)
+enum Mode { kMany, kLow, kFew };
+constexpr int kFewCtas = 2 * 148, kLowCtas = 4 * 148;
+template <Mode MODE>
+constexpr int kThreadsOf = MODE == kFew ? 512 : 128;
 
 __device__ __forceinline__ void store32(void* p, const uint32_t* w) {           // 32-byte aligned
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
+// Sixteen values to any address: up to the next 16-byte boundary one by one, then whole 16-byte blocks.
+__device__ __forceinline__ void store16_shifted(float* out, const float (&q)[kPer]) {
+  const int head = static_cast<int>((16u - (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(out)) & 15u)) >> 2) & 3;
+  float r[kPer + 2];                                          // q from `head` on
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) r[k] = head & 1 ? q[k + 1 < kPer ? k + 1 : k] : q[k];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) if (head & 2) r[k] = r[k + 2 < kPer ? k + 2 : k];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) if (k < head) out[k] = q[k];
+  float4* block = reinterpret_cast<float4*>(out + head);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) block[k] = make_float4(r[4 * k], r[4 * k + 1], r[4 * k + 2], r[4 * k + 3]);
+  if (head == 0) {
+    block[3] = make_float4(q[12], q[13], q[14], q[15]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) if (k < 4 - head) out[head + 12 + k] = r[12 + k];
+  }
+}
+// The same for bf16 patterns, with 4-byte blocks.
+__device__ __forceinline__ void store16_shifted(__nv_bfloat16* out, const uint16_t (&h)[kPer]) {
+  uint16_t* o = reinterpret_cast<uint16_t*>(out);
+  if (reinterpret_cast<uintptr_t>(out) & 2u) {
+    o[0] = h[0];
+#pragma unroll
+    for (int k = 1; k < kPer - 1; k += 2) *reinterpret_cast<uint32_t*>(o + k) = h[k] | static_cast<uint32_t>(h[k + 1]) << 16;
+    o[kPer - 1] = h[kPer - 1];
+  } else {
+#pragma unroll
+    for (int k = 0; k < kPer; k += 2) *reinterpret_cast<uint32_t*>(o + k) = h[k] | static_cast<uint32_t>(h[k + 1]) << 16;
+  }
 }
 
 struct QuantParams {
@@ -41,19 +83,21 @@ struct QuantParams {
 };
 
 // CTAs of an SM that the registers must leave room for: the loads in flight are what hides the memory's latency
-template <typename T, int FORMAT>
-constexpr int kResident = sizeof(T) == 4 ? 5 : 8;
+template <typename T, Mode MODE>
+constexpr int kResident = MODE == kFew ? 2 : sizeof(T) == 4 ? 5 : 8;
 
-// VALUES: 0 none, 1 bf16, 2 fp32, 3 none and tiles side by side or few CTAs (see the launcher)
-template <typename T, int FORMAT, int VALUES>
-__global__ void __launch_bounds__(kThreads, kResident<T, FORMAT>)
+// VALUES: 0 none, 1 bf16, 2 fp32
+template <typename T, int FORMAT, int VALUES, Mode MODE>
+__global__ void __launch_bounds__(kThreadsOf<MODE>, kResident<T, MODE>)
 quantize_kernel(const QuantParams p) {
+  constexpr int kThreads = kThreadsOf<MODE>;
   constexpr int kChunks = sf_cols(FORMAT) / kPer;             // threads to a row of a tile: 4 or 8
-  constexpr int kRows = kSfRows * kChunks / kThreads;         // rows of a thread: 4 or 8
+  constexpr int kRows = kSfRows * kChunks / kThreads;         // rows of a thread: 4 or 8, kFew 1 or 2
+  constexpr int kBatch = kRows < 4 ? kRows : 4;
   extern __shared__ __align__(16) uint8_t sf[];               // [side][kSfTileBytes]
   ptx::pdl_launch_dependents();                               // a product launched behind this may start on its weight
-  const int side = VALUES == 3 ? p.side : 1;
-  const int n_sf = static_cast<int>(p.n_sf), ctas = VALUES == 3 ? (n_sf + side - 1) / side : n_sf;
+  const int side = MODE == kLow ? p.side : 1;
+  const int n_sf = static_cast<int>(p.n_sf), ctas = MODE == kLow ? (n_sf + side - 1) / side : n_sf;
   const int v = blockIdx.x / ctas;                            // tile row
   const int tile0 = (blockIdx.x - v * ctas) * side;           // first of the tiles side by side
   int first, count;
@@ -92,7 +136,7 @@ quantize_kernel(const QuantParams p) {
         sf_at[(r & 31) * 16 + (r >> 5) * 4] = static_cast<uint8_t>(live ? b.byte : 0u);
       if (!live) continue;
       *reinterpret_cast<uint2*>(codes + r * p.ld) = c;
-      if (VALUES == 1 || VALUES == 2) {
+      if (VALUES != 0) {
         const int64_t row = static_cast<int64_t>(first) + r;
         const float s = b.finite ? b.s : __uint_as_float(0x7fffffffu);
         float q[kPer];
@@ -111,6 +155,11 @@ quantize_kernel(const QuantParams p) {
               w[k] = *reinterpret_cast<const uint32_t*>(&h);
             }
             store32(out, w);
+          } else if (n == kPer) {
+            uint16_t h[kPer];
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) h[k] = __bfloat16_as_ushort(__float2bfloat16_rn(q[k]));
+            store16_shifted(out, h);
           } else {
 #pragma unroll
             for (int k = 0; k < kPer; ++k) if (k < n) out[k] = __float2bfloat16_rn(q[k]);
@@ -120,6 +169,8 @@ quantize_kernel(const QuantParams p) {
           if (n == kPer && p.wide_v) {
             store32(out, reinterpret_cast<const uint32_t*>(q));
             store32(out + 8, reinterpret_cast<const uint32_t*>(q) + 8);
+          } else if (n == kPer) {
+            store16_shifted(out, q);
           } else {
 #pragma unroll
             for (int k = 0; k < kPer; ++k) if (k < n) out[k] = q[k];
@@ -175,25 +226,29 @@ absmax_kernel(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx, 
   if ((threadIdx.x & 31) == 0 && top != 0) atomicMax(reinterpret_cast<unsigned int*>(amax), top);
 }
 
-template <typename T, int FORMAT, int VALUES>
+template <typename T, int FORMAT, int VALUES, Mode MODE>
 int launch(const QuantParams& p, dim3 grid, cudaStream_t st) {
   // A product behind this kernel starts while this one runs and needs nearly all of an SM's shared memory:
-  // if this kernel left the SM with a small share, the product would wait until the SM is empty.  With few
-  // CTAs (VALUES = 3) the share is therefore set to the most; with many that would cost the kernel the
-  // cache its loads in flight need (8192 x 4096 bf16: 27 us instead of 16).
-  if (VALUES == 3) {
+  // if this kernel left the SM with a small share, the product would wait until the SM is empty.  Except with
+  // many CTAs, where it would cost the cache that the loads in flight need, the share is therefore set to the most.
+  if (VALUES == 0 && MODE != kMany) {
     static std::atomic<uint64_t> done{0};
-    const int rc = set_once(quantize_kernel<T, FORMAT, VALUES>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    const int rc = set_once(quantize_kernel<T, FORMAT, VALUES, MODE>, cudaFuncAttributePreferredSharedMemoryCarveout,
                             cudaSharedmemCarveoutMaxShared, done);
     if (rc != ADADIM_OK) return rc;
   }
-  quantize_kernel<T, FORMAT, VALUES><<<grid, kThreads, static_cast<size_t>(p.side) * kSfTileBytes, st>>>(p);
+  quantize_kernel<T, FORMAT, VALUES, MODE><<<grid, kThreadsOf<MODE>, static_cast<size_t>(p.side) * kSfTileBytes, st>>>(p);
   return cudaGetLastError() == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
+}
+template <typename T, int FORMAT, int VALUES>
+int launch_mode(const QuantParams& p, dim3 grid, cudaStream_t st) {
+  if (VALUES == 0 && (p.side > 1 || (grid.x > kFewCtas && (p.lt < kSfRows || grid.x <= kLowCtas)))) return launch<T, FORMAT, VALUES, VALUES == 0 ? kLow : kMany>(p, grid, st);
+  return grid.x <= kFewCtas ? launch<T, FORMAT, VALUES, kFew>(p, grid, st) : launch<T, FORMAT, VALUES, kMany>(p, grid, st);
 }
 template <typename T, int FORMAT>
 int launch_values(const QuantParams& p, int vsel, dim3 grid, cudaStream_t st) {
-  if (vsel == 0) return p.side > 1 || grid.x <= 4 * 148 ? launch<T, FORMAT, 3>(p, grid, st) : launch<T, FORMAT, 0>(p, grid, st);
-  return vsel == 1 ? launch<T, FORMAT, 1>(p, grid, st) : launch<T, FORMAT, 2>(p, grid, st);
+  if (vsel == 0) return launch_mode<T, FORMAT, 0>(p, grid, st);
+  return vsel == 1 ? launch_mode<T, FORMAT, 1>(p, grid, st) : launch_mode<T, FORMAT, 2>(p, grid, st);
 }
 template <typename T>
 int launch_format(const QuantParams& p, int format, int vsel, dim3 grid, cudaStream_t st) {
