@@ -369,7 +369,8 @@ ADADIM_API int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int6
  * Y = A B^T of two 4-bit matrices of one format: A [n_tokens][in] (activations), B [out][in] (a weight),
  * Y [n_tokens][out], ydtype any, ldy in elements, element-aligned.  Products are exact, sums binary32
  * in the tensor cores' accumulators, one rounding to ydtype at the end.
- * Any sizes with 1 <= in <= 2^20; n_tokens and out up to 2^22, n_experts * out below 2^31.
+ * Any sizes with 1 <= in <= 2^20; n_tokens and out up to 2^22, n_experts * out and the number of 128-byte pieces of
+ * either operand's scales below 2^31 - 2^20.
  */
 ADADIM_API int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,
                         int format, void* Y, int ydtype, int64_t ldy, int* status_dev, void* cuda_stream);

@@ -66,6 +66,7 @@ bool known_dtype(int dtype) { return dtype == ADADIM_F32 || dtype == ADADIM_F16 
 int64_t dtype_size(int dtype) { return dtype == ADADIM_F32 ? 4 : 2; }
 
 constexpr int64_t kFp4MaxIn = 1 << 20, kFp4MaxRows = 1 << 22;
+constexpr int64_t kFp4MaxIndex = 0x7fffffff - (1 << 20);          // 32-bit coordinates, and a tile or a stage beyond the end
 
 // A matrix of 16- or 32-bit elements: any row pitch, element-aligned.
 int check_matrix(const void* X, int dtype, int64_t cols, int64_t ld) {
@@ -101,7 +102,7 @@ int check_fp4_product(int64_t rows, int64_t out, int64_t in, int format, const i
   if (rc != ADADIM_OK) return rc;
   if (out < 0 || out > kFp4MaxRows) return ADADIM_ERR_SHAPE;
   if ((rc = check_groups(offsets, n_experts)) != ADADIM_OK) return rc;
-  if (n_experts > 0 && out * n_experts > 0x7fffffff) return ADADIM_ERR_SHAPE;
+  if (n_experts > 0 && out * n_experts > kFp4MaxIndex) return ADADIM_ERR_SHAPE;
   *empty = rows == 0 || out == 0;
   if (*empty) return ADADIM_OK;
   if (in == 0) return ADADIM_ERR_SHAPE;
@@ -110,7 +111,7 @@ int check_fp4_product(int64_t rows, int64_t out, int64_t in, int format, const i
   const int64_t weights = n_experts > 0 ? n_experts : 1;
   const int64_t sf_rows = weights * static_cast<int64_t>(fp4::scale_bytes(format, out, in, 0)) / 128;
   const int64_t a_sf_rows = fp4_most_tile_rows(rows, n_experts) * fp4::sf_tiles(format, in) * 4;
-  if (tiles > 0x7fffffff || sf_rows > 0x7fffffff || a_sf_rows > 0x7fffffff) return ADADIM_ERR_SHAPE;
+  if (tiles > kFp4MaxIndex || sf_rows > kFp4MaxIndex || a_sf_rows > kFp4MaxIndex) return ADADIM_ERR_SHAPE;
   if ((rc = check_fp4(B, in)) != ADADIM_OK) return rc;
   return check_matrix(Y, ydtype, out, ldy);
 }

@@ -116,3 +116,56 @@ def block_gptq_ada(layers, bits: int, group: int, percdamp: float = 0.01, status
             rows += W.shape[0]
         flush()
     return result
+
+
+# ---- layers in microscaled 4-bit floating point ----------------------------------------------------
+
+def fp4_weight(Ws, fmt: int) -> B.Fp4Tensor:
+    """A weight [out, in], or a list of equally shaped expert weights as one stack, in MXFP4 or NVFP4.  NVFP4's tensor
+    scale is taken from the largest magnitude of all of them."""
+    stacked = isinstance(Ws, (list, tuple))
+    weights = list(Ws) if stacked else [Ws]
+    amax = None
+    if fmt == B.NVFP4:
+        amax = torch.zeros(1, dtype=torch.float32, device=weights[0].device)
+        for W in weights:
+            B.absmax(W, amax)
+    out, inp = weights[0].shape
+    q = B.Fp4Tensor(out, inp, fmt, experts=len(weights) if stacked else 0, device=weights[0].device)
+    for e, W in enumerate(weights):
+        B.quantize_fp4(W, fmt, amax=amax, q=q.expert(e) if stacked else q)
+    return q
+
+
+def rows_by_expert(experts: torch.Tensor, n_experts: int):
+    """For expert numbers [n_tokens, top] on the device: (order, row_index, offsets).  order[r] is the position in the
+    flattened `experts` that sorted row r comes from (rows of one expert keep their order), row_index[r] its token,
+    offsets int32[n_experts + 1] where each expert's rows begin.  No host round trip."""
+    flat = experts.reshape(-1)
+    order = torch.argsort(flat, stable=True)
+    counts = torch.zeros(n_experts, dtype=torch.int64, device=flat.device).scatter_add_(0, flat.long(), torch.ones_like(flat, dtype=torch.int64))
+    offsets = torch.zeros(n_experts + 1, dtype=torch.int32, device=flat.device)
+    offsets[1:] = counts.cumsum(0)
+    return order, (order // experts.shape[1]).int(), offsets
+
+
+def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor, gate: B.Fp4Tensor, up: B.Fp4Tensor,
+                   down: B.Fp4Tensor, x_amax: Optional[torch.Tensor] = None, act_amax: Optional[torch.Tensor] = None,
+                   status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The feed-forward part of a decoder layer with experts, all three products in 4 bits: token t's output is
+    sum_k weights[t, k] * down_e(silu(gate_e(x_t)) * up_e(x_t)) with e = experts[t, k].
+    x [n_tokens, hidden], experts int [n_tokens, top], weights [n_tokens, top]; gate, up stacks [ffn, hidden], down a
+    stack [hidden, ffn].  x is gathered and quantized once for gate and up.  x_amax, act_amax: the largest magnitudes
+    that calibration found (NVFP4; None: tensor scale 1)."""
+    order, row_index, offsets = rows_by_expert(experts, gate.experts)
+    q = B.quantize_fp4(x, gate.fmt, amax=x_amax, row_index=row_index, offsets=offsets)
+    rows = row_index.numel()
+    g = torch.empty(rows, gate.rows, dtype=x.dtype, device=x.device)
+    u = torch.empty_like(g)
+    B.fp4_linear_grouped(q, offsets, gate, y=g, status=status)
+    B.fp4_linear_grouped(q, offsets, up, y=u, status=status)
+    h = torch.nn.functional.silu(g).mul_(u)
+    d = B.fp4_linear_grouped(h, offsets, down, x_amax=act_amax, status=status)
+    back = torch.empty_like(d)
+    back[order] = d                                      # rows back to (token, k): the sum below has a fixed order
+    return (back.view(x.shape[0], -1, d.shape[1]).float() * weights[..., None].float()).sum(1).to(x.dtype)

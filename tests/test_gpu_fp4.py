@@ -11,6 +11,7 @@ import torch
 
 from oracle import fp4_oracle as F
 from paper_2309_15531_b200 import binding as B
+from paper_2309_15531_b200 import flows
 
 pytestmark = pytest.mark.gpu
 
@@ -236,6 +237,62 @@ def test_linear_grouped(fmt, counts, inp, out):
     assert torch.equal(y2, y)
 
 
+# Shapes that the many-token kernel takes, with token tiles of different heights, results that can and cannot leave as
+# bulk stores (rows that are not 16-byte aligned), edges inside a tile in both directions, and short last stages.
+MANY = [(3000, 320, 2000, "bf16", 0), (600, 1344, 4104, "f16", 0), (1500, 1000, 3000, "f32", 0), (2000, 192, 2056, "bf16", 3),
+        (3001, 330, 2008, "f16", 0), (2500, 130, 5000, "bf16", 8), (1536, 4160, 2048, "bf16", 0)]
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("tokens,inp,out,dtype,gap", MANY)
+def test_linear_many_tokens(fmt, tokens, inp, out, dtype, gap):
+    x = _x(tokens, inp, dtype, 3 * tokens + inp)
+    w = _x(out, inp, "f16", out + inp, 0.02)
+    xa, wa = B.absmax(x), B.absmax(w)
+    W = B.quantize_fp4(w, FMT[fmt], amax=wa)
+    qx = F.quantize(_np(x), fmt, float(xa.item()))[2]
+    qw = F.quantize(_np(w), fmt, float(wa.item()))[2]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for a, kw in ((x, {"x_amax": xa}), (B.quantize_fp4(x, FMT[fmt], amax=xa), {})):
+        y = torch.full((tokens + 1, out + gap), -7.0, dtype=x.dtype, device="cuda")
+        B.fp4_linear(a, W, y=y[:tokens, :out], status=status, **kw)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        assert bool((y[tokens] == -7.0).all().item()) and bool((y[:, out:] == -7.0).all().item())
+        _assert_product(y[:tokens, :out], qx, qw, inp, dtype)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("counts,inp,out,dtype", [((700, 0, 901, 799), 330, 3000, "bf16"), ((1, 2047, 1252), 200, 4104, "f16"),
+                                                  ((0, 1700, 33, 1650, 17, 1600), 96, 2600, "f32")])
+def test_linear_grouped_many_tokens(fmt, counts, inp, out, dtype):
+    off = np.concatenate(([0], np.cumsum(counts))).astype(np.int32)
+    E, rows, x_rows = len(counts), int(off[-1]) + 40, 500
+    x = _x(x_rows, inp, dtype, inp)
+    idx = torch.randint(0, x_rows, (rows,), generator=torch.Generator().manual_seed(3)).int().cuda()
+    xa = B.absmax(x)
+    ws = [_x(out, inp, "f16", 200 + e, 0.02) for e in range(E)]
+    wa = torch.zeros(1, device="cuda")
+    for w in ws:
+        B.absmax(w, wa)
+    W = B.Fp4Tensor(out, inp, FMT[fmt], experts=E)
+    for e, w in enumerate(ws):
+        B.quantize_fp4(w, FMT[fmt], amax=wa, q=W.expert(e))
+    o = torch.as_tensor(off).cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    qx = F.quantize(_np(x), fmt, float(xa.item()))[2][idx.cpu().numpy()]
+    q = B.quantize_fp4(x, FMT[fmt], amax=xa, row_index=idx, offsets=o)
+    for a, kw in ((x, {"row_index": idx, "x_amax": xa}), (q, {})):
+        y = torch.full((rows, out), -7.0, dtype=x.dtype, device="cuda")
+        B.fp4_linear_grouped(a, o, W, y=y, status=status, **kw)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0 and bool((y[int(off[-1]):] == -7.0).all().item())
+        for e in range(E):
+            if counts[e]:
+                _assert_product(y[off[e]:off[e + 1]], qx[off[e]:off[e + 1]],
+                                F.quantize(_np(ws[e]), fmt, float(wa.item()))[2], inp, f"expert {e}")
+
+
 def test_bad_offsets_are_reported_and_clamped():
     W = B.Fp4Tensor(64, 128, B.MXFP4, experts=3)
     x = torch.zeros(10, 128, dtype=torch.bfloat16, device="cuda")
@@ -293,3 +350,36 @@ def test_binding_refuses_what_does_not_match():
         B.fp4_linear(torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda"), W,
                      workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 6
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("tokens", [5, 300])
+def test_expert_ffn_flow_against_each_expert_alone(fmt, tokens):
+    """The flow against the dense product of every expert on its rows.  The two may add up in another order (2^-22 of
+    the sums), which can flip a bf16 rounding of an intermediate and then a 4-bit code now and then: the results agree
+    to far better than the step between neighbouring codes, 2^-6 in the norm."""
+    E, top, hidden, ffn = 6, 2, 256, 384
+    x = _x(tokens, hidden, "bf16", 5)
+    g = torch.Generator().manual_seed(6)
+    experts = torch.stack([torch.randperm(E - 1, generator=g)[:top] for _ in range(tokens)]).cuda()     # the last gets nothing
+    weights = torch.rand(tokens, top, generator=g).cuda()
+    raw = {n: [_x(*s, "f16", 50 * k + e, 0.05) for e in range(E)] for k, (n, s) in
+           enumerate({"gate": (ffn, hidden), "up": (ffn, hidden), "down": (hidden, ffn)}.items())}
+    gate, up, down = (flows.fp4_weight(raw[n], FMT[fmt]) for n in ("gate", "up", "down"))
+    xa, ha = B.absmax(x), torch.tensor([4000.0], device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = flows.fp4_expert_ffn(x, experts, weights, gate, up, down, xa, ha, status=status)
+    want = torch.zeros(tokens, hidden, device="cuda")
+    for e in range(E):
+        t, k = (experts == e).nonzero(as_tuple=True)
+        if len(t) == 0:
+            continue
+        xe = x[t].contiguous()
+        h = torch.nn.functional.silu(B.fp4_linear(xe, gate.expert(e), x_amax=xa)) * B.fp4_linear(xe, up.expert(e), x_amax=xa)
+        want.index_add_(0, t, B.fp4_linear(h, down.expert(e), x_amax=ha).float() * weights[t, k, None])
+    assert int(status.item()) == 0
+    assert float((y.float() - want).norm() / want.norm()) < 2.0 ** -6
+    order, row_index, offsets = flows.rows_by_expert(experts, E)
+    flat = experts.reshape(-1)
+    assert bool((flat[order][1:] >= flat[order][:-1]).all().item()) and offsets.tolist()[-1] == tokens * top
+    assert row_index.tolist() == (order // top).tolist() and offsets.tolist()[E - 1] == tokens * top
