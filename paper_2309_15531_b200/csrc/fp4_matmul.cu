@@ -795,19 +795,24 @@ constexpr int kMinPairTile = 160;                      // the pair kernel's lowe
 constexpr int kFusedTokens = 8;
 
 // The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
-// kernels below (1.9 GHz, 148 SMs):
-//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256, and a CTA takes in no more than 130 bytes a
-//          nanosecond; a tile 1000 on top; start and end 5000;
-//          it streams no faster than 1 / 1.7 of the split kernel
-//   split  a CTA's stage takes no less than 300 whatever its size, an SM takes in 80 bytes a nanosecond; start and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token;
-//          and in all no less than the weights' bytes at 6000 a nanosecond
-//   and the result's bytes leave at 5000 (pair) or 2500 (split) a nanosecond, hardly beside the rest.
+// kernels (1.9 GHz, 148 SMs); over a sweep of 25 shapes its choice was within a tenth of the best plan's time.
+//   pair   a 256-column stage of a 256 x n tile takes 270 n / 256, and a CTA takes in no more than 130 bytes
+//          a nanosecond; a tile 1000 on top, 1500 where its accumulators share columns; start and end 5000;
+//          it streams a weight no faster than 1 / 1.7 of the split kernel.
+//   split  a CTA's stage takes no less than 300 whatever its size, an SM takes in 80 bytes a nanosecond; start
+//          and end 4000, an exchange between the CTAs of a cluster 1500 + 15 a token; and in all no less than
+//          the weights' bytes at 6000 a nanosecond.
+//   The result's bytes leave at 5000 (pair) or 2500 (split) a nanosecond, hardly beside the rest.
 Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format, bool quantized, bool fuse, int sms) {
   const int64_t weights = n_experts > 0 ? (n_experts < rows ? n_experts : rows) : 1;
   const int64_t typical = (rows + weights - 1) / weights;            // rows of one expert if they were equal
   const int64_t num_k = (in + kKT - 1) / kKT;
-  // tiles of an expert's rows; experts are not equal, so half a tile more than an equal share would take
-  auto token_tiles = [&](int64_t n) { return n_experts > 0 ? weights * ((typical + typical / 2 + n - 1) / n) : (rows + n - 1) / n; };
+  // tiles of an expert's rows: experts are not equal, which costs half a tile each, or with few rows takes some of
+  // them a tile further
+  auto token_tiles = [&](int64_t n) {
+    if (n_experts == 0) return (rows + n - 1) / n;
+    return typical > 2 * n ? (weights * typical + weights * n / 2) / n : weights * ((typical + typical / 2 + n - 1) / n);
+  };
   Fp4Plan best = {true, 256, 1, 1, false};
   double best_ns = 1e300;
   const double floor_ns = static_cast<double>(weights * out) * static_cast<double>(in) * (format == ADADIM_MXFP4 ? 0.53125 : 0.5625) / 6000.0;
@@ -816,7 +821,7 @@ Fp4Plan plan_of(int64_t rows, int64_t out, int64_t in, int n_experts, int format
     const int64_t tiles = (out + 255) / 256 * token_tiles(n_tile), waves = (tiles + sms / 2 - 1) / (sms / 2);
     const double n = typical < n_tile ? static_cast<double>((typical + 15) / 16 * 16) : n_tile;
     const double bytes = stage_bytes(format, true, n_tile) / 130.0, stage = 1.055 * n < bytes ? bytes : 1.055 * n;
-    double ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + 1000.0);
+    double ns = static_cast<double>(waves) * (static_cast<double>(num_k) * stage + (n_tile > 240 ? 1500.0 : 1000.0));
     if (ns < 1.7 * floor_ns) ns = 1.7 * floor_ns;
     ns += 5000.0 + y_bytes / 5000.0;
     if (ns < best_ns) { best_ns = ns; best.n_tile = n_tile; }
