@@ -341,6 +341,10 @@ def dequant_gemv(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
     return y
 
 
+def _ptr(t: Optional[torch.Tensor]):
+    return t.data_ptr() if t is not None else None
+
+
 class Fp4Tensor:
     """Device buffers of a matrix in microscaled 4-bit floating point (see include/adadim.h for the layout).
     `groups` > 0: the rows are in that many groups given by an offsets tensor (activations sorted by
@@ -356,6 +360,8 @@ class Fp4Tensor:
         self.codes = torch.zeros(n * rows, ld, dtype=torch.uint8, device=device)
         self.scales = torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device)
         self.amax: Optional[torch.Tensor] = None
+        self.amax_set = False
+        self.stack: Optional["Fp4Tensor"] = None          # of an expert's view
         self._c = None
 
     def expert(self, e: int) -> "Fp4Tensor":
@@ -366,28 +372,25 @@ class Fp4Tensor:
         one.scale_bytes = self.scale_bytes
         one.codes = self.codes[e * self.rows:(e + 1) * self.rows]
         one.scales = self.scales[e * self.scale_bytes:(e + 1) * self.scale_bytes]
-        one._parent = self
-        one.amax, one._c = self.amax, None
+        one.stack, one.amax, one.amax_set, one._c = self, self.amax, self.amax_set, None
         return one
 
     def set_amax(self, amax: Optional[torch.Tensor]) -> None:
+        """The largest magnitude that NVFP4's tensor scale is taken from.  A stack has one for all its experts: the
+        first expert that is quantized sets it, or a call on the stack itself."""
         if amax is not None:
             assert amax.is_cuda and amax.dtype == torch.float32 and amax.numel() == 1
-        self.amax, self._c = amax, None
-        parent = getattr(self, "_parent", None)          # the experts of a stack share one amax
-        if parent is not None:
-            assert parent.amax is None or amax is None or parent.amax.data_ptr() == amax.data_ptr()
-            parent.set_amax(amax)
+        if self.stack is not None:
+            if self.stack.amax_set and _ptr(self.stack.amax) != _ptr(amax):
+                raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
+            self.stack.amax, self.stack.amax_set, self.stack._c = amax, True, None
+        self.amax, self.amax_set, self._c = amax, True, None
 
     def c(self) -> Fp4TensorC:
         if self._c is None:
             self._c = Fp4TensorC(self.codes.data_ptr(), self.scales.data_ptr(),
                                  self.amax.data_ptr() if self.amax is not None else None, self.codes.stride(0))
         return self._c
-
-
-def _ptr(t: Optional[torch.Tensor]):
-    return t.data_ptr() if t is not None else None
 
 
 def _i32(t: torch.Tensor) -> torch.Tensor:

@@ -195,12 +195,12 @@ struct Source {
   int64_t ldx, x_rows;
   const int32_t* row_index;   // row r is X[row_index[r]], zeros where that is outside; NULL: X[r]
   uintptr_t begin, end;       // the bytes of X: no 16-byte block that leaves them is loaded whole
-  int wide;                   // every row starts on a 32-byte boundary
+  int wide;                   // every row (or the only one) starts on a 32-byte boundary
 };
 inline Source source_of(const void* X, int dtype, int64_t ldx, int64_t x_rows, int64_t cols, const int32_t* row_index) {
   const int64_t esz = dtype == ADADIM_F32 ? 4 : 2;
   const uintptr_t x0 = reinterpret_cast<uintptr_t>(X);
-  Source s = {X, ldx, x_rows, row_index, x0, x0, x0 % 32 == 0 && (ldx * esz) % 32 == 0};
+  Source s = {X, ldx, x_rows, row_index, x0, x0, x0 % 32 == 0 && (x_rows == 1 || (ldx * esz) % 32 == 0)};
   if (x_rows > 0) s.end = x0 + static_cast<uintptr_t>(((x_rows - 1) * ldx + cols) * esz);
   return s;
 }

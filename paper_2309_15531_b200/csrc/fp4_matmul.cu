@@ -396,10 +396,13 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     };
     const bool bulk_y = sizeof(T) == 2 && p.bulk_y;
     int out_buf = 0;
+    const int out_id = 1 + side * 2 + (q >> 1);        // named barrier of the warp pair
     TileWalk walk = {};
     for (int t = pair0; t < num_tiles; t += pairs) {
       const Tile x = walk.next(t, pairs, num_tiles, p, prefix);
-      if (!ptx::mbar_wait_warp(&acc_full[buf], acc_phase, dead, p.status_dev)) break;
+      bool ok = ptx::mbar_wait_warp(&acc_full[buf], acc_phase, dead, p.status_dev);
+      if (bulk_y) ok = ptx::named_all(out_id, 64, ok);                        // both warps of a pair go on, or neither
+      if (!ok) break;
       ptx::tc_fence_after_sync();
       const int64_t o = x.m + static_cast<int>(rank) * 128 + q * 32 + lane;
       T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
@@ -412,12 +415,10 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         // the matrix's last tile may be cut anywhere (what lies behind the matrix is not written), others at 16
         if (left > 0 && bulk_y && (left >= 32 || left == 16 || (p.n_experts == 0 && x.row + x.count == p.rows))) {
           float lo[16], hi[16];
-          ptx::tmem_ld_rows16_nowait(acc + c, lo);
-          ptx::tmem_ld_rows16_nowait(acc + c + (16u << 16), hi);
-          ptx::tmem_ld_wait();
+          ptx::tmem_ld_fragments(acc + c, lo, hi);
           if (hand_back) give_back();
           if (lane == 0 && (q & 1) == 0) ptx::bulk_wait_read_but_one();       // this buffer's last store has read it
-          ptx::named_sync(1 + side * 2 + (q >> 1), 64);
+          ptx::named_sync(out_id, 64);
           const uint32_t tile = out_at + (side * 4 + (q >> 1) * 2 + out_buf) * 4096;
           const uint32_t unit = (q & 1) * 4 + (lane >> 3);                    // 16 bytes: eight weight rows
 #pragma unroll
@@ -429,7 +430,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
                                 packed<T>(hi[4 * u + 2] * scale, hi[4 * u + 3] * scale));
           }
           ptx::fence_proxy_async();
-          ptx::named_sync(1 + side * 2 + (q >> 1), 64);
+          ptx::named_sync(out_id, 64);
           const int y_col = x.m + static_cast<int>(rank) * 128 + (q >> 1) * 64;
           if (lane == 0 && (q & 1) == 0) {
             if (y_col < p.out) {

@@ -294,19 +294,24 @@ __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, float (&v)[16])
 #pragma unroll
   for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
 }
-// 32 fp32 columns of 16 TMEM lanes (16 or 0 of this warp's 32): lane t of the warp gets, of every eight columns u,
-// columns 2 (t % 4) and + 1 of row t / 4 in r[4 u], r[4 u + 1] and of row t / 4 + 8 in r[4 u + 2], r[4 u + 3].
-// The caller waits (tmem_ld_wait).
-__device__ __forceinline__ void tmem_ld_rows16_nowait(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
+// 32 fp32 columns of this warp's 32 TMEM lanes in the order of matrix fragments: lane t of the warp gets, of every
+// eight columns u, columns 2 (t % 4) and + 1 of rows t / 4 (lo[4 u], lo[4 u + 1]), t / 4 + 8 (lo[4 u + 2], ..), and of
+// rows t / 4 + 16 and t / 4 + 24 the same in hi.
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, float (&lo)[16], float (&hi)[16]) {
+  uint32_t r[32];
   asm volatile(
       "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr) : "memory");
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]),
+        "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]),
+        "=&r"(r[16]), "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]),
+        "=&r"(r[24]), "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31])
+      : "r"(taddr), "r"(taddr + (16u << 16)) : "memory");
 #pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < 16; ++k) { lo[k] = __uint_as_float(r[k]); hi[k] = __uint_as_float(r[16 + k]); }
 }
 // Four 8 x 8 matrices of 16-bit elements to shared memory, transposed: lane t holds elements (2 (t % 4), t / 4) and
 // (2 (t % 4) + 1, t / 4) of each; lane 8 i + j gives the address of row j (16 bytes) of matrix i.
@@ -314,6 +319,13 @@ __device__ __forceinline__ void stmatrix_trans(uint32_t addr, uint32_t a, uint32
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// The same, telling all of them whether `v` held for all of them.
+__device__ __forceinline__ bool named_all(int id, int threads, bool v) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.and.pred p, %2, %3, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(r) : "r"(static_cast<uint32_t>(v)), "r"(id), "r"(threads) : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- descriptors ----------------------------------------------------------------------------

@@ -346,6 +346,12 @@ def test_binding_refuses_what_does_not_match():
                              torch.zeros(3, dtype=torch.int32, device="cuda"), W)
     with pytest.raises(ValueError):
         B.quantize_fp4(x, B.MXFP4, q=W)
+    stack, amax = B.Fp4Tensor(4, 64, B.NVFP4, experts=2), B.absmax(x)
+    B.quantize_fp4(x, B.NVFP4, amax=amax, q=stack.expert(0))
+    with pytest.raises(ValueError):
+        B.quantize_fp4(x, B.NVFP4, q=stack.expert(1))                # the experts of a stack share one amax
+    stack.set_amax(None)
+    B.quantize_fp4(x, B.NVFP4, q=stack.expert(1))
     with pytest.raises(B.AdadimError) as e:
         B.fp4_linear(torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda"), W,
                      workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
