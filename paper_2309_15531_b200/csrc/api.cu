@@ -399,8 +399,9 @@ size_t adadim_fp4_scale_bytes(int format, int64_t rows, int64_t cols, int n_grou
 
 int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, void* cuda_stream) {
   if (!known_dtype(xdtype)) return ADADIM_ERR_DTYPE;
-  if (rows < 0 || cols < 0 || rows > (int64_t{1} << 40) || cols > (int64_t{1} << 40)) return ADADIM_ERR_SHAPE;
+  if (rows < 0 || cols < 0) return ADADIM_ERR_SHAPE;
   if (rows == 0 || cols == 0) return ADADIM_OK;
+  if (cols > (int64_t{1} << 60) / rows) return ADADIM_ERR_SHAPE;
   const int rc = check_matrix(X, xdtype, cols, ldx);
   if (rc != ADADIM_OK) return rc;
   if (amax == nullptr) return ADADIM_ERR_NULL;

@@ -190,40 +190,62 @@ quantize_kernel(const QuantParams p) {
   for (int k = threadIdx.x; k < tiles * (kSfTileBytes / 16); k += kThreads) dst[k] = reinterpret_cast<const uint4*>(sf)[k];
 }
 
+// Segments of a row (of the whole matrix where its rows follow one another), four 16-byte loads of a thread in flight;
+// one atomic per CTA.
+constexpr int kMaxThreads = 256, kMaxLoads = 4;
 template <typename T>
-__global__ void __launch_bounds__(256)
+constexpr int kSegment = kMaxThreads * kMaxLoads * 16 / static_cast<int>(sizeof(T));
+template <typename T>
+__device__ __forceinline__ uint32_t magnitude(const uint4& raw) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  if constexpr (sizeof(T) == 2) {
+    typename Elem<T>::Two m = Elem<T>::abs2(w[0]);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) m = __hmax2_nan(m, Elem<T>::abs2(w[k]));
+    return __float_as_uint(Elem<T>::top_f32(m)) & 0x7fffffffu;
+  } else {
+    return max(max(w[0] & 0x7fffffffu, w[1] & 0x7fffffffu), max(w[2] & 0x7fffffffu, w[3] & 0x7fffffffu));
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t magnitude(const T* p) {
+  if constexpr (sizeof(T) == 2) return __float_as_uint(Elem<T>::to_f32(*reinterpret_cast<const uint16_t*>(p))) & 0x7fffffffu;
+  else return *reinterpret_cast<const uint32_t*>(p) & 0x7fffffffu;
+}
+template <typename T>
+__global__ void __launch_bounds__(kMaxThreads)
 absmax_kernel(const T* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx, int wide, float* amax) {
   constexpr int kVec = 16 / sizeof(T);
+  __shared__ uint32_t tops[kMaxThreads / 32];
+  const int64_t segments = (cols + kSegment<T> - 1) / kSegment<T>, total = rows * segments;
   uint32_t top = 0;
-  const int64_t per_row = (cols + kVec - 1) / kVec, total = rows * per_row;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t r = i / per_row, c = (i - r * per_row) * kVec;
-    const T* p = X + r * ldx + c;
-    if (wide && c + kVec <= cols) {
-      const uint4 raw = __ldg(reinterpret_cast<const uint4*>(p));
-      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-      if constexpr (sizeof(T) == 2) {
-        uint32_t m = 0;
+  for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
+    const int64_t r = segments == 1 ? i : i / segments, c0 = (i - r * segments) * kSegment<T>;
+    const int n = static_cast<int>(cols - c0 < kSegment<T> ? cols - c0 : kSegment<T>);
+    const T* p = X + r * ldx + c0;
+    int done = 0;
+    if (wide) {
+      uint4 raw[kMaxLoads];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) m = __vmaxu2(m, w[k] & 0x7fff7fffu);
-        top = max(top, __float_as_uint(Elem<T>::to_f32(static_cast<uint16_t>(max(m & 0xffffu, m >> 16)))) & 0x7fffffffu);
-      } else {
+      for (int k = 0; k < kMaxLoads; ++k) {
+        const int at = (k * kMaxThreads + threadIdx.x) * kVec;
+        raw[k] = at + kVec <= n ? __ldg(reinterpret_cast<const uint4*>(p + at)) : make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top = max(top, w[k] & 0x7fffffffu);
-      }
-    } else {
-      for (int k = 0; k < kVec && c + k < cols; ++k) {
-        if constexpr (sizeof(T) == 2) {
-          top = max(top, __float_as_uint(Elem<T>::to_f32(reinterpret_cast<const uint16_t*>(p)[k])) & 0x7fffffffu);
-        } else {
-          top = max(top, reinterpret_cast<const uint32_t*>(p)[k] & 0x7fffffffu);
-        }
-      }
+      for (int k = 0; k < kMaxLoads; ++k) top = max(top, magnitude<T>(raw[k]));
+      done = n / kVec * kVec;
     }
+#pragma unroll 4
+    for (int at = done + threadIdx.x; at < n; at += kMaxThreads) top = max(top, magnitude<T>(p + at));
   }
   top = __reduce_max_sync(0xffffffffu, top);
-  // patterns of non-negative floats are ordered as unsigned integers: the result has no order to depend on
-  if ((threadIdx.x & 31) == 0 && top != 0) atomicMax(reinterpret_cast<unsigned int*>(amax), top);
+  if ((threadIdx.x & 31) == 0) tops[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    top = __reduce_max_sync(0xffffffffu, threadIdx.x < kMaxThreads / 32 ? tops[threadIdx.x] : 0u);
+    // patterns of non-negative floats are ordered as unsigned integers: the result has no order to depend on
+    if (threadIdx.x == 0 && top != 0) atomicMax(reinterpret_cast<unsigned int*>(amax), top);
+  }
 }
 
 template <typename T, int FORMAT, int VALUES, Mode MODE>
@@ -259,12 +281,14 @@ int launch_format(const QuantParams& p, int format, int vsel, dim3 grid, cudaStr
 
 int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, cudaStream_t st) {
   const int64_t esz = xdtype == ADADIM_F32 ? 4 : 2;
-  const int wide = aligned16(X) && (ldx * esz) % 16 == 0;
-  const int64_t vecs = rows * ((cols * esz + 15) / 16);
-  const unsigned grid = static_cast<unsigned>(vecs / 256 + 1 < 148 * 8 ? vecs / 256 + 1 : 148 * 8);
-  if (xdtype == ADADIM_F32) absmax_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float*>(X), rows, cols, ldx, wide, amax);
-  else if (xdtype == ADADIM_F16) absmax_kernel<__half><<<grid, 256, 0, st>>>(static_cast<const __half*>(X), rows, cols, ldx, wide, amax);
-  else absmax_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(X), rows, cols, ldx, wide, amax);
+  if (ldx == cols || rows == 1) { cols *= rows; ldx = cols; rows = 1; }
+  const int wide = aligned16(X) && (rows == 1 || (ldx * esz) % 16 == 0);
+  const int64_t segment = esz == 4 ? kSegment<float> : kSegment<__half>;
+  const int64_t segments = rows * ((cols + segment - 1) / segment);
+  const unsigned grid = static_cast<unsigned>(segments < 148 * 8 ? segments : 148 * 8);
+  if (xdtype == ADADIM_F32) absmax_kernel<float><<<grid, kMaxThreads, 0, st>>>(static_cast<const float*>(X), rows, cols, ldx, wide, amax);
+  else if (xdtype == ADADIM_F16) absmax_kernel<__half><<<grid, kMaxThreads, 0, st>>>(static_cast<const __half*>(X), rows, cols, ldx, wide, amax);
+  else absmax_kernel<__nv_bfloat16><<<grid, kMaxThreads, 0, st>>>(static_cast<const __nv_bfloat16*>(X), rows, cols, ldx, wide, amax);
   return cudaGetLastError() == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
 }
 

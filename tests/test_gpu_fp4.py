@@ -141,6 +141,22 @@ def test_absmax_over_chunks_and_nan():
     assert float(B.absmax(x[:0]).item()) == 0.0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,gap", [(1, 1, 0), (1, 8191, 0), (3, 8193, 0), (5, 20000, 8), (7, 9001, 3), (300, 129, 0)])
+def test_absmax_finds_the_largest_wherever_it_is(dtype, rows, cols, gap):
+    g = torch.Generator().manual_seed(rows + cols)
+    x = torch.rand(rows, cols + gap, generator=g).to(DT[dtype]).cuda()[:, :cols]
+    if gap:
+        x.as_strided((rows, cols + gap), (cols + gap, 1))[:, cols:] = 100.0          # what lies between rows is not read
+    for at in (0, cols - 1, cols // 2, cols // 3):
+        r = at % rows
+        old = x[r, at].item()
+        x[r, at] = -9.0
+        assert float(B.absmax(x).item()) == 9.0
+        x[r, at] = old
+    assert float(B.absmax(x).item()) == float(x.abs().max().float().item())
+
+
 def _assert_product(y, xa, wb, inp, what=""):
     """xa, wb: quantized values float64 of the rows of y and of the weight."""
     ref = xa @ wb.T
