@@ -393,6 +393,20 @@ class Fp4Tensor:
         return self._c
 
 
+def _amax(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32
+    return t.data_ptr()
+
+
+def _status(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.int32
+    return t.data_ptr()
+
+
 def _i32(t: torch.Tensor) -> torch.Tensor:
     assert t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
     return t
@@ -412,8 +426,7 @@ def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor
     _rows_of(X)
     if amax is None:
         amax = torch.zeros(1, dtype=torch.float32, device=X.device)
-    assert amax.dtype == torch.float32 and amax.is_cuda
-    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), amax.data_ptr(), _raw_stream(X)),
+    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), _amax(amax), _raw_stream(X)),
            "adadim_absmax")
     return amax
 
@@ -473,7 +486,7 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
             raise ValueError("fp4_linear: X and W do not match")
         y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
         _check(lib().adadim_fp4_matmul(C.byref(X.c()), X.rows, C.byref(W.c()), W.rows, W.cols, W.fmt, y.data_ptr(),
-                                       _DT[y.dtype], _ld(y), _ptr(status), _raw_stream(X.codes)), "adadim_fp4_matmul")
+                                       _DT[y.dtype], _ld(y), _status(status), _raw_stream(X.codes)), "adadim_fp4_matmul")
         return y
     xp, xdt, rows, inp, ldx, dev = _matrix_in(X)
     if inp != W.cols:
@@ -484,9 +497,10 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
     assert y_rows == rows and y_cols == W.rows
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
-    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, x_amax.data_ptr() if x_amax is not None else None,
+    assert workspace.is_cuda and workspace.dtype == torch.uint8
+    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, _amax(x_amax),
                                  C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
-                                 status.data_ptr() if status is not None else None, workspace.data_ptr(),
+                                 _status(status), workspace.data_ptr(),
                                  workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear")
@@ -507,7 +521,7 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
             raise ValueError("fp4_linear_grouped: X and W do not match")
         y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
         _check(lib().adadim_fp4_matmul_grouped(C.byref(X.c()), X.rows, offsets.data_ptr(), n, C.byref(W.c()), W.rows,
-                                               W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _ptr(status),
+                                               W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _status(status),
                                                _raw_stream(X.codes)), "adadim_fp4_matmul_grouped")
         return y
     xp, xdt, x_rows, inp, ldx, dev = _matrix_in(X)
@@ -520,9 +534,10 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
     assert y_rows == rows and y_cols == W.rows
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, n), X.device)
-    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, x_amax.data_ptr() if x_amax is not None else None,
+    assert workspace.is_cuda and workspace.dtype == torch.uint8
+    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, _amax(x_amax),
                                          ip, offsets.data_ptr(), n, rows, C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
-                                         status.data_ptr() if status is not None else None, workspace.data_ptr(),
+                                         _status(status), workspace.data_ptr(),
                                          workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear_grouped")

@@ -742,6 +742,11 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
 constexpr size_t kSmem = 220 * 1024;                   // dynamic shared memory of one SM's split CTAs
 constexpr size_t kSmemPair = 226 * 1024 - 512;         // and of a pair CTA
+// A split CTA takes at least so much shared memory for each TMEM column: an SM's shared memory (228 KB) then runs
+// out before its 512 columns do.  A CTA that had to wait for columns could keep its cluster waiting, whose other
+// CTAs hold columns that another cluster needs, of this kernel or of one on another stream.
+constexpr size_t kSmemPerTmemColumn = 368;
+static_assert(kSmemPerTmemColumn * (512 + 128) > 228 * 1024, "one CTA more than the columns allow must not fit");
 
 template <auto KERNEL>
 int launch(const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem, bool chained,
@@ -943,7 +948,8 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, co
     if (p.n_stages > k) p.n_stages = k;
   }
   if (p.n_stages > kMaxStages) p.n_stages = kMaxStages;
-  const size_t smem = p.n_stages * per + fixed;
+  size_t smem = p.n_stages * per + fixed;
+  if (!pair && smem < kSmemPerTmemColumn * p.tmem_cols) smem = kSmemPerTmemColumn * p.tmem_cols;
   if (ydtype == ADADIM_F32) return launch_format<float>(pair, plan.fused, format, tm, p, grid, smem, chained, st);
   if (ydtype == ADADIM_F16) return launch_format<__half>(pair, plan.fused, format, tm, p, grid, smem, chained, st);
   return launch_format<__nv_bfloat16>(pair, plan.fused, format, tm, p, grid, smem, chained, st);

@@ -372,6 +372,36 @@ def test_binding_refuses_what_does_not_match():
         B.fp4_linear(torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda"), W,
                      workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 6
+    big = torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda")
+    for wrong in (dict(x_amax=torch.zeros(1)), dict(x_amax=torch.zeros(1, dtype=torch.float64, device="cuda")),
+                  dict(status=torch.zeros(1, dtype=torch.int32)), dict(status=torch.zeros(1, device="cuda")),
+                  dict(workspace=torch.empty(1 << 20, dtype=torch.uint8)), dict(y=torch.empty(4, 32, dtype=torch.bfloat16))):
+        with pytest.raises(AssertionError):
+            B.fp4_linear(big, W, **wrong)
+        with pytest.raises(AssertionError):
+            B.fp4_linear_grouped(big, torch.zeros(2, dtype=torch.int32, device="cuda"),
+                                 B.Fp4Tensor(32, 128, B.MXFP4, experts=1), **wrong)
+
+
+def test_products_of_many_streams_do_not_hold_each_other_up():
+    """Products whose clusters exchange partial sums, on eight streams at a time: each gives what it gives alone."""
+    shapes = [(12, 1024, 2048), (3, 640, 4096), (16, 512, 1920), (100, 384, 2048)] * 2
+    jobs = []
+    for i, (rows, out, inp) in enumerate(shapes):
+        g = torch.Generator().manual_seed(i)
+        x = torch.randn(rows, inp, generator=g).to(torch.bfloat16).cuda()
+        W = B.quantize_fp4(torch.randn(out, inp, generator=g).to(torch.bfloat16).cuda(), B.MXFP4 if i % 2 else B.NVFP4)
+        jobs.append((x, W, B.fp4_linear(x, W), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    ys = []
+    for _ in range(25):
+        for x, W, _, status, stream in jobs:
+            with torch.cuda.stream(stream):
+                ys.append(B.fp4_linear(x, W, status=status))
+    torch.cuda.synchronize()
+    for k, y in enumerate(ys):
+        assert torch.equal(y, jobs[k % len(jobs)][2])
+    assert all(int(status.item()) == 0 for _, _, _, status, _ in jobs)
 
 
 @pytest.mark.parametrize("fmt", ["mx", "nv"])
