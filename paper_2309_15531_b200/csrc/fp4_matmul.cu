@@ -180,9 +180,20 @@ __device__ __forceinline__ uint32_t packed(float a, float b) {       // a in the
   else if constexpr (__is_same(T, __half)) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
   else { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
 }
+// 2^(ta + tb), which lies between 2^-200 and 2^234, as two factors that binary32 holds (one could be 0 or infinite where
+// the result is neither).  Multiplied one after the other they round once at most: a sum is 0, or between 2^-20 (the
+// smallest product of two codes and their scales) and 2^43, so that v * a is exact, or infinite where v * a * b is too.
+struct ProductScale { float a, b; };
+__device__ __forceinline__ float operator*(float v, const ProductScale& s) { return v * s.a * s.b; }
+template <bool NV>
+__device__ __forceinline__ ProductScale product_scale(const MmParams& p) {
+  if (!NV) return {1.0f, 1.0f};
+  const int e = tensor_scale_log2(p.a_amax) + tensor_scale_log2(p.b_amax), half = e / 2;
+  return {exp2_int(half), exp2_int(e - half)};
+}
 // 32 tokens of one weight row: y + j * ldy receives v[j] * scale, j < n
 template <typename T>
-__device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, float scale, const float (&v)[32]) {
+__device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, const ProductScale& scale, const float (&v)[32]) {
   if (n >= 32) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) { put(y, v[j] * scale); y += ldy; }
@@ -190,12 +201,6 @@ __device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, float sca
 #pragma unroll
     for (int j = 0; j < 32; ++j) { if (j < n) put(y, v[j] * scale); y += ldy; }
   }
-}
-// 2^(ta + tb).  Each lies between 2^-100 and 2^117: the product is 0 or infinite only where |amax| of both
-// matrices are so far out that every result is.
-template <bool NV>
-__device__ __forceinline__ float product_scale(const MmParams& p) {
-  return NV ? exp2_int(tensor_scale_log2(p.a_amax)) * exp2_int(tensor_scale_log2(p.b_amax)) : 1.0f;
 }
 // After a wait that ran out: time for the copies already issued to land before shared memory goes away
 // (they take microseconds).
@@ -387,7 +392,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     const int side = (warp - 2) >> 2;                  // of each 64 columns, the 32 that this warp takes
     int buf = 0;
     uint32_t acc_phase = 0;
-    const float scale = product_scale<NV>(p);
+    const ProductScale scale = product_scale<NV>(p);
     const uint32_t part_bar = ptx::map_to_cta(ptx::smem_addr(&part_empty), 0);
     auto give_back = [&]() {
       ptx::tc_fence_before_sync();
@@ -674,7 +679,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     if (warp < 6) {
     // ------------------------------------------------------------------ epilogue (warps 2..5)
     const int q = warp & 3;                            // TMEM lane quadrant this warp may read
-    const float scale = product_scale<NV>(p);
+    const ProductScale scale = product_scale<NV>(p);
     const int row = q * 32 + lane;
     const int64_t o = x.m + row;
     T* y = static_cast<T*>(p.Y) + static_cast<int64_t>(x.row) * p.ldy + o;
