@@ -321,6 +321,8 @@ ADADIM_API int adadim_dequant_gemv(const adadim_qtensor* q, int dim, int64_t out
  *           the largest E2M1 times the largest E4M3).  NULL, zero, infinite or NaN: t = 1.
  *           A power of two costs no precision (E4M3 carries its own exponent) and keeps every
  *           decision below exact.  MXFP4: not used.
+ *           Every call that uses the tensor reads the value: between the quantizer and the last product it
+ *           must not change (adadim_quantize_fp4_amax keeps a copy of an amax that goes on changing).
  * Rows in groups (experts): rows offsets[e] .. offsets[e+1]-1 of the matrix belong to group e, and
  * every group starts a scale tile of its own, so that a group's scales can be loaded as whole
  * tiles wherever it begins: the scale tiles of group e start at tile row offsets[e] / 128 + e.
@@ -364,6 +366,15 @@ ADADIM_API int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t co
 ADADIM_API int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows,
                         int format, const int32_t* row_index, const int32_t* offsets, int n_groups,
                         const adadim_fp4tensor* q, void* values, int vdtype, int64_t ldv, void* cuda_stream);
+
+/*
+ * The same with an amax that q does not depend on afterwards: NVFP4's tensor scale is taken from *amax and the
+ * value is written to *q->amax as well (which the call may write, unlike every other).  NULL: as adadim_quantize_fp4.
+ */
+ADADIM_API int adadim_quantize_fp4_amax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows,
+                        int format, const int32_t* row_index, const int32_t* offsets, int n_groups,
+                        const adadim_fp4tensor* q, void* values, int vdtype, int64_t ldv, const float* amax,
+                        void* cuda_stream);
 
 /*
  * Y = A B^T of two 4-bit matrices of one format: A [n_tokens][in] (activations), B [out][in] (a weight),

@@ -89,6 +89,8 @@ def lib():
         L.adadim_absmax.argtypes = [vp, ci, i64, i64, i64, vp, vp]
         L.adadim_quantize_fp4.restype = ci
         L.adadim_quantize_fp4.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, ci, fp, vp, ci, i64, vp]
+        L.adadim_quantize_fp4_amax.restype = ci
+        L.adadim_quantize_fp4_amax.argtypes = L.adadim_quantize_fp4.argtypes[:-1] + [vp, vp]
         L.adadim_fp4_matmul.restype = ci
         L.adadim_fp4_matmul.argtypes = [fp, i64, fp, i64, i64, ci, vp, ci, i64, vp, vp]
         L.adadim_fp4_matmul_grouped.restype = ci
@@ -345,6 +347,54 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr() if t is not None else None
 
 
+class _TensorScale:
+    """The amax that NVFP4's tensor scale is taken from, of a matrix or of a stack of experts: a copy of its value on the
+    device, so that what the caller does with an amax later changes no product, and which of the matrices were quantized
+    with it."""
+
+    def __init__(self, device, shared: bool):
+        self.shared = shared                              # by the experts of a stack
+        self.value = torch.empty(1, dtype=torch.float32, device=device)
+        self.present = False                              # False: no amax, tensor scale 1
+        self.fixed = False                                # a stack has one; its first expert or set_amax fixes it
+        self.given: Optional[torch.Tensor] = None         # the tensor that a stack's was copied from, and its version
+        self.version = 0
+        self.done: set = set()                            # matrices that were quantized with it
+        self.stale: set = set()                           # .. and with an earlier one, not again since
+        self.state = object()                             # another one whenever `present` or `stale` changes
+
+    @staticmethod
+    def _version(t: torch.Tensor) -> int:
+        return 0 if t.is_inference() else t._version
+
+    def same(self, amax: Optional[torch.Tensor]) -> bool:
+        """Whether it is known that amax holds the value kept here."""
+        if amax is None or not self.present:
+            return amax is None and not self.present
+        p = amax.data_ptr()
+        return p == self.value.data_ptr() or (self.given is not None and p == self.given.data_ptr()
+                                              and self._version(amax) == self.version)
+
+    def _fix(self, amax: Optional[torch.Tensor]) -> None:
+        self.present, self.fixed, self.state = amax is not None, True, object()
+        if self.shared and amax is not None and amax.data_ptr() != self.value.data_ptr():
+            self.given, self.version = amax, self._version(amax)
+
+    def change(self, amax: Optional[torch.Tensor]) -> None:
+        if not self.same(amax):
+            self.stale |= self.done
+            self.done.clear()
+        if amax is not None and amax.data_ptr() != self.value.data_ptr():
+            self.value.copy_(amax.reshape(1))
+        self._fix(amax)
+
+    def quantized(self, k: int, amax: Optional[torch.Tensor]) -> None:
+        """Matrix k was quantized with amax, and a call that had to fix the amax has copied it."""
+        self.done.add(k)
+        self.stale.discard(k)
+        self._fix(amax)
+
+
 class Fp4Tensor:
     """Device buffers of a matrix in microscaled 4-bit floating point (see include/adadim.h for the layout).
     `groups` > 0: the rows are in that many groups given by an offsets tensor (activations sorted by
@@ -359,10 +409,10 @@ class Fp4Tensor:
         ld = ((cols + 1) // 2 + 15) // 16 * 16
         self.codes = torch.zeros(n * rows, ld, dtype=torch.uint8, device=device)
         self.scales = torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device)
-        self.amax: Optional[torch.Tensor] = None
-        self.amax_set = False
         self.stack: Optional["Fp4Tensor"] = None          # of an expert's view
-        self._c = None
+        self._index = 0                                   # of this matrix in the stack
+        self._scale = _TensorScale(device, experts > 0)
+        self._c = self._product = self._state = None
 
     def expert(self, e: int) -> "Fp4Tensor":
         if not 0 <= e < self.experts:
@@ -372,25 +422,42 @@ class Fp4Tensor:
         one.scale_bytes = self.scale_bytes
         one.codes = self.codes[e * self.rows:(e + 1) * self.rows]
         one.scales = self.scales[e * self.scale_bytes:(e + 1) * self.scale_bytes]
-        one.stack, one.amax, one.amax_set, one._c = self, self.amax, self.amax_set, None
+        one.stack, one._index, one._scale = self, e, self._scale
+        one._c = one._product = one._state = None
         return one
 
+    @property
+    def amax(self) -> Optional[torch.Tensor]:
+        """float32[1], the largest magnitude that NVFP4's tensor scale is taken from; None: tensor scale 1 (or MXFP4)."""
+        return self._scale.value if self._scale.present else None
+
     def set_amax(self, amax: Optional[torch.Tensor]) -> None:
-        """The largest magnitude that NVFP4's tensor scale is taken from.  A stack has one for all its experts: the
+        """Sets the amax (its value is copied).  Matrices that were quantized with another have to be quantized again:
+        a product that needs one of them raises ValueError until then.  A stack has one amax for all its experts: the
         first expert that is quantized sets it, or a call on the stack itself."""
         if amax is not None:
             assert amax.is_cuda and amax.dtype == torch.float32 and amax.numel() == 1
-        if self.stack is not None:
-            if self.stack.amax_set and _ptr(self.stack.amax) != _ptr(amax):
-                raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
-            self.stack.amax, self.stack.amax_set, self.stack._c = amax, True, None
-        self.amax, self.amax_set, self._c = amax, True, None
+        if self.fmt != NVFP4:
+            return                                        # MXFP4 has no tensor scale
+        if self.stack is not None and self._scale.fixed and not self._scale.same(amax):
+            raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
+        self._scale.change(amax)
+
+    def _structs(self):
+        """Without an amax and with the one that is kept."""
+        if self._c is None:
+            p, s, ld = self.codes.data_ptr(), self.scales.data_ptr(), self.codes.stride(0)
+            self._c = (Fp4TensorC(p, s, None, ld), Fp4TensorC(p, s, self._scale.value.data_ptr(), ld))
+        return self._c
 
     def c(self) -> Fp4TensorC:
-        if self._c is None:
-            self._c = Fp4TensorC(self.codes.data_ptr(), self.scales.data_ptr(),
-                                 self.amax.data_ptr() if self.amax is not None else None, self.codes.stride(0))
-        return self._c
+        """What a product takes."""
+        scale = self._scale
+        if self._state is not scale.state:
+            if scale.stale and (self.experts or self._index in scale.stale):
+                raise ValueError("the amax was changed after this was quantized: quantize it again")
+            self._product, self._state = self._structs()[scale.present], scale.state
+        return self._product
 
 
 def _amax(t: Optional[torch.Tensor]):
@@ -428,6 +495,7 @@ def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor
         amax = torch.zeros(1, dtype=torch.float32, device=X.device)
     _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), _amax(amax), _raw_stream(X)),
            "adadim_absmax")
+    torch.autograd.graph.increment_version(amax)         # as any operation in place does
     return amax
 
 
@@ -435,25 +503,35 @@ def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None,
                  values: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
                  offsets: Optional[torch.Tensor] = None) -> Fp4Tensor:
     """Quantize X[rows, cols] (fp32, fp16 or bf16) to MXFP4 or NVFP4.  amax: float32[1], NVFP4's tensor scale is
-    taken from it (None: 1) and it is remembered in the result.  values (bf16 or fp32 [rows, cols]): receives the
+    taken from it (None: 1) and the result keeps a copy of it.  values (bf16 or fp32 [rows, cols]): receives the
     quantized values.  row_index int32[rows]: take row r from X[row_index[r]].  offsets int32[n + 1]: the rows are in
     n groups (see Fp4Tensor)."""
-    _rows_of(X)
-    cols = X.shape[1]
-    rows = X.shape[0] if row_index is None else _i32(row_index).numel()
+    xp, xdt, x_rows, cols, ldx, dev = _matrix_in(X)
+    rows = x_rows if row_index is None else _i32(row_index).numel()
     groups = _i32(offsets).numel() - 1 if offsets is not None else 0
     if q is None:
         q = Fp4Tensor(rows, cols, fmt, groups=groups, device=X.device)
-    if (q.rows, q.cols, q.fmt, q.groups, q.experts) != (rows, cols, fmt, groups, 0):
+    if q.rows != rows or q.cols != cols or q.fmt != fmt or q.groups != groups or q.experts:
         raise ValueError("quantize_fp4: q was made for another shape or format")
-    q.set_amax(amax)
+    vp, vdt, ldv = None, BF16, 0
     if values is not None:
-        _rows_of(values)
-        assert values.shape == (rows, cols)
-    _check(lib().adadim_quantize_fp4(X.data_ptr(), _DT[X.dtype], rows, cols, _ld(X), X.shape[0], fmt, _ptr(row_index),
-                                     _ptr(offsets), groups, C.byref(q.c()), _ptr(values),
-                                     _DT[values.dtype] if values is not None else BF16,
-                                     _ld(values) if values is not None else 0, _raw_stream(X)), "adadim_quantize_fp4")
+        vp, vdt, v_rows, v_cols, ldv, _ = _matrix_in(values)
+        assert v_rows == rows and v_cols == cols
+    scale, nv, alone = q._scale, fmt == NVFP4, q.stack is None
+    given = _amax(amax) if nv else None
+    if alone or not scale.fixed:
+        source = given                                    # the call copies its value to where q keeps it
+    elif not nv or scale.same(amax):
+        source = None
+    else:
+        raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
+    rc = lib().adadim_quantize_fp4_amax(xp, xdt, rows, cols, ldx, x_rows, fmt, _ptr(row_index), _ptr(offsets), groups,
+                                        C.byref((q._c or q._structs())[given is not None]), vp, vdt, ldv, source,
+                                        torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check(rc, "adadim_quantize_fp4")
+    if nv and not (alone and scale.done and scale.present == (given is not None)):
+        scale.quantized(q._index, amax)
     return q
 
 

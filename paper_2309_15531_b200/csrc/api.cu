@@ -146,7 +146,7 @@ int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ld
   const fp4::Source x = fp4::source_of(X, xdtype, ldx, x_rows, in, row_index);
   const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, false, xdtype == ydtype && x.wide != 0 && in % fp4::kPer == 0);
   if (!plan.fused) {
-    rc = quantize_fp4_launch(x, xdtype, rows, in, format, offsets, n_experts, A, plan.n_tile, nullptr, ADADIM_BF16, 0, st);
+    rc = quantize_fp4_launch(x, xdtype, rows, in, format, offsets, n_experts, A, nullptr, plan.n_tile, nullptr, ADADIM_BF16, 0, st);
     if (rc != ADADIM_OK) return rc;
   }
   return fp4_matmul_launch(plan, A, plan.n_tile, x, rows, offsets, n_experts, *B, out, in, format, Y, ydtype, ldy, status_dev,
@@ -412,6 +412,13 @@ int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t
 int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
                         const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor* q,
                         void* values, int vdtype, int64_t ldv, void* cuda_stream) {
+  return adadim_quantize_fp4_amax(X, xdtype, rows, cols, ldx, x_rows, format, row_index, offsets, n_groups, q, values, vdtype,
+                                  ldv, nullptr, cuda_stream);
+}
+
+int adadim_quantize_fp4_amax(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, int64_t x_rows, int format,
+                             const int32_t* row_index, const int32_t* offsets, int n_groups, const adadim_fp4tensor* q,
+                             void* values, int vdtype, int64_t ldv, const float* amax, void* cuda_stream) {
   int rc = check_fp4_shape(format, rows, cols);
   if (rc != ADADIM_OK) return rc;
   if (!known_dtype(xdtype) || (values != nullptr && vdtype != ADADIM_BF16 && vdtype != ADADIM_F32)) return ADADIM_ERR_DTYPE;
@@ -421,9 +428,11 @@ int adadim_quantize_fp4(const void* X, int xdtype, int64_t rows, int64_t cols, i
   if (x_rows > 0 && (rc = check_matrix(X, xdtype, cols, ldx)) != ADADIM_OK) return rc;
   if ((reinterpret_cast<uintptr_t>(row_index) & 3u) != 0) return ADADIM_ERR_ALIGN;
   if ((rc = check_fp4(q, cols)) != ADADIM_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(amax) & 3u) != 0) return ADADIM_ERR_ALIGN;
+  if (format == ADADIM_NVFP4 && amax != nullptr && q->amax == nullptr) return ADADIM_ERR_NULL;
   if (values != nullptr && (rc = check_matrix(values, vdtype, cols, ldv)) != ADADIM_OK) return rc;
   return quantize_fp4_launch(fp4::source_of(X, xdtype, ldx, x_rows, cols, row_index), xdtype, rows, cols, format, offsets,
-                             n_groups, *q, fp4::kSfRows, values, vdtype, ldv, static_cast<cudaStream_t>(cuda_stream));
+                             n_groups, *q, amax, fp4::kSfRows, values, vdtype, ldv, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_fp4_matmul(const adadim_fp4tensor* A, int64_t n_tokens, const adadim_fp4tensor* B, int64_t out, int64_t in,

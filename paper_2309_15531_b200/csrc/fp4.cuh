@@ -348,8 +348,9 @@ int set_once(K kernel, cudaFuncAttribute attr, int value, std::atomic<uint64_t>&
 
 // implemented in fp4_quant.cu and fp4_matmul.cu
 int absmax_launch(const void* X, int xdtype, int64_t rows, int64_t cols, int64_t ldx, float* amax, cudaStream_t st);
+// amax: where the tensor scale comes from and what q.amax is set to; NULL: it comes from q.amax
 int quantize_fp4_launch(const fp4::Source& x, int xdtype, int64_t rows, int64_t cols, int format, const int32_t* offsets,
-                        int n_groups, const adadim_fp4tensor& q, int lt, void* values, int vdtype, int64_t ldv,
+                        int n_groups, const adadim_fp4tensor& q, const float* amax, int lt, void* values, int vdtype, int64_t ldv,
                         cudaStream_t st);
 // How a product is laid out on the SMs.
 struct Fp4Plan {
