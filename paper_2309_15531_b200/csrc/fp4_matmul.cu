@@ -191,6 +191,12 @@ __device__ __forceinline__ ProductScale product_scale(const MmParams& p) {
   const int e = tensor_scale_log2(p.a_amax) + tensor_scale_log2(p.b_amax), half = e / 2;
   return {exp2_int(half), exp2_int(e - half)};
 }
+// The same for two sums at once, rounded to a pair of 16-bit results.
+template <typename T>
+__device__ __forceinline__ uint32_t packed(float x, float y, const ProductScale& s) {
+  unpack2(mul2(mul2(pack2(x, y), pack2(s.a, s.a)), pack2(s.b, s.b)), x, y);
+  return packed<T>(x, y);
+}
 // 32 tokens of one weight row: y + j * ldy receives v[j] * scale, j < n
 template <typename T>
 __device__ __forceinline__ void store_tokens(T* y, int64_t ldy, int n, const ProductScale& scale, const float (&v)[32]) {
@@ -429,10 +435,10 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int token = u * 8 + (lane & 7);
-            ptx::stmatrix_trans(tile + token * 128 + ((unit ^ (token & 7)) << 4), packed<T>(lo[4 * u] * scale, lo[4 * u + 1] * scale),
-                                packed<T>(lo[4 * u + 2] * scale, lo[4 * u + 3] * scale),
-                                packed<T>(hi[4 * u] * scale, hi[4 * u + 1] * scale),
-                                packed<T>(hi[4 * u + 2] * scale, hi[4 * u + 3] * scale));
+            ptx::stmatrix_trans(tile + token * 128 + ((unit ^ (token & 7)) << 4), packed<T>(lo[4 * u], lo[4 * u + 1], scale),
+                                packed<T>(lo[4 * u + 2], lo[4 * u + 3], scale),
+                                packed<T>(hi[4 * u], hi[4 * u + 1], scale),
+                                packed<T>(hi[4 * u + 2], hi[4 * u + 3], scale));
           }
           ptx::fence_proxy_async();
           ptx::named_sync(out_id, 64);
