@@ -125,9 +125,8 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
-def _raw_stream(t: torch.Tensor) -> int:
-    """The same handle for t's device without building a Stream object (3.5 us on the measured host)."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+# The current device, and the handle of a device's current stream without a Stream object (3.5 us on the measured host).
+_device, _raw_stream = (getattr(torch._C, name, None) for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def _check(rc: int, where: str):
@@ -343,10 +342,6 @@ def dequant_gemv(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
     return y
 
 
-def _ptr(t: Optional[torch.Tensor]):
-    return t.data_ptr() if t is not None else None
-
-
 class _TensorScale:
     """The amax that NVFP4's tensor scale is taken from, of a matrix or of a stack of experts: a copy of its value on the
     device, so that what the caller does with an amax later changes no product, and which of the matrices were quantized
@@ -409,6 +404,7 @@ class Fp4Tensor:
         ld = ((cols + 1) // 2 + 15) // 16 * 16
         self.codes = torch.zeros(n * rows, ld, dtype=torch.uint8, device=device)
         self.scales = torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device)
+        self.dev = self.codes.get_device()
         self.stack: Optional["Fp4Tensor"] = None          # of an expert's view
         self._index = 0                                   # of this matrix in the stack
         self._scale = _TensorScale(device, experts > 0)
@@ -419,7 +415,7 @@ class Fp4Tensor:
             raise IndexError(e)
         one = object.__new__(Fp4Tensor)
         one.rows, one.cols, one.fmt, one.groups, one.experts = self.rows, self.cols, self.fmt, 0, 0
-        one.scale_bytes = self.scale_bytes
+        one.scale_bytes, one.dev = self.scale_bytes, self.dev
         one.codes = self.codes[e * self.rows:(e + 1) * self.rows]
         one.scales = self.scales[e * self.scale_bytes:(e + 1) * self.scale_bytes]
         one.stack, one._index, one._scale = self, e, self._scale
@@ -436,111 +432,51 @@ class Fp4Tensor:
         a product that needs one of them raises ValueError until then.  A stack has one amax for all its experts: the
         first expert that is quantized sets it, or a call on the stack itself."""
         if amax is not None:
-            assert amax.is_cuda and amax.dtype == torch.float32 and amax.numel() == 1
+            _amax(amax, self.dev)
+            assert amax.numel() == 1
         if self.fmt != NVFP4:
             return                                        # MXFP4 has no tensor scale
         if self.stack is not None and self._scale.fixed and not self._scale.same(amax):
             raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
         self._scale.change(amax)
 
-    def _structs(self):
-        """Without an amax and with the one that is kept."""
+    def _both(self):
+        """What the quantizer takes: without an amax, and with the one that is kept."""
         if self._c is None:
             p, s, ld = self.codes.data_ptr(), self.scales.data_ptr(), self.codes.stride(0)
             self._c = (Fp4TensorC(p, s, None, ld), Fp4TensorC(p, s, self._scale.value.data_ptr(), ld))
         return self._c
 
     def c(self) -> Fp4TensorC:
-        """What a product takes."""
+        return self._both()[self._scale.present]
+
+    def _operand(self):
+        """What a product takes, by reference."""
         scale = self._scale
         if self._state is not scale.state:
             if scale.stale and (self.experts or self._index in scale.stale):
                 raise ValueError("the amax was changed after this was quantized: quantize it again")
-            self._product, self._state = self._structs()[scale.present], scale.state
+            self._product, self._state = C.byref(self.c()), scale.state
         return self._product
 
 
-def _amax(t: Optional[torch.Tensor]):
+def _amax(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.float32
+    assert t.get_device() == dev >= 0 and t.dtype == torch.float32
     return t.data_ptr()
 
 
-def _status(t: Optional[torch.Tensor]):
+def _status(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.int32
+    assert t.get_device() == dev and t.dtype == torch.int32
     return t.data_ptr()
 
 
-def _i32(t: torch.Tensor) -> torch.Tensor:
-    assert t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+def _i32(t: torch.Tensor, dev: int) -> torch.Tensor:
+    assert t.get_device() == dev and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
     return t
-
-
-def _rows_of(X: torch.Tensor) -> torch.Tensor:
-    assert X.is_cuda and X.dim() == 2 and (X.shape[1] <= 1 or X.stride(1) == 1)
-    return X
-
-
-def _ld(X: torch.Tensor) -> int:
-    return X.stride(0) if X.shape[0] > 1 else max(X.stride(0), X.shape[1])
-
-
-def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """float32[1] = max(amax, max |X|); pass the same tensor for several chunks."""
-    _rows_of(X)
-    if amax is None:
-        amax = torch.zeros(1, dtype=torch.float32, device=X.device)
-    _check(lib().adadim_absmax(X.data_ptr(), _DT[X.dtype], X.shape[0], X.shape[1], _ld(X), _amax(amax), _raw_stream(X)),
-           "adadim_absmax")
-    torch.autograd.graph.increment_version(amax)         # as any operation in place does
-    return amax
-
-
-def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None, q: Optional[Fp4Tensor] = None,
-                 values: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
-                 offsets: Optional[torch.Tensor] = None) -> Fp4Tensor:
-    """Quantize X[rows, cols] (fp32, fp16 or bf16) to MXFP4 or NVFP4.  amax: float32[1], NVFP4's tensor scale is
-    taken from it (None: 1) and the result keeps a copy of it.  values (bf16 or fp32 [rows, cols]): receives the
-    quantized values.  row_index int32[rows]: take row r from X[row_index[r]].  offsets int32[n + 1]: the rows are in
-    n groups (see Fp4Tensor)."""
-    xp, xdt, x_rows, cols, ldx, dev = _matrix_in(X)
-    rows = x_rows if row_index is None else _i32(row_index).numel()
-    groups = _i32(offsets).numel() - 1 if offsets is not None else 0
-    if q is None:
-        q = Fp4Tensor(rows, cols, fmt, groups=groups, device=X.device)
-    if q.rows != rows or q.cols != cols or q.fmt != fmt or q.groups != groups or q.experts:
-        raise ValueError("quantize_fp4: q was made for another shape or format")
-    vp, vdt, ldv = None, BF16, 0
-    if values is not None:
-        vp, vdt, v_rows, v_cols, ldv, _ = _matrix_in(values)
-        assert v_rows == rows and v_cols == cols
-    scale, nv, alone = q._scale, fmt == NVFP4, q.stack is None
-    given = _amax(amax) if nv else None
-    if alone or not scale.fixed:
-        source = given                                    # the call copies its value to where q keeps it
-    elif not nv or scale.same(amax):
-        source = None
-    else:
-        raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
-    rc = lib().adadim_quantize_fp4_amax(xp, xdt, rows, cols, ldx, x_rows, fmt, _ptr(row_index), _ptr(offsets), groups,
-                                        C.byref((q._c or q._structs())[given is not None]), vp, vdt, ldv, source,
-                                        torch._C._cuda_getCurrentRawStream(dev))
-    if rc:
-        _check(rc, "adadim_quantize_fp4")
-    if nv and not (alone and scale.done and scale.present == (given is not None)):
-        scale.quantized(q._index, amax)
-    return q
-
-
-def _product_out(y, rows, out, dtype, device):
-    if y is None:
-        return torch.empty(rows, out, dtype=dtype, device=device)
-    _rows_of(y)
-    assert y.shape == (rows, out)
-    return y
 
 
 def _matrix_in(X: torch.Tensor):
@@ -553,6 +489,69 @@ def _matrix_in(X: torch.Tensor):
     return X.data_ptr(), _DT[X.dtype], rows, cols, (ld if rows > 1 or ld > cols else cols), dev
 
 
+def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """float32[1] = max(amax, max |X|); pass the same tensor for several chunks."""
+    xp, xdt, rows, cols, ldx, dev = _matrix_in(X)
+    if amax is None:
+        amax = torch.zeros(1, dtype=torch.float32, device=X.device)
+    with torch.cuda.device(dev):
+        _check(lib().adadim_absmax(xp, xdt, rows, cols, ldx, _amax(amax, dev), _raw_stream(dev)), "adadim_absmax")
+    torch.autograd.graph.increment_version(amax)         # as any operation in place does
+    return amax
+
+
+def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None, q: Optional[Fp4Tensor] = None,
+                 values: Optional[torch.Tensor] = None, row_index: Optional[torch.Tensor] = None,
+                 offsets: Optional[torch.Tensor] = None) -> Fp4Tensor:
+    """Quantize X[rows, cols] (fp32, fp16 or bf16) to MXFP4 or NVFP4.  amax: float32[1], NVFP4's tensor scale is
+    taken from it (None: 1) and the result keeps a copy of it.  values (bf16 or fp32 [rows, cols]): receives the
+    quantized values.  row_index int32[rows]: take row r from X[row_index[r]].  offsets int32[n + 1]: the rows are in
+    n groups (see Fp4Tensor)."""
+    xp, xdt, x_rows, cols, ldx, dev = _matrix_in(X)
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return quantize_fp4(X, fmt, amax, q, values, row_index, offsets)
+    rows, ip = (x_rows, None) if row_index is None else (_i32(row_index, dev).numel(), row_index.data_ptr())
+    groups, op = (0, None) if offsets is None else (_i32(offsets, dev).numel() - 1, offsets.data_ptr())
+    if q is None:
+        q = Fp4Tensor(rows, cols, fmt, groups=groups, device=X.device)
+    if q.rows != rows or q.cols != cols or q.fmt != fmt or q.groups != groups or q.experts or q.dev != dev:
+        raise ValueError("quantize_fp4: q was made for another shape, format or device")
+    vp, vdt, ldv = None, BF16, 0
+    if values is not None:
+        vp, vdt, v_rows, v_cols, ldv, v_dev = _matrix_in(values)
+        assert v_rows == rows and v_cols == cols and v_dev == dev
+    scale, nv, alone = q._scale, fmt == NVFP4, q.stack is None
+    given = _amax(amax, dev)
+    if not nv:
+        given = None
+    if alone or not scale.fixed:
+        source = given                                    # the call copies its value to where q keeps it
+    elif not nv or scale.same(amax):
+        source = None
+    else:
+        raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
+    rc = lib().adadim_quantize_fp4_amax(xp, xdt, rows, cols, ldx, x_rows, fmt, ip, op, groups,
+                                        C.byref((q._c or q._both())[given is not None]), vp, vdt, ldv, source,
+                                        _raw_stream(dev))
+    if rc:
+        _check(rc, "adadim_quantize_fp4")
+    if nv and not (alone and scale.done and scale.present == (given is not None)):
+        scale.quantized(q._index, amax)
+    return q
+
+
+def _fp4_operands(X: Fp4Tensor, W: Fp4Tensor, y: Optional[torch.Tensor]):
+    """The result of a product of two 4-bit matrices, with its pointer, dtype code and pitch."""
+    if W.dev != X.dev:
+        raise ValueError("X and W are on different devices")
+    if y is None:
+        y = torch.empty(X.rows, W.rows, dtype=torch.bfloat16, device=X.codes.device)
+    yp, ydt, rows, cols, ldy, dev = _matrix_in(y)
+    assert rows == X.rows and cols == W.rows and dev == X.dev
+    return y, yp, ydt, ldy
+
+
 def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y = Q(X) W^T for activations X[n_tokens, in] (fp32, fp16, bf16; quantized in the call with x_amax) or for an
@@ -562,24 +561,26 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
     if isinstance(X, Fp4Tensor):
         if X.fmt != W.fmt or X.cols != W.cols or X.groups or X.experts:
             raise ValueError("fp4_linear: X and W do not match")
-        y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
-        _check(lib().adadim_fp4_matmul(C.byref(X.c()), X.rows, C.byref(W.c()), W.rows, W.cols, W.fmt, y.data_ptr(),
-                                       _DT[y.dtype], _ld(y), _status(status), _raw_stream(X.codes)), "adadim_fp4_matmul")
+        y, yp, ydt, ldy = _fp4_operands(X, W, y)
+        with torch.cuda.device(X.dev):
+            _check(lib().adadim_fp4_matmul(X._operand(), X.rows, W._operand(), W.rows, W.cols, W.fmt, yp, ydt, ldy,
+                                           _status(status, X.dev), _raw_stream(X.dev)), "adadim_fp4_matmul")
         return y
     xp, xdt, rows, inp, ldx, dev = _matrix_in(X)
-    if inp != W.cols:
+    if inp != W.cols or dev != W.dev:
         raise ValueError("fp4_linear: X and W do not match")
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return fp4_linear(X, W, x_amax, y, workspace, status)
     if y is None:
         y = torch.empty(rows, W.rows, dtype=X.dtype, device=X.device)
-    yp, ydt, y_rows, y_cols, ldy, _ = _matrix_in(y)
-    assert y_rows == rows and y_cols == W.rows
+    yp, ydt, y_rows, out, ldy, y_dev = _matrix_in(y)
+    assert y_rows == rows and out == W.rows and y_dev == dev
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
-    assert workspace.is_cuda and workspace.dtype == torch.uint8
-    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, _amax(x_amax),
-                                 C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
-                                 _status(status), workspace.data_ptr(),
-                                 workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    assert workspace.get_device() == dev and workspace.dtype == torch.uint8
+    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, _amax(x_amax, dev), W._operand(), out, W.fmt, yp, ydt, ldy,
+                                 _status(status, dev), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear")
     return y
@@ -591,32 +592,35 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
     """The product for rows sorted by expert: rows offsets[e] .. offsets[e+1]-1 (int32 on the device) are
     multiplied by expert e of the stack W.  Row r is X[row_index[r]] (None: X[r]); X may be an Fp4Tensor with
     groups.  Rows of no expert are not written."""
-    n = _i32(offsets).numel() - 1
+    n = _i32(offsets, W.dev).numel() - 1
     if W.experts != n or n < 1:
         raise ValueError("fp4_linear_grouped: offsets do not match the stack of experts")
     if isinstance(X, Fp4Tensor):
         if X.fmt != W.fmt or X.cols != W.cols or X.groups != n or row_index is not None:
             raise ValueError("fp4_linear_grouped: X and W do not match")
-        y = _product_out(y, X.rows, W.rows, torch.bfloat16, X.codes.device)
-        _check(lib().adadim_fp4_matmul_grouped(C.byref(X.c()), X.rows, offsets.data_ptr(), n, C.byref(W.c()), W.rows,
-                                               W.cols, W.fmt, y.data_ptr(), _DT[y.dtype], _ld(y), _status(status),
-                                               _raw_stream(X.codes)), "adadim_fp4_matmul_grouped")
+        y, yp, ydt, ldy = _fp4_operands(X, W, y)
+        with torch.cuda.device(X.dev):
+            _check(lib().adadim_fp4_matmul_grouped(X._operand(), X.rows, offsets.data_ptr(), n, W._operand(), W.rows, W.cols,
+                                                   W.fmt, yp, ydt, ldy, _status(status, X.dev), _raw_stream(X.dev)),
+                   "adadim_fp4_matmul_grouped")
         return y
     xp, xdt, x_rows, inp, ldx, dev = _matrix_in(X)
-    if inp != W.cols:
+    if inp != W.cols or dev != W.dev:
         raise ValueError("fp4_linear_grouped: X and W do not match")
-    rows, ip = (x_rows, None) if row_index is None else (_i32(row_index).numel(), row_index.data_ptr())
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return fp4_linear_grouped(X, offsets, W, row_index, x_amax, y, workspace, status)
+    rows, ip = (x_rows, None) if row_index is None else (_i32(row_index, dev).numel(), row_index.data_ptr())
     if y is None:
         y = torch.empty(rows, W.rows, dtype=X.dtype, device=X.device)
-    yp, ydt, y_rows, y_cols, ldy, _ = _matrix_in(y)
-    assert y_rows == rows and y_cols == W.rows
+    yp, ydt, y_rows, out, ldy, y_dev = _matrix_in(y)
+    assert y_rows == rows and out == W.rows and y_dev == dev
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, n), X.device)
-    assert workspace.is_cuda and workspace.dtype == torch.uint8
-    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, _amax(x_amax),
-                                         ip, offsets.data_ptr(), n, rows, C.byref(W.c()), y_cols, W.fmt, yp, ydt, ldy,
-                                         _status(status), workspace.data_ptr(),
-                                         workspace.numel(), torch._C._cuda_getCurrentRawStream(dev))
+    assert workspace.get_device() == dev and workspace.dtype == torch.uint8
+    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, _amax(x_amax, dev), ip, offsets.data_ptr(), n, rows,
+                                         W._operand(), out, W.fmt, yp, ydt, ldy, _status(status, dev),
+                                         workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear_grouped")
     return y
