@@ -168,4 +168,4 @@ def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor
     d = B.fp4_linear_grouped(h, offsets, down, x_amax=act_amax, status=status)
     back = torch.empty_like(d)
     back[order] = d                                      # rows back to (token, k): the sum below has a fixed order
-    return (back.view(x.shape[0], -1, d.shape[1]).float() * weights[..., None].float()).sum(1).to(x.dtype)
+    return (back.view(x.shape[0], experts.shape[1], d.shape[1]).float() * weights[..., None].float()).sum(1).to(x.dtype)
