@@ -140,12 +140,15 @@ def fp4_weight(Ws, fmt: int) -> B.Fp4Tensor:
 def rows_by_expert(experts: torch.Tensor, n_experts: int):
     """For expert numbers [n_tokens, top] on the device: (order, row_index, offsets).  order[r] is the position in the
     flattened `experts` that sorted row r comes from (rows of one expert keep their order), row_index[r] its token,
-    offsets int32[n_experts + 1] where each expert's rows begin.  No host round trip."""
-    flat = experts.reshape(-1)
-    order = torch.argsort(flat, stable=True)
-    counts = torch.zeros(n_experts, dtype=torch.int64, device=flat.device).scatter_add_(0, flat.long(), torch.ones_like(flat, dtype=torch.int64))
+    offsets int32[n_experts + 1] where each expert's rows begin.  Numbers outside 0 .. n_experts - 1 (a place that a router
+    dropped, an expert of another rank) belong to no expert: their rows come last, behind offsets[-1].  No host round
+    trip."""
+    flat = experts.reshape(-1).long()
+    key = torch.where((flat >= 0) & (flat < n_experts), flat, n_experts)
+    order = torch.argsort(key, stable=True)
+    counts = torch.zeros(n_experts + 1, dtype=torch.int64, device=flat.device).scatter_add_(0, key, torch.ones_like(key))
     offsets = torch.zeros(n_experts + 1, dtype=torch.int32, device=flat.device)
-    offsets[1:] = counts.cumsum(0)
+    offsets[1:] = counts[:n_experts].cumsum(0)
     return order, (order // experts.shape[1]).int(), offsets
 
 
@@ -153,7 +156,8 @@ def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor
                    down: B.Fp4Tensor, x_amax: Optional[torch.Tensor] = None, act_amax: Optional[torch.Tensor] = None,
                    status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The feed-forward part of a decoder layer with experts, all three products in 4 bits: token t's output is
-    sum_k weights[t, k] * down_e(silu(gate_e(x_t)) * up_e(x_t)) with e = experts[t, k].
+    sum_k weights[t, k] * down_e(silu(gate_e(x_t)) * up_e(x_t)) with e = experts[t, k], over the k whose e is an expert of the
+    stacks.
     x [n_tokens, hidden], experts int [n_tokens, top], weights [n_tokens, top]; gate, up stacks [ffn, hidden], down a
     stack [hidden, ffn].  x is gathered and quantized once for gate and up.  x_amax, act_amax: the largest magnitudes
     that calibration found (NVFP4; None: tensor scale 1)."""
@@ -165,7 +169,9 @@ def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor
     B.fp4_linear_grouped(q, offsets, gate, y=g, status=status)
     B.fp4_linear_grouped(q, offsets, up, y=u, status=status)
     h = torch.nn.functional.silu(g).mul_(u)
-    d = B.fp4_linear_grouped(h, offsets, down, x_amax=act_amax, status=status)
+    d = torch.zeros(rows, down.rows, dtype=x.dtype, device=x.device)     # rows of no expert stay zero
+    B.fp4_linear_grouped(h, offsets, down, x_amax=act_amax, y=d, status=status)
     back = torch.empty_like(d)
     back[order] = d                                      # rows back to (token, k): the sum below has a fixed order
-    return (back.view(x.shape[0], experts.shape[1], d.shape[1]).float() * weights[..., None].float()).sum(1).to(x.dtype)
+    share = torch.where((experts >= 0) & (experts < gate.experts), weights.float(), 0.0)
+    return (back.view(x.shape[0], experts.shape[1], d.shape[1]) * share[..., None]).sum(1).to(x.dtype)

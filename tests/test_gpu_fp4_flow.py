@@ -26,3 +26,28 @@ def test_a_batch_without_tokens(fmt, dtype):
     assert y.shape == (0, 64) and y.dtype == dtype
     order, row_index, offsets = flows.rows_by_expert(experts, 3)
     assert order.numel() == row_index.numel() == 0 and offsets.tolist() == [0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("fmt", [B.MXFP4, B.NVFP4])
+def test_places_of_no_expert_add_nothing(fmt):
+    """Against the same places given to expert 0 with weight 0: a row's sums do not depend on the rows beside it, so the
+    bits are the same."""
+    E, tokens, top = 3, 40, 2
+    _, stacks = _stacks(E, 128, 96, fmt)
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(tokens, 128, generator=g).bfloat16().cuda()
+    experts = torch.randint(-1, E + 2, (tokens, top), generator=g).cuda()
+    weights = torch.rand(tokens, top, generator=g).cuda()
+    inside = (experts >= 0) & (experts < E)
+    assert bool(inside.any().item()) and not bool(inside.all().item())
+    weights[~inside] = float("nan")                       # nobody says what a router writes there
+    amax = torch.tensor([8.0], device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    trash = torch.full((1 << 22,), float("nan"), device="cuda")           # what freed memory may hold
+    del trash
+    y = flows.fp4_expert_ffn(x, experts, weights, *stacks, amax, amax, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and bool(torch.isfinite(y).all().item())
+    assert not bool(y[~inside.any(1)].any().item()) and bool(y[inside.any(1)].any().item())
+    want = flows.fp4_expert_ffn(x, torch.where(inside, experts, 0), torch.where(inside, weights, 0.0), *stacks, amax, amax)
+    assert torch.equal(y, want)
