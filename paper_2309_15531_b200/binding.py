@@ -433,7 +433,6 @@ class Fp4Tensor:
         first expert that is quantized sets it, or a call on the stack itself."""
         if amax is not None:
             _amax(amax, self.dev)
-            assert amax.numel() == 1
         if self.fmt != NVFP4:
             return                                        # MXFP4 has no tensor scale
         if self.stack is not None and self._scale.fixed and not self._scale.same(amax):
@@ -463,14 +462,14 @@ class Fp4Tensor:
 def _amax(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.get_device() == dev >= 0 and t.dtype == torch.float32
+    assert t.get_device() == dev >= 0 and t.dtype == torch.float32 and t.numel() == 1
     return t.data_ptr()
 
 
 def _status(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.get_device() == dev and t.dtype == torch.int32
+    assert t.get_device() == dev and t.dtype == torch.int32 and t.numel() >= 1
     return t.data_ptr()
 
 

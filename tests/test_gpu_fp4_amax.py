@@ -157,3 +157,21 @@ def test_graph_replays_take_the_amax_of_their_time():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(y, B.fp4_linear(x, W, x_amax=xa))
+
+
+def test_an_amax_or_a_status_of_another_size_is_refused():
+    x, (w, w2) = _data()
+    W = B.quantize_fp4(w, B.NVFP4, amax=B.absmax(w))
+    S = flows.fp4_weight([w, w2], B.NVFP4)
+    none, two = torch.empty(0, device="cuda"), torch.ones(2, device="cuda")
+    no_status = torch.empty(0, dtype=torch.int32, device="cuda")
+    for wrong in (none, two):
+        for call in (lambda: B.fp4_linear(x, W, x_amax=wrong), lambda: B.quantize_fp4(w, B.NVFP4, amax=wrong),
+                     lambda: B.fp4_linear_grouped(x, _offsets(0, 4, 6), S, x_amax=wrong), lambda: B.absmax(x, wrong),
+                     lambda: W.set_amax(wrong)):
+            with pytest.raises(AssertionError):
+                call()
+    for call in (lambda: B.fp4_linear(x, W, status=no_status), lambda: B.fp4_linear(B.quantize_fp4(x, B.NVFP4), W, status=no_status),
+                 lambda: B.fp4_linear_grouped(x, _offsets(0, 4, 6), S, status=no_status)):
+        with pytest.raises(AssertionError):
+            call()
