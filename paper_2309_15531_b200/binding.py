@@ -402,25 +402,62 @@ class Fp4Tensor:
         n = max(experts, 1)
         self.scale_bytes = int(lib().adadim_fp4_scale_bytes(fmt, rows, cols, groups))
         ld = ((cols + 1) // 2 + 15) // 16 * 16
-        self.codes = torch.zeros(n * rows, ld, dtype=torch.uint8, device=device)
-        self.scales = torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device)
-        self.dev = self.codes.get_device()
+        self._buffers = (torch.zeros(n * rows, ld, dtype=torch.uint8, device=device),
+                         torch.zeros(n * self.scale_bytes, dtype=torch.uint8, device=device))
+        self.dev = self._buffers[0].get_device()
         self.stack: Optional["Fp4Tensor"] = None          # of an expert's view
         self._index = 0                                   # of this matrix in the stack
         self._scale = _TensorScale(device, experts > 0)
-        self._c = self._product = self._state = None
+        self._c = self._c_of = self._product = self._state = None
 
     def expert(self, e: int) -> "Fp4Tensor":
         if not 0 <= e < self.experts:
             raise IndexError(e)
         one = object.__new__(Fp4Tensor)
         one.rows, one.cols, one.fmt, one.groups, one.experts = self.rows, self.cols, self.fmt, 0, 0
-        one.scale_bytes, one.dev = self.scale_bytes, self.dev
-        one.codes = self.codes[e * self.rows:(e + 1) * self.rows]
-        one.scales = self.scales[e * self.scale_bytes:(e + 1) * self.scale_bytes]
-        one.stack, one._index, one._scale = self, e, self._scale
-        one._c = one._product = one._state = None
+        one.scale_bytes, one.dev, one.stack, one._index, one._scale = self.scale_bytes, self.dev, self, e, self._scale
+        one._c = one._c_of = one._product = one._state = None
         return one
+
+    # Buffers may be replaced (by ones that were loaded, say), in a stack those of all experts together; views follow.
+    @property
+    def codes(self) -> torch.Tensor:
+        if self.stack is not None:
+            return self.stack.codes[self._index * self.rows:(self._index + 1) * self.rows]
+        return self._buffers[0]
+
+    @codes.setter
+    def codes(self, t: torch.Tensor) -> None:
+        old = self._replaceable(t)[0]
+        if t.shape != old.shape or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError("Fp4Tensor: codes of another shape or order")
+        self._replace(t, self._buffers[1])
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self.stack is not None:
+            return self.stack.scales[self._index * self.scale_bytes:(self._index + 1) * self.scale_bytes]
+        return self._buffers[1]
+
+    @scales.setter
+    def scales(self, t: torch.Tensor) -> None:
+        old = self._replaceable(t)[1]
+        if t.shape != old.shape or not t.is_contiguous():
+            raise ValueError("Fp4Tensor: scales of another shape or order")
+        self._replace(self._buffers[0], t)
+
+    def _replaceable(self, t: torch.Tensor):
+        if self.stack is not None:
+            raise ValueError("Fp4Tensor: replace the buffers of the stack")
+        if t.dtype != torch.uint8 or t.get_device() != self.dev:
+            raise ValueError("Fp4Tensor: a buffer of another type or device")
+        return self._buffers
+
+    def _replace(self, codes: torch.Tensor, scales: torch.Tensor) -> None:
+        self._buffers = (codes, scales)
+        self._scale.state = object()
+        self._scale.done.clear()                          # the caller answers for what comes from elsewhere
+        self._scale.stale.clear()
 
     @property
     def amax(self) -> Optional[torch.Tensor]:
@@ -432,6 +469,7 @@ class Fp4Tensor:
         a product that needs one of them raises ValueError until then.  A stack has one amax for all its experts: the
         first expert that is quantized sets it, or a call on the stack itself."""
         if amax is not None:
+            assert amax.is_cuda
             _amax(amax, self.dev)
         if self.fmt != NVFP4:
             return                                        # MXFP4 has no tensor scale
@@ -441,9 +479,11 @@ class Fp4Tensor:
 
     def _both(self):
         """What the quantizer takes: without an amax, and with the one that is kept."""
-        if self._c is None:
-            p, s, ld = self.codes.data_ptr(), self.scales.data_ptr(), self.codes.stride(0)
-            self._c = (Fp4TensorC(p, s, None, ld), Fp4TensorC(p, s, self._scale.value.data_ptr(), ld))
+        buffers = (self.stack or self)._buffers
+        if self._c_of is not buffers:
+            codes, scales = self.codes, self.scales
+            p, s, ld = codes.data_ptr(), scales.data_ptr(), codes.stride(0)
+            self._c, self._c_of = (Fp4TensorC(p, s, None, ld), Fp4TensorC(p, s, self._scale.value.data_ptr(), ld)), buffers
         return self._c
 
     def c(self) -> Fp4TensorC:
@@ -462,15 +502,16 @@ class Fp4Tensor:
 def _amax(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.get_device() == dev >= 0 and t.dtype == torch.float32 and t.numel() == 1
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.numel() == 1
     return t.data_ptr()
 
 
 def _status(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
-    assert t.get_device() == dev and t.dtype == torch.int32 and t.numel() >= 1
-    return t.data_ptr()
+    p = t.data_ptr()                                      # 0 if it is empty
+    assert p and t.get_device() == dev and t.dtype == torch.int32
+    return p
 
 
 def _i32(t: torch.Tensor, dev: int) -> torch.Tensor:
@@ -493,8 +534,10 @@ def absmax(X: torch.Tensor, amax: Optional[torch.Tensor] = None) -> torch.Tensor
     xp, xdt, rows, cols, ldx, dev = _matrix_in(X)
     if amax is None:
         amax = torch.zeros(1, dtype=torch.float32, device=X.device)
-    with torch.cuda.device(dev):
-        _check(lib().adadim_absmax(xp, xdt, rows, cols, ldx, _amax(amax, dev), _raw_stream(dev)), "adadim_absmax")
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return absmax(X, amax)
+    _check(lib().adadim_absmax(xp, xdt, rows, cols, ldx, _amax(amax, dev), _raw_stream(dev)), "adadim_absmax")
     torch.autograd.graph.increment_version(amax)         # as any operation in place does
     return amax
 
@@ -530,9 +573,9 @@ def quantize_fp4(X: torch.Tensor, fmt: int, amax: Optional[torch.Tensor] = None,
         source = None
     else:
         raise ValueError("the experts of a stack share one amax: set_amax on the stack first")
-    rc = lib().adadim_quantize_fp4_amax(xp, xdt, rows, cols, ldx, x_rows, fmt, ip, op, groups,
-                                        C.byref((q._c or q._both())[given is not None]), vp, vdt, ldv, source,
-                                        _raw_stream(dev))
+    rc = (_lib or lib()).adadim_quantize_fp4_amax(xp, xdt, rows, cols, ldx, x_rows, fmt, ip, op, groups,
+                                                  C.byref(q._both()[given is not None]), vp, vdt, ldv, source,
+                                                  _raw_stream(dev))
     if rc:
         _check(rc, "adadim_quantize_fp4")
     if nv and not (alone and scale.done and scale.present == (given is not None)):
@@ -578,8 +621,9 @@ def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Option
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, 0), X.device)
     assert workspace.get_device() == dev and workspace.dtype == torch.uint8
-    rc = lib().adadim_fp4_linear(xp, xdt, rows, inp, ldx, _amax(x_amax, dev), W._operand(), out, W.fmt, yp, ydt, ldy,
-                                 _status(status, dev), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+    rc = (_lib or lib()).adadim_fp4_linear(xp, xdt, rows, inp, ldx, _amax(x_amax, dev), W._operand(), out, W.fmt, yp, ydt,
+                                           ldy, _status(status, dev), workspace.data_ptr(), workspace.numel(),
+                                           _raw_stream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear")
     return y
@@ -617,9 +661,9 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
     if workspace is None:
         workspace = _ws(workspace_bytes(WS_FP4, rows, inp, 4, n), X.device)
     assert workspace.get_device() == dev and workspace.dtype == torch.uint8
-    rc = lib().adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, _amax(x_amax, dev), ip, offsets.data_ptr(), n, rows,
-                                         W._operand(), out, W.fmt, yp, ydt, ldy, _status(status, dev),
-                                         workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+    rc = (_lib or lib()).adadim_fp4_linear_grouped(xp, xdt, x_rows, inp, ldx, _amax(x_amax, dev), ip, offsets.data_ptr(), n,
+                                                   rows, W._operand(), out, W.fmt, yp, ydt, ldy, _status(status, dev),
+                                                   workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if rc:
         _check(rc, "adadim_fp4_linear_grouped")
     return y
