@@ -18,7 +18,7 @@
 //          quantizer it starts streaming the weight at once and waits only before it reads the
 //          activations.
 #include "fp4.cuh"
-#include "umma.cuh"
+#include "umma_fp4.cuh"
 
 namespace adadim {
 namespace {
@@ -718,7 +718,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
           }
         }
       }
-      ok = ptx::mbar_wait_warp<true>(&red_full, 0, dead, p.status_dev) && ok;
+      ok = ptx::mbar_wait_warp_cluster(&red_full, 0, dead, p.status_dev) && ok;
       y += rank * mine * p.ldy;
       for (int f = 0; f * 4 < tokens && ok; ++f) {
         float4 s = red[f * 128 + row];
@@ -758,6 +758,35 @@ constexpr size_t kSmemPair = 226 * 1024 - 512;         // and of a pair CTA
 // CTAs hold columns that another cluster needs, of this kernel or of one on another stream.
 constexpr size_t kSmemPerTmemColumn = 368;
 static_assert(kSmemPerTmemColumn * (512 + 128) > 228 * 1024, "one CTA more than the columns allow must not fit");
+
+// ---- host: tensor maps ----------------------------------------------------------------------------
+// A 2-D tensor of `inner` elements per row with boxes of {box_inner, box_rows}, outside of which 0 is read.
+int encode(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
+           uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion) {
+  typedef decltype(&cuTensorMapEncodeTiled) Fn;
+  static const Fn fn = []() -> Fn {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess) return nullptr;
+    return q == cudaDriverEntryPointSuccess ? reinterpret_cast<Fn>(p) : nullptr;
+  }();
+  if (fn == nullptr) return ADADIM_ERR_CUDA;
+  const cuuint64_t dims[2] = {inner, rows}, strides[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {box_inner, box_rows}, step[2] = {1, 1};
+  return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? ADADIM_OK : ADADIM_ERR_CUDA;
+}
+// 16-bit elements with 128-byte swizzle, for stores.
+int make_tmap_u16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes, uint32_t box_rows) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, base, inner, rows, pitch_bytes, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_NONE);
+}
+// Bytes with 128-byte swizzle (packed codes) or without (scale tiles as 128-byte rows).
+int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint64_t pitch_bytes, uint32_t box_rows,
+                 bool swizzle) {
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, inner, rows, pitch_bytes, 128, box_rows,
+                swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
 
 template <auto KERNEL>
 int launch(const CUtensorMap (&tm)[5], const MmParams& p, dim3 grid, int threads, int cluster, size_t smem, bool chained,

@@ -8,7 +8,7 @@
 // it moves (24 instructions an element were the limit at 39 us for W[11008,4096] with its values): packed
 // magnitude maximum, packed binary32 for the quotients, hardware conversions to and from E2M1.
 #include "fp4.cuh"
-#include "umma.cuh"
+#include "umma_fp4.cuh"
 
 namespace adadim {
 namespace {
