@@ -33,7 +33,8 @@ constexpr uint32_t kWBytes = 128 * 128;
 constexpr uint32_t kOutBytes = 8 * 4096;               // pair kernel: tiles of Y on their way out
 constexpr int kFusedThreads = 320;                     // split kernel that quantizes: four warps more,
 constexpr int kFusedPerSm = 3;                         // CTAs of an SM (by its registers)
-constexpr int kFusedTile = 16;                         // and tokens of a tile
+constexpr int kFusedTile = 16;                         // the tokens of a tile, of which it has
+constexpr int kFusedTokens = 8;                        // up to so many: see plan_of
 constexpr int kBand = 8;                               // weight tiles that share a sweep over the tokens
 
 struct MmParams {
@@ -503,7 +504,7 @@ __host__ __device__ __forceinline__ int exchange_floats(int n_tile, int splits) 
 }
 
 // FUSED: the activations are p.x, of type T, and eight warps (the epilogue's four among them) quantize
-// them into the ring; a tile has up to 16 tokens, a warp takes two of them.
+// them into the ring; there is one tile of up to kFusedTokens tokens, dense, and a warp takes two of them.
 template <int FORMAT, typename T, bool FUSED>
 __global__ void __launch_bounds__(FUSED ? kFusedThreads : kThreads, FUSED ? kFusedPerSm : 4)
 fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmA,
@@ -532,7 +533,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
   Tile x = {};
   bool work = true;
-  if (p.n_experts > 0) {
+  if (!FUSED && p.n_experts > 0) {
     if (warp == 2) tile_prefix(p, lane, prefix);
     __syncthreads();
     work = t < prefix[p.n_experts];       // the grid is an upper bound
@@ -566,7 +567,7 @@ fp4_split_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   const int ahead = work ? min(k1 - k0, p.n_stages) : 0;
   // FUSED: warps that share a stage (two tokens each), and stages under way at once.  Not more than the ring
   // has: a warp's wait for its next place would otherwise be two phases of that barrier ahead.
-  const int sharing = x.count > 8 ? 8 : x.count > 4 ? 4 : x.count > 2 ? 2 : 1;
+  const int sharing = x.count > 4 ? 4 : x.count > 2 ? 2 : 1;
   const int in_turn = min(8 / sharing, p.n_stages);
   if (warp == 0) {
     // the ring's first fill starts before anything else: the weight does not depend on the launch ahead
@@ -834,11 +835,11 @@ int launch_format(bool pair, bool fused, int format, const CUtensorMap (&tm)[5],
 // expert), which bounds the scale tiles of the activations.
 constexpr int kMinCut = 32, kMaxCutRows = 512;
 constexpr int kMinPairTile = 160;                      // the pair kernel's lowest token tile, two scale tile rows
-// Rows up to which a dense product quantizes them itself: every weight tile's CTA repeats the work, which at
+// kFusedTokens, the rows up to which a dense product quantizes them itself: every weight tile's CTA repeats the work, which at
 // 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us fused, 24.5 us behind
 // the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).  Not with experts, some of which have more rows than the
 // typical one (128 rows over 32: 27.4 us fused, 25.0 us behind the quantizer).
-constexpr int kFusedTokens = 8;
+static_assert(kFusedTokens <= 8, "the quantizing warps take two tokens each, up to four warps to a stage");
 
 // The plan of least estimated time, in nanoseconds.  What the estimate is made of was measured on the
 // kernels (1.9 GHz, 148 SMs); over a sweep of 25 shapes its choice was within a tenth of the best plan's time.
