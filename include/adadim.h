@@ -416,6 +416,16 @@ ADADIM_API int adadim_fp4_linear_grouped(const void* X, int xdtype, int64_t x_ro
                         const adadim_fp4tensor* B, int64_t out, int format, void* Y, int ydtype, int64_t ldy,
                         int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * How a product is laid out (host only, nothing is launched): for tests and for choosing sizes.
+ *   quantized    the activations come quantized (adadim_fp4_matmul, .._grouped; otherwise adadim_fp4_linear, .._grouped)
+ *   aligned      X and Y are of one type, rows of X start on 32-byte boundaries
+ *   plan         host int[5]: 1 for the kernel for many tokens, 0 for the one for few; tokens of a tile; CTAs that share
+ *                a tile's columns; CTAs of an SM; 1 where the product's kernel quantizes the activations itself
+ */
+ADADIM_API int adadim_fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, int quantized, int aligned,
+                        int* plan);
+
 /* Helpers. */
 ADADIM_API size_t adadim_workspace_bytes(int kind, int64_t out, int64_t in, int bits, int group);
 /* Unpack the bitstream format above: dst [out][in] uint8 (device). */

@@ -9,6 +9,7 @@ every call fails with an ImportError naming the missing file.
 from __future__ import annotations
 
 import ctypes as C
+from collections import namedtuple
 import os
 from typing import Optional
 
@@ -100,6 +101,8 @@ def lib():
         L.adadim_fp4_linear_grouped.restype = ci
         L.adadim_fp4_linear_grouped.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, ci, i64, fp, i64, ci, vp, ci, i64,
                                                 vp, vp, sz, vp]
+        L.adadim_fp4_plan.restype = ci
+        L.adadim_fp4_plan.argtypes = [i64, i64, i64, ci, ci, ci, ci, C.POINTER(C.c_int)]
         L.adadim_unpack_codes.restype = C.c_int
         L.adadim_unpack_codes.argtypes = [vp, i64, i64, C.c_int, vp, vp]
         _lib = L
@@ -667,6 +670,16 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
     if rc:
         _check(rc, "adadim_fp4_linear_grouped")
     return y
+
+
+Fp4Plan = namedtuple("Fp4Plan", "many token_tile splits ctas_per_sm fused")
+
+
+def fp4_plan(rows: int, out: int, inp: int, fmt: int, experts: int = 0, quantized: bool = False, aligned: bool = True) -> Fp4Plan:
+    """How fp4_linear lays out a product (fp4_linear_grouped with `experts`): see include/adadim.h.  Host only."""
+    plan = (C.c_int * 5)()
+    _check(lib().adadim_fp4_plan(rows, out, inp, experts, fmt, quantized, aligned, plan), "adadim_fp4_plan")
+    return Fp4Plan(bool(plan[0]), plan[1], plan[2], plan[3], bool(plan[4]))
 
 
 def static_scratch_bytes() -> int:

@@ -123,6 +123,7 @@ size_t fp4_workspace_bytes(int64_t rows, int64_t in, int n_groups) {
   return fp4_code_bytes(rows, in) +
          round_up(static_cast<size_t>(fp4_most_tile_rows(rows, n_groups)) * fp4::sf_tiles(ADADIM_NVFP4, in) * fp4::kSfTileBytes, 256);
 }
+bool fp4_fusable(bool aligned, int64_t in) { return aligned && in % fp4::kPer == 0; }
 int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ldx, const float* x_amax,
                const int32_t* row_index, const int32_t* offsets, int n_experts, int64_t rows, const adadim_fp4tensor* B,
                int64_t out, int format, void* Y, int ydtype, int64_t ldy, int* status_dev, void* workspace,
@@ -144,7 +145,7 @@ int fp4_linear(const void* X, int xdtype, int64_t x_rows, int64_t in, int64_t ld
   A.amax = x_amax;
   A.ld = fp4::code_pitch(in);
   const fp4::Source x = fp4::source_of(X, xdtype, ldx, x_rows, in, row_index);
-  const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, false, xdtype == ydtype && x.wide != 0 && in % fp4::kPer == 0);
+  const Fp4Plan plan = fp4_plan(rows, out, in, n_experts, format, false, fp4_fusable(xdtype == ydtype && x.wide != 0, in));
   if (!plan.fused) {
     rc = quantize_fp4_launch(x, xdtype, rows, in, format, offsets, n_experts, A, nullptr, plan.n_tile, nullptr, ADADIM_BF16, 0, st);
     if (rc != ADADIM_OK) return rc;
@@ -471,6 +472,18 @@ int adadim_fp4_linear_grouped(const void* X, int xdtype, int64_t x_rows, int64_t
   if (n_experts == 0) return ADADIM_ERR_PARAM;
   return fp4_linear(X, xdtype, x_rows, in, ldx, x_amax, row_index, offsets, n_experts, n_rows, B, out, format, Y, ydtype,
                     ldy, status_dev, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, int quantized, int aligned, int* plan) {
+  const int rc = check_fp4_shape(format, rows, in);
+  if (rc != ADADIM_OK) return rc;
+  if (rows == 0 || out <= 0 || out > kFp4MaxRows || in == 0) return ADADIM_ERR_SHAPE;
+  if (n_experts < 0 || n_experts > fp4::kMaxGroups) return ADADIM_ERR_PARAM;
+  if (plan == nullptr) return ADADIM_ERR_NULL;
+  const Fp4Plan p = fp4_plan(rows, out, in, n_experts, format, quantized != 0, fp4_fusable(quantized == 0 && aligned != 0, in));
+  const int v[5] = {p.pair, p.n_tile, p.splits, p.per_sm, p.fused};
+  for (int k = 0; k < 5; ++k) plan[k] = v[k];
+  return ADADIM_OK;
 }
 
 int adadim_unpack_codes(const uint32_t* codes, int64_t out, int64_t in, int bits, uint8_t* dst, void* cuda_stream) {
