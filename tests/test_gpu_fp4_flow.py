@@ -1,7 +1,9 @@
-"""The expert feed-forward flow at the ends of its range."""
+"""The expert feed-forward flow: against the oracle, and at the ends of its range."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import fp4_oracle as F
 from paper_2309_15531_b200 import binding as B
 from paper_2309_15531_b200 import flows
 
@@ -51,3 +53,38 @@ def test_places_of_no_expert_add_nothing(fmt):
     assert not bool(y[~inside.any(1)].any().item()) and bool(y[inside.any(1)].any().item())
     want = flows.fp4_expert_ffn(x, torch.where(inside, experts, 0), torch.where(inside, weights, 0.0), *stacks, amax, amax)
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens", [5, 260])
+def test_the_flow_against_the_oracle(fmt, dtype, tokens):
+    """Routing, gather, quantization, products and the weighted sum in binary64, rounded to x's type where the flow keeps a
+    matrix (gate, up, silu, their product, down).  Sums in another order can flip such a rounding and, one step further, a
+    4-bit code: with bf16 a flip moves an element of the intermediate by 2^-8, a code by up to a fourth of itself, for a
+    small part of the elements only.  2^-5 in the norm allows for one element in sixty-four to be a whole code off
+    ((1/4) / sqrt(64)); a wrong row, scale or expert is off by about 1."""
+    E, top, hidden, ffn = 4, 2, 160, 224
+    raw, stacks = _stacks(E, hidden, ffn, B.MXFP4 if fmt == "mx" else B.NVFP4, seed=9)
+    g = torch.Generator().manual_seed(tokens)
+    x = torch.randn(tokens, hidden, generator=g).to(dtype).cuda()
+    experts = torch.stack([torch.randperm(E, generator=g)[:top] for _ in range(tokens)]).cuda()
+    weights = torch.rand(tokens, top, generator=g).cuda()
+    xa, ha = B.absmax(x), torch.tensor([16.0], device="cuda")
+    y = flows.fp4_expert_ffn(x, experts, weights, *stacks, xa, ha)
+
+    def rounded(m):
+        return torch.as_tensor(m).to(dtype).double().numpy()
+
+    def quantized(m, amax):
+        return F.quantize(m, fmt, float(amax))[2]
+
+    wa = [max(float(w.abs().max().item()) for w in ws) for ws in raw]
+    gate, up, down = ([quantized(w.double().cpu().numpy(), wa[k]) for w in ws] for k, ws in enumerate(raw))
+    xq, want = quantized(x.double().cpu().numpy(), xa.item()), np.zeros((tokens, hidden))
+    for t in range(tokens):
+        for k, e in enumerate(experts[t].tolist()):
+            a, b = rounded(xq[t] @ gate[e].T), rounded(xq[t] @ up[e].T)
+            h = rounded(rounded(a / (1.0 + np.exp(-a))) * b)
+            want[t] += float(weights[t, k]) * rounded(quantized(h[None], ha.item())[0] @ down[e].T)
+    assert np.linalg.norm(y.double().cpu().numpy() - want) < 2.0 ** -5 * np.linalg.norm(want)
