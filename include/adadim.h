@@ -319,8 +319,10 @@ ADADIM_API int adadim_dequant_gemv(const adadim_qtensor* q, int dim, int64_t out
  *   amax    NVFP4: device float with the largest magnitude the matrix is expected to hold (see
  *           adadim_absmax), or NULL; it fixes t = 2^max(ceil(log2(amax / 2688)), -100) (2688 = 6 * 448,
  *           the largest E2M1 times the largest E4M3).  NULL, zero, infinite or NaN: t = 1.
- *           A power of two costs no precision (E4M3 carries its own exponent) and keeps every
- *           decision below exact.  MXFP4: not used.
+ *           A power of two keeps every decision below exact and costs no precision as long as the block scales are
+ *           normal E4M3 numbers (up to a bit where they are not: blocks below 0.094 t).  A tensor scale that is not a
+ *           power of two, as a checkpoint may have, cannot be expressed.  With t = 1 blocks above 2688 saturate and
+ *           blocks below 0.0058 become zero.  MXFP4: not used.
  *           Every call that uses the tensor reads the value: between the quantizer and the last product it
  *           must not change (adadim_quantize_fp4_amax keeps a copy of an amax that goes on changing).
  * Rows in groups (experts): rows offsets[e] .. offsets[e+1]-1 of the matrix belong to group e, and
@@ -353,8 +355,8 @@ ADADIM_API int adadim_absmax(const void* X, int xdtype, int64_t rows, int64_t co
  *          most 6; zero where s is 0.  (The sign bit of a zero code is not specified.)
  *   A block that holds an infinity or a NaN gets a NaN scale (0xFF / 0x7F) and codes 0: its
  *   values, and every product with it, are NaN.
- *   X          [x_rows][cols], xdtype any, ldx in elements.  16-byte aligned rows take the wide
- *              loads; any element-aligned X is accepted.
+ *   X          [x_rows][cols], xdtype any, ldx in elements.  Rows that all start on 32-byte boundaries take
+ *              the wide loads; any element-aligned X is accepted.
  *   row_index  optional device int32[rows]: row r is taken from X[row_index[r]]; an index outside
  *              0 .. x_rows-1 gives a row of zeros.  NULL: row r is X[r], x_rows >= rows.
  *   offsets    optional device int32[n_groups + 1] (n_groups 1 .. 1024), not falling, within
@@ -399,7 +401,8 @@ ADADIM_API int adadim_fp4_matmul_grouped(const adadim_fp4tensor* A, int64_t n_ro
 
 /*
  * Linear layer with 4-bit weights and activations in the model's own type: X is quantized as by
- * adadim_quantize_fp4 (x_amax: its amax) and multiplied as by adadim_fp4_matmul.
+ * adadim_quantize_fp4 (x_amax: its amax) and multiplied as by adadim_fp4_matmul.  Up to 8 tokens are quantized
+ * by the product's own kernel where Y is of X's type, X's rows start on 32-byte boundaries and in is a multiple of 16.
  *   workspace  adadim_workspace_bytes(ADADIM_WS_FP4, n_tokens, in, 4, 0) bytes, 256-byte aligned.
  */
 ADADIM_API int adadim_fp4_linear(const void* X, int xdtype, int64_t n_tokens, int64_t in, int64_t ldx, const float* x_amax,

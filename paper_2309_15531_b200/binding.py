@@ -600,7 +600,8 @@ def _fp4_operands(X: Fp4Tensor, W: Fp4Tensor, y: Optional[torch.Tensor]):
 def fp4_linear(X, W: Fp4Tensor, x_amax: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y = Q(X) W^T for activations X[n_tokens, in] (fp32, fp16, bf16; quantized in the call with x_amax) or for an
-    Fp4Tensor X that is quantized already (y is bf16 then unless given).  y has X's type unless given."""
+    Fp4Tensor X that is quantized already (y is bf16 then unless given).  y has X's type unless given.  NVFP4 without an
+    x_amax has tensor scale 1: what lies above 2688 saturates.  For inference: no gradient passes to X."""
     if W.experts:
         raise ValueError("fp4_linear: W is a stack of experts")
     if isinstance(X, Fp4Tensor):
@@ -637,7 +638,7 @@ def fp4_linear_grouped(X, offsets: torch.Tensor, W: Fp4Tensor, row_index: Option
                        workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The product for rows sorted by expert: rows offsets[e] .. offsets[e+1]-1 (int32 on the device) are
     multiplied by expert e of the stack W.  Row r is X[row_index[r]] (None: X[r]); X may be an Fp4Tensor with
-    groups.  Rows of no expert are not written."""
+    groups.  Rows of no expert are not written.  For inference: no gradient passes to X."""
     n = _i32(offsets, W.dev).numel() - 1
     if W.experts != n or n < 1:
         raise ValueError("fp4_linear_grouped: offsets do not match the stack of experts")

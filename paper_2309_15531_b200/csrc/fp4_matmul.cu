@@ -17,6 +17,9 @@
 //          tiles are under way at once and share the memory's bandwidth evenly.  Launched behind the
 //          quantizer it starts streaming the weight at once and waits only before it reads the
 //          activations.
+// Times in the comments below are the best of a graph's replays at 1.9 GHz.  In a run of seconds the power cap (1.3 to 1.6
+// GHz) lengthens the many-token cases (2048 x W[11008,4096] 41-44 -> 53 us, 8 experts x 8192 rows 163-173 -> 196-201 us),
+// and a caller in Python the shortest ones (1 x W[4096,4096] 6.3 -> 8.2 us).
 #include "fp4.cuh"
 #include "umma_fp4.cuh"
 
@@ -837,7 +840,8 @@ constexpr int kMinCut = 32, kMaxCutRows = 512;
 constexpr int kMinPairTile = 160;                      // the pair kernel's lowest token tile, two scale tile rows
 // kFusedTokens, the rows up to which a dense product quantizes them itself: every weight tile's CTA repeats the work, which at
 // 8 rows hides behind the weight's bytes and at 16 does not (16 x W[28672,8192]: 35.3 us fused, 24.5 us behind
-// the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).  Not with experts, some of which have more rows than the
+// the quantizer; 8 x W[4096,4096]: 6.7 and 7.4 us).  Where the weight is in L2 it does not quite at 8 either (8 x
+// W[11008,4096]: 11.6 us, 16 behind the quantizer 10.3 us).  Not with experts, some of which have more rows than the
 // typical one (128 rows over 32: 27.4 us fused, 25.0 us behind the quantizer).
 static_assert(kFusedTokens <= 8, "the quantizing warps take two tokens each, up to four warps to a stage");
 
@@ -974,7 +978,8 @@ int fp4_matmul_launch(const Fp4Plan& plan, const adadim_fp4tensor& A, int lt, co
     const int64_t ysz = ydtype == ADADIM_F32 ? 4 : 2;
     // All CTAs drain at the same time, and their stores hold up each other's loads: pauses spread the stores over
     // the next tile's time (270 ns a stage, four stores of a warp pair) where that is long enough.  2048 tokens x
-    // W[11008,4096] 42.3 -> 40.7 us, experts 177 -> 170 us; with four stages a tile (in = 1024) it lost 7 %.
+    // W[11008,4096] 42.3 -> 40.7 us, experts 177 -> 170 us (16 stages a tile); with four stages (in = 1024) it lost 7 %.
+    // Between those two the bound at 16 is not measured.
     p.pace_ns = p.num_k < 16 ? 0u : p.num_k < 32 ? 30u * static_cast<unsigned>(p.num_k) : 960u;
     p.bulk_y = ysz == 2 && aligned16(Y) && (ldy * ysz) % 16 == 0;
     if (p.bulk_y && (rc = make_tmap_u16(&tm[4], Y, static_cast<uint64_t>(out), static_cast<uint64_t>(n_rows),

@@ -16,11 +16,15 @@ namespace {
 using namespace fp4;
 
 // How the work is laid out, by the number of CTAs (one to a scale tile):
-//   kMany  128 threads, a thread takes 4 or 8 rows, the loads of four in flight together
+//   kMany  128 threads, a thread takes 4 or 8 rows, the loads of four in flight together (with 8, MXFP4 with few
+//          CTAs makes two dependent round trips to memory)
 //   kLow   the same for a product's low token tiles, which may lie side by side in a CTA, and for up to kLowCtas
 //          CTAs in front of a product: with the SM's shared memory left to the product (see the launcher)
 //   kFew   up to kFewCtas: 512 threads with one or two rows each, to have something to hide the latencies behind
-// (333 x 5003 fp32, 237 CTAs: 13.4 us as kMany, 7.4 us as kFew; 2048 x 4096 bf16 to MXFP4, 512 CTAs: 6.8 and 7.8 us)
+// Measured on one size on each side of the bound, with the data in L2: 333 x 5003 fp32, 237 CTAs, 13.4 us as kMany and
+// 7.4 us as kFew; 2048 x 4096 bf16 to MXFP4, 512 CTAs, 6.8 us as kMany and 7.8 us as kFew (from DRAM 9.7 us as kMany).
+// Times are the best of a graph's replays; sustained from Python W[11008,4096] with its values takes 36.9 us (35.2), 333 x
+// 5003 8.2 us (7.1).  Codes only: W[11008,4096] 23.2 us to NVFP4 (floor 17.6), 22.1 us to MXFP4; 2048 x 4096 7.5 and 8.4 us.
 enum Mode { kMany, kLow, kFew };
 constexpr int kFewCtas = 2 * 148, kLowCtas = 4 * 148;
 template <Mode MODE>
@@ -195,6 +199,8 @@ quantize_kernel(const QuantParams p) {
 
 // Segments of a row (of the whole matrix where its rows follow one another), four 16-byte loads of a thread in flight;
 // one atomic per CTA.  Bound by memory: 8192 x 8192 bf16 21.6 us, 6220 GB/s (with a division for every load: 31.4 us).
+// Rows that do not start on 16-byte boundaries are read element by element (3333 x 5003 fp32 13.7 us, 4870 GB/s, 0.74 of
+// the copy rate), and of a row shorter than a segment the other threads are idle (200000 x 50 bf16 119 us).
 constexpr int kMaxThreads = 256, kMaxLoads = 4;
 template <typename T>
 constexpr int kSegment = kMaxThreads * kMaxLoads * 16 / static_cast<int>(sizeof(T));

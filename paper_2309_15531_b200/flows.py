@@ -160,7 +160,8 @@ def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor
     stacks.
     x [n_tokens, hidden], experts int [n_tokens, top], weights [n_tokens, top]; gate, up stacks [ffn, hidden], down a
     stack [hidden, ffn].  x is gathered and quantized once for gate and up.  x_amax, act_amax: the largest magnitudes
-    that calibration found (NVFP4; None: tensor scale 1)."""
+    that calibration found, of x and of silu(gate) * up (NVFP4; None: tensor scale 1, with which blocks above 2688 saturate
+    and blocks below 0.0058 become zero).  For inference: no gradient passes."""
     order, row_index, offsets = rows_by_expert(experts, gate.experts)
     q = B.quantize_fp4(x, gate.fmt, amax=x_amax, row_index=row_index, offsets=offsets)
     rows = row_index.numel()
