@@ -467,6 +467,10 @@ class Fp4Tensor:
         """float32[1], the largest magnitude that NVFP4's tensor scale is taken from; None: tensor scale 1 (or MXFP4)."""
         return self._scale.value if self._scale.present else None
 
+    @amax.setter
+    def amax(self, amax: Optional[torch.Tensor]) -> None:
+        self.set_amax(amax)
+
     def set_amax(self, amax: Optional[torch.Tensor]) -> None:
         """Sets the amax (its value is copied).  Matrices that were quantized with another have to be quantized again:
         a product that needs one of them raises ValueError until then.  A stack has one amax for all its experts: the

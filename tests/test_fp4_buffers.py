@@ -46,3 +46,17 @@ def test_views_follow_the_buffers_of_their_stack():
         one.codes = one.codes.clone()
     with pytest.raises(ValueError):
         one.scales = one.scales.clone()
+
+
+def test_the_quantizer_that_keeps_the_amax_checks_its_arguments():
+    import ctypes as C
+    L = B.lib()
+
+    def call(amax, kept, fmt=B.NVFP4):
+        q = B.Fp4TensorC(256, 256, kept, 48)
+        return L.adadim_quantize_fp4_amax(256, B.BF16, 0 if amax == 0 else 40, 96, 96, 40, fmt, None, None, 0, C.byref(q), None,
+                                          B.BF16, 0, amax or None, None)
+
+    assert call(256, None) == 1                           # nowhere to keep it
+    assert call(258, 256) == 5 and call(256, 258) == 5    # alignment
+    assert call(0, None) == 0                             # an empty matrix

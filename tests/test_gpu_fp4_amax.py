@@ -175,3 +175,13 @@ def test_an_amax_or_a_status_of_another_size_is_refused():
                  lambda: B.fp4_linear_grouped(x, _offsets(0, 4, 6), S, status=no_status)):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_an_amax_that_is_assigned_is_set():
+    x, (w, _) = _data()
+    a = _amax(0.1)
+    W = B.quantize_fp4(w, B.NVFP4, amax=a)
+    loaded = B.Fp4Tensor(96, 192, B.NVFP4)
+    loaded.codes, loaded.scales, loaded.amax = W.codes.clone(), W.scales.clone(), a
+    a.zero_()
+    assert torch.equal(B.fp4_linear(x, loaded), B.fp4_linear(x, W))
