@@ -57,7 +57,8 @@ typedef enum {
   ADADIM_ERR_NOT_PD = 7,     /* (device) damped Hessian is not positive definite            */
   ADADIM_ERR_NUMERIC = 8,    /* (device) a reconstruction error is NaN                      */
   ADADIM_ERR_TIMEOUT = 9,    /* (device) an internal wait exceeded its limit                */
-  ADADIM_ERR_CUDA = 10       /* a CUDA runtime / driver call failed                         */
+  ADADIM_ERR_CUDA = 10,      /* a CUDA runtime / driver call failed                         */
+  ADADIM_ERR_PAGES = 11      /* (device) no free page left, or a page or table out of range */
 } adadim_status;
 
 typedef enum { ADADIM_F32 = 0, ADADIM_F16 = 1, ADADIM_BF16 = 2 } adadim_dtype;
@@ -428,6 +429,112 @@ ADADIM_API int adadim_fp4_linear_grouped(const void* X, int xdtype, int64_t x_ro
  */
 ADADIM_API int adadim_fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int format, int quantized, int aligned,
                         int* plan);
+
+/*
+ * ---- key-value cache in 4 bits ------------------------------------------------------------------
+ * Keys and values of one attention layer as NVFP4 (E2M1 codes, one E4M3 scale for every 16 channels of a
+ * head, as adadim_quantize_fp4 forms them with each token's head as a row), in pages of `page` tokens:
+ *   codes   [n_pages][2][kv_heads][page][held / 2] bytes (0: keys, 1: values), the even channel in the low half
+ *   scales  [n_pages][2][kv_heads][page][held / 16] bytes;  both 256-byte aligned
+ *   held    head_dim rounded up to 64, 128 or 256; channels from head_dim on are written as zeros
+ *   page    a power of two, 16 .. 1024;  head_dim a multiple of 16, 16 .. 256;  n_pages * page < 2^31
+ *   amax    device float[2], the largest magnitudes expected of keys and of values (see adadim_fp4tensor; zero,
+ *           infinite or NaN: tensor scale 1), or NULL; must not change while the cache holds anything
+ * MXFP4 is not offered: NVFP4's code * scale is exact in fp16, in which the products are formed.
+ * A token's place is its slot, page number * page + place inside the page.  A request's tokens are found
+ * through its row of a block table: token j lies in page table[j / page].
+ */
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  const float* amax;
+  int64_t n_pages;
+  int32_t page, kv_heads, head_dim;
+} adadim_kv4cache;
+
+/* Bytes of `codes` (what = 0) or `scales` (what = 1); 0 for bad sizes. */
+ADADIM_API size_t adadim_kv4_bytes(int64_t n_pages, int page, int kv_heads, int head_dim, int what);
+
+/*
+ * Block tables and slot maps of a step.  Request i holds past[i] tokens, in the pages that its row of `table`
+ * [n_requests][ldt] (the first `width` entries are used) lists, and gets fresh[i] more.  The
+ * ceil((past + fresh) / page) - ceil(past / page) pages it needs are taken from free_pages[0 .. n_free-1] in order, request
+ * after request, from place *cursor on (NULL: 0), and written to its row.
+ *   lengths    [n_requests] past + fresh;  offsets [n_requests + 1] exclusive sums of fresh, at most `rows`
+ *   requests, positions, slots  [rows]: of new token r (requests in order) its request, its place in the
+ *              request, its slot.  Rows behind the last new token get -1, 0, -1.
+ *   next       *cursor + pages taken (not the same word as cursor)
+ * Nothing but those entries of `table` is changed, so a call may be repeated.  past and fresh are not negative, and
+ * past + fresh < 2^31; otherwise (device) ADADIM_ERR_SHAPE, and they count as 0.  More new tokens than
+ * rows: ADADIM_ERR_SHAPE.  A token whose page cannot be had (the list is used up, the row too narrow, an entry
+ * negative) has slot -1, and its entry -1 where the list is used up: ADADIM_ERR_PAGES.
+ * n_requests up to 8192, n_free and rows below 2^31; page a power of two, 16 .. 1024.
+ */
+ADADIM_API int adadim_page_tables(const int32_t* past, const int32_t* fresh, int64_t n_requests, int page,
+                        int32_t* table, int64_t ldt, int64_t width, const int32_t* free_pages, int64_t n_free,
+                        const int32_t* cursor, int64_t rows, int32_t* lengths, int32_t* offsets, int32_t* requests,
+                        int32_t* positions, int32_t* slots, int32_t* next, int* status_dev, void* cuda_stream);
+
+/*
+ * Rotary positions: channel pair j = 0 .. dim / 2 - 1 of a head turns by positions[axis[j]][token] * freq[j] radians,
+ * a' = a cos - b sin, b' = b cos + a sin, with (a, b) channels (j, j + dim / 2), or (2 j, 2 j + 1) where `adjacent`.
+ * Channels from dim on stay as they are.  One axis for text, three for images and video (time, row, column).
+ *   positions  int32 [axes][ld];  freq  double [dim / 2];  axis  uint8 [dim / 2], values below axes (others
+ *              count as axes - 1), NULL: all 0;  dim a multiple of 16, up to head_dim
+ */
+typedef struct {
+  const int32_t* positions;
+  const double* freq;
+  const uint8_t* axis;
+  int64_t ld;
+  int32_t axes, dim, adjacent;
+} adadim_rotary;
+
+/* Heads of tokens: channel c of head h of token t at p + t * ld + h * lh + c (elements). */
+typedef struct {
+  void* p;
+  int64_t ld, lh;
+} adadim_heads;
+
+/*
+ * Rotates queries and keys and puts keys and values into the cache.
+ *   K, V       [n_tokens][kv_heads][head_dim], dtype any.  slots int32[n_tokens]: where each token goes; tokens with a
+ *              slot outside the cache are not stored.  Slots have to differ.
+ *   Q, Qr      [n_tokens][q_heads][head_dim] of the same dtype, Q rotated into Qr (may be Q itself), rounded once;
+ *              Q NULL: none.  Q, K, V may lie side by side in one matrix.
+ *   rotary     NULL: nothing is rotated (Q must be NULL)
+ *   k_values, v_values  optional: the values that the cache then stands for, [n_tokens][kv_heads][head_dim], vdtype ADADIM_BF16 or
+ *              ADADIM_F32 (both hold them exactly, up to their own range)
+ * Keys are quantized from the rotation in binary64, every decision as in adadim_quantize_fp4; a block with an
+ * infinity or NaN gets scale 0x7F: its values are NaN, and so is what attends to them.
+ */
+ADADIM_API int adadim_kv4_append(const adadim_heads* Q, const adadim_heads* Qr, int q_heads, const adadim_heads* K, const adadim_heads* V,
+                        int dtype, int64_t n_tokens, const int32_t* slots, const adadim_rotary* rotary,
+                        const adadim_kv4cache* cache, const adadim_heads* k_values, const adadim_heads* v_values, int vdtype,
+                        void* cuda_stream);
+
+/*
+ * Attention of new tokens over the cache.  Request i has the query rows offsets[i] .. offsets[i+1]-1 (int32
+ * [n_requests + 1], not falling, within 0 .. n_rows) and lengths[i] tokens in the cache, its new ones the last of them.
+ *   Q, O       [n_rows][q_heads][head_dim], dtype ADADIM_F16 or ADADIM_BF16; query head h reads key head
+ *              h / (q_heads / kv_heads).  Rows of no request are not written.
+ *   scale      of the products q k
+ *   causal     query row j of n sees positions up to lengths - n + j; 0: all
+ *   window     > 0: of those only positions above lengths - n + j - window
+ *   A row that sees nothing (a length of zero, more rows than tokens) gets zeros.  What a row does not see
+ *   does not reach it, NaN included.
+ *   max_new    no request has more query rows than this: picks the kernels and has no part in the result.  0: not known.
+ *   workspace  adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, kv_heads, head_dim), 256-byte aligned.
+ * The values that the codes stand for are used as they are (exact in fp16); queries too (bf16 ones times a power of
+ * two in fp16), weights are rounded to fp16, sums are binary32, and O is rounded once.  A table entry outside the
+ * cache: its tokens are left out, (device) ADADIM_ERR_PAGES.  Offsets that fall or leave 0 .. n_rows, lengths outside
+ * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads < 2^31.
+ */
+ADADIM_API int adadim_kv4_attention(const adadim_heads* Q, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
+                        const int32_t* lengths, int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width,
+                        const adadim_kv4cache* cache, float scale, int causal, int64_t window, int64_t max_new,
+                        const adadim_heads* O, int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
+ADADIM_API size_t adadim_kv4_workspace_bytes(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim);
 
 /* Helpers. */
 ADADIM_API size_t adadim_workspace_bytes(int kind, int64_t out, int64_t in, int bits, int group);

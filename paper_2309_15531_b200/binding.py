@@ -40,6 +40,20 @@ class Fp4TensorC(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("amax", C.c_void_p), ("ld", C.c_int64)]
 
 
+class Kv4CacheC(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("amax", C.c_void_p), ("n_pages", C.c_int64),
+                ("page", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class RotaryC(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("freq", C.c_void_p), ("axis", C.c_void_p), ("ld", C.c_int64),
+                ("axes", C.c_int32), ("dim", C.c_int32), ("adjacent", C.c_int32)]
+
+
+class HeadsC(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64), ("lh", C.c_int64)]
+
+
 class GptqLayerC(C.Structure):
     _fields_ = [("W", C.c_void_p), ("out", C.c_int64), ("ldw", C.c_int64), ("q_oc", C.POINTER(QTensorC)),
                 ("q_ic", C.POINTER(QTensorC)), ("dim", C.c_int), ("chosen", C.c_void_p), ("gptq_loss", C.c_void_p)]
@@ -103,6 +117,17 @@ def lib():
                                                 vp, vp, sz, vp]
         L.adadim_fp4_plan.restype = ci
         L.adadim_fp4_plan.argtypes = [i64, i64, i64, ci, ci, ci, ci, C.POINTER(C.c_int)]
+        cp, hp = C.POINTER(Kv4CacheC), C.POINTER(HeadsC)
+        L.adadim_kv4_bytes.restype = sz
+        L.adadim_kv4_bytes.argtypes = [i64, ci, ci, ci, ci]
+        L.adadim_page_tables.restype = ci
+        L.adadim_page_tables.argtypes = [vp, vp, i64, ci, vp, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.adadim_kv4_append.restype = ci
+        L.adadim_kv4_append.argtypes = [hp, hp, ci, hp, hp, ci, i64, vp, C.POINTER(RotaryC), cp, hp, hp, ci, vp]
+        L.adadim_kv4_attention.restype = ci
+        L.adadim_kv4_attention.argtypes = [hp, ci, i64, ci, vp, vp, i64, vp, i64, i64, cp, C.c_float, ci, i64, i64, hp, vp, vp, sz, vp]
+        L.adadim_kv4_workspace_bytes.restype = sz
+        L.adadim_kv4_workspace_bytes.argtypes = [i64, i64, ci, ci, ci]
         L.adadim_unpack_codes.restype = C.c_int
         L.adadim_unpack_codes.argtypes = [vp, i64, i64, C.c_int, vp, vp]
         _lib = L
@@ -685,6 +710,214 @@ def fp4_plan(rows: int, out: int, inp: int, fmt: int, experts: int = 0, quantize
     plan = (C.c_int * 5)()
     _check(lib().adadim_fp4_plan(rows, out, inp, experts, fmt, quantized, aligned, plan), "adadim_fp4_plan")
     return Fp4Plan(bool(plan[0]), plan[1], plan[2], plan[3], bool(plan[4]))
+
+
+# ---- key-value cache in 4 bits --------------------------------------------------------------------
+
+class PageTables:
+    """What page_tables writes for up to `requests` requests and `rows` new tokens (see include/adadim.h): int32 tensors
+    lengths [requests], offsets [requests + 1], requests, positions, slots [rows], cursor [1]."""
+
+    def __init__(self, requests: int, rows: int, device="cuda"):
+        if requests < 0 or rows < 0:
+            raise ValueError("PageTables: bad sizes")
+        def ints(n):
+            return torch.zeros(n, dtype=torch.int32, device=device)
+        self.n_requests, self.n_rows = requests, rows
+        self.lengths, self.offsets, self.cursor = ints(requests), ints(requests + 1), ints(1)
+        self.requests, self.positions, self.slots = ints(rows), ints(rows), ints(rows)
+        self.dev = self.offsets.get_device()
+        self._p = [t.data_ptr() for t in (self.lengths, self.offsets, self.requests, self.positions, self.slots, self.cursor)]
+
+
+def page_tables(past: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, page_size: int,
+                out: Optional[PageTables] = None, rows: Optional[int] = None, cursor: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None) -> PageTables:
+    """Block tables and slot maps of a step: request i holds past[i] tokens and gets new[i] more (int32 on the device).  The
+    pages this needs are taken from free_pages in order, from place cursor[0] on (None: 0), and written to the request's
+    row of table int32 [requests, width].  `rows` (or out.n_rows): new tokens of the step, or more: rows behind the last one get
+    slot -1, request -1.  out.cursor: where the next step goes on; pass it as `cursor` with another `out`, or a copy."""
+    dev = table.get_device()
+    n, (t_rows, width) = _i32(past, dev).numel(), table.shape
+    if _i32(new, dev).numel() != n or t_rows != n:
+        raise ValueError("page_tables: past, new and table are of different numbers of requests")
+    assert dev >= 0 and table.dtype == torch.int32 and (width <= 1 or table.stride(1) == 1)
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return page_tables(past, new, table, free_pages, page_size, out, rows, cursor, status)
+    if out is None:
+        if rows is None:
+            raise ValueError("page_tables: out or rows is needed")
+        out = PageTables(n, rows, device=table.device)
+    if out.n_requests != n or out.dev != dev or (rows is not None and rows != out.n_rows):
+        raise ValueError("page_tables: out was made for another number of requests or rows, or another device")
+    cp = None
+    if cursor is not None:
+        cp = _i32(cursor, dev).data_ptr()
+        if cursor.numel() != 1 or cp == out._p[5]:
+            raise ValueError("page_tables: cursor is one int32, and not the one that is written")
+    lengths, offsets, requests, positions, slots, after = out._p
+    rc = (_lib or lib()).adadim_page_tables(past.data_ptr(), new.data_ptr(), n, page_size, table.data_ptr(),
+                                            table.stride(0) if n > 1 else width, width, _i32(free_pages, dev).data_ptr(),
+                                            free_pages.numel(), cp, out.n_rows, lengths, offsets, requests, positions, slots,
+                                            after, _status(status, dev), _raw_stream(dev))
+    if rc:
+        _check(rc, "adadim_page_tables")
+    return out
+
+
+class Kv4Cache:
+    """Keys and values of one attention layer in NVFP4, in n_pages pages of page_size tokens (see include/adadim.h for the
+    layout).  k_amax, v_amax: float32[1], the largest magnitudes expected (absmax over calibration chunks; rotation can
+    make a key's sqrt(2) larger); their values are copied, and stay for the cache's life.  None: tensor scale 1."""
+
+    def __init__(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, k_amax: Optional[torch.Tensor] = None,
+                 v_amax: Optional[torch.Tensor] = None, device="cuda"):
+        size = lib().adadim_kv4_bytes
+        if n_pages < 1 or not size(n_pages, page_size, kv_heads, head_dim, 0):
+            raise ValueError("Kv4Cache: page_size is a power of two from 16 to 1024, head_dim a multiple of 16 up to 256")
+        self.n_pages, self.page_size, self.kv_heads, self.head_dim = n_pages, page_size, kv_heads, head_dim
+        self.held = 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256
+        shape = (n_pages, 2, kv_heads, page_size)
+        self.codes = torch.zeros(*shape, self.held // 2, dtype=torch.uint8, device=device)
+        self.scales = torch.zeros(*shape, self.held // 16, dtype=torch.uint8, device=device)
+        self.dev = self.codes.get_device()
+        self.amax = None
+        if k_amax is not None or v_amax is not None:
+            self.amax = torch.zeros(2, dtype=torch.float32, device=device)
+            for at, amax in enumerate((k_amax, v_amax)):
+                if amax is not None:
+                    _amax(amax, self.dev)
+                    self.amax[at:at + 1].copy_(amax.reshape(1))
+        self._c = Kv4CacheC(self.codes.data_ptr(), self.scales.data_ptr(), self.amax.data_ptr() if self.amax is not None else None,
+                            n_pages, page_size, kv_heads, head_dim)
+        self._ref = C.byref(self._c)
+
+
+class Rotary:
+    """Rotary positions: pair j of a head turns by position * freq[j] on axis axis[j] (None: one axis).  freq [dim / 2] in
+    radians a position (kept in binary64), axis [dim / 2] whole numbers; the pair is channels (j, j + dim / 2), or (2 j, 2 j + 1)
+    where `adjacent`.  dim is a multiple of 16; further channels of a head are not turned."""
+
+    def __init__(self, freq: torch.Tensor, axis: Optional[torch.Tensor] = None, adjacent: bool = False):
+        if freq.dim() != 1 or freq.numel() % 8 or not 8 <= freq.numel() <= 128 or not freq.is_cuda:
+            raise ValueError("Rotary: freq [dim / 2] on the device, dim a multiple of 16 up to 256")
+        self.dim, self.adjacent, self.axes = 2 * freq.numel(), adjacent, 1
+        self.freq = freq.double().clone()
+        self.axis = None
+        if axis is not None:
+            if axis.shape != freq.shape or axis.is_floating_point() or int(axis.min()) < 0 or int(axis.max()) > 255:
+                raise ValueError("Rotary: axis has one number for each pair")
+            self.axes = int(axis.max()) + 1
+            self.axis = axis.to(device=freq.device, dtype=torch.uint8, copy=True)
+        self.dev = self.freq.get_device()
+        self._c = RotaryC(None, self.freq.data_ptr(), self.axis.data_ptr() if self.axis is not None else None, 0, self.axes,
+                          self.dim, int(adjacent))
+
+    @staticmethod
+    def of(dim: int, base: float = 10000.0, sections=None, adjacent: bool = False, device="cuda") -> "Rotary":
+        """freq[j] = base^(-2 j / dim); `sections`: how many pairs belong to each axis, in order (time, row, column)."""
+        half = dim // 2
+        freq = torch.tensor([base ** (-j / half) for j in range(half)], dtype=torch.float64, device=device)
+        if sections is None:
+            return Rotary(freq, None, adjacent)
+        if sum(sections) != half:
+            raise ValueError("Rotary: sections add up to dim / 2")
+        return Rotary(freq, torch.repeat_interleave(torch.arange(len(sections)), torch.tensor(sections)), adjacent)
+
+
+def _heads(t: torch.Tensor, dev: int, rows: int, heads: int, dim: int, dtype=None):
+    """A [tokens, heads, head_dim] tensor whose channels lie side by side, by reference."""
+    shape, stride = t.shape, t.stride()
+    assert (shape[0], shape[1], shape[2]) == (rows, heads, dim) and len(shape) == 3 and (stride[2] == 1 or dim == 1)
+    assert t.get_device() == dev and (dtype is None or t.dtype == dtype)
+    return C.byref(HeadsC(t.data_ptr(), stride[0], stride[1]))
+
+
+def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, slots: torch.Tensor, q: Optional[torch.Tensor] = None,
+               rotary: Optional[Rotary] = None, positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               k_values: Optional[torch.Tensor] = None, v_values: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Rotates q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] and puts k and v into the cache at slots
+    int32[tokens] (all different; -1: not stored), quantized to NVFP4.  fp32, fp16 or bf16, one type; views of one projection's result
+    are taken as they are.  positions int32 [tokens] or [axes, tokens].  Returns the rotated q (in q_out, which may be q, if given).
+    k_values, v_values (bf16 or fp32): receive the values that the cache then holds.  For inference: no gradient passes."""
+    dev, (n, h, d) = cache.dev, k.shape
+    if h != cache.kv_heads or d != cache.head_dim:
+        raise ValueError("kv4_append: k does not match the cache")
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return kv4_append(k, v, cache, slots, q, rotary, positions, q_out, k_values, v_values)
+    dtype, rc_ref, qp, qo, q_heads = k.dtype, None, None, None, 0
+    if _i32(slots, dev).numel() != n:
+        raise ValueError("kv4_append: one slot for each token")
+    if (rotary is None) != (positions is None) or (q is not None and rotary is None):
+        raise ValueError("kv4_append: rotary and positions go together, and q with them")
+    if rotary is not None:
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        assert positions.get_device() == dev and rotary.dev == dev and positions.dtype == torch.int32
+        if axes < rotary.axes or positions.shape[-1] != n or positions.dim() > 2 or rotary.dim > d:
+            raise ValueError("kv4_append: positions [axes, tokens] for every axis of the rotary, which is no wider than a head")
+        if n > 1 and positions.stride(-1) != 1:
+            raise ValueError("kv4_append: a token's positions lie side by side")
+        own = rotary._c
+        rc_ref = C.byref(RotaryC(positions.data_ptr(), own.freq, own.axis, positions.stride(0) if axes > 1 else 0, own.axes,
+                                 own.dim, own.adjacent))
+    if q is not None:
+        q_heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(n, q_heads, d, dtype=dtype, device=q.device)
+        qp, qo = _heads(q, dev, n, q_heads, d, dtype), _heads(q_out, dev, n, q_heads, d, dtype)
+    kv = vv = None
+    vdt = BF16
+    if k_values is not None:
+        kv, vdt = _heads(k_values, dev, n, h, d), _DT[k_values.dtype]
+    if v_values is not None:
+        vv, vdt = _heads(v_values, dev, n, h, d, None if k_values is None else k_values.dtype), _DT[v_values.dtype]
+    rc = (_lib or lib()).adadim_kv4_append(qp, qo, q_heads, _heads(k, dev, n, h, d), _heads(v, dev, n, h, d, dtype), _DT[dtype],
+                                           n, slots.data_ptr(), rc_ref, cache._ref, kv, vv, vdt, _raw_stream(dev))
+    if rc:
+        _check(rc, "adadim_kv4_append")
+    return q_out
+
+
+def kv4_workspace_bytes(requests: int, rows: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().adadim_kv4_workspace_bytes(requests, rows, q_heads, kv_heads, head_dim))
+
+
+def kv4_attention(q: torch.Tensor, cache: Kv4Cache, table: torch.Tensor, lengths: torch.Tensor, offsets: torch.Tensor,
+                  scale: Optional[float] = None, causal: bool = True, window: int = 0, max_new: int = 0,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [rows, q_heads, head_dim] (fp16 or bf16) over the cache.  Request i has rows offsets[i] .. offsets[i+1]-1
+    and lengths[i] tokens in the cache (its new ones the last of them, already appended), in the pages of its row of table
+    int32 [requests, width].  scale: head_dim^-0.5 unless given.  window > 0: a row sees the last `window` positions up to its
+    own.  Rows that see nothing get zeros, rows of no request are not written.  max_new: no request has more
+    rows than this (0: not known); picks the kernels.  Calls that may run at once need a workspace each
+    (kv4_workspace_bytes).  For inference: no gradient passes."""
+    dev, (n, h, d) = cache.dev, q.shape
+    n_req, (t_rows, width) = _i32(lengths, dev).numel(), table.shape
+    if d != cache.head_dim or h % cache.kv_heads:
+        raise ValueError("kv4_attention: q does not match the cache")
+    if t_rows != n_req or _i32(offsets, dev).numel() != n_req + 1:
+        raise ValueError("kv4_attention: table, lengths and offsets are of different numbers of requests")
+    assert table.get_device() == dev and table.dtype == torch.int32 and (width <= 1 or table.stride(1) == 1)
+    if dev != _device():
+        with torch.cuda.device(dev):
+            return kv4_attention(q, cache, table, lengths, offsets, scale, causal, window, max_new, out, workspace, status)
+    if out is None:
+        out = torch.empty(n, h, d, dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = _ws(kv4_workspace_bytes(n_req, n, h, cache.kv_heads, d), q.device)
+    assert workspace.get_device() == dev and workspace.dtype == torch.uint8
+    dtype = q.dtype
+    rc = (_lib or lib()).adadim_kv4_attention(_heads(q, dev, n, h, d), _DT[dtype], n, h, offsets.data_ptr(), lengths.data_ptr(),
+                                              n_req, table.data_ptr(), table.stride(0) if n_req > 1 else width, width, cache._ref,
+                                              d ** -0.5 if scale is None else scale, causal, window, max_new,
+                                              _heads(out, dev, n, h, d, dtype), _status(status, dev), workspace.data_ptr(),
+                                              workspace.numel(), _raw_stream(dev))
+    if rc:
+        _check(rc, "adadim_kv4_attention")
+    return out
 
 
 def static_scratch_bytes() -> int:

@@ -1,6 +1,7 @@
 // extern "C" entry points: argument validation on the host, then the kernel launchers.
 #include "common.cuh"
 #include "fp4.cuh"
+#include "kv4.cuh"
 
 namespace adadim {
 int rtn_launch(const void* W, int wdtype, int64_t out, int64_t in, int64_t ldw, int bits, int group, int dim,
@@ -55,6 +56,23 @@ int check_quant_params(int bits, int group, bool allow_256) {
   if (group != 32 && group != 64 && group != 128 && !(allow_256 && group == 256)) return ADADIM_ERR_PARAM;
   return ADADIM_OK;
 }
+
+constexpr int64_t kInt32Max = 0x7fffffff;
+
+bool kv4_page_ok(int page) { return page >= kv4::kMinPage && page <= kv4::kMaxPage && (page & (page - 1)) == 0; }
+int check_kv4_sizes(const adadim_kv4cache& c) {
+  if (!kv4_page_ok(c.page) || c.kv_heads < 1 || c.kv_heads > (1 << 16)) return ADADIM_ERR_PARAM;
+  if (c.head_dim < 16 || c.head_dim > 256 || c.head_dim % 16 != 0) return ADADIM_ERR_PARAM;
+  return c.n_pages < 0 || c.n_pages > kInt32Max / c.page ? ADADIM_ERR_SHAPE : ADADIM_OK;
+}
+int check_kv4(const adadim_kv4cache* c) {
+  if (c == nullptr) return ADADIM_ERR_NULL;
+  const int rc = check_kv4_sizes(*c);
+  if (rc != ADADIM_OK) return rc;
+  if (c->n_pages > 0 && (c->codes == nullptr || c->scales == nullptr)) return ADADIM_ERR_NULL;
+  return aligned256(c->codes) && aligned256(c->scales) ? ADADIM_OK : ADADIM_ERR_ALIGN;
+}
+Kv4Heads heads_of(const adadim_heads* h, const Kv4Heads& none) { return h == nullptr ? none : Kv4Heads{h->p, h->ld, h->lh}; }
 
 int check_qtensor(const adadim_qtensor* q) {
   if (q == nullptr || q->codes == nullptr || q->scales == nullptr || q->zeros == nullptr) return ADADIM_ERR_NULL;
@@ -196,6 +214,7 @@ const char* adadim_strerror(int status) {
     case ADADIM_ERR_NUMERIC: return "a reconstruction error is NaN";
     case ADADIM_ERR_TIMEOUT: return "an internal device-side wait exceeded its limit";
     case ADADIM_ERR_CUDA: return "a CUDA call failed";
+    case ADADIM_ERR_PAGES: return "no free page left, or a page or block table out of range";
     default: return "unknown status";
   }
 }
@@ -484,6 +503,100 @@ int adadim_fp4_plan(int64_t rows, int64_t out, int64_t in, int n_experts, int fo
   const int v[5] = {p.pair, p.n_tile, p.splits, p.per_sm, p.fused};
   for (int k = 0; k < 5; ++k) plan[k] = v[k];
   return ADADIM_OK;
+}
+
+size_t adadim_kv4_bytes(int64_t n_pages, int page, int kv_heads, int head_dim, int what) {
+  const adadim_kv4cache c = {nullptr, nullptr, nullptr, n_pages, page, kv_heads, head_dim};
+  if (check_kv4_sizes(c) != ADADIM_OK || (what != 0 && what != 1)) return 0;
+  return static_cast<size_t>(n_pages) * 2 * kv_heads * page * (kv4::held_dim(head_dim) / (what == 0 ? 2 : 16));
+}
+
+int adadim_page_tables(const int32_t* past, const int32_t* fresh, int64_t n_requests, int page, int32_t* table, int64_t ldt,
+                       int64_t width, const int32_t* free_pages, int64_t n_free, const int32_t* cursor, int64_t rows,
+                       int32_t* lengths, int32_t* offsets, int32_t* requests, int32_t* positions, int32_t* slots, int32_t* next,
+                       int* status_dev, void* cuda_stream) {
+  if (!kv4_page_ok(page)) return ADADIM_ERR_PARAM;
+  if (n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width || n_free < 0 || rows < 0) return ADADIM_ERR_SHAPE;
+  if (n_free > kInt32Max || rows > kInt32Max || width > kInt32Max) return ADADIM_ERR_SHAPE;
+  if (offsets == nullptr || next == nullptr || next == cursor) return ADADIM_ERR_NULL;
+  if (n_requests > 0 && (past == nullptr || fresh == nullptr || lengths == nullptr || (width > 0 && table == nullptr))) return ADADIM_ERR_NULL;
+  if (n_free > 0 && free_pages == nullptr) return ADADIM_ERR_NULL;
+  if (rows > 0 && (requests == nullptr || positions == nullptr || slots == nullptr)) return ADADIM_ERR_NULL;
+  return page_tables_launch(past, fresh, static_cast<int>(n_requests), page, table, ldt, width, free_pages, static_cast<int>(n_free),
+                            cursor, static_cast<int>(rows), lengths, offsets, requests, positions, slots, next, status_dev,
+                            static_cast<cudaStream_t>(cuda_stream));
+}
+
+int adadim_kv4_append(const adadim_heads* Q, const adadim_heads* Qr, int q_heads, const adadim_heads* K, const adadim_heads* V,
+                      int dtype, int64_t n_tokens, const int32_t* slots, const adadim_rotary* rotary, const adadim_kv4cache* cache,
+                      const adadim_heads* k_values, const adadim_heads* v_values, int vdtype, void* cuda_stream) {
+  int rc = check_kv4(cache);
+  if (rc != ADADIM_OK) return rc;
+  if (dtype != ADADIM_F32 && dtype != ADADIM_F16 && dtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
+  if ((k_values != nullptr || v_values != nullptr) && vdtype != ADADIM_F32 && vdtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
+  if (n_tokens < 0 || n_tokens > kInt32Max || q_heads < 0 || q_heads > (1 << 16)) return ADADIM_ERR_SHAPE;
+  if ((Q == nullptr) != (Qr == nullptr)) return ADADIM_ERR_NULL;
+  if (Q != nullptr && rotary == nullptr) return ADADIM_ERR_PARAM;
+  if (Q == nullptr) q_heads = 0;
+  if (rotary != nullptr) {
+    if (rotary->axes < 1 || rotary->dim < 16 || rotary->dim > cache->head_dim || rotary->dim % 16 != 0) return ADADIM_ERR_PARAM;
+    if (n_tokens > 0 && (rotary->positions == nullptr || rotary->freq == nullptr)) return ADADIM_ERR_NULL;
+    if (rotary->axes > 1 && rotary->axis == nullptr) return ADADIM_ERR_NULL;
+  }
+  if (n_tokens == 0) return ADADIM_OK;
+  if (K == nullptr || V == nullptr || K->p == nullptr || V->p == nullptr || slots == nullptr) return ADADIM_ERR_NULL;
+  if (Q != nullptr && q_heads > 0 && (Q->p == nullptr || Qr->p == nullptr)) return ADADIM_ERR_NULL;
+  const Kv4Heads none = {nullptr, 0, 0};
+  const Kv4Rotary still = {nullptr, nullptr, nullptr, 0, 1, 0, 0};
+  return kv4_append_launch(heads_of(Q, none), heads_of(Qr, none), q_heads, heads_of(K, none), heads_of(V, none), dtype, n_tokens, slots,
+                           rotary == nullptr ? still : Kv4Rotary{rotary->positions, rotary->freq, rotary->axis, rotary->ld, rotary->axes,
+                                                                rotary->dim, rotary->adjacent},
+                           kv4::cache_of(*cache), heads_of(k_values, none), heads_of(v_values, none), vdtype,
+                           static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t adadim_kv4_workspace_bytes(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim) {
+  if (n_requests < 0 || n_rows < 0 || kv_heads < 1 || q_heads < kv_heads || head_dim < 16 || head_dim > 256) return 0;
+  return kv4_workspace(n_requests, n_rows, q_heads, kv_heads, head_dim);
+}
+
+int adadim_kv4_attention(const adadim_heads* Q, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets, const int32_t* lengths,
+                         int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width, const adadim_kv4cache* cache, float scale,
+                         int causal, int64_t window, int64_t max_new, const adadim_heads* O, int* status_dev, void* workspace,
+                         size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_kv4(cache);
+  if (rc != ADADIM_OK) return rc;
+  if (dtype != ADADIM_F16 && dtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
+  if (q_heads < 1 || q_heads > (1 << 16) || q_heads % cache->kv_heads != 0) return ADADIM_ERR_PARAM;
+  if (window < 0 || max_new < 0) return ADADIM_ERR_PARAM;
+  if (n_rows < 0 || n_rows * q_heads > kInt32Max || n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width ||
+      width * cache->page > kInt32Max)
+    return ADADIM_ERR_SHAPE;
+  if (n_rows == 0 || n_requests == 0) return ADADIM_OK;
+  if (Q == nullptr || O == nullptr || Q->p == nullptr || O->p == nullptr || offsets == nullptr || lengths == nullptr ||
+      (width > 0 && table == nullptr) || workspace == nullptr)
+    return ADADIM_ERR_NULL;
+  if (!aligned256(workspace)) return ADADIM_ERR_ALIGN;
+  if (workspace_bytes < adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, cache->kv_heads, cache->head_dim)) return ADADIM_ERR_WORKSPACE;
+  Kv4Attention a = {};
+  a.q = {Q->p, Q->ld, Q->lh};
+  a.o = {O->p, O->ld, O->lh};
+  a.n_rows = static_cast<int>(n_rows);
+  a.q_heads = q_heads;
+  a.group = q_heads / cache->kv_heads;
+  a.offsets = offsets;
+  a.lengths = lengths;
+  a.table = table;
+  a.n_requests = static_cast<int>(n_requests);
+  a.ldt = ldt;
+  a.width = width;
+  a.cache = kv4::cache_of(*cache);
+  a.scale = scale;
+  a.causal = causal != 0;
+  a.window = static_cast<int>(window > kInt32Max / 2 ? 0 : window);   // longer than any cache
+  a.status_dev = status_dev;
+  a.workspace = static_cast<char*>(workspace);
+  return kv4_attention_launch(a, dtype, max_new == 0 || max_new > n_rows ? n_rows : max_new, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adadim_unpack_codes(const uint32_t* codes, int64_t out, int64_t in, int bits, uint8_t* dst, void* cuda_stream) {
