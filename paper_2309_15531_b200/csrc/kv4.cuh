@@ -65,6 +65,8 @@ struct Kv4Rotary {
 struct Kv4Attention {
   Kv4Heads q, o;
   int n_rows, q_heads, group;
+  uint32_t group_rcp;      // 2^32 / group + 1, 0 for 1
+  int wide_q;              // eight channels of a query are a 16-byte load, four an 8-byte one
   const int32_t *offsets, *lengths, *table;
   int n_requests;
   int64_t ldt, width;
