@@ -1,6 +1,8 @@
 // Key-value cache in 4 bits: the layout that include/adadim.h defines, and what its kernels share.  Internal header.
 #pragma once
 
+#include <type_traits>
+
 #include "fp4.cuh"
 #include "umma_fp4.cuh"
 
@@ -74,12 +76,12 @@ struct Kv4Attention {
   float scale;
   int causal;
   int window;              // 0: none
-  int few_rows;            // a request with at most so many rows a key head is the few-row kernel's
+  int64_t least_rows, most_rows;   // a kernel takes the requests with so many rows a key head
   int* status_dev;
   char* workspace;
 };
 
-// implemented in kv4_cache.cu, kv4_attention.cu
+// implemented in kv4_cache.cu, kv4_attention.cu, kv4_few.cu
 int page_tables_launch(const int32_t* past, const int32_t* fresh, int n_requests, int page, int32_t* table, int64_t ldt,
                        int64_t width, const int32_t* free_pages, int n_free, const int32_t* cursor, int rows, int32_t* lengths,
                        int32_t* offsets, int32_t* requests, int32_t* positions, int32_t* slots, int32_t* next, int* status_dev,
@@ -88,6 +90,9 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
                       int64_t n_tokens, const int32_t* slots, const Kv4Rotary& rotary, const kv4::Cache& cache,
                       const Kv4Heads& k_values, const Kv4Heads& v_values, int vdtype, cudaStream_t st);
 int kv4_attention_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
+int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
+int kv4_join_launch(const Kv4Attention& a, int dtype, int ctas, int tile_rows, bool split, cudaStream_t st);
+size_t kv4_few_workspace(int held);
 size_t kv4_workspace(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim);
 
 }  // namespace adadim
