@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadadim.so")
 SOURCES = ["api.cu", "rtn.cu", "tc_gemm.cu", "score.cu", "cholinv.cu", "gptq.cu", "gptq_tc.cu", "score_static.cu", "gemv.cu",
-           "fp4_quant.cu", "fp4_matmul.cu", "kv4_cache.cu", "kv4_attention.cu", "kv4_few.cu"]
+           "fp4_quant.cu", "fp4_matmul.cu", "kv4_cache.cu", "kv4_attention.cu", "kv4_few.cu",
+           "kv4_many.cu"]
 HEADERS = ["common.cuh", "umma.cuh", "umma_fp4.cuh", "fp4.cuh", "kv4.cuh", "kv4_line.cuh", os.path.join("..", "..", "include", "adadim.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

@@ -68,7 +68,7 @@ struct Kv4Attention {
   Kv4Heads q, o;
   int n_rows, q_heads, group;
   uint32_t group_rcp;      // 2^32 / group + 1, 0 for 1
-  int wide_q;              // eight channels of a query are a 16-byte load, four an 8-byte one
+  int wide_q, wide16_q, wide16_o;  // four, eight channels of a query (a result) are one load (store)
   const int32_t *offsets, *lengths, *table;
   int n_requests;
   int64_t ldt, width;
@@ -81,7 +81,7 @@ struct Kv4Attention {
   char* workspace;
 };
 
-// implemented in kv4_cache.cu, kv4_attention.cu, kv4_few.cu
+// implemented in kv4_cache.cu, kv4_attention.cu, kv4_few.cu, kv4_many.cu
 int page_tables_launch(const int32_t* past, const int32_t* fresh, int n_requests, int page, int32_t* table, int64_t ldt,
                        int64_t width, const int32_t* free_pages, int n_free, const int32_t* cursor, int rows, int32_t* lengths,
                        int32_t* offsets, int32_t* requests, int32_t* positions, int32_t* slots, int32_t* next, int* status_dev,
@@ -93,6 +93,8 @@ int kv4_attention_launch(const Kv4Attention& a, int dtype, int64_t max_new, cuda
 int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
 int kv4_join_launch(const Kv4Attention& a, int dtype, int ctas, int tile_rows, bool split, cudaStream_t st);
 size_t kv4_few_workspace(int held);
+int kv4_many_launch(const Kv4Attention& a, int dtype, cudaStream_t st);
+size_t kv4_many_workspace(int held);
 size_t kv4_workspace(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim);
 
 }  // namespace adadim

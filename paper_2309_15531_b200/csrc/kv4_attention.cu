@@ -103,16 +103,31 @@ int kv4_join_launch(const Kv4Attention& a, int dtype, int ctas, int tile_rows, b
   return split ? join_held<true, __nv_bfloat16>(a, ctas, tile_rows, st) : join_held<false, __nv_bfloat16>(a, ctas, tile_rows, st);
 }
 
+// The kernel for many rows holds its line of work beside 192 KB of tiles, and TMEM has no room for heads of 256 channels.
+bool kv4_many_possible(int64_t n_requests, int held) { return n_requests <= kManyRequests && held <= 128; }
+
 size_t kv4_workspace(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim) {
-  return kv4_few_workspace(held_dim(head_dim));
+  const int held = held_dim(head_dim);
+  const size_t few = kv4_few_workspace(held);
+  if (!kv4_many_possible(n_requests, held) || n_rows * (q_heads / kv_heads) <= kFewRows) return few;
+  const size_t many = kv4_many_workspace(held);
+  return few > many ? few : many;
 }
 
 int kv4_attention_launch(const Kv4Attention& given, int dtype, int64_t max_new, cudaStream_t st) {
   Kv4Attention a = given;
   a.group_rcp = a.group == 1 ? 0 : static_cast<uint32_t>((uint64_t{1} << 32) / a.group + 1);
   a.wide_q = reinterpret_cast<uintptr_t>(a.q.p) % 8 == 0 && a.q.ld % 4 == 0 && a.q.lh % 4 == 0;
+  a.wide16_q = reinterpret_cast<uintptr_t>(a.q.p) % 16 == 0 && a.q.ld % 8 == 0 && a.q.lh % 8 == 0;
+  a.wide16_o = reinterpret_cast<uintptr_t>(a.o.p) % 16 == 0 && a.o.ld % 8 == 0 && a.o.lh % 8 == 0;
   a.least_rows = 1;
-  a.most_rows = 0x7fffffff;
+  a.most_rows = int64_t{1} << 40;
+  if (max_new * a.group <= kFewRows || !kv4_many_possible(a.n_requests, a.cache.held)) return kv4_few_launch(a, dtype, max_new, st);
+  a.least_rows = kFewRows + 1;
+  int rc = kv4_many_launch(a, dtype, st);
+  if (rc != ADADIM_OK) return rc;
+  a.least_rows = 1;
+  a.most_rows = kFewRows;
   return kv4_few_launch(a, dtype, max_new, st);
 }
 
