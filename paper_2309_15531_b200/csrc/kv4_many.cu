@@ -6,10 +6,12 @@
 // one tile's softmax runs while the other one's products do:
 //   warps 0-3, 4-7   a tile each: a thread has a row, reads its 128 scores from TMEM twice (largest, then weights) and puts the
 //                    weights back as fp16 where the scores were, from where the second product takes them
-//   warps 8-15       turn 128 tokens' codes into fp16 tiles in shared memory (128-byte swizzle; keys and values alike: a token
+//   warps 8-11       turn 128 tokens' codes into fp16 tiles in shared memory (128-byte swizzle; keys and values alike: a token
 //                    is a row, which is K-major for keys and MN-major for values), two stages of each; the next
 //                    tokens' codes are loaded into registers meanwhile, so that 4-bit bytes are all that is read of the cache
-//   warp 16          issues the products
+//   warp 12          issues the products
+// Loops that the warps are in all the time are kept short (32 scores a turn): a warp that runs through a thousand instructions
+// waits for them more than it executes.
 // The largest score is taken anew only where a row passes it by more than 2^8; then the accumulator in TMEM is rescaled.
 // The line of work is cut into one part a CTA as for few rows.
 #include "kv4_line.cuh"
@@ -20,8 +22,8 @@ namespace {
 using namespace kv4;
 using fp4::exp2_int;
 
-constexpr int kTile = 128, kRows = 2 * kTile, kChunk = 128, kThreads = 17 * 32;
-constexpr int kUnpackWarps = 8;
+constexpr int kTile = 128, kRows = 2 * kTile, kChunk = 128;
+constexpr int kUnpackWarp = 8, kUnpackWarps = 4, kIssueWarp = 12, kThreads = 16 * 32;   // three warps only fill up
 constexpr int kCost = 512;                       // what a unit costs beside its tokens, in tokens
 constexpr int kLeastPart = 1024;                 // a CTA's part is no smaller
 constexpr int kRing = 8;                         // chunks whose notes about tokens are kept
@@ -82,13 +84,19 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 struct __align__(16) Shared {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2], drain;
   uint32_t tmem;
   int dead;
   uint32_t hidden[kRing][kTile / 32];            // tokens whose page lies outside the cache, a bit each
   uint32_t nan_any[kRing][kUnpackWarps];         // whether a warp's tokens have values that are NaN; which:
-  uint8_t nan_of[kRing][2][kTile];               // of a token's half of the channels, a bit for each block
+  uint8_t nan_of[kRing][kTile];                  // a bit for each of a token's blocks
 };
 
 // chunks of a tile of the piece: [c0, this)
@@ -110,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
   int* const status = p.status_dev;
   const int tid = threadIdx.x, lane = tid & 31, warp = ptx::uniform_warp();
   const Cache& cache = p.cache;
-  if (warp == 16) {
+  if (warp == kIssueWarp) {
     if (lane == 0) {
       sh.dead = 0;
       for (int k = 0; k < 2; ++k) {
@@ -195,7 +203,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
                                      query_bits<T>(raw[4 * k + 2], f1, f2) ^ sign, query_bits<T>(raw[4 * k + 3], f1, f2) ^ sign);
           *reinterpret_cast<uint4*>(q_smem + (k >> 3) * Mm::kBox + (((k & 7) ^ (row_in & 7)) << 4)) = v;
         }
-        factor = query_fine<T>(most) ? ldexpf(fabsf(p.scale) * kLog2e, t_k - e) : __int_as_float(0x7fffffff);
+        // (not zero, so that what is hidden stays at minus infinity)
+        factor = query_fine<T>(most) && p.scale == p.scale ? fmaxf(ldexpf(fabsf(p.scale) * kLog2e, t_k - e), 1.2e-38f) : __int_as_float(0x7fffffff);
       }
       ptx::fence_proxy_async();
       __syncwarp();
@@ -207,12 +216,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       // what was noted about the values of chunk ch: a row has the NaN of the tokens that it sees
       auto note_nans = [&](int ch) {
         const int slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
+        const uint4 any = *reinterpret_cast<const uint4*>(sh.nan_any[slot]);
+        if ((any.x | any.y | any.z | any.w) == 0) return;
         const int tok = x.key_lo + ch * kChunk;
-#pragma unroll
         for (int k = 0; k < kUnpackWarps; ++k) {
           if (sh.nan_any[slot][k] == 0) continue;
-          for (int t = (k & 3) * 32; t < (k & 3) * 32 + 32; ++t)
-            if (tok + t < lim && tok + t >= low) nans |= static_cast<uint32_t>(sh.nan_of[slot][k >> 2][t]) << (k >> 2) * (HELD / 32);
+          for (int t = k * 32; t < k * 32 + 32; ++t)
+            if (tok + t < lim && tok + t >= low) nans |= sh.nan_of[slot][t];
         }
       };
       for (int ch = x.c0; ch < c1; ++ch) {
@@ -221,43 +231,38 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         const int tok = x.key_lo + ch * kChunk, slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
         const uint4 hid = *reinterpret_cast<const uint4*>(sh.hidden[slot]);
         const bool edge = tok < all_lo || tok + kChunk > all_hi || (hid.x | hid.y | hid.z | hid.w) != 0;
-        const uint32_t hidden[4] = {hid.x, hid.y, hid.z, hid.w};
         if (ch > x.c0) note_nans(ch - 1);
-        // 32 tokens' bits: which this row sees
-        auto visible = [&](int q) -> uint32_t {
+        // 32 tokens' bits: which this row sees.  What it does not see is taken away before it is looked at.
+        auto hide = [&](uint32_t (&v)[32], int q) {
           const int a = low - (tok + 32 * q), z = lim - (tok + 32 * q);          // from a on, up to z
           const uint32_t up = z >= 32 ? 0xffffffffu : z <= 0 ? 0u : (1u << z) - 1u;
           const uint32_t from = a <= 0 ? 0xffffffffu : a >= 32 ? 0u : ~((1u << a) - 1u);
-          return up & from & ~hidden[q];
+          const uint32_t see = up & from & ~sh.hidden[slot][q];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) if ((see >> k & 1u) == 0) v[k] = 0xff800000u;
         };
         uint32_t va[32], vb[32];
         float top = -INFINITY;
-        auto largest = [&](const uint32_t (&v)[32], int q) {
-          float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+        for (int q = 0; q < 4; q += 2) {
+          ld32(s_at + 32 * q, va);
+          ld32(s_at + 32 * q + 32, vb);
+          ld32_wait(va);
+          ld32_wait(vb);
           if (edge) {
-            const uint32_t see = visible(q);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) if (see >> k & 1u) t[k & 3] = fmaxf(t[k & 3], __uint_as_float(v[k]));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) t[k & 3] = fmaxf(t[k & 3], __uint_as_float(v[k]));
+            hide(va, q);
+            hide(vb, q + 1);
           }
-          top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-        };
-        ld32(s_at, va);
-        ld32_wait(va);
-        ld32(s_at + 32, vb);
-        largest(va, 0);
-        ld32_wait(vb);
-        ld32(s_at + 64, va);
-        largest(vb, 1);
-        ld32_wait(va);
-        ld32(s_at + 96, vb);
-        largest(va, 2);
-        ld32_wait(vb);
-        ld32(s_at, va);
-        largest(vb, 3);
-        ld32_wait(va);
+          float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            t0 = max3(t0, __uint_as_float(va[k]), __uint_as_float(va[k + 1]));
+            t1 = max3(t1, __uint_as_float(va[k + 2]), __uint_as_float(va[k + 3]));
+            t2 = max3(t2, __uint_as_float(vb[k]), __uint_as_float(vb[k + 1]));
+            t3 = max3(t3, __uint_as_float(vb[k + 2]), __uint_as_float(vb[k + 3]));
+          }
+          top = max3(top, max3(t0, t1, t2), t3);
+        }
         const float high = top == -INFINITY ? -INFINITY : top * factor;
         if (__any_sync(0xffffffffu, high > m + 8.0f)) {
           const float now = fmaxf(m, high), f = exp2_fast((m == -INFINITY ? now : m) - (now == -INFINITY ? 0.0f : now));
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           if (ch > x.c0) {
             if (!ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status)) break;
             ptx::tc_fence_after_sync();
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < HELD / 32; ++k) {
               ld32(o_at + 32 * k, vb);
               ld32_wait(vb);
@@ -281,35 +286,31 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           }
         }
         const float base = m == -INFINITY ? 0.0f : m;
-        float sum[2] = {0.0f, 0.0f};
-        auto weights = [&](const uint32_t (&v)[32], int q) {
+        uint64_t sum[2] = {0, 0};                                    // pairs of binary32 zeros
+        const uint64_t mul = fp4::pack2(factor, factor), sub = fp4::pack2(-base, -base);
+        ld32(s_at, va);
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          ld32_wait(va);
+          if (edge) hide(va, q);
           uint32_t w[16];
-          uint32_t see = 0xffffffffu;
-          if (edge) see = visible(q);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            float a = exp2_fast(fmaf(__uint_as_float(v[2 * k]), factor, -base)), b = exp2_fast(fmaf(__uint_as_float(v[2 * k + 1]), factor, -base));
-            if (edge) {
-              if ((see >> (2 * k) & 1u) == 0) a = 0.0f;
-              if ((see >> (2 * k + 1) & 1u) == 0) b = 0.0f;
-            }
-            sum[0] += a;
-            sum[1] += b;
+            float a, b;
+            fp4::unpack2(fp4::fma2(fp4::pack2(__uint_as_float(va[2 * k]), __uint_as_float(va[2 * k + 1])), mul, sub), a, b);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+            sum[k & 1] = fp4::add2(sum[k & 1], fp4::pack2(a, b));
             w[k] = half2_bits(__floats2half2_rn(a, b));
           }
+          if (q < 3) ld32(s_at + 32 * q + 32, va);
           st16(s_at + 16 * q, w);
-        };
-        ld32(s_at + 32, vb);
-        weights(va, 0);
-        ld32_wait(vb);
-        ld32(s_at + 64, va);
-        weights(vb, 1);
-        ld32_wait(va);
-        ld32(s_at + 96, vb);
-        weights(va, 2);
-        ld32_wait(vb);
-        weights(vb, 3);
-        l += sum[0] + sum[1];
+        }
+        {
+          float a, b;
+          fp4::unpack2(fp4::add2(sum[0], sum[1]), a, b);
+          l += a + b;
+        }
         st_wait();
         ptx::tc_fence_before_sync();
         __syncwarp();
@@ -371,99 +372,108 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       }
       ptx::tc_fence_before_sync();                                   // the next piece's products write over what was read here
     }
-  } else if (warp < 16) {
+  } else if (warp < kUnpackWarp + kUnpackWarps) {
     // ---- codes to fp16 tiles: a thread has half of a token's channels
-    constexpr int kWords = HELD / 16;                                // words of codes of a thread
-    const int u = tid - 256, t = u & 127, half = u >> 7, sub = u >> 5;
-    char* const row_at = smem + (HELD == 128 ? half * Mm::kBox : 0) + t * 128;
-    const int chunk0 = HELD == 128 ? 0 : 4 * half;                   // 16-byte chunk of the row that the half begins with
+    constexpr int kWords = HELD / 8;                                 // words of codes of a thread's token
+    const int t = tid - kUnpackWarp * 32, sub = warp - kUnpackWarp;
+    char* const row_at = smem + t * 128;
+    const int64_t gap = static_cast<int64_t>(cache.kv_heads) << cache.page_log2;   // rows from a page's keys to its values
     int64_t seen = 0;
     bool paged = true;
     while (at < end && !*dead) {
       const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
       request = x.request;
-      const int key_hi = key_end(p, x, x.tile * kRows + x.rows - 1);
-      struct Raw { uint32_t k[kWords], v[kWords], ks, vs; };
-      auto page_of = [&](int ch) -> int {
-        const int64_t tok = x.key_lo + static_cast<int64_t>(ch) * kChunk + t;
-        if (ch >= x.c1 || tok >= key_hi) return -2;
-        const int page = p.table[x.request * p.ldt + (tok >> cache.page_log2)];
+      const int key_hi = key_end(p, x, x.tile * kRows + x.rows - 1), steps = x.c1 - x.c0;
+      const int tok0 = x.key_lo + x.c0 * kChunk + t;                 // this thread's token of the first chunk
+      const int32_t* const table = p.table + x.request * p.ldt;
+      // its page: -1 outside the cache, -2 none
+      auto page_of = [&](int it) -> int {
+        const int64_t tok = tok0 + static_cast<int64_t>(it) * kChunk;
+        if (it >= steps || tok >= key_hi) return -2;
+        const int page = table[tok >> cache.page_log2];
         return page < 0 || page >= cache.n_pages ? -1 : page;
       };
-      auto load = [&](int ch, int page, Raw& raw) {
-#pragma unroll
-        for (int k = 0; k < kWords; ++k) raw.k[k] = raw.v[k] = 0;
-        raw.ks = raw.vs = 0;
-        if (page < 0) return;
-        const int place = (x.key_lo + ch * kChunk + t) & ((1 << cache.page_log2) - 1);
-        const int64_t kr = cache_row(cache, page, 0, x.head, place), vr = kr + (static_cast<int64_t>(cache.kv_heads) << cache.page_log2);
-        const uint8_t *kc = cache.codes + kr * (HELD / 2) + half * (HELD / 4), *vc = cache.codes + vr * (HELD / 2) + half * (HELD / 4);
+      uint32_t kc[kWords], vc[kWords], ks[kWords / 8], vs[kWords / 8];
+      auto load = [&](int64_t row, uint32_t (&codes)[kWords], uint32_t (&scales)[kWords / 8]) {
+        const uint4* c = reinterpret_cast<const uint4*>(cache.codes + row * (HELD / 2));
 #pragma unroll
         for (int k = 0; k < kWords / 4; ++k) {
-          const uint4 a = __ldg(reinterpret_cast<const uint4*>(kc) + k), b = __ldg(reinterpret_cast<const uint4*>(vc) + k);
-          raw.k[4 * k] = a.x; raw.k[4 * k + 1] = a.y; raw.k[4 * k + 2] = a.z; raw.k[4 * k + 3] = a.w;
-          raw.v[4 * k] = b.x; raw.v[4 * k + 1] = b.y; raw.v[4 * k + 2] = b.z; raw.v[4 * k + 3] = b.w;
+          const uint4 a = __ldg(c + k);
+          codes[4 * k] = a.x; codes[4 * k + 1] = a.y; codes[4 * k + 2] = a.z; codes[4 * k + 3] = a.w;
         }
-        const uint8_t *ks = cache.scales + kr * (HELD / 16) + half * (HELD / 32), *vs = cache.scales + vr * (HELD / 16) + half * (HELD / 32);
-        if constexpr (HELD == 128) {
-          raw.ks = __ldg(reinterpret_cast<const uint32_t*>(ks));
-          raw.vs = __ldg(reinterpret_cast<const uint32_t*>(vs));
-        } else {
-          raw.ks = __ldg(reinterpret_cast<const uint16_t*>(ks));
-          raw.vs = __ldg(reinterpret_cast<const uint16_t*>(vs));
-        }
-      };
-      auto put = [&](const uint32_t (&codes)[kWords], uint32_t scales, char* to) {
-        const __half2 s01 = scales_of(scales), s23 = scales_of(scales >> 16);
+        const uint32_t* f = reinterpret_cast<const uint32_t*>(cache.scales + row * (HELD / 16));
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) {
-          const __half2 two = k < 4 ? s01 : s23, s = (k & 2) ? __high2half2(two) : __low2half2(two);
-          __half2 v[4];
-          values8(codes[k], v);
-          const uint4 w = make_uint4(half2_bits(__hmul2(v[0], s)), half2_bits(__hmul2(v[1], s)), half2_bits(__hmul2(v[2], s)), half2_bits(__hmul2(v[3], s)));
-          *reinterpret_cast<uint4*>(to + (((chunk0 + k) ^ (t & 7)) << 4)) = w;
+        for (int k = 0; k < kWords / 8; ++k) scales[k] = __ldg(f + k);
+      };
+      auto row_of = [&](int page, int it) { return cache_row(cache, page, 0, x.head, (tok0 + it * kChunk) & ((1 << cache.page_log2) - 1)); };
+      auto put = [&](const uint32_t (&codes)[kWords], const uint32_t (&scales)[kWords / 8], char* to) {
+#pragma unroll
+        for (int k = 0; k < kWords; k += 4) {
+          const __half2 two = scales_of(scales[k >> 3] >> (k & 4) * 4);          // two blocks, four words
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const __half2 s = e < 2 ? __low2half2(two) : __high2half2(two);
+            __half2 v[4];
+            values8(codes[k + e], v);
+            const uint4 w = make_uint4(half2_bits(__hmul2(v[0], s)), half2_bits(__hmul2(v[1], s)), half2_bits(__hmul2(v[2], s)), half2_bits(__hmul2(v[3], s)));
+            *reinterpret_cast<uint4*>(to + ((k + e) >> 3) * Mm::kBox + ((((k + e) & 7) ^ (t & 7)) << 4)) = w;
+          }
         }
       };
-      Raw cur, next;
-      int page = page_of(x.c0), after = page_of(x.c0 + 1);
-      if (x.c0 < x.c1) load(x.c0, page, cur);
-      for (int ch = x.c0; ch < x.c1; ++ch, ++seen) {
+#pragma unroll
+      for (int k = 0; k < kWords; ++k) kc[k] = vc[k] = 0;
+#pragma unroll
+      for (int k = 0; k < kWords / 8; ++k) ks[k] = vs[k] = 0;
+      int page = page_of(0), after = page_of(1);
+      if (page >= 0) {
+        const int64_t row = row_of(page, 0);
+        load(row, kc, ks);
+        load(row + gap, vc, vs);
+      }
+#pragma unroll 1
+      for (int it = 0; it < steps; ++it, ++seen) {
         const int stage = static_cast<int>(seen & 1), slot = static_cast<int>(seen & (kRing - 1));
         const uint32_t empty = (static_cast<uint32_t>(seen >> 1) & 1u) ^ 1u;
         const int now = page;
         page = after;
-        if (ch + 1 < x.c1) {
-          load(ch + 1, page, next);
-          after = page_of(ch + 2);
-        }
+        after = page_of(it + 2);
         const uint32_t out = __ballot_sync(0xffffffffu, now == -1);
         paged &= now != -1;
-        // blocks of values that are NaN: noted, and zero in the product
-        uint32_t bad = (((cur.vs & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-        const bool any = __any_sync(0xffffffffu, bad != 0);
-        if (any) {
-          cur.vs &= ~(bad * 0xffu);
-          sh.nan_of[slot][half][t] = static_cast<uint8_t>((bad & 1u) | (bad >> 7 & 2u) | (bad >> 14 & 4u) | (bad >> 21 & 8u));
+        if (now < 0) {                                               // a token that is not there: zeros
+#pragma unroll
+          for (int k = 0; k < kWords / 8; ++k) ks[k] = vs[k] = 0;
         }
+        // blocks of values that are NaN: noted, and zero in the product
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < kWords / 8; ++k) {
+          const uint32_t bad = (((vs[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+          vs[k] &= ~(bad * 0xffu);
+          bits |= ((bad & 1u) | (bad >> 7 & 2u) | (bad >> 14 & 4u) | (bad >> 21 & 8u)) << 4 * k;
+        }
+        const bool any = __any_sync(0xffffffffu, bits != 0);
+        if (any) sh.nan_of[slot][t] = static_cast<uint8_t>(bits);
         if (lane == 0) {
           sh.nan_any[slot][sub] = any;
-          if (half == 0) sh.hidden[slot][sub] = out;
+          sh.hidden[slot][sub] = out;
         }
+        const int64_t row = page >= 0 ? row_of(page, it + 1) : 0;
         if (!ptx::mbar_wait_warp(&sh.k_empty[stage], empty, dead, status)) break;
-        put(cur.k, cur.ks, row_at + Mm::kK + stage * Mm::kBytes);
+        put(kc, ks, row_at + Mm::kK + stage * Mm::kBytes);
+        if (page >= 0) load(row, kc, ks);
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&sh.k_full[stage]);
         if (!ptx::mbar_wait_warp(&sh.v_empty[stage], empty, dead, status)) break;
-        put(cur.v, cur.vs, row_at + Mm::kV + stage * Mm::kBytes);
+        put(vc, vs, row_at + Mm::kV + stage * Mm::kBytes);
+        if (page >= 0) load(row + gap, vc, vs);
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&sh.v_full[stage]);
-        cur = next;
       }
     }
     if (__any_sync(0xffffffffu, !paged) && lane == 0) report(status, ADADIM_ERR_PAGES);
-  } else {
+  } else if (warp == kIssueWarp) {
     // ---- products
     constexpr uint32_t kScores = idesc_f16(128, kChunk, false), kValues = idesc_f16(128, HELD, true);
     constexpr uint64_t kmajor = ptx::smem_desc_sw128(16, 1024), mnmajor = ptx::smem_desc_sw128(Mm::kBox, 1024);
@@ -556,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (warp == 16) {
+  if (warp == kIssueWarp) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem, 512);
   }
