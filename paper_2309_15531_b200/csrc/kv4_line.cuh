@@ -9,7 +9,7 @@ namespace kv4 {
 
 constexpr int kSms = 148;
 constexpr int kFewRows = 16;                     // a request with more rows a key head than this is the many-row kernel's
-constexpr int kManyRequests = 4000;              // of a call, for the many-row kernel
+constexpr int kManyRequests = 3500;              // of a call, for the many-row kernel
 constexpr float kLog2e = 1.4426950408889634f;
 
 __host__ __device__ constexpr size_t whole256(size_t bytes) { return (bytes + 255) / 256 * 256; }

@@ -4,8 +4,9 @@
 // accumulators in TMEM), and as much by the exponentials between the two products: 128 x 128 pairs are 1024 cycles of either
 // unit.  A CTA has 256 query rows in two tiles of 128 (a group of heads of one key head, tokens outer), so that
 // one tile's softmax runs while the other one's products do:
-//   warps 0-3, 4-7   a tile each: a thread has a row, reads its 128 scores from TMEM twice (largest, then weights) and puts the
-//                    weights back as fp16 where the scores were, from where the second product takes them
+//   warps 0-3, 4-7   a tile each: a thread has a row, takes its scores from TMEM and puts the weights back as fp16 where the scores
+//                    were, from where the second product takes them; 64 tokens at a time, so that the products for one half of
+//                    128 tokens run while the weights of the other are formed
 //   warps 8-11       turn 128 tokens' codes into fp16 tiles in shared memory (128-byte swizzle; keys and values alike: a token
 //                    is a row, which is K-major for keys and MN-major for values), two stages of each; the next
 //                    tokens' codes are loaded into registers meanwhile, so that 4-bit bytes are all that is read of the cache
@@ -22,7 +23,7 @@ namespace {
 using namespace kv4;
 using fp4::exp2_int;
 
-constexpr int kTile = 128, kRows = 2 * kTile, kChunk = 128;
+constexpr int kTile = 128, kRows = 2 * kTile, kChunk = 128, kHalf = kChunk / 2;
 constexpr int kUnpackWarp = 8, kUnpackWarps = 4, kIssueWarp = 12, kThreads = 16 * 32;   // three warps only fill up
 constexpr int kCost = 512;                       // what a unit costs beside its tokens, in tokens
 constexpr int kLeastPart = 1024;                 // a CTA's part is no smaller
@@ -63,17 +64,6 @@ __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t (&r)[32]) {
       : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void ld32_wait(uint32_t (&r)[32]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : ADADIM_R32(r) : : "memory"); }
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -81,6 +71,19 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t (&r)[16]) {
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ld16_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) : : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -90,8 +93,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// The same value in all lanes of a converged warp, which the compiler then knows: what the products' instructions are given stays
+// in uniform registers (60 cycles an instruction where it had to be brought there from every lane's).
+__device__ __forceinline__ int same(int v) { return __reduce_max_sync(0xffffffffu, v); }
+
 struct __align__(16) Shared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2], p_ready[2], o_done[2], drain;
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2], drain;   // [tile][half of the tokens]
   uint32_t tmem;
   int dead;
   uint32_t hidden[kRing][kTile / 32];            // tokens whose page lies outside the cache, a bit each
@@ -127,8 +134,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         ptx::mbar_init(&sh.k_empty[k], 1);
         ptx::mbar_init(&sh.v_empty[k], 1);
         ptx::mbar_init(&sh.q_ready[k], 4);
-        ptx::mbar_init(&sh.s_full[k], 1);
-        ptx::mbar_init(&sh.p_ready[k], 4);
+        for (int h = 0; h < 2; ++h) {
+          ptx::mbar_init(&sh.s_full[k][h], 1);
+          ptx::mbar_init(&sh.p_ready[k][h], 4);
+        }
         ptx::mbar_init(&sh.o_done[k], 1);
       }
       ptx::mbar_init(&sh.drain, 1);
@@ -157,7 +166,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     char* const q_smem = smem + Mm::kQ + i * Mm::kBytes + row_in * 128;
     const int t_k = cache_scale_log2(cache, 0), t_v = cache_scale_log2(cache, 1);
     int64_t seen = 0;                                                // chunks of all pieces so far, of both tiles
-    uint32_t done = 0;                                               // .. of this tile
+    uint32_t done = 0;                                               // halves of this tile's
+    uint32_t turn = 0;                                               // .. and chunks
     while (at < end && !*dead) {
       const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
       request = x.request;
@@ -225,102 +235,105 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             if (tok + t < lim && tok + t >= low) nans |= sh.nan_of[slot][t];
         }
       };
-      for (int ch = x.c0; ch < c1; ++ch) {
-        if (!ptx::mbar_wait_warp(&sh.s_full[i], done & 1u, dead, status)) break;
-        ptx::tc_fence_after_sync();
-        const int tok = x.key_lo + ch * kChunk, slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
-        const uint4 hid = *reinterpret_cast<const uint4*>(sh.hidden[slot]);
-        const bool edge = tok < all_lo || tok + kChunk > all_hi || (hid.x | hid.y | hid.z | hid.w) != 0;
-        if (ch > x.c0) note_nans(ch - 1);
-        // 32 tokens' bits: which this row sees.  What it does not see is taken away before it is looked at.
-        auto hide = [&](uint32_t (&v)[32], int q) {
-          const int a = low - (tok + 32 * q), z = lim - (tok + 32 * q);          // from a on, up to z
-          const uint32_t up = z >= 32 ? 0xffffffffu : z <= 0 ? 0u : (1u << z) - 1u;
-          const uint32_t from = a <= 0 ? 0xffffffffu : a >= 32 ? 0u : ~((1u << a) - 1u);
-          const uint32_t see = up & from & ~sh.hidden[slot][q];
-#pragma unroll
-          for (int k = 0; k < 32; ++k) if ((see >> k & 1u) == 0) v[k] = 0xff800000u;
-        };
-        uint32_t va[32], vb[32];
-        float top = -INFINITY;
+      bool ok = true;
+      for (int ch = x.c0; ok && ch < c1; ++ch, ++turn) {
+        const int slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
 #pragma unroll 1
-        for (int q = 0; q < 4; q += 2) {
-          ld32(s_at + 32 * q, va);
-          ld32(s_at + 32 * q + 32, vb);
+        for (int h = 0; h < 2; ++h) {
+          ok = ptx::mbar_wait_warp(&sh.s_full[i][h], turn & 1u, dead, status);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint32_t at_half = s_at + h * kHalf;
+          uint32_t va[32], vb[32];
+          ld32(at_half, va);
+          ld32(at_half + 32, vb);
+          const int tok = x.key_lo + ch * kChunk + h * kHalf;
+          const uint2 hid = *reinterpret_cast<const uint2*>(&sh.hidden[slot][2 * h]);
+          const bool edge = tok < all_lo || tok + kHalf > all_hi || (hid.x | hid.y) != 0;
+          if (h == 0 && ch > x.c0) note_nans(ch - 1);
           ld32_wait(va);
           ld32_wait(vb);
           if (edge) {
-            hide(va, q);
-            hide(vb, q + 1);
-          }
-          float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+            // 32 tokens' bits: which this row sees.  What it does not see is taken away before it is looked at.
+            auto hide = [&](uint32_t (&v)[32], int first, uint32_t hidden) {
+              const int a = low - first, z = lim - first;            // from a on, up to z
+              const uint32_t up = z >= 32 ? 0xffffffffu : z <= 0 ? 0u : (1u << z) - 1u;
+              const uint32_t from = a <= 0 ? 0xffffffffu : a >= 32 ? 0u : ~((1u << a) - 1u);
+              const uint32_t see = up & from & ~hidden;
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            t0 = max3(t0, __uint_as_float(va[k]), __uint_as_float(va[k + 1]));
-            t1 = max3(t1, __uint_as_float(va[k + 2]), __uint_as_float(va[k + 3]));
-            t2 = max3(t2, __uint_as_float(vb[k]), __uint_as_float(vb[k + 1]));
-            t3 = max3(t3, __uint_as_float(vb[k + 2]), __uint_as_float(vb[k + 3]));
+              for (int k = 0; k < 32; ++k) if ((see >> k & 1u) == 0) v[k] = 0xff800000u;
+            };
+            hide(va, tok, hid.x);
+            hide(vb, tok + 32, hid.y);
           }
-          top = max3(top, max3(t0, t1, t2), t3);
-        }
-        const float high = top == -INFINITY ? -INFINITY : top * factor;
-        if (__any_sync(0xffffffffu, high > m + 8.0f)) {
-          const float now = fmaxf(m, high), f = exp2_fast((m == -INFINITY ? now : m) - (now == -INFINITY ? 0.0f : now));
-          if (now > m) {
-            l = m == -INFINITY ? l : l * f;
-          }
-          const float g = now > m && m != -INFINITY ? f : 1.0f;
-          m = now;
-          if (ch > x.c0) {
-            if (!ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status)) break;
-            ptx::tc_fence_after_sync();
-#pragma unroll 1
-            for (int k = 0; k < HELD / 32; ++k) {
-              ld32(o_at + 32 * k, vb);
-              ld32_wait(vb);
+          float top;
+          {
+            float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
 #pragma unroll
-              for (int e = 0; e < 32; ++e) vb[e] = __float_as_uint(__uint_as_float(vb[e]) * g);
-              st32(o_at + 32 * k, vb);
+            for (int k = 0; k < 32; k += 4) {
+              t0 = max3(t0, __uint_as_float(va[k]), __uint_as_float(va[k + 1]));
+              t1 = max3(t1, __uint_as_float(va[k + 2]), __uint_as_float(va[k + 3]));
+              t2 = max3(t2, __uint_as_float(vb[k]), __uint_as_float(vb[k + 1]));
+              t3 = max3(t3, __uint_as_float(vb[k + 2]), __uint_as_float(vb[k + 3]));
             }
-            st_wait();
+            top = fmaxf(max3(t0, t1, t2), t3);
           }
-        }
-        const float base = m == -INFINITY ? 0.0f : m;
-        uint64_t sum[2] = {0, 0};                                    // pairs of binary32 zeros
-        const uint64_t mul = fp4::pack2(factor, factor), sub = fp4::pack2(-base, -base);
-        ld32(s_at, va);
+          const float high = top == -INFINITY ? -INFINITY : top * factor;
+          if (__any_sync(0xffffffffu, high > m + 8.0f)) {
+            const float now = high > m ? high : m, g = m == -INFINITY || now == m ? 1.0f : exp2_fast(m - now);
+            m = now;
+            l *= g;
+            if (ch > x.c0 || h > 0) {
+              // once the last product of values is done (the one before it is: these scores were issued behind it)
+              ok = ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status);
+              if (!ok) break;
+              ptx::tc_fence_after_sync();
 #pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          ld32_wait(va);
-          if (edge) hide(va, q);
-          uint32_t w[16];
+              for (int k = 0; k < HELD / 16; ++k) {
+                uint32_t o[16];
+                ld16(o_at + 16 * k, o);
+                ld16_wait(o);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float a, b;
-            fp4::unpack2(fp4::fma2(fp4::pack2(__uint_as_float(va[2 * k]), __uint_as_float(va[2 * k + 1])), mul, sub), a, b);
-            a = exp2_fast(a);
-            b = exp2_fast(b);
-            sum[k & 1] = fp4::add2(sum[k & 1], fp4::pack2(a, b));
-            w[k] = half2_bits(__floats2half2_rn(a, b));
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+                st16(o_at + 16 * k, o);
+              }
+              st_wait();
+            }
           }
-          if (q < 3) ld32(s_at + 32 * q + 32, va);
-          st16(s_at + 16 * q, w);
-        }
-        {
+          const float base = m == -INFINITY ? 0.0f : m;
+          uint64_t sum[2] = {0, 0};                                  // pairs of binary32 zeros
+          const uint64_t mul = fp4::pack2(factor, factor), sub = fp4::pack2(-base, -base);
+          auto weigh = [&](const uint32_t (&v)[32], uint32_t to) {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              float a, b;
+              fp4::unpack2(fp4::fma2(fp4::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), mul, sub), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              sum[k & 1] = fp4::add2(sum[k & 1], fp4::pack2(a, b));
+              w[k] = half2_bits(__floats2half2_rn(a, b));
+            }
+            st16(to, w);
+          };
+          weigh(va, at_half);
+          weigh(vb, at_half + 16);
+          st_wait();
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&sh.p_ready[i][h]);
+          ++done;
           float a, b;
           fp4::unpack2(fp4::add2(sum[0], sum[1]), a, b);
           l += a + b;
         }
-        st_wait();
-        ptx::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sh.p_ready[i]);
-        ++done;
       }
+      if (!ok) break;
       // the row's result
       const bool some = c1 > x.c0;
       if (some) {
-        if (!ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status)) break;
+        // the products of both halves, one after the other (a barrier tells a phase from the next one, not from the one after it)
+        if (!ptx::mbar_wait_warp(&sh.o_done[i], done & 1u, dead, status) || !ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status)) break;
         ptx::tc_fence_after_sync();
         note_nans(c1 - 1);
       }
@@ -475,84 +488,87 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     if (__any_sync(0xffffffffu, !paged) && lane == 0) report(status, ADADIM_ERR_PAGES);
   } else if (warp == kIssueWarp) {
     // ---- products
-    constexpr uint32_t kScores = idesc_f16(128, kChunk, false), kValues = idesc_f16(128, HELD, true);
+    constexpr uint32_t kScores = idesc_f16(128, kHalf, false), kValues = idesc_f16(128, HELD, true);
     constexpr uint64_t kmajor = ptx::smem_desc_sw128(16, 1024), mnmajor = ptx::smem_desc_sw128(Mm::kBox, 1024);
-    const uint32_t base = ptx::smem_addr(smem);
-    int64_t seen = 0;
-    uint32_t pieces[2] = {0, 0}, done[2] = {0, 0};
+    const uint32_t base = ptx::smem_addr(smem), tm = static_cast<uint32_t>(same(static_cast<int>(tmem)));
+    uint32_t seen = 0;                                               // chunks of all pieces so far
+    uint32_t pieces[2] = {0, 0}, turn[2] = {0, 0};                   // pieces and chunks of each tile
     int4 desc = make_int4(0, 0, 0, 0);
     bool ok = true;
     while (ok && at < end && !*dead) {
       const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
       request = x.request;
       if (!(x.starts && x.ends)) note_piece(desc, x);
-      const int c1[2] = {chunks_of_tile(p, x, 0), chunks_of_tile(p, x, 1)};
-      const int64_t first_seen = seen;
-      seen += x.c1 - x.c0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (x.rows <= i * kTile) continue;
+      const int steps = same(x.c1 - x.c0), tiles = same(x.rows > kTile ? 2 : 1);
+      const int n[2] = {same(chunks_of_tile(p, x, 0) - x.c0), same(chunks_of_tile(p, x, 1) - x.c0)};    // chunks of each tile
+      for (int i = 0; i < tiles; ++i) {
         ok = ok && ptx::mbar_wait_warp(&sh.q_ready[i], pieces[i] & 1u, dead, status);
         ++pieces[i];
       }
-      auto scores = [&](int i, int stage) {
+      auto scores = [&](int i, int h, uint32_t stage) {
+        const uint32_t d = tm + i * 128 + h * kHalf;
+        const uint64_t a = ptx::with_start(kmajor, base + Mm::kQ + i * Mm::kBytes);
+        const uint64_t b = ptx::with_start(kmajor, base + Mm::kK + stage * Mm::kBytes + h * (kHalf * 128));
         if (ptx::elect_one()) {
 #pragma unroll
-          for (int k = 0; k < HELD / 16; ++k)
-            ptx::mma_f16(tmem + i * 128, ptx::with_start(kmajor, base + Mm::kQ + i * Mm::kBytes + (k >> 2) * Mm::kBox + (k & 3) * 32),
-                         ptx::with_start(kmajor, base + Mm::kK + stage * Mm::kBytes + (k >> 2) * Mm::kBox + (k & 3) * 32), kScores, k != 0);
-          ptx::mma_commit(&sh.s_full[i]);
+          for (int k = 0; k < HELD / 16; ++k) {
+            const uint64_t step = ((k >> 2) * Mm::kBox + (k & 3) * 32) >> 4;
+            ptx::mma_f16(d, a + step, b + step, kScores, k != 0);
+          }
+          ptx::mma_commit(&sh.s_full[i][h]);
         }
         __syncwarp();
       };
-      auto wait_keys = [&](int ch) {
-        const int64_t n = first_seen + ch - x.c0;
-        const bool got = ptx::mbar_wait_warp(&sh.k_full[n & 1], static_cast<uint32_t>(n >> 1) & 1u, dead, status);
+      auto wait_keys = [&](uint32_t at_chunk) {
+        const bool got = ptx::mbar_wait_warp(&sh.k_full[at_chunk & 1u], at_chunk >> 1 & 1u, dead, status);
         ptx::tc_fence_after_sync();
         return got;
       };
-      if (ok && x.c0 < x.c1) {
-        const int stage = static_cast<int>(first_seen & 1);
-        ok = wait_keys(x.c0);
+      if (ok && steps > 0) {
+        const uint32_t stage = seen & 1u;
+        ok = wait_keys(seen);
         if (ok) {
-          if (x.c0 < c1[0]) scores(0, stage);
-          if (x.c0 < c1[1]) scores(1, stage);
+          for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < 2; ++i)
+              if (n[i] > 0) scores(i, h, stage);
           if (ptx::elect_one()) ptx::mma_commit(&sh.k_empty[stage]);
           __syncwarp();
         }
       }
-      for (int ch = x.c0; ok && ch < x.c1; ++ch) {
-        const int64_t n = first_seen + ch - x.c0;
-        const int stage = static_cast<int>(n & 1), ahead = stage ^ 1;
-        ok = ptx::mbar_wait_warp(&sh.v_full[stage], static_cast<uint32_t>(n >> 1) & 1u, dead, status);
+      for (int it = 0; ok && it < steps; ++it, ++seen) {
+        const uint32_t stage = seen & 1u, ahead = stage ^ 1u;
+        ok = ptx::mbar_wait_warp(&sh.v_full[stage], seen >> 1 & 1u, dead, status);
         bool keys = false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (!ok || ch >= c1[i]) continue;
-          ok = ptx::mbar_wait_warp(&sh.p_ready[i], done[i] & 1u, dead, status);
+#pragma unroll 1
+        for (int hi = 0; hi < 4; ++hi) {                             // halves of the tokens, tiles in turn
+          const int h = hi >> 1, i = hi & 1;
+          if (!ok || it >= (i == 0 ? n[0] : n[1])) continue;
+          ok = ptx::mbar_wait_warp(&sh.p_ready[i][h], (i == 0 ? turn[0] : turn[1]) & 1u, dead, status);
           if (!ok) continue;
-          ++done[i];
+          if (i == 0) turn[0] += h; else turn[1] += h;
           ptx::tc_fence_after_sync();
-          if (ptx::elect_one()) {
+          {
+            const uint32_t d = tm + 256 + i * HELD, a = tm + i * 128 + h * kHalf;
+            const uint64_t b = ptx::with_start(mnmajor, base + Mm::kV + stage * Mm::kBytes + h * (kHalf * 128));
+            const bool onto = it != 0 || h != 0;
+            if (ptx::elect_one()) {
 #pragma unroll
-            for (int k = 0; k < kChunk / 16; ++k)
-              mma_f16_ts(tmem + 256 + i * HELD, tmem + i * 128 + k * 8, ptx::with_start(mnmajor, base + Mm::kV + stage * Mm::kBytes + k * (16 * 128)), kValues,
-                         ch != x.c0 || k != 0);
-            ptx::mma_commit(&sh.o_done[i]);
+              for (int k = 0; k < kHalf / 16; ++k) mma_f16_ts(d, a + k * 8, b + ((k * 16 * 128) >> 4), kValues, onto || k != 0);
+              ptx::mma_commit(&sh.o_done[i]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
-          if (ch + 1 < c1[i]) {
-            if (!keys) { ok = wait_keys(ch + 1); keys = true; }
-            if (ok) scores(i, ahead);
+          if (it + 1 < (i == 0 ? n[0] : n[1])) {
+            if (!keys) { ok = wait_keys(seen + 1); keys = true; }
+            if (ok) scores(i, h, ahead);
           }
         }
+        if (ok && it + 1 < steps && !keys) ok = wait_keys(seen + 1); // a chunk that no tile takes any more
         if (ok && ptx::elect_one()) {
           ptx::mma_commit(&sh.v_empty[stage]);
-          if (ch + 1 < x.c1) ptx::mma_commit(&sh.k_empty[ahead]);
+          if (it + 1 < steps) ptx::mma_commit(&sh.k_empty[ahead]);
         }
         __syncwarp();
-        // a chunk that no tile takes any more has its keys handed back all the same
-        if (ok && ch + 1 < x.c1 && !keys) ok = wait_keys(ch + 1);
       }
     }
     if (*dead) {
