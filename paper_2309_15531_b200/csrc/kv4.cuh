@@ -81,6 +81,21 @@ struct Kv4Attention {
   char* workspace;
 };
 
+template <typename... P, typename... A>
+int chained_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, bool chained, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = chained ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
+}
+
 // implemented in kv4_cache.cu, kv4_attention.cu, kv4_few.cu, kv4_many.cu
 int page_tables_launch(const int32_t* past, const int32_t* fresh, int n_requests, int page, int32_t* table, int64_t ldt,
                        int64_t width, const int32_t* free_pages, int n_free, const int32_t* cursor, int rows, int32_t* lengths,
@@ -90,10 +105,10 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
                       int64_t n_tokens, const int32_t* slots, const Kv4Rotary& rotary, const kv4::Cache& cache,
                       const Kv4Heads& k_values, const Kv4Heads& v_values, int vdtype, cudaStream_t st);
 int kv4_attention_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
-int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
-int kv4_join_launch(const Kv4Attention& a, int dtype, int ctas, int tile_rows, bool split, cudaStream_t st);
+// ctas, tile_rows: what the joining kernel has to know.  chained: behind the kernel for many rows
+int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st);
 size_t kv4_few_workspace(int held);
-int kv4_many_launch(const Kv4Attention& a, int dtype, cudaStream_t st);
+int kv4_many_launch(const Kv4Attention& a, int dtype, int& ctas, int& tile_rows, cudaStream_t st);
 size_t kv4_many_workspace(int held);
 size_t kv4_workspace(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim);
 

@@ -8,33 +8,43 @@ using namespace kv4;
 
 // ---- joining what was cut ---------------------------------------------------------------------------
 // The unit that began in part b and went on: its parts are those of b, b + 1, .. up to the one it ends in.  A warp has a row and goes
-// through them in that order; with SPLIT, where few units are cut into many parts, the eight warps of a CTA have one row and take
-// every eighth part.  Either way the order of the sums is fixed.
+// through them in that order; with SPLIT, where few units are cut into many parts, the eight warps of a CTA have one row of the few-row
+// kernel's and take every eighth part.  Either way the order of the sums is fixed.  One launch joins both kernels' units: the first
+// few_blocks CTAs those of the kernel for few rows.
 constexpr int kJoinThreads = 256, kJoinWarps = 8;
 
+struct Joined {
+  char* workspace;
+  int ctas, tile_rows;
+};
+
 template <int HELD, bool SPLIT, typename T>
-__global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, int ctas, int tile_rows) {
-  constexpr int kEach = HELD / 32, kStride = SPLIT ? kJoinWarps : 1;
+__global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, Joined few, Joined many, int few_blocks) {
+  constexpr int kEach = HELD / 32;
   __shared__ float acc[SPLIT ? kJoinWarps : 1][HELD];
   __shared__ float2 stats[kJoinWarps];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool of_few = static_cast<int>(blockIdx.x) < few_blocks, split = SPLIT && of_few;
+  const Joined& from = of_few ? few : many;
+  const int at_block = of_few ? blockIdx.x : blockIdx.x - few_blocks, ys = split ? from.tile_rows : from.tile_rows / kJoinWarps;
+  const int b = at_block / ys, y = at_block - b * ys;
   ptx::pdl_wait();
-  const Partials part = partials_of(p.workspace, ctas, tile_rows);
+  const Partials part = partials_of(from.workspace, from.ctas, from.tile_rows);
   const int4 desc = part.desc[b];
   if ((desc.w & kBegins) == 0) return;
   int last = b + 1;                                                  // the part it ends in
-  for (int k = b + 1; k < ctas; k += 32) {
-    const uint32_t found = __ballot_sync(0xffffffffu, k + lane < ctas && (part.desc[k + lane].w & kEnds) != 0);
+  for (int k = b + 1; k < from.ctas; k += 32) {
+    const uint32_t found = __ballot_sync(0xffffffffu, k + lane < from.ctas && (part.desc[k + lane].w & kEnds) != 0);
     if (found != 0) { last = k + __ffs(static_cast<int>(found)) - 1; break; }
   }
   bool ok;
   const Request r = request_of(p.offsets, p.lengths, desc.x, p.n_rows, p.width << p.cache.page_log2, ok);
-  const int row = SPLIT ? blockIdx.y : blockIdx.y * kJoinWarps + warp, rr = desc.z * tile_rows + row;
-  if (rr >= r.rows * p.group) return;                                // with SPLIT all of the CTA
+  const int row = split ? y : y * kJoinWarps + warp, rr = desc.z * from.tile_rows + row;
+  if (rr >= r.rows * p.group) return;                                // split: all of the CTA
   float m = -INFINITY, l = 0.0f, v[kEach] = {};
 #pragma unroll 4
-  for (int k = b + (SPLIT ? warp : 0); k <= last; k += kStride) {
-    const int64_t at = (static_cast<int64_t>(k) * 2 + (k == b ? 1 : 0)) * tile_rows + row;
+  for (int k = b + (split ? warp : 0); k <= last; k += split ? kJoinWarps : 1) {
+    const int64_t at = (static_cast<int64_t>(k) * 2 + (k == b ? 1 : 0)) * from.tile_rows + row;
     const float2 s = part.stats[at];
     float o[kEach];
 #pragma unroll
@@ -49,23 +59,25 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
   const int tok = token_of(p, rr), head = desc.y * p.group + rr - tok * p.group;
   T* out = static_cast<T*>(p.o.p) + (r.first + tok) * p.o.ld + head * p.o.lh;
   const int t_v = cache_scale_log2(p.cache, 1);
-  if constexpr (SPLIT) {
+  if (split) {
+    if constexpr (SPLIT) {
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[warp][e * 32 + lane] = v[e];
-    if (lane == 0) stats[warp] = make_float2(m, l);
-    __syncthreads();
-    float top = stats[0].x;
+      for (int e = 0; e < kEach; ++e) acc[warp][e * 32 + lane] = v[e];
+      if (lane == 0) stats[warp] = make_float2(m, l);
+      __syncthreads();
+      float top = stats[0].x;
 #pragma unroll
-    for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, stats[w].x);
-    for (int d = tid; d < p.cache.dim; d += kJoinThreads) {
-      float sum = 0.0f, x = 0.0f;
+      for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, stats[w].x);
+      for (int d = tid; d < p.cache.dim; d += kJoinThreads) {
+        float sum = 0.0f, x = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = stats[w].x == -INFINITY ? 1.0f : exp2_fast(stats[w].x - top);
-        sum += stats[w].y * f;
-        x += acc[w][d] * f;
+        for (int w = 0; w < kJoinWarps; ++w) {
+          const float f = stats[w].x == -INFINITY ? 1.0f : exp2_fast(stats[w].x - top);
+          sum += stats[w].y * f;
+          x += acc[w][d] * f;
+        }
+        out[d] = static_cast<T>(sum == 0.0f ? x : ldexpf(x / sum, t_v));
       }
-      out[d] = static_cast<T>(sum == 0.0f ? x : ldexpf(x / sum, t_v));
     }
   } else {
 #pragma unroll
@@ -77,43 +89,30 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
 }
 
 template <int HELD, bool SPLIT, typename T>
-int join(const Kv4Attention& a, int ctas, int tile_rows, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(SPLIT ? tile_rows : tile_rows / kJoinWarps));
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  ADADIM_CUDA_TRY(cudaLaunchKernelEx(&cfg, kv4_join_kernel<HELD, SPLIT, T>, a, ctas, tile_rows));
-  return ADADIM_OK;
+int join(const Kv4Attention& a, const Joined& few, const Joined& many, cudaStream_t st) {
+  const int few_blocks = few.ctas * (SPLIT ? few.tile_rows : few.tile_rows / kJoinWarps), many_blocks = many.ctas * (many.tile_rows / kJoinWarps);
+  return chained_launch(kv4_join_kernel<HELD, SPLIT, T>, dim3(static_cast<unsigned>(few_blocks + many_blocks)), kJoinThreads, 0, true, st, a, few, many,
+                        few_blocks);
 }
 template <bool SPLIT, typename T>
-int join_held(const Kv4Attention& a, int ctas, int tile_rows, cudaStream_t st) {
-  if (a.cache.held == 64) return join<64, SPLIT, T>(a, ctas, tile_rows, st);
-  return a.cache.held == 128 ? join<128, SPLIT, T>(a, ctas, tile_rows, st) : join<256, SPLIT, T>(a, ctas, tile_rows, st);
-}
-
-}  // namespace
-
-int kv4_join_launch(const Kv4Attention& a, int dtype, int ctas, int tile_rows, bool split, cudaStream_t st) {
-  if (dtype == ADADIM_F16) return split ? join_held<true, __half>(a, ctas, tile_rows, st) : join_held<false, __half>(a, ctas, tile_rows, st);
-  return split ? join_held<true, __nv_bfloat16>(a, ctas, tile_rows, st) : join_held<false, __nv_bfloat16>(a, ctas, tile_rows, st);
+int join_held(const Kv4Attention& a, const Joined& few, const Joined& many, cudaStream_t st) {
+  if (a.cache.held == 64) return join<64, SPLIT, T>(a, few, many, st);
+  return a.cache.held == 128 ? join<128, SPLIT, T>(a, few, many, st) : join<256, SPLIT, T>(a, few, many, st);
 }
 
 // The kernel for many rows holds its line of work beside 192 KB of tiles, and TMEM has no room for heads of 256 channels.
-bool kv4_many_possible(int64_t n_requests, int held) { return n_requests <= kManyRequests && held <= 128; }
+bool many_possible(int64_t n_requests, int held) { return n_requests <= kManyRequests && held <= 128; }
+
+}  // namespace
 
 size_t kv4_workspace(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim) {
   const int held = held_dim(head_dim);
-  const size_t few = kv4_few_workspace(held);
-  if (!kv4_many_possible(n_requests, held) || n_rows * (q_heads / kv_heads) <= kFewRows) return few;
-  const size_t many = kv4_many_workspace(held);
-  return few > many ? few : many;
+  const bool many = many_possible(n_requests, held) && n_rows * (q_heads / kv_heads) > kFewRows;
+  return kv4_few_workspace(held) + (many ? kv4_many_workspace(held) : 0);
 }
 
+// The kernels follow one another by programmatic launches: each may begin when the one before it has begun everywhere, and ends
+// no earlier than that one, so that what comes behind the last one comes behind them all.
 int kv4_attention_launch(const Kv4Attention& given, int dtype, int64_t max_new, cudaStream_t st) {
   Kv4Attention a = given;
   a.group_rcp = a.group == 1 ? 0 : static_cast<uint32_t>((uint64_t{1} << 32) / a.group + 1);
@@ -122,13 +121,22 @@ int kv4_attention_launch(const Kv4Attention& given, int dtype, int64_t max_new, 
   a.wide16_o = reinterpret_cast<uintptr_t>(a.o.p) % 16 == 0 && a.o.ld % 8 == 0 && a.o.lh % 8 == 0;
   a.least_rows = 1;
   a.most_rows = int64_t{1} << 40;
-  if (max_new * a.group <= kFewRows || !kv4_many_possible(a.n_requests, a.cache.held)) return kv4_few_launch(a, dtype, max_new, st);
-  a.least_rows = kFewRows + 1;
-  int rc = kv4_many_launch(a, dtype, st);
+  Joined few = {a.workspace, 0, 0}, many = {a.workspace + kv4_few_workspace(a.cache.held), 0, kJoinWarps};
+  int rc;
+  if (max_new * a.group > kFewRows && many_possible(a.n_requests, a.cache.held)) {
+    a.least_rows = kFewRows + 1;
+    a.workspace = many.workspace;
+    rc = kv4_many_launch(a, dtype, many.ctas, many.tile_rows, st);
+    if (rc != ADADIM_OK) return rc;
+    a.least_rows = 1;
+    a.most_rows = kFewRows;
+    a.workspace = few.workspace;
+  }
+  rc = kv4_few_launch(a, dtype, max_new, many.ctas > 0, few.ctas, few.tile_rows, st);
   if (rc != ADADIM_OK) return rc;
-  a.least_rows = 1;
-  a.most_rows = kFewRows;
-  return kv4_few_launch(a, dtype, max_new, st);
+  const bool split = static_cast<int64_t>(a.n_requests) * a.cache.kv_heads < 64;
+  if (dtype == ADADIM_F16) return split ? join_held<true, __half>(a, few, many, st) : join_held<false, __half>(a, few, many, st);
+  return split ? join_held<true, __nv_bfloat16>(a, few, many, st) : join_held<false, __nv_bfloat16>(a, few, many, st);
 }
 
 }  // namespace adadim

@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
     for (int k = 0; k < kFewWarps * kStages; ++k) ptx::mbar_init(&bars[0][0] + k, 1);
     ptx::fence_mbar_init();
   }
+  ptx::pdl_launch_dependents();
   sum_line(p, kRows, kFewCost, line, sums);
   const int64_t total = line[p.n_requests];
   const int64_t parts = max(int64_t{1}, min(static_cast<int64_t>(gridDim.x), quick_div(total, kLeastPart)));
@@ -477,29 +478,29 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
   }
   if (tid == 0) part.desc[blockIdx.x] = desc;
   if (__any_sync(0xffffffffu, !paged) && lane == 0) report(p.status_dev, ADADIM_ERR_PAGES);
+  ptx::pdl_wait();                                                   // no earlier than the kernel before it
 }
 
 template <int HELD, int NT, typename T>
-int few_launch(const Kv4Attention& a, cudaStream_t st) {
-  constexpr int kCtas = few_ctas(HELD, NT);
+int few_launch(const Kv4Attention& a, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
+  ctas = few_ctas(HELD, NT);
+  tile_rows = 8 * NT;
   static std::atomic<uint64_t> done{0};
   const int rc = set_once(kv4_few_kernel<HELD, NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(few_ring(HELD, NT) + sizeof(int64_t) * (kMaxRequests + 1)), done);
   if (rc != ADADIM_OK) return rc;
   const size_t smem = few_ring(HELD, NT) + sizeof(int64_t) * (static_cast<size_t>(a.n_requests) + 1);
-  kv4_few_kernel<HELD, NT, T><<<kCtas, kFewThreads, smem, st>>>(a);
-  ADADIM_CUDA_TRY(cudaGetLastError());
-  return kv4_join_launch(a, std::is_same<T, __half>::value ? ADADIM_F16 : ADADIM_BF16, kCtas, 8 * NT, a.n_requests * a.cache.kv_heads < 64, st);
+  return chained_launch(kv4_few_kernel<HELD, NT, T>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, chained, st, a);
 }
 template <int HELD, typename T>
-int few_held(const Kv4Attention& a, int64_t max_new, cudaStream_t st) {
-  if (HELD < 256 && max_new * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, st);
-  return few_launch<HELD, 1, T>(a, st);
+int few_held(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
+  if (HELD < 256 && max_new * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, chained, ctas, tile_rows, st);
+  return few_launch<HELD, 1, T>(a, chained, ctas, tile_rows, st);
 }
 template <typename T>
-int few_type(const Kv4Attention& a, int64_t max_new, cudaStream_t st) {
-  if (a.cache.held == 64) return few_held<64, T>(a, max_new, st);
-  return a.cache.held == 128 ? few_held<128, T>(a, max_new, st) : few_held<256, T>(a, max_new, st);
+int few_type(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
+  if (a.cache.held == 64) return few_held<64, T>(a, max_new, chained, ctas, tile_rows, st);
+  return a.cache.held == 128 ? few_held<128, T>(a, max_new, chained, ctas, tile_rows, st) : few_held<256, T>(a, max_new, chained, ctas, tile_rows, st);
 }
 
 }  // namespace
@@ -509,8 +510,8 @@ size_t kv4_few_workspace(int held) {
   return one > two ? one : two;
 }
 
-int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st) {
-  return dtype == ADADIM_F16 ? few_type<__half>(a, max_new, st) : few_type<__nv_bfloat16>(a, max_new, st);
+int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
+  return dtype == ADADIM_F16 ? few_type<__half>(a, max_new, chained, ctas, tile_rows, st) : few_type<__nv_bfloat16>(a, max_new, chained, ctas, tile_rows, st);
 }
 
 }  // namespace adadim

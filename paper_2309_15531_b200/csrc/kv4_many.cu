@@ -98,7 +98,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ int same(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
 struct __align__(16) Shared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2], drain;   // [tile][half of the tokens]
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2][2], drain;   // [tile][half of the tokens]
   uint32_t tmem;
   int dead;
   uint32_t hidden[kRing][kTile / 32];            // tokens whose page lies outside the cache, a bit each
@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         for (int h = 0; h < 2; ++h) {
           ptx::mbar_init(&sh.s_full[k][h], 1);
           ptx::mbar_init(&sh.p_ready[k][h], 4);
+          ptx::mbar_init(&sh.o_done[k][h], 1);
         }
-        ptx::mbar_init(&sh.o_done[k], 1);
       }
       ptx::mbar_init(&sh.drain, 1);
       ptx::fence_mbar_init();
@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     ptx::tmem_relinquish();
   }
   ptx::tc_fence_before_sync();
+  ptx::pdl_launch_dependents();
   sum_line(p, kRows, kCost, line, sums);                             // ends with a barrier
   ptx::tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
@@ -166,8 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     char* const q_smem = smem + Mm::kQ + i * Mm::kBytes + row_in * 128;
     const int t_k = cache_scale_log2(cache, 0), t_v = cache_scale_log2(cache, 1);
     int64_t seen = 0;                                                // chunks of all pieces so far, of both tiles
-    uint32_t done = 0;                                               // halves of this tile's
-    uint32_t turn = 0;                                               // .. and chunks
+    uint32_t turn = 0;                                               // .. of this tile
     while (at < end && !*dead) {
       const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
       request = x.request;
@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             m = now;
             l *= g;
             if (ch > x.c0 || h > 0) {
-              // once the last product of values is done (the one before it is: these scores were issued behind it)
-              ok = ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status);
+              // once the last product of values is done, that of the other half
+              ok = ptx::mbar_wait_warp(&sh.o_done[i][h ^ 1], (turn + h + 1) & 1u, dead, status);
               if (!ok) break;
               ptx::tc_fence_after_sync();
 #pragma unroll 1
@@ -322,7 +322,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&sh.p_ready[i][h]);
-          ++done;
           float a, b;
           fp4::unpack2(fp4::add2(sum[0], sum[1]), a, b);
           l += a + b;
@@ -332,8 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       // the row's result
       const bool some = c1 > x.c0;
       if (some) {
-        // the products of both halves, one after the other (a barrier tells a phase from the next one, not from the one after it)
-        if (!ptx::mbar_wait_warp(&sh.o_done[i], done & 1u, dead, status) || !ptx::mbar_wait_warp(&sh.o_done[i], (done - 1) & 1u, dead, status)) break;
+        if (!ptx::mbar_wait_warp(&sh.o_done[i][1], (turn - 1) & 1u, dead, status)) break;
         ptx::tc_fence_after_sync();
         note_nans(c1 - 1);
       }
@@ -554,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             if (ptx::elect_one()) {
 #pragma unroll
               for (int k = 0; k < kHalf / 16; ++k) mma_f16_ts(d, a + k * 8, b + ((k * 16 * 128) >> 4), kValues, onto || k != 0);
-              ptx::mma_commit(&sh.o_done[i]);
+              ptx::mma_commit(&sh.o_done[i][h]);
             }
             __syncwarp();
           }
@@ -595,16 +593,16 @@ int many_launch(const Kv4Attention& a, cudaStream_t st) {
   const int rc = set_once(kv4_many_kernel<HELD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(Many<HELD>::kSmem + sizeof(int64_t) * (kManyRequests + 1)), done);
   if (rc != ADADIM_OK) return rc;
-  kv4_many_kernel<HELD, T><<<kSms, kThreads, smem, st>>>(a);
-  ADADIM_CUDA_TRY(cudaGetLastError());
-  return kv4_join_launch(a, std::is_same<T, __half>::value ? ADADIM_F16 : ADADIM_BF16, kSms, kRows, false, st);
+  return chained_launch(kv4_many_kernel<HELD, T>, dim3(kSms), kThreads, smem, false, st, a);
 }
 
 }  // namespace
 
 size_t kv4_many_workspace(int held) { return partials_bytes(kSms, kRows, held); }
 
-int kv4_many_launch(const Kv4Attention& a, int dtype, cudaStream_t st) {
+int kv4_many_launch(const Kv4Attention& a, int dtype, int& ctas, int& tile_rows, cudaStream_t st) {
+  ctas = kSms;
+  tile_rows = kRows;
   if (a.cache.held == 64) return dtype == ADADIM_F16 ? many_launch<64, __half>(a, st) : many_launch<64, __nv_bfloat16>(a, st);
   return dtype == ADADIM_F16 ? many_launch<128, __half>(a, st) : many_launch<128, __nv_bfloat16>(a, st);
 }

@@ -277,3 +277,14 @@ def test_nothing_to_do_and_refusals_of_the_binding():
         run(q=b.q.double())
     with pytest.raises(B.AdadimError):
         run(q=b.q.float(), out=b.q.float())
+
+
+@pytest.mark.parametrize("lengths,new", [([300, 170, 40], [40, 130, 9]), ([700], [700])])
+def test_many_calls_in_a_row_end_well(lengths, new):
+    """No wait inside the kernels runs out, whatever the warps' timing: 600 calls, the status read at the end."""
+    b = Batch(lengths, new, 8, 2, 128, seed=11)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    first, out = b.run(), torch.empty_like(b.q)
+    for _ in range(600):
+        b.run(out=out, status=status)
+    assert int(status.item()) == 0 and torch.equal(out, first)
