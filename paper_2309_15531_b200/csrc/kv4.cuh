@@ -77,23 +77,34 @@ struct Kv4Attention {
   int causal;
   int window;              // 0: none
   int64_t least_rows, most_rows;   // a kernel takes the requests with so many rows a key head
+  int cluster, tiles;      // few rows without the line: CTAs of a unit; tiles of a key head that the grid has
   int* status_dev;
   char* workspace;
 };
 
+// chained: may begin while the kernel before it runs.  cluster: CTAs of a cluster
 template <typename... P, typename... A>
-int chained_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, bool chained, cudaStream_t st, const A&... args) {
+int chained_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, bool chained, cudaStream_t st, const Kv4Attention& a, int cluster, const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (chained) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = chained ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
+  cfg.numAttrs = static_cast<unsigned>(n);
+  return cudaLaunchKernelEx(&cfg, kernel, a, args...) == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
 }
 
 // implemented in kv4_cache.cu, kv4_attention.cu, kv4_few.cu, kv4_many.cu

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
 template <int HELD, bool SPLIT, typename T>
 int join(const Kv4Attention& a, const Joined& few, const Joined& many, cudaStream_t st) {
   const int few_blocks = few.ctas * (SPLIT ? few.tile_rows : few.tile_rows / kJoinWarps), many_blocks = many.ctas * (many.tile_rows / kJoinWarps);
-  return chained_launch(kv4_join_kernel<HELD, SPLIT, T>, dim3(static_cast<unsigned>(few_blocks + many_blocks)), kJoinThreads, 0, true, st, a, few, many,
+  return chained_launch(kv4_join_kernel<HELD, SPLIT, T>, dim3(static_cast<unsigned>(few_blocks + many_blocks)), kJoinThreads, 0, true, st, a, 1, few, many,
                         few_blocks);
 }
 template <bool SPLIT, typename T>
@@ -134,6 +134,7 @@ int kv4_attention_launch(const Kv4Attention& given, int dtype, int64_t max_new, 
   }
   rc = kv4_few_launch(a, dtype, max_new, many.ctas > 0, few.ctas, few.tile_rows, st);
   if (rc != ADADIM_OK) return rc;
+  if (few.ctas + many.ctas == 0) return ADADIM_OK;
   const bool split = static_cast<int64_t>(a.n_requests) * a.cache.kv_heads < 64;
   if (dtype == ADADIM_F16) return split ? join_held<true, __half>(a, few, many, st) : join_held<false, __half>(a, few, many, st);
   return split ? join_held<true, __nv_bfloat16>(a, few, many, st) : join_held<false, __nv_bfloat16>(a, few, many, st);

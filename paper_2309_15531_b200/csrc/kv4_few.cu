@@ -14,9 +14,9 @@
 // Running maximum and sum per row, the maximum taken anew only where a score passes it by more than 2^8, which fp16 weights
 // bear (they are rounded to 11 bits and lie below 2^8).
 //
-// The work of all requests, key heads and row tiles is laid out on one line in chunks of 64 tokens and cut into equal parts,
-// one a CTA, whatever the requests' lengths; the four warps of a CTA take 16 tokens each of a chunk.  What is cut is joined by
-// a second kernel in the order of the tokens, so that results do not depend on timing.
+// The work of all requests, key heads and row tiles is laid out on one line and cut into equal parts, one a CTA, whatever the requests'
+// lengths; the four warps of a CTA take 32 tokens each of a chunk of 128.  What is cut is joined by a second kernel in the order of
+// the tokens, so that results do not depend on timing.  Small calls go to clusters instead (see kv4_few_kernel).
 #include "kv4_line.cuh"
 
 namespace adadim {
@@ -63,6 +63,12 @@ __device__ __forceinline__ uint32_t lds_scales(const char* p) {
   else if constexpr (BYTES == 2) return *reinterpret_cast<const uint16_t*>(p);
   else return *reinterpret_cast<const uint8_t*>(p);
 }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // 32 tokens in shared memory as they lie in the cache: keys' codes, values' codes, keys' scales, values' scales.
 template <int HELD> struct Stage {
   static constexpr int kCodes = kStep * HELD / 2, kScales = kStep * HELD / 16, kV = kCodes, kKs = 2 * kCodes, kVs = 2 * kCodes + kScales;
@@ -95,7 +101,9 @@ __device__ __forceinline__ void load_queries(const T* q, bool there, bool wide, 
   }
 }
 
-template <int HELD, int NT, typename T>
+// LINE: the CTAs have equal parts of the line of work.  Otherwise a cluster of p.cluster CTAs has a unit: its CTAs take every p.cluster-th chunk
+// and join their results through distributed shared memory, so that a small call is one launch without a look at all requests.
+template <int HELD, int NT, typename T, bool LINE>
 __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_kernel(Kv4Attention p) {
   constexpr int kRows = 8 * NT, kSteps = HELD / 16, kK = HELD / 8, kV = HELD / 16;   // kK, kV: bytes of a key, a value in a lane
   constexpr int kPitch = HELD + 4;
@@ -103,7 +111,9 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
   static_assert(St::kBytes == kStep * (HELD + HELD / 8), "as few_ring has it");
   extern __shared__ __align__(128) char smem[];
   float* so = reinterpret_cast<float*>(smem);                                        // [warp][row][pitch], over the ring
-  int64_t* line = reinterpret_cast<int64_t*>(smem + few_ring(HELD, NT));             // work in front of each request
+  int64_t* line = reinterpret_cast<int64_t*>(smem + few_ring(HELD, NT));             // LINE: work in front of each request
+  float* mine = reinterpret_cast<float*>(smem + few_ring(HELD, NT));                 // otherwise: the CTA's results [row][HELD]
+  __shared__ float2 mine_stats[LINE ? 1 : kRows];                                    // .. and their maxima and sums
   __shared__ float sm_m[kFewWarps][kRows], sm_l[kFewWarps][kRows];
   __shared__ int64_t sums[kFewWarps];
   __shared__ uint64_t bars[kFewWarps][kStages];
@@ -117,13 +127,29 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
     for (int k = 0; k < kFewWarps * kStages; ++k) ptx::mbar_init(&bars[0][0] + k, 1);
     ptx::fence_mbar_init();
   }
-  ptx::pdl_launch_dependents();
-  sum_line(p, kRows, kFewCost, line, sums);
-  const int64_t total = line[p.n_requests];
-  const int64_t parts = max(int64_t{1}, min(static_cast<int64_t>(gridDim.x), quick_div(total, kLeastPart)));
-  int64_t at = blockIdx.x < parts ? quick_div(total * blockIdx.x, parts) : total;
-  const int64_t end = blockIdx.x < parts ? quick_div(total * (blockIdx.x + 1), parts) : total;
+  int64_t at = 0, end = 0;
   int4 desc = make_int4(0, 0, 0, 0);
+  const int size = LINE ? 1 : p.cluster, rank = LINE ? 0 : static_cast<int>(blockIdx.x) % size, stride = kChunk * size;
+  int request = 0, unit_head = 0, unit_tile = 0, unit_tiles = 0;
+  Request unit_request = {0, 0, 0};
+  if constexpr (LINE) {
+    sum_line(p, kRows, kFewCost, line, sums);
+    const int64_t total = line[p.n_requests];
+    const int64_t parts = max(int64_t{1}, min(static_cast<int64_t>(gridDim.x), quick_div(total, kLeastPart)));
+    at = blockIdx.x < parts ? quick_div(total * blockIdx.x, parts) : total;
+    end = blockIdx.x < parts ? quick_div(total * (blockIdx.x + 1), parts) : total;
+  } else {
+    const int u = static_cast<int>(blockIdx.x) / size, of_request = cache.kv_heads * p.tiles;
+    request = u / of_request;
+    unit_head = (u - request * of_request) / p.tiles;
+    unit_tile = u - request * of_request - unit_head * p.tiles;
+    bool good;
+    unit_request = request_of(p.offsets, p.lengths, request, p.n_rows, p.width << cache.page_log2, good);
+    if (!good && tid == 0) report(p.status_dev, ADADIM_ERR_SHAPE);
+    const int64_t rows = static_cast<int64_t>(unit_request.rows) * p.group;
+    unit_tiles = rows < p.least_rows || rows > p.most_rows ? 0 : static_cast<int>((rows + kRows - 1) / kRows);
+    __syncthreads();                                                 // the barriers are set up
+  }
 
   const int t_k = kv4::cache_scale_log2(cache, 0), t_v = kv4::cache_scale_log2(cache, 1);
   char* const ring = smem + warp * (kStages * St::kBytes);
@@ -131,10 +157,10 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
   int stage = 0;
   uint32_t parity = 0;
   bool paged = true;
-  int request = 0;
-  while (at < end) {
-    const Piece x = next_piece(p, line, at, end, request, kRows, kFewCost, kChunk);
-    request = x.request;
+  while (LINE ? at < end : unit_tile < unit_tiles) {                 // p.tiles holds for the longest request, unless the caller was wrong
+    const Piece x = LINE ? next_piece(p, line, at, end, request, kRows, kFewCost, kChunk)
+                         : whole_unit(p, unit_request, request, unit_head, unit_tile, kRows, kChunk);
+    if constexpr (LINE) request = x.request; else unit_tile += p.tiles;
     const Request& r = x.r;
     const int head = x.head, tile = x.tile, rows = x.rows, own = r.length - r.rows, row0 = tile * kRows;
     const int t0 = token_of(p, row0), t1 = token_of(p, row0 + rows - 1), key_hi = key_end(p, x, row0 + rows - 1);
@@ -152,20 +178,20 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
     }
 
     // the warp's steps: 32 tokens of every chunk, in a ring
-    const int first = x.key_lo + x.c0 * kChunk + warp * kStep;
-    const int steps = first < key_hi ? min(x.c1 - x.c0, (key_hi - first + kChunk - 1) / kChunk) : 0;
+    const int first = x.key_lo + (x.c0 + rank) * kChunk + warp * kStep;
+    const int steps = first >= key_hi || *dead ? 0 : min(x.c1 - x.c0, (key_hi - first + stride - 1) / stride);
     int pages = -1;                                                  // of the sixteens of tokens of the next 16 steps, one a lane
     uint32_t usable = 0;                                             // two bits a stage: whether its sixteens lie in the cache
     auto fetch = [&](int it, int to) {
       if ((it & 15) == 0) {
-        const int64_t tok = first + static_cast<int64_t>(it + (lane >> 1)) * kChunk + (lane & 1) * 16;
+        const int64_t tok = first + static_cast<int64_t>(it + (lane >> 1)) * stride + (lane & 1) * 16;
         pages = tok < key_hi ? p.table[request * p.ldt + (tok >> cache.page_log2)] : -2;
         if (pages != -2 && (pages < 0 || pages >= cache.n_pages)) { pages = -2; paged = false; }
       }
       const int pg0 = __shfl_sync(0xffffffffu, pages, (it & 15) * 2), pg1 = __shfl_sync(0xffffffffu, pages, (it & 15) * 2 + 1);
       usable = (usable & ~(3u << 2 * to)) | (pg0 >= 0 ? 1u : 0u) << 2 * to | (pg1 >= 0 ? 2u : 0u) << 2 * to;
       if (ptx::elect_one()) {
-        const int place = (first + it * kChunk) & ((1 << cache.page_log2) - 1);
+        const int place = (first + it * stride) & ((1 << cache.page_log2) - 1);
         char* const at_stage = ring + to * St::kBytes;
         const int64_t gap = static_cast<int64_t>(cache.kv_heads) << cache.page_log2;   // rows from a page's keys to its values
         if (cache.page_log2 >= 5) {
@@ -248,7 +274,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
       const char* const from = ring + stage * St::kBytes;
       if (!ptx::mbar_wait(&bar[stage], parity, dead, p.status_dev)) break;
       const uint32_t use = usable >> 2 * stage & 3u;
-      const int tok = first + it * kChunk;
+      const int tok = first + it * stride;
       // scores of tokens tok + place and rows 2 c, 2 c + 1 of every eight
       float sc[2][NT][4] = {};
 #pragma unroll
@@ -425,7 +451,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
         }
     }
     __syncthreads();
-    if (*dead) break;
+    if (LINE && *dead) break;                                        // (a cluster goes through its barriers all the same)
 
     // the warps' parts together
 #pragma unroll
@@ -439,7 +465,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
         for (int j = 0; j < kSteps; ++j) *reinterpret_cast<float2*>(to + 2 * j) = make_float2(o[u][j][k], o[u][j][k + 2]);
       }
     __syncthreads();
-    const bool whole = x.starts && x.ends;
+    const bool whole = LINE ? x.starts && x.ends : size == 1;
     const int slot = x.starts ? 1 : 0;
     for (int e = tid; e < rows * HELD; e += kFewThreads) {
       const int row = e / HELD, d = e - row * HELD;
@@ -460,42 +486,100 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
           T* out = static_cast<T*>(p.o.p) + (r.first + tok) * p.o.ld + h * p.o.lh;
           out[d] = static_cast<T>(sum == 0.0f ? v : ldexpf(v / sum, t_v));
         }
-      } else {
+      } else if constexpr (LINE) {
         const int64_t at_row = (static_cast<int64_t>(blockIdx.x) * 2 + slot) * kRows + row;
         part.o[at_row * HELD + d] = v;
         if (d == 0) part.stats[at_row] = make_float2(top, sum);
+      } else {
+        mine[e] = v;
+        if (d == 0) mine_stats[row] = make_float2(top, sum);
       }
     }
-    if (!whole) note_piece(desc, x);
+    if (LINE && !whole) note_piece(desc, x);
+    if (!LINE && size > 1) {
+      ptx::cluster_sync();
+      const uint32_t mine_at = ptx::smem_addr(mine), stats_at = ptx::smem_addr(mine_stats);
+      for (int e = rank * kFewThreads + tid; e < rows * HELD; e += size * kFewThreads) {
+        const int row = e / HELD, d = e - row * HELD;
+        if (d >= cache.dim) continue;
+        float v[8], sm[8], sl[8], top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < size) {
+            v[k] = ld_cluster_f32(ptx::map_to_cta(mine_at + e * 4, k));
+            const uint32_t st = ptx::map_to_cta(stats_at + row * 8, k);
+            sm[k] = ld_cluster_f32(st);
+            sl[k] = ld_cluster_f32(st + 4);
+          }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (k < size) top = fmaxf(top, sm[k]);
+        float sum = 0.0f, o1 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < size) {
+            const float f = sm[k] == -INFINITY ? 1.0f : exp2_fast(sm[k] - top);
+            sum += sl[k] * f;
+            o1 += v[k] * f;
+          }
+        const int rr = row0 + row, tok = token_of(p, rr), h = head * p.group + rr - tok * p.group;
+        T* out = static_cast<T*>(p.o.p) + (r.first + tok) * p.o.ld + h * p.o.lh;
+        out[d] = static_cast<T>(sum == 0.0f ? o1 : ldexpf(o1 / sum, t_v));
+      }
+      ptx::cluster_sync();                                           // the others have read what is here
+    }
     ptx::fence_proxy_async();                                        // the ring is written by bulk copies again
     __syncthreads();
   }
+  ptx::pdl_launch_dependents();
   if (*dead) {                                                       // a wait ran out: no copy may be in flight when the CTA ends
     const long long t = clock64();
     for (int k = 0; k < kStages; ++k)
       while (!ptx::mbar_try_wait(&bar[k], parity ^ (k < stage ? 1u : 0u)) && clock64() - t < ptx::kWaitLimit / 4) {}
     desc = make_int4(0, 0, 0, 0);
   }
-  if (tid == 0) part.desc[blockIdx.x] = desc;
+  if (LINE && tid == 0) part.desc[blockIdx.x] = desc;
   if (__any_sync(0xffffffffu, !paged) && lane == 0) report(p.status_dev, ADADIM_ERR_PAGES);
   ptx::pdl_wait();                                                   // no earlier than the kernel before it
 }
 
-template <int HELD, int NT, typename T>
-int few_launch(const Kv4Attention& a, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
-  ctas = few_ctas(HELD, NT);
-  tile_rows = 8 * NT;
+// Whether a call's units go to clusters, and of how many CTAs: where there is little to read altogether (by what the table and the
+// window allow: 2^20 tokens of key heads are 25 us), so that unequal lengths cost less than the second launch that joins cut units,
+// and enough units, or short ones, that clusters of up to eight CTAs find the SMs enough to do.
+int cluster_of(const Kv4Attention& a, int tile_rows, int ctas, int64_t max_new, int& tiles) {
+  const int64_t rows = max_new * a.group, t = (rows + tile_rows - 1) / tile_rows;
+  const int64_t units = t * a.n_requests * a.cache.kv_heads;
+  int64_t span = a.width << a.cache.page_log2;
+  if (a.causal && a.window > 0 && a.window + max_new + kStep < span) span = a.window + max_new + kStep;
+  if (units > 4 * ctas || units * span > (int64_t{1} << 20) || (units < 16 && span > 8192)) return 0;
+  tiles = static_cast<int>(t);
+  int size = 1;
+  while (size < 8 && units * size * 2 <= ctas && span > kChunk * size) size *= 2;
+  return size;
+}
+
+template <int HELD, int NT, typename T, bool LINE>
+int few_start(const Kv4Attention& a, int ctas, size_t more, bool chained, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  const int rc = set_once(kv4_few_kernel<HELD, NT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const int rc = set_once(kv4_few_kernel<HELD, NT, T, LINE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(few_ring(HELD, NT) + sizeof(int64_t) * (kMaxRequests + 1)), done);
   if (rc != ADADIM_OK) return rc;
-  const size_t smem = few_ring(HELD, NT) + sizeof(int64_t) * (static_cast<size_t>(a.n_requests) + 1);
-  return chained_launch(kv4_few_kernel<HELD, NT, T>, dim3(static_cast<unsigned>(ctas)), kFewThreads, smem, chained, st, a);
+  return chained_launch(kv4_few_kernel<HELD, NT, T, LINE>, dim3(static_cast<unsigned>(ctas)), kFewThreads, few_ring(HELD, NT) + more, chained, st, a, LINE ? 1 : a.cluster);
+}
+template <int HELD, int NT, typename T>
+int few_launch(Kv4Attention a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
+  tile_rows = 8 * NT;
+  a.cluster = chained ? 0 : cluster_of(a, tile_rows, few_ctas(HELD, NT), max_new, a.tiles);
+  if (a.cluster > 0) {
+    ctas = 0;                                                        // nothing to join
+    return few_start<HELD, NT, T, false>(a, a.tiles * a.n_requests * a.cache.kv_heads * a.cluster, sizeof(float) * tile_rows * HELD, false, st);
+  }
+  ctas = few_ctas(HELD, NT);
+  return few_start<HELD, NT, T, true>(a, ctas, sizeof(int64_t) * (static_cast<size_t>(a.n_requests) + 1), chained, st);
 }
 template <int HELD, typename T>
 int few_held(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
-  if (HELD < 256 && max_new * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, chained, ctas, tile_rows, st);
-  return few_launch<HELD, 1, T>(a, chained, ctas, tile_rows, st);
+  if (HELD < 256 && max_new * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, max_new, chained, ctas, tile_rows, st);
+  return few_launch<HELD, 1, T>(a, max_new, chained, ctas, tile_rows, st);
 }
 template <typename T>
 int few_type(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {

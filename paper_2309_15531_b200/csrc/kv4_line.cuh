@@ -175,6 +175,23 @@ __device__ __forceinline__ Piece next_piece(const Kv4Attention& p, const int64_t
   x.c1 = x.ends ? x.chunks : to;
   return x;
 }
+__device__ __forceinline__ int key_end(const Kv4Attention& p, const Piece& x, int last_row);
+// A whole unit, of a request that has the tile.
+__device__ __forceinline__ Piece whole_unit(const Kv4Attention& p, const Request& r, int request, int head, int tile, int tile_rows, int chunk) {
+  Piece x;
+  x.r = r;
+  x.request = request;
+  x.head = head;
+  x.tile = tile;
+  x.rows = static_cast<int>(min(static_cast<int64_t>(tile_rows), static_cast<int64_t>(r.rows) * p.group - static_cast<int64_t>(tile) * tile_rows));
+  x.key_lo = p.window > 0 ? max(0, r.length - r.rows + token_of(p, tile * tile_rows) - p.window + 1) & ~31 : 0;
+  const int hi = key_end(p, x, tile * tile_rows + x.rows - 1);
+  x.chunks = hi > x.key_lo ? (hi - x.key_lo + chunk - 1) / chunk : 0;
+  x.c0 = 0;
+  x.c1 = x.chunks;
+  x.starts = x.ends = true;
+  return x;
+}
 __device__ __forceinline__ int key_end(const Kv4Attention& p, const Piece& x, int last_row) {      // behind the last token that a row up to last_row of the request sees
   return p.causal ? max(0, min(x.r.length, x.r.length - x.r.rows + token_of(p, last_row) + 1)) : x.r.length;
 }

@@ -593,7 +593,7 @@ int many_launch(const Kv4Attention& a, cudaStream_t st) {
   const int rc = set_once(kv4_many_kernel<HELD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(Many<HELD>::kSmem + sizeof(int64_t) * (kManyRequests + 1)), done);
   if (rc != ADADIM_OK) return rc;
-  return chained_launch(kv4_many_kernel<HELD, T>, dim3(kSms), kThreads, smem, false, st, a);
+  return chained_launch(kv4_many_kernel<HELD, T>, dim3(kSms), kThreads, smem, false, st, a, 1);
 }
 
 }  // namespace
