@@ -497,26 +497,24 @@ typedef struct {
 } adadim_heads;
 
 /*
- * Rotates queries and keys and puts keys and values into the cache.
- *   K, V       [n_tokens][kv_heads][head_dim], dtype any.  slots int32[n_tokens]: where each token goes; tokens with a
- *              slot outside the cache are not stored.  Slots have to differ.
- *   Q, Qr      [n_tokens][q_heads][head_dim] of the same dtype, Q rotated into Qr (may be Q itself), rounded once;
- *              Q NULL: none.  Q, K, V may lie side by side in one matrix.
- *   rotary     NULL: nothing is rotated (Q must be NULL)
- *   k_values, v_values  optional: the values that the cache then stands for, [n_tokens][kv_heads][head_dim], vdtype ADADIM_BF16 or
- *              ADADIM_F32 (both hold them exactly, up to their own range)
+ * Rotates queries and keys and puts keys and values into the cache.  host: heads[6], what is not there has p NULL:
+ *   heads[0], heads[1]   K, V  [n_tokens][kv_heads][head_dim], dtype any.  slots int32[n_tokens]: where each token goes;
+ *              tokens with a slot outside the cache are not stored.  Slots have to differ.
+ *   heads[2], heads[3]   optional: Q and where it goes when rotated (may be Q itself), [n_tokens][q_heads][head_dim] of the same
+ *              dtype, rounded once.  Q, K, V may lie side by side in one matrix.
+ *   heads[4], heads[5]   optional: the values of keys and of values that the cache then stands for, [n_tokens][kv_heads][head_dim],
+ *              vdtype ADADIM_BF16 or ADADIM_F32 (both hold them exactly, up to their own range)
+ *   rotary     host; NULL: nothing is rotated (then there is no Q)
  * Keys are quantized from the rotation in binary64, every decision as in adadim_quantize_fp4; a block with an
  * infinity or NaN gets scale 0x7F: its values are NaN, and so is what attends to them.
  */
-ADADIM_API int adadim_kv4_append(const adadim_heads* Q, const adadim_heads* Qr, int q_heads, const adadim_heads* K, const adadim_heads* V,
-                        int dtype, int64_t n_tokens, const int32_t* slots, const adadim_rotary* rotary,
-                        const adadim_kv4cache* cache, const adadim_heads* k_values, const adadim_heads* v_values, int vdtype,
-                        void* cuda_stream);
+ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dtype, int64_t n_tokens, const int32_t* slots,
+                        const adadim_rotary* rotary, const adadim_kv4cache* cache, int vdtype, void* cuda_stream);
 
 /*
  * Attention of new tokens over the cache.  Request i has the query rows offsets[i] .. offsets[i+1]-1 (int32
  * [n_requests + 1], not falling, within 0 .. n_rows) and lengths[i] tokens in the cache, its new ones the last of them.
- *   Q, O       [n_rows][q_heads][head_dim], dtype ADADIM_F16 or ADADIM_BF16; query head h reads key head
+ *   qo         host: qo[0] queries, qo[1] results, [n_rows][q_heads][head_dim], dtype ADADIM_F16 or ADADIM_BF16; query head h reads key head
  *              h / (q_heads / kv_heads).  Rows of no request are not written.
  *   scale      of the products q k
  *   causal     query row j of n sees positions up to lengths - n + j; 0: all
@@ -526,14 +524,14 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* Q, const adadim_heads* Qr, 
  *   max_new    no request has more query rows than this: picks the kernels and has no part in the result.  0: not known.
  *   workspace  adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, kv_heads, head_dim), 256-byte aligned.
  * The values that the codes stand for are used as they are (exact in fp16); queries too (bf16 ones times a power of
- * two in fp16), weights are rounded to fp16, sums are binary32, and O is rounded once.  A table entry outside the
+ * two in fp16), weights are rounded to fp16, sums are binary32, and results are rounded once.  A table entry outside the
  * cache: its tokens are left out, (device) ADADIM_ERR_PAGES.  Offsets that fall or leave 0 .. n_rows, lengths outside
  * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads < 2^31.
  */
-ADADIM_API int adadim_kv4_attention(const adadim_heads* Q, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
+ADADIM_API int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
                         const int32_t* lengths, int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width,
                         const adadim_kv4cache* cache, float scale, int causal, int64_t window, int64_t max_new,
-                        const adadim_heads* O, int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
+                        int* status_dev, void* workspace, size_t workspace_bytes, void* cuda_stream);
 ADADIM_API size_t adadim_kv4_workspace_bytes(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim);
 
 /* Helpers. */

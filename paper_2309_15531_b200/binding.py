@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 from collections import namedtuple
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -43,15 +44,6 @@ class Fp4TensorC(C.Structure):
 class Kv4CacheC(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("amax", C.c_void_p), ("n_pages", C.c_int64),
                 ("page", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
-
-
-class RotaryC(C.Structure):
-    _fields_ = [("positions", C.c_void_p), ("freq", C.c_void_p), ("axis", C.c_void_p), ("ld", C.c_int64),
-                ("axes", C.c_int32), ("dim", C.c_int32), ("adjacent", C.c_int32)]
-
-
-class HeadsC(C.Structure):
-    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64), ("lh", C.c_int64)]
 
 
 class GptqLayerC(C.Structure):
@@ -117,15 +109,15 @@ def lib():
                                                 vp, vp, sz, vp]
         L.adadim_fp4_plan.restype = ci
         L.adadim_fp4_plan.argtypes = [i64, i64, i64, ci, ci, ci, ci, C.POINTER(C.c_int)]
-        cp, hp = C.POINTER(Kv4CacheC), C.POINTER(HeadsC)
+        cp = C.POINTER(Kv4CacheC)
         L.adadim_kv4_bytes.restype = sz
         L.adadim_kv4_bytes.argtypes = [i64, ci, ci, ci, ci]
         L.adadim_page_tables.restype = ci
         L.adadim_page_tables.argtypes = [vp, vp, i64, ci, vp, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
         L.adadim_kv4_append.restype = ci
-        L.adadim_kv4_append.argtypes = [hp, hp, ci, hp, hp, ci, i64, vp, C.POINTER(RotaryC), cp, hp, hp, ci, vp]
+        L.adadim_kv4_append.argtypes = [vp, ci, ci, i64, vp, vp, cp, ci, vp]
         L.adadim_kv4_attention.restype = ci
-        L.adadim_kv4_attention.argtypes = [hp, ci, i64, ci, vp, vp, i64, vp, i64, i64, cp, C.c_float, ci, i64, i64, hp, vp, vp, sz, vp]
+        L.adadim_kv4_attention.argtypes = [vp, ci, i64, ci, vp, vp, i64, vp, i64, i64, cp, C.c_float, ci, i64, i64, vp, vp, sz, vp]
         L.adadim_kv4_workspace_bytes.restype = sz
         L.adadim_kv4_workspace_bytes.argtypes = [i64, i64, ci, ci, ci]
         L.adadim_unpack_codes.restype = C.c_int
@@ -802,7 +794,7 @@ class Rotary:
     def __init__(self, freq: torch.Tensor, axis: Optional[torch.Tensor] = None, adjacent: bool = False):
         if freq.dim() != 1 or freq.numel() % 8 or not 8 <= freq.numel() <= 128 or not freq.is_cuda:
             raise ValueError("Rotary: freq [dim / 2] on the device, dim a multiple of 16 up to 256")
-        self.dim, self.adjacent, self.axes = 2 * freq.numel(), adjacent, 1
+        self.dim, self.adjacent, self.axes = 2 * freq.numel(), bool(adjacent), 1
         self.freq = freq.double().clone()
         self.axis = None
         if axis is not None:
@@ -811,8 +803,7 @@ class Rotary:
             self.axes = int(axis.max()) + 1
             self.axis = axis.to(device=freq.device, dtype=torch.uint8, copy=True)
         self.dev = self.freq.get_device()
-        self._c = RotaryC(None, self.freq.data_ptr(), self.axis.data_ptr() if self.axis is not None else None, 0, self.axes,
-                          self.dim, int(adjacent))
+        self._freq_p, self._axis_p = self.freq.data_ptr(), self.axis.data_ptr() if self.axis is not None else 0
 
     @staticmethod
     def of(dim: int, base: float = 10000.0, sections=None, adjacent: bool = False, device="cuda") -> "Rotary":
@@ -826,12 +817,16 @@ class Rotary:
         return Rotary(freq, torch.repeat_interleave(torch.arange(len(sections)), torch.tensor(sections)), adjacent)
 
 
-def _heads(t: torch.Tensor, dev: int, rows: int, heads: int, dim: int, dtype=None):
-    """A [tokens, heads, head_dim] tensor whose channels lie side by side, by reference."""
-    shape, stride = t.shape, t.stride()
-    assert (shape[0], shape[1], shape[2]) == (rows, heads, dim) and len(shape) == 3 and (stride[2] == 1 or dim == 1)
-    assert t.get_device() == dev and (dtype is None or t.dtype == dtype)
-    return C.byref(HeadsC(t.data_ptr(), stride[0], stride[1]))
+# adadim_heads [6] and [2], adadim_rotary, as bytes (structures of ctypes take the host five times as long)
+_six_heads, _two_heads, _rotary = struct.Struct("18q").pack, struct.Struct("6q").pack, struct.Struct("4q4i").pack
+_NO_HEADS = (0, 0, 0)
+
+
+def _heads(t: torch.Tensor, dev: int, shape, dtype):
+    """What adadim_heads holds of a [tokens, heads, head_dim] tensor whose channels lie side by side."""
+    ld, lh, step = t.stride()
+    assert t.shape == shape and step == 1 and t.get_device() == dev and t.dtype == dtype
+    return t.data_ptr(), ld, lh
 
 
 def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, slots: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -841,40 +836,41 @@ def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, slots: torch.T
     int32[tokens] (all different; -1: not stored), quantized to NVFP4.  fp32, fp16 or bf16, one type; views of one projection's result
     are taken as they are.  positions int32 [tokens] or [axes, tokens].  Returns the rotated q (in q_out, which may be q, if given).
     k_values, v_values (bf16 or fp32): receive the values that the cache then holds.  For inference: no gradient passes."""
-    dev, (n, h, d) = cache.dev, k.shape
+    dev, shape = cache.dev, k.shape
+    n, h, d = shape
     if h != cache.kv_heads or d != cache.head_dim:
         raise ValueError("kv4_append: k does not match the cache")
     if dev != _device():
         with torch.cuda.device(dev):
             return kv4_append(k, v, cache, slots, q, rotary, positions, q_out, k_values, v_values)
-    dtype, rc_ref, qp, qo, q_heads = k.dtype, None, None, None, 0
+    dtype, turn, qp, qo, q_heads = k.dtype, None, _NO_HEADS, _NO_HEADS, 0
     if _i32(slots, dev).numel() != n:
         raise ValueError("kv4_append: one slot for each token")
-    if (rotary is None) != (positions is None) or (q is not None and rotary is None):
-        raise ValueError("kv4_append: rotary and positions go together, and q with them")
     if rotary is not None:
-        axes = 1 if positions.dim() == 1 else positions.shape[0]
-        assert positions.get_device() == dev and rotary.dev == dev and positions.dtype == torch.int32
-        if axes < rotary.axes or positions.shape[-1] != n or positions.dim() > 2 or rotary.dim > d:
+        if positions is None:
+            raise ValueError("kv4_append: rotary and positions go together, and q with them")
+        at, many = positions.stride(), len(positions.shape) == 2
+        if (positions.shape[0] < rotary.axes if many else rotary.axes != 1) or positions.shape[-1] != n or rotary.dim > d or len(at) > 2:
             raise ValueError("kv4_append: positions [axes, tokens] for every axis of the rotary, which is no wider than a head")
-        if n > 1 and positions.stride(-1) != 1:
+        if n > 1 and at[-1] != 1:
             raise ValueError("kv4_append: a token's positions lie side by side")
-        own = rotary._c
-        rc_ref = C.byref(RotaryC(positions.data_ptr(), own.freq, own.axis, positions.stride(0) if axes > 1 else 0, own.axes,
-                                 own.dim, own.adjacent))
+        assert positions.get_device() == dev and rotary.dev == dev and positions.dtype == torch.int32
+        turn = _rotary(positions.data_ptr(), rotary._freq_p, rotary._axis_p, at[0] if many else 0, rotary.axes, rotary.dim, rotary.adjacent, 0)
+    elif positions is not None or q is not None:
+        raise ValueError("kv4_append: rotary and positions go together, and q with them")
     if q is not None:
         q_heads = q.shape[1]
         if q_out is None:
             q_out = torch.empty(n, q_heads, d, dtype=dtype, device=q.device)
-        qp, qo = _heads(q, dev, n, q_heads, d, dtype), _heads(q_out, dev, n, q_heads, d, dtype)
-    kv = vv = None
-    vdt = BF16
+        q_shape = (n, q_heads, d)
+        qp, qo = _heads(q, dev, q_shape, dtype), _heads(q_out, dev, q_shape, dtype)
+    kv, vv, vdt = _NO_HEADS, _NO_HEADS, BF16
     if k_values is not None:
-        kv, vdt = _heads(k_values, dev, n, h, d), _DT[k_values.dtype]
+        kv, vdt = _heads(k_values, dev, shape, k_values.dtype), _DT[k_values.dtype]
     if v_values is not None:
-        vv, vdt = _heads(v_values, dev, n, h, d, None if k_values is None else k_values.dtype), _DT[v_values.dtype]
-    rc = (_lib or lib()).adadim_kv4_append(qp, qo, q_heads, _heads(k, dev, n, h, d), _heads(v, dev, n, h, d, dtype), _DT[dtype],
-                                           n, slots.data_ptr(), rc_ref, cache._ref, kv, vv, vdt, _raw_stream(dev))
+        vv, vdt = _heads(v_values, dev, shape, v_values.dtype if k_values is None else k_values.dtype), _DT[v_values.dtype]
+    heads = _six_heads(*_heads(k, dev, shape, dtype), *_heads(v, dev, shape, dtype), *qp, *qo, *kv, *vv)
+    rc = (_lib or lib()).adadim_kv4_append(heads, q_heads, _DT[dtype], n, slots.data_ptr(), turn, cache._ref, vdt, _raw_stream(dev))
     if rc:
         _check(rc, "adadim_kv4_append")
     return q_out
@@ -894,26 +890,28 @@ def kv4_attention(q: torch.Tensor, cache: Kv4Cache, table: torch.Tensor, lengths
     own.  Rows that see nothing get zeros, rows of no request are not written.  max_new: no request has more
     rows than this (0: not known); picks the kernels.  Calls that may run at once need a workspace each
     (kv4_workspace_bytes).  For inference: no gradient passes."""
-    dev, (n, h, d) = cache.dev, q.shape
+    dev, shape = cache.dev, q.shape
+    n, h, d = shape
     n_req, (t_rows, width) = _i32(lengths, dev).numel(), table.shape
     if d != cache.head_dim or h % cache.kv_heads:
         raise ValueError("kv4_attention: q does not match the cache")
     if t_rows != n_req or _i32(offsets, dev).numel() != n_req + 1:
         raise ValueError("kv4_attention: table, lengths and offsets are of different numbers of requests")
-    assert table.get_device() == dev and table.dtype == torch.int32 and (width <= 1 or table.stride(1) == 1)
+    ldt, step = table.stride()
+    assert table.get_device() == dev and table.dtype == torch.int32 and (width <= 1 or step == 1)
     if dev != _device():
         with torch.cuda.device(dev):
             return kv4_attention(q, cache, table, lengths, offsets, scale, causal, window, max_new, out, workspace, status)
+    dtype = q.dtype
     if out is None:
-        out = torch.empty(n, h, d, dtype=q.dtype, device=q.device)
+        out = torch.empty(n, h, d, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = _ws(kv4_workspace_bytes(n_req, n, h, cache.kv_heads, d), q.device)
     assert workspace.get_device() == dev and workspace.dtype == torch.uint8
-    dtype = q.dtype
-    rc = (_lib or lib()).adadim_kv4_attention(_heads(q, dev, n, h, d), _DT[dtype], n, h, offsets.data_ptr(), lengths.data_ptr(),
-                                              n_req, table.data_ptr(), table.stride(0) if n_req > 1 else width, width, cache._ref,
-                                              d ** -0.5 if scale is None else scale, causal, window, max_new,
-                                              _heads(out, dev, n, h, d, dtype), _status(status, dev), workspace.data_ptr(),
+    qo = _two_heads(*_heads(q, dev, shape, dtype), *_heads(out, dev, shape, dtype))
+    rc = (_lib or lib()).adadim_kv4_attention(qo, _DT[dtype], n, h, offsets.data_ptr(), lengths.data_ptr(), n_req, table.data_ptr(),
+                                              ldt if n_req > 1 else width, width, cache._ref, d ** -0.5 if scale is None else scale,
+                                              causal, window, max_new, _status(status, dev), workspace.data_ptr(),
                                               workspace.numel(), _raw_stream(dev))
     if rc:
         _check(rc, "adadim_kv4_attention")

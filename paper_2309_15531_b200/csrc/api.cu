@@ -72,7 +72,7 @@ int check_kv4(const adadim_kv4cache* c) {
   if (c->n_pages > 0 && (c->codes == nullptr || c->scales == nullptr)) return ADADIM_ERR_NULL;
   return aligned256(c->codes) && aligned256(c->scales) ? ADADIM_OK : ADADIM_ERR_ALIGN;
 }
-Kv4Heads heads_of(const adadim_heads* h, const Kv4Heads& none) { return h == nullptr ? none : Kv4Heads{h->p, h->ld, h->lh}; }
+Kv4Heads heads_of(const adadim_heads& h) { return {h.p, h.ld, h.lh}; }
 
 int check_qtensor(const adadim_qtensor* q) {
   if (q == nullptr || q->codes == nullptr || q->scales == nullptr || q->zeros == nullptr) return ADADIM_ERR_NULL;
@@ -527,32 +527,29 @@ int adadim_page_tables(const int32_t* past, const int32_t* fresh, int64_t n_requ
                             static_cast<cudaStream_t>(cuda_stream));
 }
 
-int adadim_kv4_append(const adadim_heads* Q, const adadim_heads* Qr, int q_heads, const adadim_heads* K, const adadim_heads* V,
-                      int dtype, int64_t n_tokens, const int32_t* slots, const adadim_rotary* rotary, const adadim_kv4cache* cache,
-                      const adadim_heads* k_values, const adadim_heads* v_values, int vdtype, void* cuda_stream) {
+int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dtype, int64_t n_tokens, const int32_t* slots,
+                      const adadim_rotary* rotary, const adadim_kv4cache* cache, int vdtype, void* cuda_stream) {
   int rc = check_kv4(cache);
   if (rc != ADADIM_OK) return rc;
+  if (heads == nullptr) return ADADIM_ERR_NULL;
+  const adadim_heads &K = heads[0], &V = heads[1], &Q = heads[2], &Qr = heads[3];
   if (dtype != ADADIM_F32 && dtype != ADADIM_F16 && dtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
-  if ((k_values != nullptr || v_values != nullptr) && vdtype != ADADIM_F32 && vdtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
+  if ((heads[4].p != nullptr || heads[5].p != nullptr) && vdtype != ADADIM_F32 && vdtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
   if (n_tokens < 0 || n_tokens > kInt32Max || q_heads < 0 || q_heads > (1 << 16)) return ADADIM_ERR_SHAPE;
-  if ((Q == nullptr) != (Qr == nullptr)) return ADADIM_ERR_NULL;
-  if (Q != nullptr && rotary == nullptr) return ADADIM_ERR_PARAM;
-  if (Q == nullptr) q_heads = 0;
   if (rotary != nullptr) {
     if (rotary->axes < 1 || rotary->dim < 16 || rotary->dim > cache->head_dim || rotary->dim % 16 != 0) return ADADIM_ERR_PARAM;
     if (n_tokens > 0 && (rotary->positions == nullptr || rotary->freq == nullptr)) return ADADIM_ERR_NULL;
     if (rotary->axes > 1 && rotary->axis == nullptr) return ADADIM_ERR_NULL;
   }
   if (n_tokens == 0) return ADADIM_OK;
-  if (K == nullptr || V == nullptr || K->p == nullptr || V->p == nullptr || slots == nullptr) return ADADIM_ERR_NULL;
-  if (Q != nullptr && q_heads > 0 && (Q->p == nullptr || Qr->p == nullptr)) return ADADIM_ERR_NULL;
-  const Kv4Heads none = {nullptr, 0, 0};
+  if ((Q.p == nullptr) != (Qr.p == nullptr)) return ADADIM_ERR_NULL;
+  if (Q.p != nullptr && rotary == nullptr) return ADADIM_ERR_PARAM;
+  if (K.p == nullptr || V.p == nullptr || slots == nullptr) return ADADIM_ERR_NULL;
   const Kv4Rotary still = {nullptr, nullptr, nullptr, 0, 1, 0, 0};
-  return kv4_append_launch(heads_of(Q, none), heads_of(Qr, none), q_heads, heads_of(K, none), heads_of(V, none), dtype, n_tokens, slots,
+  return kv4_append_launch(heads_of(Q), heads_of(Qr), Q.p == nullptr ? 0 : q_heads, heads_of(K), heads_of(V), dtype, n_tokens, slots,
                            rotary == nullptr ? still : Kv4Rotary{rotary->positions, rotary->freq, rotary->axis, rotary->ld, rotary->axes,
                                                                 rotary->dim, rotary->adjacent},
-                           kv4::cache_of(*cache), heads_of(k_values, none), heads_of(v_values, none), vdtype,
-                           static_cast<cudaStream_t>(cuda_stream));
+                           kv4::cache_of(*cache), heads_of(heads[4]), heads_of(heads[5]), vdtype, static_cast<cudaStream_t>(cuda_stream));
 }
 
 size_t adadim_kv4_workspace_bytes(int64_t n_requests, int64_t n_rows, int q_heads, int kv_heads, int head_dim) {
@@ -560,9 +557,9 @@ size_t adadim_kv4_workspace_bytes(int64_t n_requests, int64_t n_rows, int q_head
   return kv4_workspace(n_requests, n_rows, q_heads, kv_heads, head_dim);
 }
 
-int adadim_kv4_attention(const adadim_heads* Q, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets, const int32_t* lengths,
+int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets, const int32_t* lengths,
                          int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width, const adadim_kv4cache* cache, float scale,
-                         int causal, int64_t window, int64_t max_new, const adadim_heads* O, int* status_dev, void* workspace,
+                         int causal, int64_t window, int64_t max_new, int* status_dev, void* workspace,
                          size_t workspace_bytes, void* cuda_stream) {
   int rc = check_kv4(cache);
   if (rc != ADADIM_OK) return rc;
@@ -573,14 +570,14 @@ int adadim_kv4_attention(const adadim_heads* Q, int dtype, int64_t n_rows, int q
       width * cache->page > kInt32Max)
     return ADADIM_ERR_SHAPE;
   if (n_rows == 0 || n_requests == 0) return ADADIM_OK;
-  if (Q == nullptr || O == nullptr || Q->p == nullptr || O->p == nullptr || offsets == nullptr || lengths == nullptr ||
+  if (qo == nullptr || qo[0].p == nullptr || qo[1].p == nullptr || offsets == nullptr || lengths == nullptr ||
       (width > 0 && table == nullptr) || workspace == nullptr)
     return ADADIM_ERR_NULL;
   if (!aligned256(workspace)) return ADADIM_ERR_ALIGN;
   if (workspace_bytes < adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, cache->kv_heads, cache->head_dim)) return ADADIM_ERR_WORKSPACE;
   Kv4Attention a = {};
-  a.q = {Q->p, Q->ld, Q->lh};
-  a.o = {O->p, O->ld, O->lh};
+  a.q = heads_of(qo[0]);
+  a.o = heads_of(qo[1]);
   a.n_rows = static_cast<int>(n_rows);
   a.q_heads = q_heads;
   a.group = q_heads / cache->kv_heads;

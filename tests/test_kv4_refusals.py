@@ -1,5 +1,6 @@
 """What the entry points around the 4-bit key-value cache refuse, found on the host before anything is launched (CPU)."""
 import ctypes as C
+import struct
 
 import pytest
 
@@ -9,7 +10,7 @@ OK, NULL, SHAPE, DTYPE, PARAM, ALIGN, WORKSPACE = 0, 1, 2, 3, 4, 5, 6
 
 
 def heads(p=256, ld=1024, lh=64):
-    return C.byref(B.HeadsC(p, ld, lh))
+    return p, ld, lh
 
 
 def cache(codes=256, scales=256, n_pages=4, page=16, kv_heads=2, dim=64):
@@ -41,38 +42,39 @@ def test_page_tables(change, status):
     assert tables(**change) == status
 
 
-def append(q=None, qr=None, q_heads=4, k=heads(), v=heads(), dtype=B.F16, n=3, slots=16, rotary=None, c=None, kv=None, vv=None, vdt=B.BF16):
-    return B.lib().adadim_kv4_append(q, qr, q_heads, k, v, dtype, n, slots, rotary, c or cache(), kv, vv, vdt, None)
+def append(q=(0, 0, 0), qr=(0, 0, 0), q_heads=4, k=heads(), v=heads(), dtype=B.F16, n=3, slots=16, rotary=None, c=None, kv=(0, 0, 0), vv=(0, 0, 0), vdt=B.BF16):
+    return B.lib().adadim_kv4_append(struct.pack("18q", *k, *v, *q, *qr, *kv, *vv), q_heads, dtype, n, slots, rotary, c or cache(), vdt, None)
 
 
 def rotary(positions=16, freq=16, axis=16, axes=1, dim=64, adjacent=0):
-    return C.byref(B.RotaryC(positions, freq, axis, 8, axes, dim, adjacent))
+    return struct.pack("4q4i", positions, freq, axis, 8, axes, dim, adjacent, 0)
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(dtype=3), DTYPE), (dict(kv=heads(), vdt=B.F16), DTYPE), (dict(n=-1), SHAPE), (dict(k=None), NULL), (dict(v=heads(None)), NULL),
+    (dict(dtype=3), DTYPE), (dict(kv=heads(), vdt=B.F16), DTYPE), (dict(n=-1), SHAPE), (dict(k=heads(0)), NULL), (dict(v=heads(0)), NULL),
     (dict(slots=None), NULL), (dict(q=heads(), rotary=rotary()), NULL), (dict(q=heads(), qr=heads()), PARAM),
-    (dict(q=heads(None), qr=heads(), rotary=rotary()), NULL), (dict(rotary=rotary(positions=None)), NULL), (dict(rotary=rotary(freq=None)), NULL),
+    (dict(q=heads(0), qr=heads(), rotary=rotary()), NULL), (dict(rotary=rotary(positions=0)), NULL), (dict(rotary=rotary(freq=0)), NULL),
     (dict(rotary=rotary(axes=0)), PARAM), (dict(rotary=rotary(dim=72)), PARAM), (dict(rotary=rotary(dim=80)), PARAM), (dict(rotary=rotary(dim=0)), PARAM),
-    (dict(rotary=rotary(axes=3, axis=None)), NULL), (dict(c=cache(page=48)), PARAM), (dict(c=cache(dim=40)), PARAM), (dict(c=cache(codes=None)), NULL),
-    (dict(c=cache(scales=264)), ALIGN), (dict(n=0, k=None, v=None, slots=None), OK)])
+    (dict(rotary=rotary(axes=3, axis=0)), NULL), (dict(c=cache(page=48)), PARAM), (dict(c=cache(dim=40)), PARAM), (dict(c=cache(codes=None)), NULL),
+    (dict(c=cache(scales=264)), ALIGN), (dict(n=0, k=heads(0), v=heads(0), slots=None), OK)])
 def test_append(change, status):
     assert append(**change) == status
 
 
 def attention(q=heads(), dtype=B.BF16, rows=3, q_heads=4, offsets=16, lengths=16, n=2, table=16, ldt=4, width=4, c=None, window=0, max_new=0,
-              o=heads(), ws=256, ws_bytes=None):
+              o=heads(), ws=256, ws_bytes=None, no_heads=False):
     need = B.lib().adadim_kv4_workspace_bytes(2, 3, 4, 2, 64)
-    return B.lib().adadim_kv4_attention(q, dtype, rows, q_heads, offsets, lengths, n, table, ldt, width, c or cache(), 0.1, 1, window, max_new,
-                                        o, None, ws, need if ws_bytes is None else ws_bytes, None)
+    qo = None if no_heads else struct.pack("6q", *q, *o)
+    return B.lib().adadim_kv4_attention(qo, dtype, rows, q_heads, offsets, lengths, n, table, ldt, width, c or cache(), 0.1, 1, window, max_new,
+                                        None, ws, need if ws_bytes is None else ws_bytes, None)
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=B.F32), DTYPE), (dict(q_heads=3), PARAM), (dict(q_heads=0), PARAM), (dict(window=-1), PARAM), (dict(max_new=-1), PARAM),
     (dict(rows=-1), SHAPE), (dict(rows=1 << 30), SHAPE), (dict(n=8193), SHAPE), (dict(n=-1), SHAPE), (dict(ldt=3), SHAPE), (dict(width=1 << 30, ldt=1 << 30), SHAPE),
-    (dict(q=None), NULL), (dict(o=heads(None)), NULL), (dict(offsets=None), NULL), (dict(lengths=None), NULL), (dict(table=None), NULL),
+    (dict(no_heads=True), NULL), (dict(q=heads(0)), NULL), (dict(o=heads(0)), NULL), (dict(offsets=None), NULL), (dict(lengths=None), NULL), (dict(table=None), NULL),
     (dict(ws=None), NULL), (dict(ws=264), ALIGN), (dict(ws_bytes=100), WORKSPACE), (dict(c=cache(n_pages=1 << 28)), SHAPE),
-    (dict(rows=0, q=None, o=None, ws=None), OK), (dict(n=0), OK)])
+    (dict(rows=0, no_heads=True, ws=None), OK), (dict(n=0), OK)])
 def test_attention(change, status):
     assert attention(**change) == status
 
