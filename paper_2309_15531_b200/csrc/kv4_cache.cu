@@ -134,11 +134,11 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
 
 // ---- append ------------------------------------------------------------------------------------------
 // Bound by memory in long prompts, by latency for few tokens (then a token's heads are shared by several CTAs). A CTA has one
-// token: its angles are formed once, in binary64 (positions times frequencies lose a far position's angle in binary32), and
-// used by all its heads. A thread takes eight channels of a key or value (the two halves of a block meet in one shuffle), or
+// token, or four one after the other: their angles are formed once, in binary64 (positions times frequencies lose a far position's
+// angle in binary32), by all its threads, and used by all heads. A thread takes eight channels of a key or value (the two halves of a block meet in one shuffle), or
 // eight pairs of a query. Keys are rotated in binary64, so that a block's scale and codes are those of the exact rotation:
 // binary32 would decide otherwise for values next to the middle of two codes, and the cache would depend on the kernel.
-constexpr int kAppendThreads = 256, kMaxPairs = 128;
+constexpr int kAppendThreads = 256, kMaxPairs = 128, kMostTokens = 4;
 
 struct AppendParams {
   Kv4Heads q, qr, k, v, k_values, v_values;
@@ -148,6 +148,10 @@ struct AppendParams {
   Cache cache;
   int wide_q, wide_qr, wide_k, wide_v, wide_kv, wide_vv;             // 16-byte loads and stores
   int q_chunks;                                                      // tasks of a query head
+  uint32_t q_rcp;                                                    // 2^32 / q_chunks + 1
+  int chunk_log2;                                                    // of the eights of channels of a held head
+  int each;                                                          // tokens of a CTA
+  int64_t n_tokens;
 };
 
 template <typename T> __device__ __forceinline__ float widened(T x);
@@ -234,32 +238,40 @@ __device__ __forceinline__ uint32_t quantize_exact(const double (&z)[8], uint64_
 
 template <typename T, typename V>
 __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams p) {
-  __shared__ double turn_c[kMaxPairs], turn_s[kMaxPairs];
-  __shared__ float2 turn[kMaxPairs];
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, half = p.rotary.dim >> 1;
+  __shared__ double turns_c[kMostTokens][kMaxPairs], turns_s[kMostTokens][kMaxPairs];
+  __shared__ float2 turns[kMostTokens][kMaxPairs];
+  const int64_t first = blockIdx.x * static_cast<int64_t>(p.each);
+  const int tid = threadIdx.x, half = p.rotary.dim >> 1, tokens = static_cast<int>(min(static_cast<int64_t>(p.each), p.n_tokens - first));
   const bool adjacent = p.rotary.adjacent != 0;
-  if (tid < half) {
-    const int ax = p.rotary.axis == nullptr ? 0 : min(static_cast<int>(p.rotary.axis[tid]), p.rotary.axes - 1);
-    const double angle = static_cast<double>(p.rotary.positions[ax * p.rotary.ld + t]) * p.rotary.freq[tid];
+  for (int at = tid; at < tokens * kMaxPairs; at += kAppendThreads) {
+    const int k = at / kMaxPairs, j = at % kMaxPairs;
+    if (j >= half) continue;
+    const int ax = p.rotary.axis == nullptr ? 0 : min(static_cast<int>(p.rotary.axis[j]), p.rotary.axes - 1);
+    const double angle = static_cast<double>(p.rotary.positions[ax * p.rotary.ld + first + k]) * p.rotary.freq[j];
+    // the angle without whole turns, 2 pi as two numbers, so that sincos finds it small
+    const double whole = rint(angle * 0.15915494309189535);
+    const double rest = fma(-whole, 2.4492935982947064e-16, fma(-whole, 6.283185307179586, angle));
     double s, c;
-    sincos(angle, &s, &c);
-    turn_c[tid] = c;
-    turn_s[tid] = s;
-    turn[tid] = make_float2(static_cast<float>(c), static_cast<float>(s));
+    sincos(rest, &s, &c);
+    turns_c[k][j] = c;
+    turns_s[k][j] = s;
+    turns[k][j] = make_float2(static_cast<float>(c), static_cast<float>(s));
   }
   __syncthreads();
   const Cache& cache = p.cache;
-  const int chunks = cache.held >> 3, kv_tasks = cache.kv_heads * chunks, tasks = 2 * kv_tasks + p.q_heads * p.q_chunks;
-  const int64_t slot = p.slots[t];
-  const bool stored = slot >= 0 && slot >> cache.page_log2 < cache.n_pages;
+  const int chunks = 1 << p.chunk_log2, kv_tasks = cache.kv_heads << p.chunk_log2, tasks = 2 * kv_tasks + p.q_heads * p.q_chunks;
   const int lane = tid & 31;
   const uint32_t pair = 3u << (lane & ~1);
 
+  for (int n = 0; n < tokens; ++n) {
+  const int64_t t = first + n, slot = p.slots[t];
+  const double *const turn_c = turns_c[n], *const turn_s = turns_s[n];
+  const float2* const turn = turns[n];
+  const bool stored = slot >= 0 && slot >> cache.page_log2 < cache.n_pages;
   for (int task = blockIdx.y * kAppendThreads + tid; task < tasks; task += gridDim.y * kAppendThreads) {
     if (task < 2 * kv_tasks) {
       // kv_tasks and chunks are even, so that the two lanes of a pair have the halves of one block
-      const int value = task >= kv_tasks, at = value ? task - kv_tasks : task, head = at / chunks, chunk = at - head * chunks, c0 = chunk * 8;
+      const int value = task >= kv_tasks, at = value ? task - kv_tasks : task, head = at >> p.chunk_log2, chunk = at & (chunks - 1), c0 = chunk * 8;
       const Kv4Heads& src = value ? p.v : p.k;
       const bool wide = value ? p.wide_v : p.wide_k, inside = c0 < cache.dim;
       const T* row = static_cast<const T*>(src.p) + t * src.ld + head * src.lh;
@@ -326,7 +338,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
         store_chunk(static_cast<V*>(dst.p) + t * dst.ld + head * dst.lh + c0, value ? p.wide_vv : p.wide_kv, w);
       }
     } else {
-      const int at = task - 2 * kv_tasks, head = at / p.q_chunks, chunk = at - head * p.q_chunks;
+      const int at = task - 2 * kv_tasks, head = p.q_chunks == 1 ? at : static_cast<int>(__umulhi(static_cast<uint32_t>(at), p.q_rcp)), chunk = at - head * p.q_chunks;   // at * q_chunks < 2^32
       const T* row = static_cast<const T*>(p.q.p) + t * p.q.ld + head * p.q.lh;
       T* out = static_cast<T*>(p.qr.p) + t * p.qr.ld + head * p.qr.lh;
       float a[8], b[8];
@@ -362,6 +374,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
         store_chunk(out + c0, p.wide_qr, a);
       }
     }
+  }
   }
 }
 
@@ -413,8 +426,12 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
   p.wide_vv = wide_heads(v_values, vsz);
   p.q_chunks = rotary.adjacent ? cache.dim / 8 : rotary.dim / 16 + (cache.dim - rotary.dim) / 8;
   const int64_t tasks = static_cast<int64_t>(cache.kv_heads) * (cache.held / 8) * 2 + static_cast<int64_t>(q_heads) * p.q_chunks;
+  p.q_rcp = static_cast<uint32_t>((uint64_t{1} << 32) / p.q_chunks + 1);
+  p.chunk_log2 = kv4::log2_of(cache.held / 8);
+  p.n_tokens = n_tokens;
+  p.each = n_tokens >= 148 * 4 * kMostTokens ? kMostTokens : 1;
   const int64_t most = (tasks + kAppendThreads - 1) / kAppendThreads, wanted = 148 * 4 / n_tokens;
-  const dim3 grid(static_cast<unsigned>(n_tokens), static_cast<unsigned>(wanted < 1 ? 1 : wanted > most ? most : wanted));
+  const dim3 grid(static_cast<unsigned>((n_tokens + p.each - 1) / p.each), static_cast<unsigned>(wanted < 1 ? 1 : wanted > most ? most : wanted));
   if (dtype == ADADIM_F32) return append_types<float>(p, vdtype, grid, st);
   return dtype == ADADIM_F16 ? append_types<__half>(p, vdtype, grid, st) : append_types<__nv_bfloat16>(p, vdtype, grid, st);
 }
