@@ -12,6 +12,7 @@ using namespace kv4;
 // kernel's and take every eighth part.  Either way the order of the sums is fixed.  One launch joins both kernels' units: the first
 // few_blocks CTAs those of the kernel for few rows.
 constexpr int kJoinThreads = 256, kJoinWarps = 8;
+constexpr int kManyBlocks = 8;                   // CTAs that share a unit of the kernel for many rows, whose warps have several rows each
 
 struct Joined {
   char* workspace;
@@ -26,7 +27,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool of_few = static_cast<int>(blockIdx.x) < few_blocks, split = SPLIT && of_few;
   const Joined& from = of_few ? few : many;
-  const int at_block = of_few ? blockIdx.x : blockIdx.x - few_blocks, ys = split ? from.tile_rows : from.tile_rows / kJoinWarps;
+  const int at_block = of_few ? blockIdx.x : blockIdx.x - few_blocks, ys = split ? from.tile_rows : of_few ? from.tile_rows / kJoinWarps : kManyBlocks;
   const int b = at_block / ys, y = at_block - b * ys;
   ptx::pdl_wait();
   const Partials part = partials_of(from.workspace, from.ctas, from.tile_rows);
@@ -39,8 +40,9 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
   }
   bool ok;
   const Request r = request_of(p.offsets, p.lengths, desc.x, p.n_rows, p.width << p.cache.page_log2, ok);
-  const int row = split ? y : y * kJoinWarps + warp, rr = desc.z * from.tile_rows + row;
-  if (rr >= r.rows * p.group) return;                                // split: all of the CTA
+  const int t_v = cache_scale_log2(p.cache, 1), rows = r.rows * p.group - desc.z * from.tile_rows;
+  for (int row = split ? y : y * kJoinWarps + warp; row < min(rows, from.tile_rows); row += split ? from.tile_rows : ys * kJoinWarps) {
+  const int rr = desc.z * from.tile_rows + row;
   float m = -INFINITY, l = 0.0f, v[kEach] = {};
 #pragma unroll 4
   for (int k = b + (split ? warp : 0); k <= last; k += split ? kJoinWarps : 1) {
@@ -58,7 +60,6 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
   }
   const int tok = token_of(p, rr), head = desc.y * p.group + rr - tok * p.group;
   T* out = static_cast<T*>(p.o.p) + (r.first + tok) * p.o.ld + head * p.o.lh;
-  const int t_v = cache_scale_log2(p.cache, 1);
   if (split) {
     if constexpr (SPLIT) {
 #pragma unroll
@@ -86,11 +87,12 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(Kv4Attention p, 
       if (d < p.cache.dim) out[d] = static_cast<T>(l == 0.0f ? v[e] : ldexpf(v[e] / l, t_v));
     }
   }
+  }
 }
 
 template <int HELD, bool SPLIT, typename T>
 int join(const Kv4Attention& a, const Joined& few, const Joined& many, cudaStream_t st) {
-  const int few_blocks = few.ctas * (SPLIT ? few.tile_rows : few.tile_rows / kJoinWarps), many_blocks = many.ctas * (many.tile_rows / kJoinWarps);
+  const int few_blocks = few.ctas * (SPLIT ? few.tile_rows : few.tile_rows / kJoinWarps), many_blocks = many.ctas * kManyBlocks;
   return chained_launch(kv4_join_kernel<HELD, SPLIT, T>, dim3(static_cast<unsigned>(few_blocks + many_blocks)), kJoinThreads, 0, true, st, a, 1, few, many,
                         few_blocks);
 }

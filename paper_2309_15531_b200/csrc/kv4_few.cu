@@ -244,10 +244,10 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
       most = max(most & 0xffffu, most >> 16);
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      const int e = query_exponent<T>(most), e1 = e >> 1;            // 2^e as two factors: up to 2^141
-      const float f1 = exp2_int(e1), f2 = exp2_int(e - e1);
+      const int e = query_exponent<T>(most);
+      const float scaled = exp2_int(e);
 #pragma unroll
-      for (int k = 0; k < HELD / 8; ++k) qb[u][k >> 1][k & 1] = query_bits<T>(raw[u][k], f1, f2);
+      for (int k = 0; k < HELD / 8; ++k) qb[u][k >> 1][k & 1] = query_bits<T>(raw[u][k], scaled);
       // a query that is not finite makes every score it has with a key NaN
       const float f = query_fine<T>(most) ? ldexpf(p.scale * kLog2e, t_k - e) : __int_as_float(0x7fffffff);
 #pragma unroll

@@ -46,16 +46,17 @@ __device__ __forceinline__ int64_t quick_div(int64_t a, int64_t b) {
   if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
   return a / b;
 }
-// Two words of 16-bit queries as fp16 times 2^e, f1 f2 = 2^e (fp16 queries: as they are).
+// A word of 16-bit queries as fp16 times f = 2^e (fp16 queries: as they are).
 template <typename T>
-__device__ __forceinline__ uint32_t query_bits(uint32_t raw, float f1, float f2) {
+__device__ __forceinline__ uint32_t query_bits(uint32_t raw, float f) {
   if constexpr (std::is_same<T, __half>::value) return raw;
-  else return half2_bits(__floats2half2_rn(__uint_as_float(raw << 16) * f1 * f2, __uint_as_float(raw & 0xffff0000u) * f1 * f2));
+  else return half2_bits(__floats2half2_rn(__uint_as_float(raw << 16) * f, __uint_as_float(raw & 0xffff0000u) * f));
 }
-// bf16 rows are multiplied by the power of two that takes their largest to 2^14 .. 2^15: a number keeps all its bits
-// unless it lies 2^30 below the largest.  top: the row's largest magnitude as a pattern (patterns are ordered).
+// bf16 rows are multiplied by the power of two that takes their largest to 2^14 .. 2^15 (2^127 at most, where it is below 2^-113): a
+// number keeps all its bits unless it lies 2^16 below the largest, and then is off by 2^-25 of the largest or less.
+// top: the row's largest magnitude as a pattern (patterns are ordered).
 template <typename T>
-__device__ __forceinline__ int query_exponent(uint32_t top) { return std::is_same<T, __half>::value ? 0 : 141 - static_cast<int>(top >> 7); }
+__device__ __forceinline__ int query_exponent(uint32_t top) { return std::is_same<T, __half>::value ? 0 : min(127, 141 - static_cast<int>(top >> 7)); }
 template <typename T>
 __device__ __forceinline__ bool query_fine(uint32_t top) { return top < (std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u); }
 

@@ -11,9 +11,12 @@
 //                    is a row, which is K-major for keys and MN-major for values), two stages of each; the next
 //                    tokens' codes are loaded into registers meanwhile, so that 4-bit bytes are all that is read of the cache
 //   warp 12          issues the products
+//   warp 13          finds the CTA's next pieces of the line, and brings their queries into L2
 // Loops that the warps are in all the time are kept short (32 scores a turn): a warp that runs through a thousand instructions
 // waits for them more than it executes.
 // The largest score is taken anew only where a row passes it by more than 2^8; then the accumulator in TMEM is rescaled.
+// A unit of at most 128 rows has both tiles for itself: each takes every other 128 tokens, and the first tile's threads put
+// the two results together from TMEM.
 // The line of work is cut into one part a CTA as for few rows.
 #include "kv4_line.cuh"
 
@@ -24,8 +27,8 @@ using namespace kv4;
 using fp4::exp2_int;
 
 constexpr int kTile = 128, kRows = 2 * kTile, kChunk = 128, kHalf = kChunk / 2;
-constexpr int kUnpackWarp = 8, kUnpackWarps = 4, kIssueWarp = 12, kThreads = 16 * 32;   // three warps only fill up
-constexpr int kCost = 512;                       // what a unit costs beside its tokens, in tokens
+constexpr int kUnpackWarp = 8, kUnpackWarps = 4, kIssueWarp = 12, kJobWarp = 13, kThreads = 16 * 32;   // two warps only fill up
+constexpr int kCost = 640;                       // what a unit costs beside its tokens, in tokens
 constexpr int kLeastPart = 1024;                 // a CTA's part is no smaller
 constexpr int kRing = 8;                         // chunks whose notes about tokens are kept
 
@@ -97,20 +100,61 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // in uniform registers (60 cycles an instruction where it had to be brought there from every lane's).
 __device__ __forceinline__ int same(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
+// A piece as all warps of the CTA take it.  Chunks of tile i: [c0, c1_of[i]), or of those every other one from c0 + i on where both
+// tiles have the same rows.
+struct __align__(16) Job {
+  int first, rows_all, length, request, head, tile, rows, key_lo, c0, c1, c1_of[2], key_hi, starts, ends, none;
+};
+constexpr int kJobs = 4;                         // that lie ready
+
+template <typename T>
+__device__ __forceinline__ uint32_t two_of(float a, float b) {       // rounded, side by side
+  if constexpr (std::is_same<T, __half>::value) return half2_bits(__floats2half2_rn(a, b));
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T>
+__device__ __forceinline__ T* of_lane(T* p, int lane) { return reinterpret_cast<T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(p), lane)); }
+
 struct __align__(16) Shared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2][2], drain;   // [tile][half of the tokens]
+  Job jobs[kJobs];
+  uint64_t job_full[kJobs], job_empty[kJobs];
+
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2][2],   // [tile][half of the tokens]
+           twin_full, twin_free, drain;
   uint32_t tmem;
   int dead;
   uint32_t hidden[kRing][kTile / 32];            // tokens whose page lies outside the cache, a bit each
   uint32_t nan_any[kRing][kUnpackWarps];         // whether a warp's tokens have values that are NaN; which:
   uint8_t nan_of[kRing][kTile];                  // a bit for each of a token's blocks
+  float twin_m[kTile], twin_l[kTile];            // the second tile's maxima, sums and NaN blocks of the rows that both have
+  uint32_t twin_nans[kTile];
 };
 
-// chunks of a tile of the piece: [c0, this)
-__device__ __forceinline__ int chunks_of_tile(const Kv4Attention& p, const Piece& x, int i) {
-  if (x.rows <= i * kTile) return x.c0;
-  const int hi = key_end(p, x, x.tile * kRows + min(x.rows, (i + 1) * kTile) - 1);
-  return max(x.c0, min(x.c1, hi > x.key_lo ? (hi - x.key_lo + kChunk - 1) / kChunk : 0));
+__device__ __forceinline__ bool is_twin(int rows) { return rows <= kTile; }   // both tiles have the same rows
+__device__ __forceinline__ Job job_of(const Kv4Attention& p, const Piece& x) {
+  const int row0 = x.tile * kRows;
+  Job j;
+  j.first = x.r.first;
+  j.rows_all = x.r.rows;
+  j.length = x.r.length;
+  j.request = x.request;
+  j.head = x.head;
+  j.tile = x.tile;
+  j.rows = x.rows;
+  j.key_lo = x.key_lo;
+  j.c0 = x.c0;
+  j.c1 = x.c1;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int hi = key_end(p, x, row0 + min(x.rows, (i + 1) * kTile) - 1);
+    j.c1_of[i] = is_twin(x.rows) ? x.c1 : max(x.c0, min(x.c1, hi > x.key_lo ? (hi - x.key_lo + kChunk - 1) / kChunk : 0));
+  }
+  j.key_hi = key_end(p, x, row0 + x.rows - 1);
+  j.starts = x.starts;
+  j.ends = x.ends;
+  j.none = 0;
+  return j;
 }
 
 template <int HELD, typename T>
@@ -128,6 +172,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
   if (warp == kIssueWarp) {
     if (lane == 0) {
       sh.dead = 0;
+      for (int k = 0; k < kJobs; ++k) {
+        ptx::mbar_init(&sh.job_full[k], 1);
+        ptx::mbar_init(&sh.job_empty[k], kIssueWarp + 1);           // warps that take it
+      }
       for (int k = 0; k < 2; ++k) {
         ptx::mbar_init(&sh.k_full[k], kUnpackWarps);
         ptx::mbar_init(&sh.v_full[k], kUnpackWarps);
@@ -140,6 +188,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           ptx::mbar_init(&sh.o_done[k][h], 1);
         }
       }
+      ptx::mbar_init(&sh.twin_full, 4);
+      ptx::mbar_init(&sh.twin_free, 4);
       ptx::mbar_init(&sh.drain, 1);
       ptx::fence_mbar_init();
     }
@@ -153,11 +203,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
   ptx::tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
   const Partials part = partials_of(p.workspace, gridDim.x, kRows);
-  const int64_t total = line[p.n_requests];
-  const int64_t parts = max(int64_t{1}, min(static_cast<int64_t>(gridDim.x), quick_div(total, kLeastPart)));
-  int64_t at = blockIdx.x < parts ? quick_div(total * blockIdx.x, parts) : total;
-  const int64_t end = blockIdx.x < parts ? quick_div(total * (blockIdx.x + 1), parts) : total;
-  int request = 0;
+  uint32_t jobs = 0;
+  auto take = [&](Job& x) -> bool {                                  // the next piece, for a whole warp; false after the last one
+    const uint32_t slot = jobs % kJobs;
+    if (!ptx::mbar_wait_warp(&sh.job_full[slot], jobs / kJobs & 1u, dead, status)) return false;
+    x = sh.jobs[slot];
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sh.job_empty[slot]);
+    ++jobs;
+    return x.none == 0;
+  };
 
   if (warp < 8) {
     // ---- softmax: a thread has a row of tile i
@@ -166,63 +221,84 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     const uint32_t s_at = tmem + quad + i * 128, o_at = tmem + quad + 256 + i * HELD;
     char* const q_smem = smem + Mm::kQ + i * Mm::kBytes + row_in * 128;
     const int t_k = cache_scale_log2(cache, 0), t_v = cache_scale_log2(cache, 1);
+    constexpr int kLanes = HELD / 8, kAtOnce = 32 / kLanes;          // a row's 16-byte pieces are copied by so many lanes, so many rows at once
+    const int in_row = lane % kLanes, rows0 = (warp & 3) * 32;
+    // this lane's 16-byte piece of row r of the warp's: at q_tile + r * 128 + (r % 8 * 16 ^ swizzled)
+    char* const q_tile = smem + Mm::kQ + i * Mm::kBytes + (in_row >> 3) * Mm::kBox;
+    const int swizzled = (in_row & 7) << 4;
+    auto piece_of_row = [&](int k) { return reinterpret_cast<uint4*>(q_smem + (k >> 3) * Mm::kBox + (((k & 7) ^ (row_in & 7)) << 4)); };
     int64_t seen = 0;                                                // chunks of all pieces so far, of both tiles
     uint32_t turn = 0;                                               // .. of this tile
-    while (at < end && !*dead) {
-      const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
-      request = x.request;
+    uint32_t twins = 0;                                              // pieces so far that both tiles had for themselves
+    Job x;
+    while (take(x)) {
       const int64_t first_seen = seen;
       seen += x.c1 - x.c0;
-      const int rows = min(x.rows - i * kTile, kTile);
-      if (rows <= 0) continue;
-      const int row = x.tile * kRows + i * kTile + row_in, own = x.r.length - x.r.rows;
+      const bool twin = is_twin(x.rows);
+      const int tile_row = twin ? 0 : i * kTile, rows = min(x.rows - tile_row, kTile), by = twin ? 2 : 1;
+      const int row = x.tile * kRows + tile_row + row_in, own = x.length - x.rows_all;
       const bool there = row_in < rows;
-      const int tok_of = token_of(p, min(row, x.r.rows * p.group - 1)), head = x.head * p.group + (there ? row - tok_of * p.group : 0);
-      const int lim = p.causal ? min(x.r.length, own + tok_of + 1) : x.r.length, low = p.window > 0 ? own + tok_of - p.window + 1 : 0;
-      const int first_row = x.tile * kRows + i * kTile, ta = token_of(p, first_row), tb = token_of(p, first_row + rows - 1);
-      const int all_hi = p.causal ? min(x.r.length, own + ta + 1) : x.r.length, all_lo = p.window > 0 ? own + tb - p.window + 1 : 0;
+      const int tok_of = token_of(p, min(row, x.rows_all * p.group - 1)), head = x.head * p.group + (there ? row - tok_of * p.group : 0);
+      const int lim = p.causal ? min(x.length, own + tok_of + 1) : x.length, low = p.window > 0 ? own + tok_of - p.window + 1 : 0;
+      const int first_row = x.tile * kRows + tile_row, ta = token_of(p, first_row), tb = token_of(p, first_row + rows - 1);
+      const int all_hi = p.causal ? min(x.length, own + ta + 1) : x.length, all_lo = p.window > 0 ? own + tb - p.window + 1 : 0;
       // the row of queries as fp16 into shared memory
       float factor;
       {
-        const T* q = static_cast<const T*>(p.q.p) + (x.r.first + tok_of) * p.q.ld + head * p.q.lh;
-        uint32_t raw[HELD / 2], most = 0;
+        // A warp copies its 32 rows to shared memory as they are, neighbouring lanes a row's neighbouring channels; then each thread
+        // goes through its own row there.  Short loops: what is gone through once costs what it takes to fetch the instructions.
+        const T* const q_row = static_cast<const T*>(p.q.p) + (x.first + tok_of) * p.q.ld + head * p.q.lh;
+        const bool in_head = 8 * in_row < cache.dim;
+#pragma unroll 4
+        for (int n = 0; n < kLanes; ++n) {
+          const int r = rows0 + n * kAtOnce + lane / kLanes;
+          const T* const src = of_lane(q_row, r & 31) + (in_head ? 8 * in_row : 0);
+          const bool valid = r < rows && in_head;
+          char* const dst = q_tile + r * 128 + ((r & 7) << 4 ^ swizzled);
+          if (p.wide16_q) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_addr(dst)), "l"(src), "r"(valid ? 16 : 0) : "memory");
+          } else {
+            const uint16_t* u = reinterpret_cast<const uint16_t*>(src);
+            uint16_t w[8] = {};
 #pragma unroll
-        for (int k = 0; k < HELD / 8; ++k) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (there && 8 * k < cache.dim) {
-            if (p.wide16_q) {
-              v = *reinterpret_cast<const uint4*>(q + 8 * k);
-            } else {
-              const uint16_t* u = reinterpret_cast<const uint16_t*>(q + 8 * k);
-              v.x = u[0] | static_cast<uint32_t>(u[1]) << 16; v.y = u[2] | static_cast<uint32_t>(u[3]) << 16;
-              v.z = u[4] | static_cast<uint32_t>(u[5]) << 16; v.w = u[6] | static_cast<uint32_t>(u[7]) << 16;
-            }
+            for (int k = 0; k < 8; ++k) if (valid) w[k] = u[k];
+            *reinterpret_cast<uint4*>(dst) = make_uint4(w[0] | static_cast<uint32_t>(w[1]) << 16, w[2] | static_cast<uint32_t>(w[3]) << 16,
+                                                        w[4] | static_cast<uint32_t>(w[5]) << 16, w[6] | static_cast<uint32_t>(w[7]) << 16);
           }
-          raw[4 * k] = v.x; raw[4 * k + 1] = v.y; raw[4 * k + 2] = v.z; raw[4 * k + 3] = v.w;
         }
-#pragma unroll
-        for (int k = 0; k < HELD / 2; ++k) most = __vmaxu2(most, raw[k] & 0x7fff7fffu);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        uint32_t most = 0;
+#pragma unroll 4
+        for (int k = 0; k < HELD / 8; ++k) {
+          const uint4 v = *piece_of_row(k);
+          most = __vmaxu2(most, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+        }
         most = max(most & 0xffffu, most >> 16);
-        const int e = query_exponent<T>(most), e1 = e >> 1;
-        const float f1 = exp2_int(e1), f2 = exp2_int(e - e1);
+        const int e = query_exponent<T>(most);
+        const float f = exp2_int(e);
         // a negative scale turns the queries' signs, so that the factor of the scores is not negative
         const uint32_t sign = p.scale < 0.0f ? 0x80008000u : 0u;
-#pragma unroll
-        for (int k = 0; k < HELD / 8; ++k) {
-          const uint4 v = make_uint4(query_bits<T>(raw[4 * k], f1, f2) ^ sign, query_bits<T>(raw[4 * k + 1], f1, f2) ^ sign,
-                                     query_bits<T>(raw[4 * k + 2], f1, f2) ^ sign, query_bits<T>(raw[4 * k + 3], f1, f2) ^ sign);
-          *reinterpret_cast<uint4*>(q_smem + (k >> 3) * Mm::kBox + (((k & 7) ^ (row_in & 7)) << 4)) = v;
+        if (!std::is_same<T, __half>::value || sign != 0) {
+#pragma unroll 4
+          for (int k = 0; k < HELD / 8; ++k) {
+            const uint4 v = *piece_of_row(k);
+            *piece_of_row(k) = make_uint4(query_bits<T>(v.x, f) ^ sign, query_bits<T>(v.y, f) ^ sign, query_bits<T>(v.z, f) ^ sign,
+                                          query_bits<T>(v.w, f) ^ sign);
+          }
         }
         // (not zero, so that what is hidden stays at minus infinity)
         factor = query_fine<T>(most) && p.scale == p.scale ? fmaxf(ldexpf(fabsf(p.scale) * kLog2e, t_k - e), 1.2e-38f) : __int_as_float(0x7fffffff);
       }
+      // the second tile's last result has been taken in
+      if (i == 1 && twins > 0 && !ptx::mbar_wait_warp(&sh.twin_free, (twins - 1) & 1u, dead, status)) break;
       ptx::fence_proxy_async();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&sh.q_ready[i]);
 
       float m = -INFINITY, l = 0.0f;
       uint32_t nans = 0;                                             // blocks of the row's result that are NaN
-      const int c1 = chunks_of_tile(p, x, i);
+      const int c1 = i == 0 ? x.c1_of[0] : x.c1_of[1];
       // what was noted about the values of chunk ch: a row has the NaN of the tokens that it sees
       auto note_nans = [&](int ch) {
         const int slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
@@ -236,7 +312,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         }
       };
       bool ok = true;
-      for (int ch = x.c0; ok && ch < c1; ++ch, ++turn) {
+      const int from = twin ? x.c0 + i : x.c0;
+      int last = -1;                                                 // chunk
+      for (int ch = from; ok && ch < c1; last = ch, ch += by, ++turn) {
         const int slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
@@ -250,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           const int tok = x.key_lo + ch * kChunk + h * kHalf;
           const uint2 hid = *reinterpret_cast<const uint2*>(&sh.hidden[slot][2 * h]);
           const bool edge = tok < all_lo || tok + kHalf > all_hi || (hid.x | hid.y) != 0;
-          if (h == 0 && ch > x.c0) note_nans(ch - 1);
+          if (h == 0 && last >= 0) note_nans(last);
           ld32_wait(va);
           ld32_wait(vb);
           if (edge) {
@@ -283,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             const float now = high > m ? high : m, g = m == -INFINITY || now == m ? 1.0f : exp2_fast(m - now);
             m = now;
             l *= g;
-            if (ch > x.c0 || h > 0) {
+            if (last >= 0 || h > 0) {
               // once the last product of values is done, that of the other half
               ok = ptx::mbar_wait_warp(&sh.o_done[i][h ^ 1], (turn + h + 1) & 1u, dead, status);
               if (!ok) break;
@@ -329,59 +407,109 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       }
       if (!ok) break;
       // the row's result
-      const bool some = c1 > x.c0;
+      const bool some = last >= 0;
       if (some) {
         if (!ptx::mbar_wait_warp(&sh.o_done[i][1], (turn - 1) & 1u, dead, status)) break;
         ptx::tc_fence_after_sync();
-        note_nans(c1 - 1);
+        note_nans(last);
+      }
+      // rows that both tiles have: what the first tile's threads have to know of the second's, and the factors of the two results
+      float mine = 1.0f, others = 0.0f;
+      bool both = false;
+      if (twin) {
+        if (i == 1) {
+          sh.twin_m[row_in] = m;
+          sh.twin_l[row_in] = l;
+          sh.twin_nans[row_in] = nans;
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&sh.twin_full);
+          ++twins;
+          continue;
+        }
+        if (!ptx::mbar_wait_warp(&sh.twin_full, twins & 1u, dead, status)) break;
+        ptx::tc_fence_after_sync();
+        ++twins;
+        const float om = sh.twin_m[row_in], ol = sh.twin_l[row_in], top = fmaxf(m, om);
+        nans |= sh.twin_nans[row_in];
+        both = x.c1 - x.c0 > 1;                                      // the second tile had chunks
+        mine = m == -INFINITY ? 1.0f : exp2_fast(m - top);
+        others = om == -INFINITY ? 1.0f : exp2_fast(om - top);       // (without a maximum there are zeros, or NaN)
+        l = l * mine + (both ? ol * others : 0.0f);
+        m = top;
       }
       const bool whole = x.starts && x.ends;
       const int slot = x.starts ? 1 : 0;
-      const int64_t at_row = (static_cast<int64_t>(blockIdx.x) * 2 + slot) * kRows + i * kTile + row_in;
+      const int64_t slot_row = (static_cast<int64_t>(blockIdx.x) * 2 + slot) * kRows + tile_row;
       const float inv = l == 0.0f ? 1.0f : exp2_int(t_v) / l;
-      T* out = static_cast<T*>(p.o.p) + (x.r.first + tok_of) * p.o.ld + head * p.o.lh;
-      if (!whole && there) part.stats[at_row] = make_float2(m, l);
+      T* const o_row = static_cast<T*>(p.o.p) + (x.first + tok_of) * p.o.ld + head * p.o.lh;
+      if (!whole && there) part.stats[slot_row + row_in] = make_float2(m, l);
+      // Through the queries' place in shared memory, which no product reads any more: a row's numbers leave side by side.  A part of
+      // a unit is binary32 and takes two turns.
+      const int columns = whole ? HELD : HELD / 2;
+      for (int from_column = 0; from_column < HELD; from_column += columns) {
 #pragma unroll 1
-      for (int k = 0; k < HELD / 32; ++k) {
-        uint32_t v[32];
-        if (some) {
-          ld32(o_at + 32 * k, v);
-          ld32_wait(v);
-        } else {
+        for (int k = 0; k < columns / 32; ++k) {
+          uint32_t v[32];
+          const int column = from_column + 32 * k;
+          if (some) {
+            ld32(o_at + column, v);
+            ld32_wait(v);
+            if (both) {                                              // the same for the whole CTA
+              uint32_t w[32];
+              ld32(o_at + HELD + column, w);
+              ld32_wait(w);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = 0u;
+              for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * mine + __uint_as_float(w[e]) * others);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = 0u;
+          }
+          if (nans != 0) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (nans >> ((column >> 4) + (e >> 4)) & 1u) v[e] = 0x7fffffffu;
+          }
+          if (whole) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t h[4];
+#pragma unroll
+              for (int n = 0; n < 4; ++n) h[n] = two_of<T>(__uint_as_float(v[8 * e + 2 * n]) * inv, __uint_as_float(v[8 * e + 2 * n + 1]) * inv);
+              *piece_of_row(4 * k + e) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *piece_of_row(8 * k + e) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          }
         }
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          float f = __uint_as_float(v[e]);
-          if (nans >> (2 * k + (e >> 4)) & 1u) f = __int_as_float(0x7fffffff);
-          if (whole) f *= inv;
-          v[e] = __float_as_uint(f);
-        }
-        if (!there) continue;
-        if (!whole) {
-          float4* to = reinterpret_cast<float4*>(part.o + at_row * HELD + 32 * k);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            to[e] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]), __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
-        } else {
-          __align__(16) T h[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) h[e] = static_cast<T>(__uint_as_float(v[e]));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int d = 32 * k + 8 * e;
-            if (d >= cache.dim) continue;
+        __syncwarp();
+#pragma unroll 4
+        for (int n = 0; n < kLanes; ++n) {
+          const int r = rows0 + n * kAtOnce + lane / kLanes;
+          const uint4 v = *reinterpret_cast<const uint4*>(q_tile + r * 128 + ((r & 7) << 4 ^ swizzled));
+          T* const out = of_lane(o_row, r & 31) + 8 * in_row;
+          if (r >= rows) continue;
+          if (!whole) {
+            *reinterpret_cast<uint4*>(part.o + (slot_row + r) * HELD + from_column + 4 * in_row) = v;
+          } else if (8 * in_row < cache.dim) {
             if (p.wide16_o) {
-              *reinterpret_cast<uint4*>(out + d) = reinterpret_cast<uint4*>(h)[e];
+              *reinterpret_cast<uint4*>(out) = v;
             } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int n = 0; n < 8; ++n) out[d + n] = h[8 * e + n];
+              for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(out)[e] = static_cast<uint16_t>(w[e >> 1] >> (e & 1) * 16);
             }
           }
         }
+        __syncwarp();
       }
       ptx::tc_fence_before_sync();                                   // the next piece's products write over what was read here
+      if (twin) {
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sh.twin_free);
+      }
     }
   } else if (warp < kUnpackWarp + kUnpackWarps) {
     // ---- codes to fp16 tiles: a thread has half of a token's channels
@@ -391,10 +519,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     const int64_t gap = static_cast<int64_t>(cache.kv_heads) << cache.page_log2;   // rows from a page's keys to its values
     int64_t seen = 0;
     bool paged = true;
-    while (at < end && !*dead) {
-      const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
-      request = x.request;
-      const int key_hi = key_end(p, x, x.tile * kRows + x.rows - 1), steps = x.c1 - x.c0;
+    Job x;
+    while (take(x)) {
+      const int key_hi = x.key_hi, steps = x.c1 - x.c0;
       const int tok0 = x.key_lo + x.c0 * kChunk + t;                 // this thread's token of the first chunk
       const int32_t* const table = p.table + x.request * p.ldt;
       // its page: -1 outside the cache, -2 none
@@ -416,6 +543,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
 #pragma unroll
         for (int k = 0; k < kWords / 8; ++k) scales[k] = __ldg(f + k);
       };
+      auto zero = [&](uint32_t (&codes)[kWords], uint32_t (&scales)[kWords / 8]) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) codes[k] = 0;
+#pragma unroll
+        for (int k = 0; k < kWords / 8; ++k) scales[k] = 0;
+      };
       auto row_of = [&](int page, int it) { return cache_row(cache, page, 0, x.head, (tok0 + it * kChunk) & ((1 << cache.page_log2) - 1)); };
       auto put = [&](const uint32_t (&codes)[kWords], const uint32_t (&scales)[kWords / 8], char* to) {
 #pragma unroll
@@ -431,29 +564,43 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           }
         }
       };
-#pragma unroll
-      for (int k = 0; k < kWords; ++k) kc[k] = vc[k] = 0;
-#pragma unroll
-      for (int k = 0; k < kWords / 8; ++k) ks[k] = vs[k] = 0;
-      int page = page_of(0), after = page_of(1);
-      if (page >= 0) {
-        const int64_t row = row_of(page, 0);
+      // Keys run a chunk ahead of values: keys of chunk it + 1, then values of chunk it, so that the scores of the next tokens
+      // never wait behind the values of these.  Each one's next codes are asked for when the present ones are used up.
+      int here = page_of(0), soon = page_of(1), later = page_of(2);  // pages of chunks it, it + 1, it + 2
+      if (here >= 0) {
+        const int64_t row = row_of(here, 0);
         load(row, kc, ks);
         load(row + gap, vc, vs);
       }
+      auto keys = [&](int64_t n, int page) {                         // chunk n of all, whose codes are there
+        const int stage = static_cast<int>(n & 1), slot = static_cast<int>(n & (kRing - 1));
+        const uint32_t out = __ballot_sync(0xffffffffu, page == -1);
+        paged &= page != -1;
+        if (lane == 0) sh.hidden[slot][sub] = out;
+        if (page < 0) zero(kc, ks);                                  // a token that is not there
+        if (!ptx::mbar_wait_warp(&sh.k_empty[stage], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, dead, status)) return false;
+        put(kc, ks, row_at + Mm::kK + stage * Mm::kBytes);
+        return true;
+      };
+      auto given = [&](uint64_t* bar) {
+        ptx::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar);
+      };
+      bool ok = true;
 #pragma unroll 1
-      for (int it = 0; it < steps; ++it, ++seen) {
-        const int stage = static_cast<int>(seen & 1), slot = static_cast<int>(seen & (kRing - 1));
-        const uint32_t empty = (static_cast<uint32_t>(seen >> 1) & 1u) ^ 1u;
-        const int now = page;
-        page = after;
-        after = page_of(it + 2);
-        const uint32_t out = __ballot_sync(0xffffffffu, now == -1);
-        paged &= now != -1;
-        if (now < 0) {                                               // a token that is not there: zeros
-#pragma unroll
-          for (int k = 0; k < kWords / 8; ++k) ks[k] = vs[k] = 0;
+      for (int it = -1; ok && it < steps; ++it) {
+        if (it + 1 < steps) {
+          ok = keys(seen + it + 1, it < 0 ? here : soon);
+          if (!ok) break;
+          const int next = it < 0 ? soon : later;                    // page of chunk it + 2
+          if (next >= 0) load(row_of(next, it + 2), kc, ks);
+          given(&sh.k_full[(seen + it + 1) & 1]);
         }
+        if (it < 0) continue;
+        const int64_t n = seen + it;
+        const int stage = static_cast<int>(n & 1), slot = static_cast<int>(n & (kRing - 1));
+        if (here < 0) zero(vc, vs);
         // blocks of values that are NaN: noted, and zero in the product
         uint32_t bits = 0;
 #pragma unroll
@@ -464,24 +611,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         }
         const bool any = __any_sync(0xffffffffu, bits != 0);
         if (any) sh.nan_of[slot][t] = static_cast<uint8_t>(bits);
-        if (lane == 0) {
-          sh.nan_any[slot][sub] = any;
-          sh.hidden[slot][sub] = out;
-        }
-        const int64_t row = page >= 0 ? row_of(page, it + 1) : 0;
-        if (!ptx::mbar_wait_warp(&sh.k_empty[stage], empty, dead, status)) break;
-        put(kc, ks, row_at + Mm::kK + stage * Mm::kBytes);
-        if (page >= 0) load(row, kc, ks);
-        ptx::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sh.k_full[stage]);
-        if (!ptx::mbar_wait_warp(&sh.v_empty[stage], empty, dead, status)) break;
+        if (lane == 0) sh.nan_any[slot][sub] = any;
+        ok = ptx::mbar_wait_warp(&sh.v_empty[stage], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, dead, status);
+        if (!ok) break;
         put(vc, vs, row_at + Mm::kV + stage * Mm::kBytes);
-        if (page >= 0) load(row + gap, vc, vs);
-        ptx::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sh.v_full[stage]);
+        if (soon >= 0) load(row_of(soon, it + 1) + gap, vc, vs);
+        given(&sh.v_full[stage]);
+        here = soon;
+        soon = later;
+        later = page_of(it + 3);
       }
+      seen += steps;
+      if (!ok) break;
     }
     if (__any_sync(0xffffffffu, !paged) && lane == 0) report(status, ADADIM_ERR_PAGES);
   } else if (warp == kIssueWarp) {
@@ -491,15 +632,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     const uint32_t base = ptx::smem_addr(smem), tm = static_cast<uint32_t>(same(static_cast<int>(tmem)));
     uint32_t seen = 0;                                               // chunks of all pieces so far
     uint32_t pieces[2] = {0, 0}, turn[2] = {0, 0};                   // pieces and chunks of each tile
-    int4 desc = make_int4(0, 0, 0, 0);
     bool ok = true;
-    while (ok && at < end && !*dead) {
-      const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
-      request = x.request;
-      if (!(x.starts && x.ends)) note_piece(desc, x);
-      const int steps = same(x.c1 - x.c0), tiles = same(x.rows > kTile ? 2 : 1);
-      const int n[2] = {same(chunks_of_tile(p, x, 0) - x.c0), same(chunks_of_tile(p, x, 1) - x.c0)};    // chunks of each tile
-      for (int i = 0; i < tiles; ++i) {
+    Job x;
+    while (ok && take(x)) {
+      const int steps = same(x.c1 - x.c0), twin = same(is_twin(x.rows));
+      const int n[2] = {same(x.c1_of[0] - x.c0), same(x.c1_of[1] - x.c0)};    // chunks of each tile
+      for (int i = 0; i < 2; ++i) {
         ok = ok && ptx::mbar_wait_warp(&sh.q_ready[i], pieces[i] & 1u, dead, status);
         ++pieces[i];
       }
@@ -522,25 +660,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         ptx::tc_fence_after_sync();
         return got;
       };
-      if (ok && steps > 0) {
-        const uint32_t stage = seen & 1u;
-        ok = wait_keys(seen);
-        if (ok) {
-          for (int h = 0; h < 2; ++h)
-            for (int i = 0; i < 2; ++i)
-              if (n[i] > 0) scores(i, h, stage);
-          if (ptx::elect_one()) ptx::mma_commit(&sh.k_empty[stage]);
-          __syncwarp();
-        }
+      // The scores of the first chunk, both tiles'; of the first two where each tile has its own.
+      for (int it = 0; ok && it < min(steps, twin ? 2 : 1); ++it) {
+        const uint32_t stage = (seen + it) & 1u;
+        ok = wait_keys(seen + it);
+        if (!ok) break;
+        for (int h = 0; h < 2; ++h)
+          for (int i = 0; i < 2; ++i)
+            if (twin ? i == it : n[i] > 0) scores(i, h, stage);
+        if (ptx::elect_one()) ptx::mma_commit(&sh.k_empty[stage]);
+        __syncwarp();
       }
       for (int it = 0; ok && it < steps; ++it, ++seen) {
-        const uint32_t stage = seen & 1u, ahead = stage ^ 1u;
+        const uint32_t stage = seen & 1u;
+        const int next = it + (twin ? 2 : 1);                        // the chunk whose scores follow these weights' products
+        const uint32_t ahead = (seen + next - it) & 1u;
         ok = ptx::mbar_wait_warp(&sh.v_full[stage], seen >> 1 & 1u, dead, status);
         bool keys = false;
 #pragma unroll 1
         for (int hi = 0; hi < 4; ++hi) {                             // halves of the tokens, tiles in turn
-          const int h = hi >> 1, i = hi & 1;
-          if (!ok || it >= (i == 0 ? n[0] : n[1])) continue;
+          const int h = hi >> 1, i = hi & 1, mine = i == 0 ? n[0] : n[1];
+          if (!ok || it >= mine || (twin && i != (it & 1))) continue;
           ok = ptx::mbar_wait_warp(&sh.p_ready[i][h], (i == 0 ? turn[0] : turn[1]) & 1u, dead, status);
           if (!ok) continue;
           if (i == 0) turn[0] += h; else turn[1] += h;
@@ -548,7 +688,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           {
             const uint32_t d = tm + 256 + i * HELD, a = tm + i * 128 + h * kHalf;
             const uint64_t b = ptx::with_start(mnmajor, base + Mm::kV + stage * Mm::kBytes + h * (kHalf * 128));
-            const bool onto = it != 0 || h != 0;
+            const bool onto = it > (twin ? i : 0) || h != 0;
             if (ptx::elect_one()) {
 #pragma unroll
               for (int k = 0; k < kHalf / 16; ++k) mma_f16_ts(d, a + k * 8, b + ((k * 16 * 128) >> 4), kValues, onto || k != 0);
@@ -556,30 +696,62 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             }
             __syncwarp();
           }
-          if (it + 1 < (i == 0 ? n[0] : n[1])) {
-            if (!keys) { ok = wait_keys(seen + 1); keys = true; }
+          if (next < mine) {
+            if (!keys) { ok = wait_keys(seen + next - it); keys = true; }
             if (ok) scores(i, h, ahead);
           }
         }
-        if (ok && it + 1 < steps && !keys) ok = wait_keys(seen + 1); // a chunk that no tile takes any more
+        if (ok && next < steps && !keys) ok = wait_keys(seen + next - it);       // a chunk that no tile takes any more
         if (ok && ptx::elect_one()) {
           ptx::mma_commit(&sh.v_empty[stage]);
-          if (it + 1 < steps) ptx::mma_commit(&sh.k_empty[ahead]);
+          if (next < steps) ptx::mma_commit(&sh.k_empty[ahead]);
         }
         __syncwarp();
       }
     }
     if (*dead) {
-      desc = make_int4(0, 0, 0, 0);
       if (ptx::elect_one()) ptx::mma_commit(&sh.drain);
       __syncwarp();
       const long long t = clock64();
       while (!ptx::mbar_try_wait(&sh.drain, 0) && clock64() - t < ptx::kWaitLimit / 4) {}
     }
+  } else if (warp == kJobWarp) {
+    // ---- pieces
+    const int64_t total = line[p.n_requests];
+    const int64_t parts = max(int64_t{1}, min(static_cast<int64_t>(gridDim.x), quick_div(total, kLeastPart)));
+    int64_t at = blockIdx.x < parts ? quick_div(total * blockIdx.x, parts) : total;
+    const int64_t end = blockIdx.x < parts ? quick_div(total * (blockIdx.x + 1), parts) : total;
+    int4 desc = make_int4(0, 0, 0, 0);
+    int request = 0;
+    for (bool more = true; more;) {
+      Job j = {};
+      more = at < end;
+      j.none = !more;
+      if (more) {
+        const Piece x = next_piece(p, line, at, end, request, kRows, kCost, kChunk);
+        request = x.request;
+        if (!(x.starts && x.ends)) note_piece(desc, x);
+        j = job_of(p, x);
+      }
+      const uint32_t slot = jobs % kJobs;
+      if (!ptx::mbar_wait_warp(&sh.job_empty[slot], (jobs / kJobs & 1u) ^ 1u, dead, status)) break;
+      if (lane == 0) {
+        sh.jobs[slot] = j;
+        ptx::mbar_arrive(&sh.job_full[slot]);
+      }
+      __syncwarp();
+      ++jobs;
+      for (int row = lane; row < j.rows; row += 32) {
+        const int of = j.tile * kRows + row, tk = token_of(p, of), hd = j.head * p.group + of - tk * p.group;
+        const char* q = reinterpret_cast<const char*>(static_cast<const T*>(p.q.p) + (j.first + tk) * p.q.ld + hd * p.q.lh);
+        for (int b = 0; b < cache.dim * 2; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + b));
+      }
+    }
     if (lane == 0) part.desc[blockIdx.x] = desc;
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
+  if (*dead && tid == 0) part.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (warp == kIssueWarp) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tmem, 512);
