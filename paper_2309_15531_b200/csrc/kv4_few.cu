@@ -578,7 +578,8 @@ int few_launch(Kv4Attention a, int64_t max_new, bool chained, int& ctas, int& ti
 }
 template <int HELD, typename T>
 int few_held(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st) {
-  if (HELD < 256 && max_new * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, max_new, chained, ctas, tile_rows, st);
+  // behind the kernel for many rows this one has requests of one token, or of a few
+  if (HELD < 256 && (chained ? 1 : max_new) * a.group > 8) return few_launch<HELD, HELD < 256 ? 2 : 1, T>(a, max_new, chained, ctas, tile_rows, st);
   return few_launch<HELD, 1, T>(a, max_new, chained, ctas, tile_rows, st);
 }
 template <typename T>
