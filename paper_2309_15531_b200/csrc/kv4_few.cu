@@ -26,7 +26,8 @@ using namespace kv4;
 using fp4::exp2_int;
 
 constexpr int kFewThreads = 128, kFewWarps = 4, kStep = 32, kChunk = kStep * kFewWarps;
-constexpr int kFewCost = 640;                    // what a unit costs beside its tokens, in tokens (64 requests of up to 16384 tokens: 178 us with 128)
+// What a unit costs beside its tokens, in tokens: with 300, 640, 1000 and 1500, 64 requests of up to 16384 tokens take 171, 150, 140 and 146 us.
+constexpr int kFewCost = 1000;
 constexpr int kLeastPart = 256;                  // a CTA's part is no smaller
 constexpr int kStages = 3;                       // steps of a warp on their way or being worked on
 // CTAs of an SM: what registers (a thread's 128, 168 or 255) and the ring of steps leave room for
