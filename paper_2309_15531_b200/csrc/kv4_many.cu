@@ -120,7 +120,7 @@ struct __align__(16) Shared {
   Job jobs[kJobs];
   uint64_t job_full[kJobs], job_empty[kJobs];
 
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2], s_full[2][2], p_ready[2][2], o_done[2][2],   // [tile][half of the tokens]
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_ready[2][kJobs], s_full[2][2], p_ready[2][2], o_done[2][2],   // [tile][half of the tokens]
            twin_full, twin_free, drain;
   uint32_t tmem;
   int dead;
@@ -175,14 +175,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       for (int k = 0; k < kJobs; ++k) {
         ptx::mbar_init(&sh.job_full[k], 1);
         ptx::mbar_init(&sh.job_empty[k], kIssueWarp + 1);           // warps that take it
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.q_ready[i][k], 4);
       }
       for (int k = 0; k < 2; ++k) {
         ptx::mbar_init(&sh.k_full[k], kUnpackWarps);
         ptx::mbar_init(&sh.v_full[k], kUnpackWarps);
         ptx::mbar_init(&sh.k_empty[k], 1);
         ptx::mbar_init(&sh.v_empty[k], 1);
-        ptx::mbar_init(&sh.q_ready[k], 4);
-        for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < 2; ++h) {
           ptx::mbar_init(&sh.s_full[k][h], 1);
           ptx::mbar_init(&sh.p_ready[k][h], 4);
           ptx::mbar_init(&sh.o_done[k][h], 1);
@@ -204,14 +204,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
   const uint32_t tmem = sh.tmem;
   const Partials part = partials_of(p.workspace, gridDim.x, kRows);
   uint32_t jobs = 0;
-  auto take = [&](Job& x) -> bool {                                  // the next piece, for a whole warp; false after the last one
+  // The next piece, for a whole warp; false after the last one.  taken() gives its place in the ring back: a tile without tokens in a
+  // piece goes on at once, and may write and announce the queries of later ones, so a place carries its own barriers of queries, and
+  // is given back after they have been arrived at and waited for.
+  auto take = [&](Job& x) -> bool {
     const uint32_t slot = jobs % kJobs;
     if (!ptx::mbar_wait_warp(&sh.job_full[slot], jobs / kJobs & 1u, dead, status)) return false;
     x = sh.jobs[slot];
     __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(&sh.job_empty[slot]);
-    ++jobs;
     return x.none == 0;
+  };
+  auto taken = [&]() {
+    if (lane == 0) ptx::mbar_arrive(&sh.job_empty[jobs % kJobs]);
+    ++jobs;
   };
 
   if (warp < 8) {
@@ -294,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       if (i == 1 && twins > 0 && !ptx::mbar_wait_warp(&sh.twin_free, (twins - 1) & 1u, dead, status)) break;
       ptx::fence_proxy_async();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&sh.q_ready[i]);
+      if (lane == 0) ptx::mbar_arrive(&sh.q_ready[i][jobs % kJobs]);
+      taken();
 
       float m = -INFINITY, l = 0.0f;
       uint32_t nans = 0;                                             // blocks of the row's result that are NaN
@@ -521,6 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     bool paged = true;
     Job x;
     while (take(x)) {
+      taken();
       const int key_hi = x.key_hi, steps = x.c1 - x.c0;
       const int tok0 = x.key_lo + x.c0 * kChunk + t;                 // this thread's token of the first chunk
       const int32_t* const table = p.table + x.request * p.ldt;
@@ -631,16 +638,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     constexpr uint64_t kmajor = ptx::smem_desc_sw128(16, 1024), mnmajor = ptx::smem_desc_sw128(Mm::kBox, 1024);
     const uint32_t base = ptx::smem_addr(smem), tm = static_cast<uint32_t>(same(static_cast<int>(tmem)));
     uint32_t seen = 0;                                               // chunks of all pieces so far
-    uint32_t pieces[2] = {0, 0}, turn[2] = {0, 0};                   // pieces and chunks of each tile
+    uint32_t turn[2] = {0, 0};                                       // .. of each tile
     bool ok = true;
     Job x;
     while (ok && take(x)) {
       const int steps = same(x.c1 - x.c0), twin = same(is_twin(x.rows));
       const int n[2] = {same(x.c1_of[0] - x.c0), same(x.c1_of[1] - x.c0)};    // chunks of each tile
-      for (int i = 0; i < 2; ++i) {
-        ok = ok && ptx::mbar_wait_warp(&sh.q_ready[i], pieces[i] & 1u, dead, status);
-        ++pieces[i];
-      }
+      for (int i = 0; i < 2; ++i) ok = ok && ptx::mbar_wait_warp(&sh.q_ready[i][jobs % kJobs], jobs / kJobs & 1u, dead, status);
+      taken();
       auto scores = [&](int i, int h, uint32_t stage) {
         const uint32_t d = tm + i * 128 + h * kHalf;
         const uint64_t a = ptx::with_start(kmajor, base + Mm::kQ + i * Mm::kBytes);

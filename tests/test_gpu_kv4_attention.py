@@ -288,3 +288,28 @@ def test_many_calls_in_a_row_end_well(lengths, new):
     for _ in range(600):
         b.run(out=out, status=status)
     assert int(status.item()) == 0 and torch.equal(out, first)
+
+
+def test_many_rows_that_see_nothing_between_rows_that_do():
+    """Requests with hundreds of query rows and fewer tokens, or none: whole 128-row tiles without a token, one after another, beside
+    tiles that have work.  Every call gives the first one's bits."""
+    heads, kv_heads, dim = 4, 2, 64
+    lengths = [(0, 300, 40, 700, 0, 0, 129, 5)[i % 8] for i in range(120)]
+    rows = [(200, 200, 130, 256, 150, 64, 300, 128)[i % 8] for i in range(120)]
+    b = Batch(lengths, [min(n, m) for n, m in zip(lengths, rows)], heads, kv_heads, dim, seed=11)
+    g = torch.Generator().manual_seed(12)
+    q = torch.randn(sum(rows), heads, dim, generator=g).bfloat16().cuda()
+    offsets = torch.tensor(np.concatenate(([0], np.cumsum(rows))), dtype=torch.int32).cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = B.kv4_attention(q, b.cache, b.table, b.lengths, offsets, status=status)
+    for _ in range(100):
+        assert torch.equal(out, B.kv4_attention(q, b.cache, b.table, b.lengths, offsets, status=status))
+    assert int(status.item()) == 0
+    k, v = b.values()
+    at = row = 0
+    for n, m in zip(lengths, rows):
+        mine = q[row:row + m].double().cpu().numpy()
+        want, spread = K.attend(mine, k[at:at + n], v[at:at + n], dim ** -0.5)
+        got = out[row:row + m].double().cpu().numpy()
+        assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -9 * spread)
+        at, row = at + n, row + m
