@@ -176,3 +176,29 @@ def fp4_expert_ffn(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor
     back[order] = d                                      # rows back to (token, k): the sum below has a fixed order
     share = torch.where((experts >= 0) & (experts < gate.experts), weights.float(), 0.0)
     return (back.view(x.shape[0], experts.shape[1], d.shape[1]) * share[..., None]).sum(1).to(x.dtype)
+
+
+def fp4_attention(x: torch.Tensor, qkv: B.Fp4Tensor, proj: B.Fp4Tensor, cache: B.Kv4Cache, table: torch.Tensor, step: B.PageTables,
+                  heads: int, rotary: Optional[B.Rotary] = None, positions: Optional[torch.Tensor] = None, window: int = 0,
+                  max_new: int = 0, x_amax: Optional[torch.Tensor] = None, out_amax: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The attention part of a decoder layer, both products and the keys and values in 4 bits: x [rows, hidden] (fp16 or bf16)
+    through qkv [(heads + 2 kv_heads) * head_dim, hidden] (rows of q, then of k, then of v), rotated, k and v put into the layer's
+    `cache`, attention over it, and through proj [hidden, heads * head_dim].
+    `step` and `table`: what binding.page_tables wrote for the step, once for all layers.  positions: int32 [rows] or
+    [axes, rows] where they are not step.positions.  window, max_new: as for binding.kv4_attention.  x_amax, out_amax: the
+    largest magnitudes that calibration found, of x and of the attention's results.  Rows of no request give zeros.  No host round
+    trip, so that a step can be captured in a graph.  For inference: no gradient passes."""
+    rows, d, kv_heads = x.shape[0], cache.head_dim, cache.kv_heads
+    if qkv.rows != (heads + 2 * kv_heads) * d or proj.cols != heads * d:
+        raise ValueError("fp4_attention: the weights do not match the cache's heads")
+    if step.n_rows != rows:
+        raise ValueError("fp4_attention: step was made for another number of rows")
+    q, k, v = B.fp4_linear(x, qkv, x_amax=x_amax, status=status).view(rows, heads + 2 * kv_heads, d).split((heads, kv_heads, kv_heads), dim=1)
+    if rotary is None:
+        B.kv4_append(k, v, cache, step.slots)
+    else:
+        B.kv4_append(k, v, cache, step.slots, q=q, rotary=rotary, positions=step.positions if positions is None else positions, q_out=q)
+    o = torch.zeros(rows, heads, d, dtype=x.dtype, device=x.device)      # rows of no request stay zero
+    B.kv4_attention(q, cache, table, step.lengths, step.offsets, window=window, max_new=max_new, out=o, status=status)
+    return B.fp4_linear(o.view(rows, heads * d), proj, x_amax=out_amax, status=status)

@@ -313,3 +313,20 @@ def test_many_rows_that_see_nothing_between_rows_that_do():
         got = out[row:row + m].double().cpu().numpy()
         assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -9 * spread)
         at, row = at + n, row + m
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 8, 64), (16, 2, 128), (8, 1, 256)])
+def test_a_hint_that_is_too_small(heads, kv_heads, dim):
+    """max_new picks kernels; requests with more rows are worked on all the same."""
+    b = Batch([300, 1000, 40, 5], [300, 77, 3, 1], heads, kv_heads, dim, seed=14)
+    for hint in (1, 2, 20):
+        _against(b, max_new=hint)
+        _against(b, max_new=hint, window=60)
+
+
+def test_many_requests_with_prompts_among_them():
+    """More requests than the kernel for many rows takes, so that the one for few rows has them all."""
+    n = 3600
+    lengths, new = [3 + i % 5 for i in range(n)], [1] * n
+    lengths[7], new[7], lengths[3599], new[3599] = 300, 200, 90, 90
+    _against(Batch(lengths, new, 2, 1, 64, seed=15))
