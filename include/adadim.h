@@ -514,8 +514,8 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
 /*
  * Attention of new tokens over the cache.  Request i has the query rows offsets[i] .. offsets[i+1]-1 (int32
  * [n_requests + 1], not falling, within 0 .. n_rows) and lengths[i] tokens in the cache, its new ones the last of them.
- *   qo         host: qo[0] queries, qo[1] results, [n_rows][q_heads][head_dim], dtype ADADIM_F16 or ADADIM_BF16; query head h reads key head
- *              h / (q_heads / kv_heads).  Rows of no request are not written.
+ *   qo         host: qo[0] queries, qo[1] results (may be the queries' place), [n_rows][q_heads][head_dim], dtype ADADIM_F16 or
+ *              ADADIM_BF16; query head h reads key head h / (q_heads / kv_heads).  Rows of no request are not written.
  *   scale      of the products q k
  *   causal     query row j of n sees positions up to lengths - n + j; 0: all
  *   window     > 0: of those only positions above lengths - n + j - window
@@ -526,7 +526,7 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
  * The values that the codes stand for are used as they are (exact in fp16); queries too (bf16 ones times a power of
  * two in fp16), weights are rounded to fp16, sums are binary32, and results are rounded once.  A table entry outside the
  * cache: its tokens are left out, (device) ADADIM_ERR_PAGES.  Offsets that fall or leave 0 .. n_rows, lengths outside
- * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads < 2^31.
+ * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads and width * page up to 2^31 - 4096.
  */
 ADADIM_API int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
                         const int32_t* lengths, int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width,

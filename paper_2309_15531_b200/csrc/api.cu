@@ -60,6 +60,7 @@ int check_quant_params(int bits, int group, bool allow_256) {
 constexpr int64_t kInt32Max = 0x7fffffff;
 
 bool kv4_page_ok(int page) { return page >= kv4::kMinPage && page <= kv4::kMaxPage && (page & (page - 1)) == 0; }
+constexpr int64_t kKv4Most = kInt32Max - 4095;   // tokens of a request, rows of a head
 int check_kv4_sizes(const adadim_kv4cache& c) {
   if (!kv4_page_ok(c.page) || c.kv_heads < 1 || c.kv_heads > (1 << 16)) return ADADIM_ERR_PARAM;
   if (c.head_dim < 16 || c.head_dim > 256 || c.head_dim % 16 != 0) return ADADIM_ERR_PARAM;
@@ -566,8 +567,9 @@ int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int 
   if (dtype != ADADIM_F16 && dtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
   if (q_heads < 1 || q_heads > (1 << 16) || q_heads % cache->kv_heads != 0) return ADADIM_ERR_PARAM;
   if (window < 0 || max_new < 0) return ADADIM_ERR_PARAM;
-  if (n_rows < 0 || n_rows * q_heads > kInt32Max || n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width ||
-      width * cache->page > kInt32Max)
+  // the kernels count tokens and rows in 32 bits, up to a chunk or a tile beyond the last one
+  if (n_rows < 0 || n_rows > kKv4Most / q_heads || n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width ||
+      width > kKv4Most / cache->page)
     return ADADIM_ERR_SHAPE;
   if (n_rows == 0 || n_requests == 0) return ADADIM_OK;
   if (qo == nullptr || qo[0].p == nullptr || qo[1].p == nullptr || offsets == nullptr || lengths == nullptr ||
@@ -590,7 +592,7 @@ int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int 
   a.cache = kv4::cache_of(*cache);
   a.scale = scale;
   a.causal = causal != 0;
-  a.window = static_cast<int>(window > kInt32Max / 2 ? 0 : window);   // longer than any cache
+  a.window = static_cast<int>(window >= width * cache->page ? 0 : window);   // as long as any request may be
   a.status_dev = status_dev;
   a.workspace = static_cast<char*>(workspace);
   return kv4_attention_launch(a, dtype, max_new == 0 || max_new > n_rows ? n_rows : max_new, static_cast<cudaStream_t>(cuda_stream));

@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(TableParams 
       paged &= had + k < p.width && page >= 0;
     }
   }
-  for (int r = blockIdx.x * kTableRows + tid; r < min(static_cast<int64_t>(p.rows), (blockIdx.x + int64_t{1}) * kTableRows); r += kTableThreads) {
+  for (int64_t r = int64_t{blockIdx.x} * kTableRows + tid; r < min(static_cast<int64_t>(p.rows), (blockIdx.x + int64_t{1}) * kTableRows); r += kTableThreads) {
     int request = -1, position = 0, slot = -1;
     if (r < all_a) {
       int lo = 0, hi = p.n;                                          // before[lo] <= r < before[hi]

@@ -330,3 +330,17 @@ def test_many_requests_with_prompts_among_them():
     lengths, new = [3 + i % 5 for i in range(n)], [1] * n
     lengths[7], new[7], lengths[3599], new[3599] = 300, 200, 90, 90
     _against(Batch(lengths, new, 2, 1, 64, seed=15))
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(300, 1, 64), (129, 1, 128), (40, 2, 256)])
+def test_more_heads_of_a_key_head_than_rows_of_a_tile(heads, kv_heads, dim):
+    b = Batch([200, 33, 1], [3, 1, 1], heads, kv_heads, dim, seed=16)
+    for more in (dict(), dict(max_new=3), dict(window=20), dict(causal=False)):
+        _against(b, **more)
+
+
+def test_results_in_the_queries_place():
+    for new in ([1, 1, 1], [200, 40, 3]):
+        b = Batch([700, 40, 3], new, 8, 2, 128, seed=17)
+        want = b.run()
+        assert torch.equal(b.run(out=b.q), want)

@@ -92,3 +92,11 @@ def test_rotary_of_bad_sizes():
             B.Rotary(bad)
     with pytest.raises(ValueError):
         B.Rotary.of(64, sections=(16, 8), device="cpu")
+
+
+@pytest.mark.parametrize("change", [
+    dict(rows=1 << 60), dict(rows=(1 << 29) - 1000), dict(width=1 << 60, ldt=1 << 60), dict(width=(1 << 27) - 1, ldt=1 << 27)])
+def test_attention_over_more_than_32_bits_hold(change):
+    """Products that would wrap, and rows and tokens whose numbers leave no room for a tile or a chunk beyond the last one."""
+    assert attention(**change) == SHAPE
+    assert attention(rows=1 << 28, width=1 << 26, ldt=1 << 26, ws=None) == NULL
