@@ -344,3 +344,19 @@ def test_results_in_the_queries_place():
         b = Batch([700, 40, 3], new, 8, 2, 128, seed=17)
         want = b.run()
         assert torch.equal(b.run(out=b.q), want)
+
+
+@pytest.mark.parametrize("dim,dtype", [(128, BF16), (64, F16), (80, BF16)])
+def test_rows_that_fill_a_part_of_a_tile(dim, dtype):
+    """Query rows a key head around the halves and quarters of a tile, over many chunks, few, and none; some values are NaN."""
+    new = [17, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 129, 160, 161, 200, 257, 40]
+    lengths = [n + (900, 0, 130, 300)[i % 4] for i, n in enumerate(new)]
+    b = Batch(lengths, new, 2, 2, dim, dtype=dtype, seed=18)
+    _against(b)
+    _against(b, window=100)
+    _against(b, causal=False)
+    b = Batch([5000, 129, 257], [20, 64, 10], 8, 2, dim, dtype=dtype, seed=19)
+    _against(b)
+    b.v[100, 0, 3] = float("nan")
+    B.kv4_append(b.k, b.v, b.cache, b.slots)
+    _against(b)
