@@ -538,95 +538,94 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         const int page = table[tok >> cache.page_log2];
         return page < 0 || page >= cache.n_pages ? -1 : page;
       };
-      uint32_t kc[kWords], vc[kWords], ks[kWords / 8], vs[kWords / 8];
-      auto load = [&](int64_t row, uint32_t (&codes)[kWords], uint32_t (&scales)[kWords / 8]) {
-        const uint4* c = reinterpret_cast<const uint4*>(cache.codes + row * (HELD / 2));
-#pragma unroll
-        for (int k = 0; k < kWords / 4; ++k) {
-          const uint4 a = __ldg(c + k);
-          codes[4 * k] = a.x; codes[4 * k + 1] = a.y; codes[4 * k + 2] = a.z; codes[4 * k + 3] = a.w;
+      // Turns: keys of chunk 0, of 1, values of 0, keys of 2, values of 1, ..: keys run a chunk ahead, so that the scores of the next
+      // tokens never wait behind the values of these.  Every turn is the same short loop; the codes of the next two are on their way.
+      struct Turn { int chunk; bool values; };
+      struct Codes { uint32_t w[kWords], s[kWords / 8]; int page; };
+      auto after = [&](const Turn& a) {
+        if (a.values) return a.chunk + 2 < steps ? Turn{a.chunk + 2, false} : Turn{a.chunk + 1, true};
+        return a.chunk > 0 ? Turn{a.chunk - 1, true} : steps > 1 ? Turn{1, false} : Turn{0, true};
+      };
+      int soon = page_of(0), page = -2, before = -2, keys = -1;      // pages of the next keys' chunk, of the last one's, of the one's before; which the last one is
+      auto fetch = [&](const Turn& a, Codes& to) {
+        to.page = -2;
+        if (a.chunk < steps) {
+          if (!a.values) {
+            before = page;
+            page = soon;
+            keys = a.chunk;
+            soon = page_of(a.chunk + 1);
+          }
+          to.page = keys == a.chunk ? page : before;
         }
-        const uint32_t* f = reinterpret_cast<const uint32_t*>(cache.scales + row * (HELD / 16));
+        if (to.page >= 0) {
+          const int64_t row = cache_row(cache, to.page, 0, x.head, (tok0 + a.chunk * kChunk) & ((1 << cache.page_log2) - 1)) + (a.values ? gap : 0);
+          const uint4* c = reinterpret_cast<const uint4*>(cache.codes + row * (HELD / 2));
 #pragma unroll
-        for (int k = 0; k < kWords / 8; ++k) scales[k] = __ldg(f + k);
+          for (int k = 0; k < kWords / 4; ++k) {
+            const uint4 u = __ldg(c + k);
+            to.w[4 * k] = u.x; to.w[4 * k + 1] = u.y; to.w[4 * k + 2] = u.z; to.w[4 * k + 3] = u.w;
+          }
+          const uint32_t* f = reinterpret_cast<const uint32_t*>(cache.scales + row * (HELD / 16));
+#pragma unroll
+          for (int k = 0; k < kWords / 8; ++k) to.s[k] = __ldg(f + k);
+        } else {                                                     // a token that is not there
+#pragma unroll
+          for (int k = 0; k < kWords; ++k) to.w[k] = 0;
+#pragma unroll
+          for (int k = 0; k < kWords / 8; ++k) to.s[k] = 0;
+        }
       };
-      auto zero = [&](uint32_t (&codes)[kWords], uint32_t (&scales)[kWords / 8]) {
+      Turn ta = {0, false}, tb = after(ta), tc = after(tb);
+      Codes a, b, c;
+      fetch(ta, a);
+      fetch(tb, b);
+      bool ok = true;
+#pragma unroll 1
+      for (int turn = 0; turn < 2 * steps; ++turn) {
+        fetch(tc, c);
+        const int64_t n = seen + ta.chunk;                           // of all
+        const int stage = static_cast<int>(n & 1), slot = static_cast<int>(n & (kRing - 1));
+        if (!ta.values) {
+          const uint32_t out = __ballot_sync(0xffffffffu, a.page == -1);
+          paged &= a.page != -1;
+          if (lane == 0) sh.hidden[slot][sub] = out;
+        } else {
+          // blocks of values that are NaN: noted, and zero in the product
+          uint32_t bits = 0;
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) codes[k] = 0;
-#pragma unroll
-        for (int k = 0; k < kWords / 8; ++k) scales[k] = 0;
-      };
-      auto row_of = [&](int page, int it) { return cache_row(cache, page, 0, x.head, (tok0 + it * kChunk) & ((1 << cache.page_log2) - 1)); };
-      auto put = [&](const uint32_t (&codes)[kWords], const uint32_t (&scales)[kWords / 8], char* to) {
+          for (int k = 0; k < kWords / 8; ++k) {
+            const uint32_t bad = (((a.s[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+            a.s[k] &= ~(bad * 0xffu);
+            bits |= ((bad & 1u) | (bad >> 7 & 2u) | (bad >> 14 & 4u) | (bad >> 21 & 8u)) << 4 * k;
+          }
+          const bool any = __any_sync(0xffffffffu, bits != 0);
+          if (any) sh.nan_of[slot][t] = static_cast<uint8_t>(bits);
+          if (lane == 0) sh.nan_any[slot][sub] = any;
+        }
+        ok = ptx::mbar_wait_warp(ta.values ? &sh.v_empty[stage] : &sh.k_empty[stage], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, dead, status);
+        if (!ok) break;
+        char* const to = row_at + (ta.values ? Mm::kV : Mm::kK) + stage * Mm::kBytes;
 #pragma unroll
         for (int k = 0; k < kWords; k += 4) {
-          const __half2 two = scales_of(scales[k >> 3] >> (k & 4) * 4);          // two blocks, four words
+          const __half2 two = scales_of(a.s[k >> 3] >> (k & 4) * 4);             // two blocks, four words
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const __half2 s = e < 2 ? __low2half2(two) : __high2half2(two);
             __half2 v[4];
-            values8(codes[k + e], v);
+            values8(a.w[k + e], v);
             const uint4 w = make_uint4(half2_bits(__hmul2(v[0], s)), half2_bits(__hmul2(v[1], s)), half2_bits(__hmul2(v[2], s)), half2_bits(__hmul2(v[3], s)));
             *reinterpret_cast<uint4*>(to + ((k + e) >> 3) * Mm::kBox + ((((k + e) & 7) ^ (t & 7)) << 4)) = w;
           }
         }
-      };
-      // Keys run a chunk ahead of values: keys of chunk it + 1, then values of chunk it, so that the scores of the next tokens
-      // never wait behind the values of these.  Each one's next codes are asked for when the present ones are used up.
-      int here = page_of(0), soon = page_of(1), later = page_of(2);  // pages of chunks it, it + 1, it + 2
-      if (here >= 0) {
-        const int64_t row = row_of(here, 0);
-        load(row, kc, ks);
-        load(row + gap, vc, vs);
-      }
-      auto keys = [&](int64_t n, int page) {                         // chunk n of all, whose codes are there
-        const int stage = static_cast<int>(n & 1), slot = static_cast<int>(n & (kRing - 1));
-        const uint32_t out = __ballot_sync(0xffffffffu, page == -1);
-        paged &= page != -1;
-        if (lane == 0) sh.hidden[slot][sub] = out;
-        if (page < 0) zero(kc, ks);                                  // a token that is not there
-        if (!ptx::mbar_wait_warp(&sh.k_empty[stage], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, dead, status)) return false;
-        put(kc, ks, row_at + Mm::kK + stage * Mm::kBytes);
-        return true;
-      };
-      auto given = [&](uint64_t* bar) {
         ptx::fence_proxy_async();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar);
-      };
-      bool ok = true;
-#pragma unroll 1
-      for (int it = -1; ok && it < steps; ++it) {
-        if (it + 1 < steps) {
-          ok = keys(seen + it + 1, it < 0 ? here : soon);
-          if (!ok) break;
-          const int next = it < 0 ? soon : later;                    // page of chunk it + 2
-          if (next >= 0) load(row_of(next, it + 2), kc, ks);
-          given(&sh.k_full[(seen + it + 1) & 1]);
-        }
-        if (it < 0) continue;
-        const int64_t n = seen + it;
-        const int stage = static_cast<int>(n & 1), slot = static_cast<int>(n & (kRing - 1));
-        if (here < 0) zero(vc, vs);
-        // blocks of values that are NaN: noted, and zero in the product
-        uint32_t bits = 0;
-#pragma unroll
-        for (int k = 0; k < kWords / 8; ++k) {
-          const uint32_t bad = (((vs[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-          vs[k] &= ~(bad * 0xffu);
-          bits |= ((bad & 1u) | (bad >> 7 & 2u) | (bad >> 14 & 4u) | (bad >> 21 & 8u)) << 4 * k;
-        }
-        const bool any = __any_sync(0xffffffffu, bits != 0);
-        if (any) sh.nan_of[slot][t] = static_cast<uint8_t>(bits);
-        if (lane == 0) sh.nan_any[slot][sub] = any;
-        ok = ptx::mbar_wait_warp(&sh.v_empty[stage], (static_cast<uint32_t>(n >> 1) & 1u) ^ 1u, dead, status);
-        if (!ok) break;
-        put(vc, vs, row_at + Mm::kV + stage * Mm::kBytes);
-        if (soon >= 0) load(row_of(soon, it + 1) + gap, vc, vs);
-        given(&sh.v_full[stage]);
-        here = soon;
-        soon = later;
-        later = page_of(it + 3);
+        if (lane == 0) ptx::mbar_arrive(ta.values ? &sh.v_full[stage] : &sh.k_full[stage]);
+        a = b;
+        b = c;
+        ta = tb;
+        tb = tc;
+        tc = after(tc);
       }
       seen += steps;
       if (!ok) break;
