@@ -118,6 +118,7 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
 int kv4_attention_launch(const Kv4Attention& a, int dtype, int64_t max_new, cudaStream_t st);
 // ctas, tile_rows: what the joining kernel has to know.  chained: behind the kernel for many rows
 int kv4_few_launch(const Kv4Attention& a, int dtype, int64_t max_new, bool chained, int& ctas, int& tile_rows, cudaStream_t st);
+bool kv4_few_suits(const Kv4Attention& a, int64_t max_new);
 size_t kv4_few_workspace(int held);
 int kv4_many_launch(const Kv4Attention& a, int dtype, int& ctas, int& tile_rows, cudaStream_t st);
 size_t kv4_many_workspace(int held);

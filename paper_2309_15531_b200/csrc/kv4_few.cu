@@ -3,9 +3,11 @@
 //   o = softmax(scale q K^T) V,  K and V = code * scale * 2^t
 //
 // Bound by the cache's bytes, 9/16 of a byte an element; what it executes comes next (a byte holds two elements, each of which
-// has to become an fp16 number times its block's scale).  So codes go from memory into the registers that the matrix instruction
-// (m16n8k16) takes, with no shared memory between: tokens are the M side of S^T = K Q^T and channels that of O^T = V^T P^T, so that eight
-// query rows (a group of heads, a few tokens) fill the N side.  The order of the channels inside a product is free: lane
+// has to become an fp16 number times its block's scale).  So a warp has 32 tokens' codes at a time in a ring of three steps in shared memory,
+// as they lie in the cache, brought by bulk copies (fragments loaded straight from memory: 394 us where this takes 140), and
+// takes them from there into the registers of the matrix instruction (m16n8k16), each byte once: tokens are the M side of
+// S^T = K Q^T and channels that of O^T = V^T P^T, so that eight query rows (a group of heads, a few tokens) fill the N side, which
+// a tile of tcgen05 with 128 rows of queries would leave empty.  The order of the channels inside a product is free: lane
 // (g, c) = (lane / 4, lane % 4) takes held / 4 neighbouring channels of a key and uses them over all steps, and of a value held / 8
 // neighbouring channels of four tokens; q and o follow that order.  S^T comes out with tokens down and is turned
 // into the B side of the second product by movmatrix.
@@ -17,6 +19,9 @@
 // The work of all requests, key heads and row tiles is laid out on one line and cut into equal parts, one a CTA, whatever the requests'
 // lengths; the four warps of a CTA take 32 tokens each of a chunk of 128.  What is cut is joined by a second kernel in the order of
 // the tokens, so that results do not depend on timing.  Small calls go to clusters instead (see kv4_few_kernel).
+//
+// 64 requests of up to 16384 tokens, 8 key heads of 128 channels with 8 query heads each: 140 us, 649 MB, 4.6 TB/s, 0.71 of a copy's
+// rate; two thirds of the issue slots are taken, half of the ALU's, and a CTA's last piece and the join come on top.  One token over 4096: 11.4 us.
 #include "kv4_line.cuh"
 
 namespace adadim {
@@ -29,7 +34,7 @@ constexpr int kFewThreads = 128, kFewWarps = 4, kStep = 32, kChunk = kStep * kFe
 // What a unit costs beside its tokens, in tokens: with 300, 640, 1000 and 1500, 64 requests of up to 16384 tokens take 171, 150, 140 and 146 us.
 constexpr int kFewCost = 1000;
 constexpr int kLeastPart = 256;                  // a CTA's part is no smaller
-constexpr int kStages = 3;                       // steps of a warp on their way or being worked on
+constexpr int kStages = 3;                       // steps of a warp on their way or being worked on (2 and 4: the same time within 2 us of 150)
 // CTAs of an SM: what registers (a thread's 128, 168 or 255) and the ring of steps leave room for
 constexpr int few_per_sm(int held, int nt) { return held == 256 ? 2 : held == 128 && nt == 2 ? 3 : 4; }
 constexpr int few_ctas(int held, int nt) { return kSms * few_per_sm(held, nt); }
@@ -543,16 +548,21 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
   ptx::pdl_wait();                                                   // no earlier than the kernel before it
 }
 
-// Whether a call's units go to clusters, and of how many CTAs: where there is little to read altogether (by what the table and the
-// window allow: 2^20 tokens of key heads are 25 us), so that unequal lengths cost less than the second launch that joins cut units,
-// and enough units, or short ones, that clusters of up to eight CTAs find the SMs enough to do.
+// A call's units, and the tokens that the table and the window allow each.
+int64_t units_of(const Kv4Attention& a, int tile_rows, int64_t max_new) {
+  return (max_new * a.group + tile_rows - 1) / tile_rows * a.n_requests * a.cache.kv_heads;
+}
+int64_t span_of(const Kv4Attention& a, int64_t max_new) {
+  const int64_t span = a.width << a.cache.page_log2;
+  return a.causal && a.window > 0 && a.window + max_new + kStep < span ? a.window + max_new + kStep : span;
+}
+// Whether a call's units go to clusters, and of how many CTAs: where there is little to read altogether (2^20 tokens of key heads are
+// 25 us), so that unequal lengths cost less than the second launch that joins cut units, and enough units, or short ones, that clusters of
+// up to eight CTAs find the SMs enough to do.
 int cluster_of(const Kv4Attention& a, int tile_rows, int ctas, int64_t max_new, int& tiles) {
-  const int64_t rows = max_new * a.group, t = (rows + tile_rows - 1) / tile_rows;
-  const int64_t units = t * a.n_requests * a.cache.kv_heads;
-  int64_t span = a.width << a.cache.page_log2;
-  if (a.causal && a.window > 0 && a.window + max_new + kStep < span) span = a.window + max_new + kStep;
+  const int64_t units = units_of(a, tile_rows, max_new), span = span_of(a, max_new);
   if (units > 4 * ctas || units * span > (int64_t{1} << 20) || (units < 16 && span > 8192)) return 0;
-  tiles = static_cast<int>(t);
+  tiles = static_cast<int>((max_new * a.group + tile_rows - 1) / tile_rows);
   int size = 1;
   while (size < 8 && units * size * 2 <= ctas && span > kChunk * size) size *= 2;
   return size;
@@ -591,6 +601,13 @@ int few_type(const Kv4Attention& a, int64_t max_new, bool chained, int& ctas, in
 
 }  // namespace
 
+// Many rows, but few units of this kernel over few tokens, which clusters are done with before the other kernel's tiles are set up: 40
+// tokens of 32 heads over themselves 9.7 us against 38, eight such prompts 22 against 38, 128 rows of 8 key heads over 8192 (2^19 tokens) 38
+// against 46, four times 64 rows over as many (2^20) 55 against 47.
+bool kv4_few_suits(const Kv4Attention& a, int64_t max_new) {
+  int tiles;
+  return units_of(a, 16, max_new) * span_of(a, max_new) <= (int64_t{1} << 19) && cluster_of(a, 16, few_ctas(a.cache.held, 2), max_new, tiles) > 0;
+}
 size_t kv4_few_workspace(int held) {
   const size_t one = partials_bytes(few_ctas(held, 1), 8, held), two = held < 256 ? partials_bytes(few_ctas(held, 2), 16, held) : 0;
   return one > two ? one : two;

@@ -11,6 +11,7 @@ HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}       # half a ste
 class Batch:
     """Requests with `lengths` tokens in a cache, of which the last `new` are queries.  Pages in random order, some pages
     of nobody, memory that nothing was written to full of NaN scales."""
+    more_tokens = 0                                      # that tables have room for: a longer reach takes small calls to other kernels
 
     def __init__(self, lengths, new, heads, kv_heads, dim, page=16, dtype=torch.bfloat16, seed=0, amax=True, loud=4.0, gap=0,
                  width_more=1, k=None, v=None):
@@ -18,6 +19,8 @@ class Batch:
         self.lengths_, self.new_, self.heads, self.kv_heads, self.dim, self.page = list(lengths), list(new), heads, kv_heads, dim, page
         counts = [-(-n // page) for n in lengths]
         self.n_pages, width = sum(counts) + 3, max(counts + [0]) + width_more
+        if len(lengths) <= 300:
+            width += self.more_tokens // page
         order = torch.randperm(self.n_pages, generator=g).tolist()
         table, at = torch.full((len(lengths), width), -7, dtype=torch.int32), 0
         for i, c in enumerate(counts):

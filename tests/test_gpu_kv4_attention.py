@@ -12,6 +12,12 @@ pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
 
 
+@pytest.fixture(autouse=True, params=[0, 1 << 20], ids=["narrow", "wide"])
+def reach(request, monkeypatch):
+    """Every test with tables that just hold the tokens, and with tables for so many that no call counts as a small one."""
+    monkeypatch.setattr(Batch, "more_tokens", request.param)
+
+
 def _against(b, **more):
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     out = torch.full(b.q.shape, 77.0, dtype=b.q.dtype, device="cuda")
