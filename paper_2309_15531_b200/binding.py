@@ -728,7 +728,8 @@ def page_tables(past: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free
     """Block tables and slot maps of a step: request i holds past[i] tokens and gets new[i] more (int32 on the device).  The
     pages this needs are taken from free_pages in order, from place cursor[0] on (None: 0), and written to the request's
     row of table int32 [requests, width].  `rows` (or out.n_rows): new tokens of the step, or more: rows behind the last one get
-    slot -1, request -1.  out.cursor: where the next step goes on; pass it as `cursor` with another `out`, or a copy."""
+    slot -1, request -1.  out.cursor: where the next step goes on, out.lengths: what its past is; pass them with another `out`, or
+    copies."""
     dev = table.get_device()
     n, (t_rows, width) = _i32(past, dev).numel(), table.shape
     if _i32(new, dev).numel() != n or t_rows != n:

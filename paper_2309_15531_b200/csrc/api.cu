@@ -523,6 +523,11 @@ int adadim_page_tables(const int32_t* past, const int32_t* fresh, int64_t n_requ
   if (n_requests > 0 && (past == nullptr || fresh == nullptr || lengths == nullptr || (width > 0 && table == nullptr))) return ADADIM_ERR_NULL;
   if (n_free > 0 && free_pages == nullptr) return ADADIM_ERR_NULL;
   if (rows > 0 && (requests == nullptr || positions == nullptr || slots == nullptr)) return ADADIM_ERR_NULL;
+  // some CTAs still read what others have written by then
+  const auto apart = [](const int32_t* a, int64_t n, const int32_t* b, int64_t m) { return a + n <= b || b + m <= a; };
+  if (!apart(past, n_requests, lengths, n_requests) || !apart(fresh, n_requests, lengths, n_requests) ||
+      !apart(past, n_requests, offsets, n_requests + 1) || !apart(fresh, n_requests, offsets, n_requests + 1))
+    return ADADIM_ERR_PARAM;
   return page_tables_launch(past, fresh, static_cast<int>(n_requests), page, table, ldt, width, free_pages, static_cast<int>(n_free),
                             cursor, static_cast<int>(rows), lengths, offsets, requests, positions, slots, next, status_dev,
                             static_cast<cudaStream_t>(cuda_stream));

@@ -100,3 +100,11 @@ def test_attention_over_more_than_32_bits_hold(change):
     """Products that would wrap, and rows and tokens whose numbers leave no room for a tile or a chunk beyond the last one."""
     assert attention(**change) == SHAPE
     assert attention(rows=1 << 28, width=1 << 26, ldt=1 << 26, ws=None) == NULL
+
+
+@pytest.mark.parametrize("change", [
+    dict(past=4096, lengths=4096), dict(past=4096, lengths=4100), dict(past=4100, lengths=4096), dict(fresh=4096, lengths=4096),
+    dict(past=4096, offsets=4096), dict(fresh=4104, offsets=4096)])
+def test_tables_that_would_be_written_over_what_is_read(change):
+    apart = dict(past=1024, fresh=1280, lengths=1536, offsets=1792)
+    assert tables(**{**apart, **change}) == PARAM
