@@ -14,7 +14,7 @@
 //
 // code * scale has six significant bits and is exact in fp16; 2^t goes into the factor of the scores and of the result.
 // Running maximum and sum per row, the maximum taken anew only where a score passes it by more than 2^8, which fp16 weights
-// bear (they are rounded to 11 bits and lie below 2^8).
+// bear (see kLift); the sums are those of the rounded weights.
 //
 // The work of all requests, key heads and row tiles is laid out on one line and cut into equal parts, one a CTA, whatever the requests'
 // lengths; the four warps of a CTA take 32 tokens each of a chunk of 128.  What is cut is joined by a second kernel in the order of
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           top[u][k] = fmaxf(fmaxf(sc[0][u][k], sc[0][u][k + 2]), fmaxf(sc[1][u][k], sc[1][u][k + 2]));
-          grows |= top[u][k] > m[u][k] + 8.0f;
+          grows |= top[u][k] > m[u][k] + kGrowth;
         }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
       uint32_t pb[2][NT][2];
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        const float base0 = m[u][0] == -INFINITY ? 0.0f : m[u][0], base1 = m[u][1] == -INFINITY ? 0.0f : m[u][1];
+        const float base0 = m[u][0] == -INFINITY ? 0.0f : m[u][0] - kLift, base1 = m[u][1] == -INFINITY ? 0.0f : m[u][1] - kLift;
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
           pb[hh][u][0] = transposed(half2_bits(__floats2half2_rn(exp2_fast(sc[hh][u][0] - base0), exp2_fast(sc[hh][u][1] - base1))));

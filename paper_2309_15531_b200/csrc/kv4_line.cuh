@@ -13,6 +13,10 @@ constexpr int kSms = 148;
 constexpr int kFewRows = 32, kFewBeside = 16;
 constexpr int kManyRequests = 3500;              // of a call, for the many-row kernel
 constexpr float kLog2e = 1.4426950408889634f;
+// Weights are fp16, 2^7 times what they are to the row's reference: its largest score when it was last taken, which is done where a score
+// passes it by more than 2^8, so that they end at 2^15.  So they have their 11 bits down to 2^-21 of the reference's, below that
+// fp16's least step, 2^-31 of it, and a reference's own weight is in every row's sum.  (Without the 2^7, 2^-14 and 2^-24.)
+constexpr float kGrowth = 8.0f, kLift = 7.0f;
 
 __host__ __device__ constexpr size_t whole256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
