@@ -258,6 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       const int all_hi = p.causal ? min(x.length, own + ta + 1) : x.length, all_lo = p.window > 0 ? own + tb - p.window + 1 : 0;
       // the row of queries as fp16 into shared memory
       float factor;
+      bool fine;                                                     // the row's query and the scale are finite
       {
         // A warp copies its 32 rows to shared memory as they are, neighbouring lanes a row's neighbouring channels; then each thread
         // goes through its own row there.  Short loops: what is gone through once costs what it takes to fetch the instructions.
@@ -293,16 +294,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         const float f = exp2_int(e);
         // a negative scale turns the queries' signs, so that the factor of the scores is not negative
         const uint32_t sign = p.scale < 0.0f ? 0x80008000u : 0u;
-        if (!std::is_same<T, __half>::value || sign != 0) {
+        fine = query_fine<T>(most) && p.scale == p.scale;
+        if (!std::is_same<T, __half>::value || sign != 0 || !fine) {
 #pragma unroll 4
           for (int k = 0; k < HELD / 8; ++k) {
             const uint4 v = *piece_of_row(k);
-            *piece_of_row(k) = make_uint4(query_bits<T>(v.x, f) ^ sign, query_bits<T>(v.y, f) ^ sign, query_bits<T>(v.z, f) ^ sign,
-                                          query_bits<T>(v.w, f) ^ sign);
+            *piece_of_row(k) = !fine ? make_uint4(0u, 0u, 0u, 0u)
+                                     : make_uint4(query_bits<T>(v.x, f) ^ sign, query_bits<T>(v.y, f) ^ sign, query_bits<T>(v.z, f) ^ sign,
+                                                  query_bits<T>(v.w, f) ^ sign);
           }
         }
-        // (not zero, so that what is hidden stays at minus infinity)
-        factor = query_fine<T>(most) && p.scale == p.scale ? fmaxf(ldexpf(fabsf(p.scale) * kLog2e, t_k - e), 1.2e-38f) : __int_as_float(0x7fffffff);
+        // Neither zero nor NaN, so that what is hidden stays at minus infinity.  A row that is not fine has scores of zero, and so a maximum if
+        // it sees anything; then it is NaN.
+        factor = fine ? fmaxf(ldexpf(fabsf(p.scale) * kLog2e, t_k - e), 1.2e-38f) : 1.2e-38f;
       }
       // the second tile's last result has been taken in
       if (i == 1 && twins > 0 && !ptx::mbar_wait_warp(&sh.twin_free, (twins - 1) & 1u, dead, status)) break;
@@ -422,6 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         }
       }
       if (!ok) break;
+      if (!fine && m != -INFINITY) l = __int_as_float(0x7fffffff);
       // the row's result
       const bool some = last >= 0;
       if (some) {
