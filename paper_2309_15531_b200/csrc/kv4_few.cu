@@ -191,7 +191,8 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
     auto fetch = [&](int it, int to) {
       if ((it & 15) == 0) {
         const int64_t tok = first + static_cast<int64_t>(it + (lane >> 1)) * stride + (lane & 1) * 16;
-        pages = tok < key_hi ? p.table[request * p.ldt + (tok >> cache.page_log2)] : -2;
+        // a page whose last token lies behind every row's window is not looked at
+        pages = tok < key_hi && (tok | ((1 << cache.page_log2) - 1)) >= x.seen_lo ? p.table[request * p.ldt + (tok >> cache.page_log2)] : -2;
         if (pages != -2 && (pages < 0 || pages >= cache.n_pages)) { pages = -2; paged = false; }
       }
       const int pg0 = __shfl_sync(0xffffffffu, pages, (it & 15) * 2), pg1 = __shfl_sync(0xffffffffu, pages, (it & 15) * 2 + 1);

@@ -141,7 +141,7 @@ __device__ __forceinline__ void sum_line(const Kv4Attention& p, int tile_rows, i
 struct Piece {
   Request r;
   int request, head, tile, rows;       // rows of the tile
-  int key_lo, chunks;                  // first token that some row sees (a multiple of 32), chunks of all of them
+  int seen_lo, key_lo, chunks;         // first token that some row sees, that rounded down to a multiple of 32, chunks of all of them
   int c0, c1;                          // this piece's chunks
   bool starts, ends;                   // the unit begins, ends in it
 };
@@ -174,7 +174,8 @@ __device__ __forceinline__ Piece next_piece(const Kv4Attention& p, const int64_t
   x.rows = static_cast<int>(min(static_cast<int64_t>(tile_rows), static_cast<int64_t>(x.r.rows) * p.group - static_cast<int64_t>(t) * tile_rows));
   const int t0 = token_of(p, t * tile_rows), t1 = token_of(p, t * tile_rows + x.rows - 1), own = x.r.length - x.r.rows;
   const int key_hi = p.causal ? max(0, min(x.r.length, own + t1 + 1)) : x.r.length;
-  x.key_lo = p.window > 0 ? max(0, own + t0 - p.window + 1) & ~31 : 0;
+  x.seen_lo = p.window > 0 ? max(0, own + t0 - p.window + 1) : 0;
+  x.key_lo = x.seen_lo & ~31;
   x.chunks = key_hi > x.key_lo ? (key_hi - x.key_lo + chunk - 1) / chunk : 0;
   const int from = begin <= cost ? 0 : static_cast<int>(min(static_cast<int64_t>(x.chunks), (begin - cost + chunk - 1) / chunk));
   const int to = stop <= cost ? 0 : static_cast<int>(min(static_cast<int64_t>(x.chunks), (stop - cost + chunk - 1) / chunk));
@@ -191,7 +192,8 @@ __device__ __forceinline__ Piece whole_unit(const Kv4Attention& p, const Request
   x.head = head;
   x.tile = tile;
   x.rows = static_cast<int>(min(static_cast<int64_t>(tile_rows), static_cast<int64_t>(r.rows) * p.group - static_cast<int64_t>(tile) * tile_rows));
-  x.key_lo = p.window > 0 ? max(0, r.length - r.rows + token_of(p, tile * tile_rows) - p.window + 1) & ~31 : 0;
+  x.seen_lo = p.window > 0 ? max(0, r.length - r.rows + token_of(p, tile * tile_rows) - p.window + 1) : 0;
+  x.key_lo = x.seen_lo & ~31;
   const int hi = key_end(p, x, tile * tile_rows + x.rows - 1);
   x.chunks = hi > x.key_lo ? (hi - x.key_lo + chunk - 1) / chunk : 0;
   x.c0 = 0;

@@ -110,9 +110,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ int same(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
 // A piece as all warps of the CTA take it.  Chunks of tile i: [c0, c1_of[i]), or of those every other one from c0 + i on where both
-// tiles have the same rows.
+// tiles have the same rows; they begin at token key_lo, chunk 0's first.
 struct __align__(16) Job {
-  int first, rows_all, length, request, head, tile, rows, key_lo, c0, c1, c1_of[2], key_hi, starts, ends, none;
+  int first, rows_all, length, request, head, tile, rows, seen_lo, c0, c1, c1_of[2], key_hi, starts, ends, none;
+  __device__ __forceinline__ int key_lo() const { return seen_lo & ~31; }
 };
 constexpr int kJobs = 4;                         // that lie ready
 
@@ -151,7 +152,7 @@ __device__ __forceinline__ Job job_of(const Kv4Attention& p, const Piece& x) {
   j.head = x.head;
   j.tile = x.tile;
   j.rows = x.rows;
-  j.key_lo = x.key_lo;
+  j.seen_lo = x.seen_lo;
   j.c0 = x.c0;
   j.c1 = x.c1;
 #pragma unroll
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         const int slot = static_cast<int>((first_seen + ch - x.c0) & (kRing - 1));
         const uint4 any = *reinterpret_cast<const uint4*>(sh.nan_any[slot]);
         if ((any.x | any.y | any.z | any.w) == 0) return;
-        const int tok = x.key_lo + ch * kChunk;
+        const int tok = x.key_lo() + ch * kChunk;
         for (int k = 0; k < kUnpackWarps; ++k) {
           if (sh.nan_any[slot][k] == 0) continue;
           for (int t = k * 32; t < k * 32 + 32; ++t)
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           uint32_t va[32], vb[32];
           ld32(at_half, va);
           ld32(at_half + 32, vb);
-          const int tok = x.key_lo + ch * kChunk + h * kHalf;
+          const int tok = x.key_lo() + ch * kChunk + h * kHalf;
           const uint2 hid = *reinterpret_cast<const uint2*>(&sh.hidden[slot][2 * h]);
           const bool edge = tok < all_lo || tok + kHalf > all_hi || (hid.x | hid.y) != 0;
           if (h == 0 && last >= 0) note_nans(last);
@@ -544,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
     while (take(x)) {
       taken();
       const int key_hi = x.key_hi, steps = x.c1 - x.c0;
-      const int tok0 = x.key_lo + x.c0 * kChunk + t;                 // this thread's token of the first chunk
+      const int tok0 = x.key_lo() + x.c0 * kChunk + t;                 // this thread's token of the first chunk
       const int32_t* const table = p.table + x.request * p.ldt;
       // its page: -1 outside the cache, -2 none
       auto page_of = [&](int it) -> int {
@@ -561,7 +562,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         if (a.values) return a.chunk + 2 < steps ? Turn{a.chunk + 2, false} : Turn{a.chunk + 1, true};
         return a.chunk > 0 ? Turn{a.chunk - 1, true} : steps > 1 ? Turn{1, false} : Turn{0, true};
       };
-      int soon = page_of(0), page = -2, before = -2, keys = -1;      // pages of the next keys' chunk, of the last one's, of the one's before; which the last one is
+      // (tokens behind every row's window lie in chunk 0 only; their pages are not looked at)
+      int soon = tok0 < x.seen_lo ? -2 : page_of(0), page = -2, before = -2, keys = -1;      // pages of the next keys' chunk, of the last one's, of the one's before; which the last one is
       auto fetch = [&](const Turn& a, Codes& to) {
         to.page = -2;
         if (a.chunk < steps) {
