@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 from collections import namedtuple
+from operator import attrgetter
 import os
 import struct
 from typing import Optional
@@ -706,9 +707,24 @@ def fp4_plan(rows: int, out: int, inp: int, fmt: int, experts: int = 0, quantize
 
 # ---- key-value cache in 4 bits --------------------------------------------------------------------
 
+def _replaceable(name: str) -> property:
+    """A buffer that another of its type, shape and device may replace (one that was loaded, say): later calls take the new one."""
+    at = "_" + name
+
+    def replace(self, t: torch.Tensor) -> None:
+        old = getattr(self, at)
+        if t.dtype != old.dtype or t.shape != old.shape or t.device != old.device or not t.is_contiguous():
+            raise ValueError(f"{type(self).__name__}: {name} of another type, shape, order or device")
+        setattr(self, at, t)
+        self._place()
+    return property(attrgetter(at), replace)
+
+
 class PageTables:
     """What page_tables writes for up to `requests` requests and `rows` new tokens (see include/adadim.h): int32 tensors
     lengths [requests], offsets [requests + 1], requests, positions, slots [rows], cursor [1]."""
+    lengths, offsets, cursor = _replaceable("lengths"), _replaceable("offsets"), _replaceable("cursor")
+    requests, positions, slots = _replaceable("requests"), _replaceable("positions"), _replaceable("slots")
 
     def __init__(self, requests: int, rows: int, device="cuda"):
         if requests < 0 or rows < 0:
@@ -716,9 +732,12 @@ class PageTables:
         def ints(n):
             return torch.zeros(n, dtype=torch.int32, device=device)
         self.n_requests, self.n_rows = requests, rows
-        self.lengths, self.offsets, self.cursor = ints(requests), ints(requests + 1), ints(1)
-        self.requests, self.positions, self.slots = ints(rows), ints(rows), ints(rows)
+        self._lengths, self._offsets, self._cursor = ints(requests), ints(requests + 1), ints(1)
+        self._requests, self._positions, self._slots = ints(rows), ints(rows), ints(rows)
         self.dev = self.offsets.get_device()
+        self._place()
+
+    def _place(self) -> None:
         self._p = [t.data_ptr() for t in (self.lengths, self.offsets, self.requests, self.positions, self.slots, self.cursor)]
 
 
@@ -762,7 +781,9 @@ def page_tables(past: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free
 class Kv4Cache:
     """Keys and values of one attention layer in NVFP4, in n_pages pages of page_size tokens (see include/adadim.h for the
     layout).  k_amax, v_amax: float32[1], the largest magnitudes expected (absmax over calibration chunks; rotation can
-    make a key's sqrt(2) larger); their values are copied, and stay for the cache's life.  None: tensor scale 1."""
+    make a key's sqrt(2) larger); their values are copied, and stay for the cache's life.  None: tensor scale 1.
+    codes, scales and amax (float32[2], or None) may be replaced together, by those of a cache that was saved."""
+    codes, scales = _replaceable("codes"), _replaceable("scales")
 
     def __init__(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, k_amax: Optional[torch.Tensor] = None,
                  v_amax: Optional[torch.Tensor] = None, device="cuda"):
@@ -772,39 +793,71 @@ class Kv4Cache:
         self.n_pages, self.page_size, self.kv_heads, self.head_dim = n_pages, page_size, kv_heads, head_dim
         self.held = 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256
         shape = (n_pages, 2, kv_heads, page_size)
-        self.codes = torch.zeros(*shape, self.held // 2, dtype=torch.uint8, device=device)
-        self.scales = torch.zeros(*shape, self.held // 16, dtype=torch.uint8, device=device)
+        self._codes = torch.zeros(*shape, self.held // 2, dtype=torch.uint8, device=device)
+        self._scales = torch.zeros(*shape, self.held // 16, dtype=torch.uint8, device=device)
         self.dev = self.codes.get_device()
-        self.amax = None
+        self._amax = None
         if k_amax is not None or v_amax is not None:
-            self.amax = torch.zeros(2, dtype=torch.float32, device=device)
+            self._amax = torch.zeros(2, dtype=torch.float32, device=device)
             for at, amax in enumerate((k_amax, v_amax)):
                 if amax is not None:
                     _amax(amax, self.dev)
-                    self.amax[at:at + 1].copy_(amax.reshape(1))
+                    self._amax[at:at + 1].copy_(amax.reshape(1))
+        self._place()
+
+    @property
+    def amax(self) -> Optional[torch.Tensor]:
+        return self._amax
+
+    @amax.setter
+    def amax(self, t: Optional[torch.Tensor]) -> None:
+        if t is not None and (t.dtype != torch.float32 or t.shape != (2,) or t.device != self.codes.device or not t.is_contiguous()):
+            raise ValueError("Kv4Cache: amax is float32[2] on the cache's device, of keys and of values")
+        self._amax = t
+        self._place()
+
+    def _place(self) -> None:
         self._c = Kv4CacheC(self.codes.data_ptr(), self.scales.data_ptr(), self.amax.data_ptr() if self.amax is not None else None,
-                            n_pages, page_size, kv_heads, head_dim)
+                            self.n_pages, self.page_size, self.kv_heads, self.head_dim)
         self._ref = C.byref(self._c)
 
 
 class Rotary:
     """Rotary positions: pair j of a head turns by position * freq[j] on axis axis[j] (None: one axis).  freq [dim / 2] in
     radians a position (kept in binary64), axis [dim / 2] whole numbers; the pair is channels (j, j + dim / 2), or (2 j, 2 j + 1)
-    where `adjacent`.  dim is a multiple of 16; further channels of a head are not turned."""
+    where `adjacent`.  dim is a multiple of 16; further channels of a head are not turned.  freq and axis may be replaced by
+    others of the same length; their values are copied."""
 
     def __init__(self, freq: torch.Tensor, axis: Optional[torch.Tensor] = None, adjacent: bool = False):
         if freq.dim() != 1 or freq.numel() % 8 or not 8 <= freq.numel() <= 128 or not freq.is_cuda:
             raise ValueError("Rotary: freq [dim / 2] on the device, dim a multiple of 16 up to 256")
-        self.dim, self.adjacent, self.axes = 2 * freq.numel(), bool(adjacent), 1
-        self.freq = freq.double().clone()
-        self.axis = None
-        if axis is not None:
-            if axis.shape != freq.shape or axis.is_floating_point() or int(axis.min()) < 0 or int(axis.max()) > 255:
-                raise ValueError("Rotary: axis has one number for each pair")
-            self.axes = int(axis.max()) + 1
-            self.axis = axis.to(device=freq.device, dtype=torch.uint8, copy=True)
-        self.dev = self.freq.get_device()
-        self._freq_p, self._axis_p = self.freq.data_ptr(), self.axis.data_ptr() if self.axis is not None else 0
+        self.dim, self.adjacent, self.dev = 2 * freq.numel(), bool(adjacent), freq.get_device()
+        self.freq, self.axis = freq, axis
+
+    @property
+    def freq(self) -> torch.Tensor:
+        return self._freq
+
+    @freq.setter
+    def freq(self, freq: torch.Tensor) -> None:
+        if freq.shape != (self.dim // 2,) or freq.get_device() != self.dev:
+            raise ValueError("Rotary: freq of another length or device")
+        self._freq = freq.double().clone()
+        self._freq_p = self._freq.data_ptr()
+
+    @property
+    def axis(self) -> Optional[torch.Tensor]:
+        return self._axis
+
+    @axis.setter
+    def axis(self, axis: Optional[torch.Tensor]) -> None:
+        if axis is None:
+            self._axis, self._axis_p, self.axes = None, 0, 1
+            return
+        if axis.shape != self.freq.shape or axis.is_floating_point() or int(axis.min()) < 0 or int(axis.max()) > 255:
+            raise ValueError("Rotary: axis has one number for each pair")
+        self._axis = axis.to(device=self.freq.device, dtype=torch.uint8, copy=True)
+        self._axis_p, self.axes = self._axis.data_ptr(), int(axis.max()) + 1
 
     @staticmethod
     def of(dim: int, base: float = 10000.0, sections=None, adjacent: bool = False, device="cuda") -> "Rotary":
