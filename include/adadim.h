@@ -505,6 +505,10 @@ typedef struct {
  *              dtype, rounded once.  Q, K, V may lie side by side in one matrix.
  *   heads[4], heads[5]   optional: the values of keys and of values that the cache then stands for, [n_tokens][kv_heads][head_dim],
  *              vdtype ADADIM_BF16 or ADADIM_F32 (both hold them exactly, up to their own range)
+ * What is written (heads[3 .. 5]) shares no memory with what is read or written beside it, except that heads[3] may be Q, heads[5]
+ * may be V, and heads[4] may be K unless pairs of channels dim / 2 apart are rotated, each the very place in the same size of element;
+ * else ADADIM_ERR_PARAM (also for strides that put heads on top of one another, and for orders that columns of one matrix, heads side by
+ * side and parts of every head do not cover).
  *   rotary     host; NULL: nothing is rotated (then there is no Q)
  * Keys are quantized from the rotation in binary64, every decision as in adadim_quantize_fp4; a block with an
  * infinity or NaN gets scale 0x7F: its values are NaN, and so is what attends to them.

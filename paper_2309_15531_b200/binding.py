@@ -889,7 +889,8 @@ def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, slots: torch.T
     """Rotates q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] and puts k and v into the cache at slots
     int32[tokens] (all different; -1: not stored), quantized to NVFP4.  fp32, fp16 or bf16, one type; views of one projection's result
     are taken as they are.  positions int32 [tokens] or [axes, tokens].  Returns the rotated q (in q_out, which may be q, if given).
-    k_values, v_values (bf16 or fp32): receive the values that the cache then holds.  For inference: no gradient passes."""
+    k_values, v_values (bf16 or fp32): receive the values that the cache then holds, in memory of their own (v_values may be v, k_values
+    may be k where no halves are rotated).  For inference: no gradient passes."""
     dev, shape = cache.dev, k.shape
     n, h, d = shape
     if h != cache.kv_heads or d != cache.head_dim:

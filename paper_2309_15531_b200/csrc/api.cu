@@ -75,6 +75,46 @@ int check_kv4(const adadim_kv4cache* c) {
 }
 Kv4Heads heads_of(const adadim_heads& h) { return {h.p, h.ld, h.lh}; }
 
+// Where heads of tokens lie, in bytes.
+struct Place {
+  const char* p;
+  int64_t n, heads, ld, lh, width;
+};
+Place place_of(const adadim_heads& h, int64_t n, int64_t heads, int64_t dim, int64_t esz) {
+  return {static_cast<const char*>(h.p), n, heads, n > 1 ? h.ld * esz : 0, heads > 1 ? h.lh * esz : 0, dim * esz};
+}
+bool same_place(const Place& a, const Place& b) { return a.p == b.p && a.ld == b.ld && a.lh == b.lh && a.width == b.width; }
+// A token's heads, or two tokens, on top of one another: not all such orders are found, and none is that has room for every head.
+bool folded(const Place& a) {
+  const int64_t ld = a.ld < 0 ? -a.ld : a.ld, lh = a.lh < 0 ? -a.lh : a.lh;
+  return (a.n > 1 && ld < a.width) || (a.heads > 1 && lh < a.width) || (a.n > 1 && a.heads > 1 && ld == lh);
+}
+int64_t gcd(int64_t a, int64_t b) {
+  while (b != 0) { const int64_t r = a % b; a = b; b = r; }
+  return a < 0 ? -a : a;
+}
+// Whether no byte belongs to both: their ranges are apart, or apart within the period of the tokens (columns of one matrix), of the
+// heads (tokens inside heads), or of both (parts of every head).  False as well for orders that none of these tells apart.
+bool apart(const Place& a, const Place& b) {
+  typedef __int128 wide;
+  struct Range { wide from, bytes; };
+  const auto range = [](const Place& x, bool tokens, bool heads) {
+    const wide t = tokens ? static_cast<wide>(x.n - 1) * x.ld : 0, h = heads ? static_cast<wide>(x.heads - 1) * x.lh : 0;
+    return Range{static_cast<wide>(reinterpret_cast<uintptr_t>(x.p)) + (t < 0 ? t : 0) + (h < 0 ? h : 0), (t < 0 ? -t : t) + (h < 0 ? -h : h) + x.width};
+  };
+  const Range x = range(a, true, true), y = range(b, true, true);
+  if (x.from + x.bytes <= y.from || y.from + y.bytes <= x.from) return true;
+  const auto within = [](int64_t period, const Range& x, const Range& y) {
+    if (period == 0) return false;
+    wide s = (y.from - x.from) % period;
+    if (s < 0) s += period;
+    return s >= x.bytes && s + y.bytes <= period;
+  };
+  const int64_t tokens = gcd(a.ld, b.ld), heads = gcd(a.lh, b.lh);
+  return within(tokens, range(a, false, true), range(b, false, true)) || within(heads, range(a, true, false), range(b, true, false)) ||
+         within(gcd(tokens, heads), range(a, false, false), range(b, false, false));
+}
+
 int check_qtensor(const adadim_qtensor* q) {
   if (q == nullptr || q->codes == nullptr || q->scales == nullptr || q->zeros == nullptr) return ADADIM_ERR_NULL;
   if (!aligned16(q->codes) || !aligned16(q->scales) || !aligned16(q->zeros)) return ADADIM_ERR_ALIGN;
@@ -550,7 +590,23 @@ int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dtype, int64_t
   if (n_tokens == 0) return ADADIM_OK;
   if ((Q.p == nullptr) != (Qr.p == nullptr)) return ADADIM_ERR_NULL;
   if (Q.p != nullptr && rotary == nullptr) return ADADIM_ERR_PARAM;
-  if (K.p == nullptr || V.p == nullptr || slots == nullptr) return ADADIM_ERR_NULL;
+  if (K.p == nullptr || V.p == nullptr) return ADADIM_ERR_NULL;
+  {
+    // What is written lies in memory of its own, or where each thread's numbers come from: a turned key with halves as pairs has its
+    // partner's place read by another thread.
+    const int64_t esz = dtype == ADADIM_F32 ? 4 : 2, vsz = vdtype == ADADIM_F32 ? 4 : 2, d = cache->head_dim, h = cache->kv_heads;
+    const Place k = place_of(K, n_tokens, h, d, esz), v = place_of(V, n_tokens, h, d, esz), q = place_of(Q, n_tokens, q_heads, d, esz);
+    const Place to_q = place_of(Qr, n_tokens, q_heads, d, esz), to_k = place_of(heads[4], n_tokens, h, d, vsz), to_v = place_of(heads[5], n_tokens, h, d, vsz);
+    const auto clear = [](const Place& to, const Place& from) { return to.p == nullptr || from.p == nullptr || apart(to, from); };
+    const bool whole_keys = rotary == nullptr || rotary->adjacent != 0;
+    for (const Place& to : {to_q, to_k, to_v})
+      if (to.p != nullptr && folded(to)) return ADADIM_ERR_PARAM;
+    if (!(clear(to_q, q) || same_place(to_q, q)) || !clear(to_q, k) || !clear(to_q, v)) return ADADIM_ERR_PARAM;
+    if (!(clear(to_k, k) || (whole_keys && same_place(to_k, k))) || !clear(to_k, v) || !clear(to_k, q)) return ADADIM_ERR_PARAM;
+    if (!(clear(to_v, v) || same_place(to_v, v)) || !clear(to_v, k) || !clear(to_v, q)) return ADADIM_ERR_PARAM;
+    if (!clear(to_q, to_k) || !clear(to_q, to_v) || !clear(to_k, to_v)) return ADADIM_ERR_PARAM;
+  }
+  if (slots == nullptr) return ADADIM_ERR_NULL;
   const Kv4Rotary still = {nullptr, nullptr, nullptr, 0, 1, 0, 0};
   return kv4_append_launch(heads_of(Q), heads_of(Qr), Q.p == nullptr ? 0 : q_heads, heads_of(K), heads_of(V), dtype, n_tokens, slots,
                            rotary == nullptr ? still : Kv4Rotary{rotary->positions, rotary->freq, rotary->axis, rotary->ld, rotary->axes,
