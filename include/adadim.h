@@ -519,7 +519,7 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
 /*
  * Attention of new tokens over the cache.  Request i has the query rows offsets[i] .. offsets[i+1]-1 (int32
  * [n_requests + 1], not falling, within 0 .. n_rows) and lengths[i] tokens in the cache, its new ones the last of them.
- *   qo         host: qo[0] queries, qo[1] results (may be the queries' place), [n_rows][q_heads][head_dim], dtype ADADIM_F16 or
+ *   qo         host: qo[0] queries, qo[1] results (the queries' very place, or apart from them: ADADIM_ERR_PARAM), [n_rows][q_heads][head_dim], dtype ADADIM_F16 or
  *              ADADIM_BF16; query head h reads key head h / (q_heads / kv_heads).  Rows of no request are not written.
  *   scale      of the products q k
  *   causal     query row j of n sees positions up to lengths - n + j; 0: all

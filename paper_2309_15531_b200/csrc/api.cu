@@ -633,9 +633,14 @@ int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int 
       width > kKv4Most / cache->page)
     return ADADIM_ERR_SHAPE;
   if (n_rows == 0 || n_requests == 0) return ADADIM_OK;
-  if (qo == nullptr || qo[0].p == nullptr || qo[1].p == nullptr || offsets == nullptr || lengths == nullptr ||
-      (width > 0 && table == nullptr) || workspace == nullptr)
+  if (qo == nullptr || qo[0].p == nullptr || qo[1].p == nullptr || offsets == nullptr || lengths == nullptr || (width > 0 && table == nullptr))
     return ADADIM_ERR_NULL;
+  {
+    // a row's results are written when its queries have been read, other rows' have not
+    const Place q = place_of(qo[0], n_rows, q_heads, cache->head_dim, 2), o = place_of(qo[1], n_rows, q_heads, cache->head_dim, 2);
+    if (folded(o) || !(same_place(q, o) || apart(q, o))) return ADADIM_ERR_PARAM;
+  }
+  if (workspace == nullptr) return ADADIM_ERR_NULL;
   if (!aligned256(workspace)) return ADADIM_ERR_ALIGN;
   if (workspace_bytes < adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, cache->kv_heads, cache->head_dim)) return ADADIM_ERR_WORKSPACE;
   Kv4Attention a = {};

@@ -3,7 +3,7 @@ launched.  What may lie where gets as far as the next check, a missing list of s
 import pytest
 
 from paper_2309_15531_b200 import binding as B
-from test_kv4_refusals import NULL, PARAM, append, cache, rotary
+from test_kv4_refusals import NULL, PARAM, append, attention, cache, rotary
 
 N, D, HEADS, KV = 3, 64, 4, 2                            # tokens, and what the calls of test_kv4_refusals have
 FAR = 1 << 20
@@ -66,3 +66,28 @@ def test_keys_that_are_not_turned_in_halves_may_be_replaced_by_their_values():
 def test_one_token_and_one_head_have_no_strides():
     assert append(n=1, k=(FAR, 0, D), v=(2 * FAR, 5, D), kv=(3 * FAR, 0, D), slots=None) == NULL
     assert append(n=3, k=(FAR, D, 0), v=(2 * FAR, D, 0), kv=(3 * FAR, D, 0), vv=(2 * FAR, D, 7), c=cache(kv_heads=1), slots=None) == NULL
+
+
+def attend(q, o, rows=N, q_heads=HEADS):
+    """As far as the workspace, which is missing."""
+    return attention(q=q, o=o, rows=rows, q_heads=q_heads, ws=None)
+
+
+@pytest.mark.parametrize("q,o", [
+    (column(0), column(0)), (column(0), column(HEADS)), (column(0), column(HEADS, size=2, base=FAR + 2 * N * ROW)), (column(0), (FAR + 2 * N * ROW, HEADS * D, D)),
+    ((FAR, D, N * D), (FAR, D, N * D)), ((FAR, 2 * HEADS * D, 2 * D), (FAR + 2 * D, 2 * HEADS * D, 2 * D))])
+def test_attention_in_the_place_of_its_queries_or_apart_from_them(q, o):
+    assert attend(q, o) == NULL
+
+
+@pytest.mark.parametrize("q,o", [
+    (column(0), column(1)), (column(0), (FAR, HEADS * D, D)), (column(0), (FAR + 2 * ROW, ROW, D)), (column(0), (FAR, ROW, 2 * D)),
+    (column(0), (4 * FAR, 0, D)), (column(0), (4 * FAR, HEADS * D, 0)), (column(0), (4 * FAR, HEADS * D, D - 8)), (column(0), (4 * FAR, D, D))])
+def test_attention_partly_over_its_queries(q, o):
+    assert attend(q, o) == PARAM
+
+
+def test_attention_of_one_row_and_of_one_head():
+    assert attend((FAR, 0, D), (4 * FAR, 0, D), rows=1) == NULL
+    assert attend((FAR, D, 0), (4 * FAR, D, 0), q_heads=2) == PARAM
+    assert attention(q=(FAR, D, 0), o=(4 * FAR, D, 0), q_heads=1, c=cache(kv_heads=1), ws=None) == NULL
