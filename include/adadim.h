@@ -464,8 +464,8 @@ ADADIM_API size_t adadim_kv4_bytes(int64_t n_pages, int page, int kv_heads, int 
  *   requests, positions, slots  [rows]: of new token r (requests in order) its request, its place in the
  *              request, its slot.  Rows behind the last new token get -1, 0, -1.
  *   next       *cursor + pages taken (not the same word as cursor)
- * Nothing but those entries of `table` is changed, so a call may be repeated; lengths and offsets do not overlap past and
- * fresh (ADADIM_ERR_PARAM).  past and fresh are not negative, and
+ * Nothing but those entries of `table` is changed, so a call may be repeated.  What is written shares no memory with anything else
+ * (ADADIM_ERR_PARAM).  past and fresh are not negative, and
  * past + fresh < 2^31; otherwise (device) ADADIM_ERR_SHAPE, and they count as 0.  More new tokens than
  * rows: ADADIM_ERR_SHAPE.  A token whose page cannot be had (the list is used up, the row too narrow, an entry
  * negative) has slot -1, and its entry -1 where the list is used up: ADADIM_ERR_PAGES.

@@ -558,16 +558,33 @@ int adadim_page_tables(const int32_t* past, const int32_t* fresh, int64_t n_requ
                        int* status_dev, void* cuda_stream) {
   if (!kv4_page_ok(page)) return ADADIM_ERR_PARAM;
   if (n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width || n_free < 0 || rows < 0) return ADADIM_ERR_SHAPE;
-  if (n_free > kInt32Max || rows > kInt32Max || width > kInt32Max) return ADADIM_ERR_SHAPE;
+  if (n_free > kInt32Max || rows > kInt32Max || width > kInt32Max || ldt > (int64_t{1} << 40)) return ADADIM_ERR_SHAPE;
   if (offsets == nullptr || next == nullptr || next == cursor) return ADADIM_ERR_NULL;
   if (n_requests > 0 && (past == nullptr || fresh == nullptr || lengths == nullptr || (width > 0 && table == nullptr))) return ADADIM_ERR_NULL;
   if (n_free > 0 && free_pages == nullptr) return ADADIM_ERR_NULL;
   if (rows > 0 && (requests == nullptr || positions == nullptr || slots == nullptr)) return ADADIM_ERR_NULL;
-  // some CTAs still read what others have written by then
-  const auto apart = [](const int32_t* a, int64_t n, const int32_t* b, int64_t m) { return a + n <= b || b + m <= a; };
-  if (!apart(past, n_requests, lengths, n_requests) || !apart(fresh, n_requests, lengths, n_requests) ||
-      !apart(past, n_requests, offsets, n_requests + 1) || !apart(fresh, n_requests, offsets, n_requests + 1))
-    return ADADIM_ERR_PARAM;
+  {
+    // Some CTAs still read what others have written by then.
+    struct Ints { const int32_t* p; int64_t n; };
+    const Ints read[] = {{past, n_requests}, {fresh, n_requests}, {free_pages, n_free}, {cursor, cursor != nullptr}};
+    const Ints written[] = {{lengths, n_requests}, {offsets, n_requests + 1}, {requests, rows}, {positions, rows}, {slots, rows}, {next, 1}};
+    const Place whole = {reinterpret_cast<const char*>(table), n_requests, 1, n_requests > 1 ? ldt * 4 : 0, 0, width * 4};
+    const auto clear = [](const Ints& a, const Ints& b) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+      return a.n == 0 || b.n == 0 || x + 4 * a.n <= y || y + 4 * b.n <= x;
+    };
+    const Ints all_rows = {table, n_requests == 0 || width == 0 ? 0 : (n_requests - 1) * ldt + width};
+    const auto beside_table = [&](const Ints& a) {                   // in front, behind, or between the used entries of two rows
+      return clear(all_rows, a) || apart(whole, Place{reinterpret_cast<const char*>(a.p), 1, 1, 0, 0, 4 * a.n});
+    };
+    for (const Ints& a : read)
+      if (!beside_table(a)) return ADADIM_ERR_PARAM;
+    for (const Ints& a : written) {
+      if (!beside_table(a)) return ADADIM_ERR_PARAM;
+      for (const Ints& b : read) if (!clear(a, b)) return ADADIM_ERR_PARAM;
+      for (const Ints& b : written) if (&a != &b && !clear(a, b)) return ADADIM_ERR_PARAM;
+    }
+  }
   return page_tables_launch(past, fresh, static_cast<int>(n_requests), page, table, ldt, width, free_pages, static_cast<int>(n_free),
                             cursor, static_cast<int>(rows), lengths, offsets, requests, positions, slots, next, status_dev,
                             static_cast<cudaStream_t>(cuda_stream));

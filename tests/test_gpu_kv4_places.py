@@ -37,3 +37,16 @@ def test_results_in_the_places_of_what_is_read(tokens, adjacent):
     with pytest.raises(B.AdadimError):
         run(k_values=v)
     assert torch.equal(both, kept)
+
+
+def test_tables_with_their_cursors_beside_them_in_one_buffer():
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()
+    both = torch.zeros(3, 8, dtype=torch.int32, device="cuda")
+    step = B.PageTables(3, 6)
+    both[0, 5] = 1
+    step.cursor = both[1, 6:7]
+    B.page_tables(ints(0, 16, 3), ints(2, 3, 1), both[:, :4], ints(9, 5, 6, 7), 16, out=step, cursor=both[0, 5:6])
+    assert both.tolist() == [[5, 0, 0, 0, 0, 1, 0, 0], [0, 6, 0, 0, 0, 0, 3, 0], [0] * 8] and step.slots.tolist() == [80, 81, 96, 97, 98, 3]
+    step.cursor = both[2, 3:4]
+    with pytest.raises(B.AdadimError):
+        B.page_tables(ints(0, 16, 3), ints(2, 3, 1), both[:, :4], ints(9, 5, 6, 7), 16, out=step)

@@ -3,7 +3,7 @@ launched.  What may lie where gets as far as the next check, a missing list of s
 import pytest
 
 from paper_2309_15531_b200 import binding as B
-from test_kv4_refusals import NULL, PARAM, append, attention, cache, rotary
+from test_kv4_refusals import NULL, PARAM, append, attention, cache, rotary, tables
 
 N, D, HEADS, KV = 3, 64, 4, 2                            # tokens, and what the calls of test_kv4_refusals have
 FAR = 1 << 20
@@ -91,3 +91,26 @@ def test_attention_of_one_row_and_of_one_head():
     assert attend((FAR, 0, D), (4 * FAR, 0, D), rows=1) == NULL
     assert attend((FAR, D, 0), (4 * FAR, D, 0), q_heads=2) == PARAM
     assert attention(q=(FAR, D, 0), o=(4 * FAR, D, 0), q_heads=1, c=cache(kv_heads=1), ws=None) == NULL
+
+
+PLACES = dict(past=1 << 12, fresh=2 << 12, free=3 << 12, cursor=4 << 12, table=5 << 12, lengths=6 << 12, offsets=7 << 12, requests=8 << 12,
+              positions=9 << 12, slots=10 << 12, after=11 << 12)
+SIZES = dict(past=2, fresh=2, free=9, cursor=1, lengths=2, offsets=3, requests=3, positions=3, slots=3, after=1)     # what `tables` has
+WRITTEN = ("lengths", "offsets", "requests", "positions", "slots", "after")
+
+
+@pytest.mark.parametrize("name", WRITTEN)
+@pytest.mark.parametrize("other", [n for n in PLACES if n != "table"])
+def test_tables_written_over_one_another_or_what_is_read(name, other):
+    if name == other or (name, other) == ("after", "cursor"):        # the latter has a status of its own
+        return
+    assert tables(**{**PLACES, name: PLACES[other] + 4 * SIZES[other] - 4}) == PARAM
+    assert tables(**{**PLACES, name: PLACES[other] - 4 * SIZES[name] + 4}) == PARAM
+
+
+@pytest.mark.parametrize("name", [n for n in PLACES if n != "table"])
+def test_a_table_over_what_is_read_or_written(name):
+    """Rows of 6 entries, 4 of them used, of which the call's is the first 10."""
+    for at in (0, 3, 6, 9):
+        assert tables(**{**PLACES, name: PLACES["table"] + 4 * at}, ldt=6) == PARAM
+    assert tables(**{**PLACES, name: PLACES["table"] - 4 * SIZES[name] + 4}, ldt=6) == PARAM
