@@ -194,6 +194,11 @@ def fp4_attention(x: torch.Tensor, qkv: B.Fp4Tensor, proj: B.Fp4Tensor, cache: B
         raise ValueError("fp4_attention: the weights do not match the cache's heads")
     if step.n_rows != rows:
         raise ValueError("fp4_attention: step was made for another number of rows")
+    # what the attention would refuse, before the append has changed the cache
+    if x.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("fp4_attention: x is fp16 or bf16")
+    if heads % kv_heads or table.shape[0] != step.n_requests or table.dtype != torch.int32 or window < 0 or max_new < 0:
+        raise ValueError("fp4_attention: heads, table, window or max_new do not fit")
     q, k, v = B.fp4_linear(x, qkv, x_amax=x_amax, status=status).view(rows, heads + 2 * kv_heads, d).split((heads, kv_heads, kv_heads), dim=1)
     if rotary is None:
         B.kv4_append(k, v, cache, step.slots)
