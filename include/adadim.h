@@ -531,7 +531,8 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
  * The values that the codes stand for are used as they are (exact in fp16); queries too (bf16 ones times a power of
  * two in fp16), weights are rounded to fp16, sums are binary32, and results are rounded once.  A table entry outside the
  * cache: its tokens are left out, (device) ADADIM_ERR_PAGES.  Entries for pages that lie behind every row's window may be anything.  Offsets that fall or leave 0 .. n_rows, lengths outside
- * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads and width * page up to 2^31 - 4096.
+ * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads and width * page up to
+ * 2^31 - 4096, and n_rows + window with a window that is not causal.
  */
 ADADIM_API int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
                         const int32_t* lengths, int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width,

@@ -649,6 +649,9 @@ int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int 
   if (n_rows < 0 || n_rows > kKv4Most / q_heads || n_requests < 0 || n_requests > kv4::kMaxRequests || width < 0 || ldt < width ||
       width > kKv4Most / cache->page)
     return ADADIM_ERR_SHAPE;
+  if (window >= width * cache->page) window = 0;                     // as long as any request may be
+  // rows may stand in front of token 0, and see tokens where they are not causal: the window's begin, up to rows + window in front of it
+  if (causal == 0 && window > 0 && n_rows > kKv4Most - window) return ADADIM_ERR_SHAPE;
   if (n_rows == 0 || n_requests == 0) return ADADIM_OK;
   if (qo == nullptr || qo[0].p == nullptr || qo[1].p == nullptr || offsets == nullptr || lengths == nullptr || (width > 0 && table == nullptr))
     return ADADIM_ERR_NULL;
@@ -675,7 +678,7 @@ int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int 
   a.cache = kv4::cache_of(*cache);
   a.scale = scale;
   a.causal = causal != 0;
-  a.window = static_cast<int>(window >= width * cache->page ? 0 : window);   // as long as any request may be
+  a.window = static_cast<int>(window);
   a.status_dev = status_dev;
   a.workspace = static_cast<char*>(workspace);
   return kv4_attention_launch(a, dtype, max_new == 0 || max_new > n_rows ? n_rows : max_new, static_cast<cudaStream_t>(cuda_stream));
