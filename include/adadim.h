@@ -502,7 +502,7 @@ typedef struct {
  *   heads[0], heads[1]   K, V  [n_tokens][kv_heads][head_dim], dtype any.  slots int32[n_tokens]: where each token goes;
  *              tokens with a slot outside the cache are not stored.  Slots have to differ.
  *   heads[2], heads[3]   optional: Q and where it goes when rotated (may be Q itself), [n_tokens][q_heads][head_dim] of the same
- *              dtype, rounded once.  Q, K, V may lie side by side in one matrix.
+ *              dtype: fp32 from binary64, fp16 and bf16 from binary32 (2^-22 of the pair).  Q, K, V may lie side by side in one matrix.
  *   heads[4], heads[5]   optional: the values of keys and of values that the cache then stands for, [n_tokens][kv_heads][head_dim],
  *              vdtype ADADIM_BF16 or ADADIM_F32 (both hold them exactly, up to their own range)
  * What is written (heads[3 .. 5]) shares no memory with what is read or written beside it, except that heads[3] may be Q, heads[5]

@@ -191,6 +191,22 @@ __device__ __forceinline__ void store_chunk(T* p, bool wide, const float (&v)[8]
   }
 }
 
+// Pair j of a query: 16-bit ones in binary32 with the rounded sine and cosine (off by 2^-22 of the pair, far below half of their step); binary32
+// ones in binary64, rounded once.
+template <typename T>
+__device__ __forceinline__ void turn_query(float& a, float& b, int j, const float2* turn, const double* turn_c, const double* turn_s) {
+  if constexpr (sizeof(T) == 4) {
+    const double c = turn_c[j], s = turn_s[j], u = a, w = b;
+    a = static_cast<float>(u * c - w * s);
+    b = static_cast<float>(w * c + u * s);
+  } else {
+    const float2 cs = turn[j];
+    const float u = a, w = b;
+    a = u * cs.x - w * cs.y;
+    b = w * cs.x + u * cs.y;
+  }
+}
+
 // Scale byte and codes of eight channels of a block, from binary64; `m`: bits of the block's largest magnitude.
 __device__ __forceinline__ uint32_t quantize_exact(const double (&z)[8], uint64_t m_bits, int t_log2, uint32_t& byte, float& s) {
   s = 0.0f;
@@ -348,12 +364,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
         load_chunk(row + c0, p.wide_q, a);
         if (c0 < 2 * half) {
 #pragma unroll
-          for (int k = 0; k < 8; k += 2) {
-            const float2 cs = turn[(c0 + k) >> 1];
-            const float u = a[k], w = a[k + 1];
-            a[k] = u * cs.x - w * cs.y;
-            a[k + 1] = w * cs.x + u * cs.y;
-          }
+          for (int k = 0; k < 8; k += 2) turn_query<T>(a[k], a[k + 1], (c0 + k) >> 1, turn, turn_c, turn_s);
         }
         store_chunk(out + c0, p.wide_qr, a);
       } else if (chunk * 8 < half) {
@@ -361,12 +372,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
         load_chunk(row + j0, p.wide_q, a);
         load_chunk(row + j0 + half, p.wide_q, b);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float2 cs = turn[j0 + k];
-          const float u = a[k], w = b[k];
-          a[k] = u * cs.x - w * cs.y;
-          b[k] = w * cs.x + u * cs.y;
-        }
+        for (int k = 0; k < 8; ++k) turn_query<T>(a[k], b[k], j0 + k, turn, turn_c, turn_s);
         store_chunk(out + j0, p.wide_qr, a);
         store_chunk(out + j0 + half, p.wide_qr, b);
       } else {
