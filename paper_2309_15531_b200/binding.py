@@ -893,6 +893,7 @@ def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, slots: torch.T
     may be k where no halves are rotated).  For inference: no gradient passes."""
     dev, shape = cache.dev, k.shape
     n, h, d = shape
+    assert dev >= 0
     if h != cache.kv_heads or d != cache.head_dim:
         raise ValueError("kv4_append: k does not match the cache")
     if dev != _device():
@@ -946,6 +947,7 @@ def kv4_attention(q: torch.Tensor, cache: Kv4Cache, table: torch.Tensor, lengths
     rows than this (0: not known); picks the kernels.  Calls that may run at once need a workspace each
     (kv4_workspace_bytes).  For inference: no gradient passes."""
     dev, shape = cache.dev, q.shape
+    assert dev >= 0
     n, h, d = shape
     n_req, (t_rows, width) = _i32(lengths, dev).numel(), table.shape
     if d != cache.head_dim or h % cache.kv_heads:
