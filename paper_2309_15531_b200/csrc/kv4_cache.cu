@@ -436,7 +436,10 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
   p.q_rcp = static_cast<uint32_t>((uint64_t{1} << 32) / p.q_chunks + 1);
   p.chunk_log2 = kv4::log2_of(cache.held / 8);
   p.n_tokens = n_tokens;
-  p.each = n_tokens >= 148 * 4 * kMostTokens ? kMostTokens : 1;      // a long prompt: 8192 tokens 85 us, 89 with a token a CTA
+  // Four tokens a CTA from three waves of such CTAs on; fewer leave SMs idle in the last one.  Four against one, in us, 64 + 8 + 8 heads of 128
+  // (12 + 3 + 3 of 80): 3000 tokens 46 and 37 (19.4 and 15.7), 4096 47.8 and 43 (19.9 and 19.1), 7104 79 and 78 (29.3 and 30.1), 8192 85 and
+  // 89 (29.5 and 33.8), 12000 128 and 126 (41 and 45), 16384 164 and 170.
+  p.each = n_tokens >= 3 * 148 * 4 * kMostTokens ? kMostTokens : 1;
   const int64_t most = (tasks + kAppendThreads - 1) / kAppendThreads, wanted = 148 * 4 / n_tokens;
   const dim3 grid(static_cast<unsigned>((n_tokens + p.each - 1) / p.each), static_cast<unsigned>(wanted < 1 ? 1 : wanted > most ? most : wanted));
   if (dtype == ADADIM_F32) return append_types<float>(p, vdtype, grid, st);
