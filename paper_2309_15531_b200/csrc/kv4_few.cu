@@ -31,8 +31,10 @@ using namespace kv4;
 using fp4::exp2_int;
 
 constexpr int kFewThreads = 128, kFewWarps = 4, kStep = 32, kChunk = kStep * kFewWarps;
-// What a unit costs beside its tokens, in tokens: with 300, 640, 1000 and 1500, 64 requests of up to 16384 tokens take 171, 150, 140 and 146 us.
-constexpr int kFewCost = 1000;
+// What a unit costs beside its tokens, in tokens: the least mean time over 43 sets of 24 to 200 requests with lengths up to 3000 .. 30000 and
+// heads of 64, 128 and 256 channels: with 300, 500, 640, 750, 850, 1000 and 1500, 93.9, 88.5, 88.3, 88.6, 89.5, 90.6 and 93.8 us; the slowest of them,
+// 64 requests of up to 16384 tokens, 167, 154, 147, 138, 139, 139 and 146.
+constexpr int kFewCost = 750;
 constexpr int kLeastPart = 256;                  // a CTA's part is no smaller
 constexpr int kStages = 3;                       // steps of a warp on their way or being worked on (2 and 4: the same time within 2 us of 150)
 // CTAs of an SM: what registers (a thread's 128, 168 or 255) and the ring of steps leave room for
