@@ -20,8 +20,9 @@
 // lengths; the four warps of a CTA take 32 tokens each of a chunk of 128.  What is cut is joined by a second kernel in the order of
 // the tokens, so that results do not depend on timing.  Small calls go to clusters instead (see kv4_few_kernel).
 //
-// 64 requests of up to 16384 tokens, 8 key heads of 128 channels with 8 query heads each: 140 us, 649 MB, 4.6 TB/s, 0.71 of a copy's
-// rate; two thirds of the issue slots are taken, half of the ALU's, and a CTA's last piece and the join come on top.  One token over 4096: 11.4 us.
+// 64 requests of up to 16384 tokens, 8 key heads of 128 channels with 8 query heads each: 141 us in replays of a graph, 649 MB, 4.6 TB/s, 0.70 of
+// a copy's rate (passes launched one after another 145 to 155 us, 0.64 to 0.68); two thirds of the issue slots are taken, half of the ALU's, and
+// a CTA's last piece and the join come on top.  One token over 4096: 11.4 us.
 #include "kv4_line.cuh"
 
 namespace adadim {
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           top[u][k] = fmaxf(fmaxf(sc[0][u][k], sc[0][u][k + 2]), fmaxf(sc[1][u][k], sc[1][u][k + 2]));
-          grows |= top[u][k] > m[u][k] + kGrowth;
+          grows |= top[u][k] - m[u][k] > kGrowth;
         }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
       uint32_t pb[2][NT][2];
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        const float base0 = m[u][0] == -INFINITY ? 0.0f : m[u][0] - kLift, base1 = m[u][1] == -INFINITY ? 0.0f : m[u][1] - kLift;
+        const float base0 = lifted(m[u][0]), base1 = lifted(m[u][1]);
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
           pb[hh][u][0] = transposed(half2_bits(__floats2half2_rn(exp2_fast(sc[hh][u][0] - base0), exp2_fast(sc[hh][u][1] - base1))));
@@ -561,7 +562,8 @@ int64_t span_of(const Kv4Attention& a, int64_t max_new) {
 }
 // Whether a call's units go to clusters, and of how many CTAs: where there is little to read altogether (2^20 tokens of key heads are
 // 25 us), so that unequal lengths cost less than the second launch that joins cut units, and enough units, or short ones, that clusters of
-// up to eight CTAs find the SMs enough to do.
+// up to eight CTAs find the SMs enough to do.  (One token of a request with 8 key heads, line against clusters: 8256 tokens 16.1 and 14.2 us,
+// 16384 19.7 and 21.2, 32768 24 and 36, 131072 46 and 129; with one key head 8256 11.7 and 13.8, 16384 13.4 and 21.)
 int cluster_of(const Kv4Attention& a, int tile_rows, int ctas, int64_t max_new, int& tiles) {
   const int64_t units = units_of(a, tile_rows, max_new), span = span_of(a, max_new);
   if (units > 4 * ctas || units * span > (int64_t{1} << 20) || (units < 16 && span > 8192)) return 0;

@@ -17,6 +17,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 // passes it by more than 2^8, so that they end at 2^15.  So they have their 11 bits down to 2^-21 of the reference's, below that
 // fp16's least step, 2^-31 of it, and a reference's own weight is in every row's sum.  (Without the 2^7, 2^-14 and 2^-24.)
 constexpr float kGrowth = 8.0f, kLift = 7.0f;
+// What is subtracted from scores whose reference is m: rounded up, so that no weight passes 2^15 where binary32 holds scores in steps of two
+// and more (how far a score passes m is asked for by their difference, which such steps do not change).
+__device__ __forceinline__ float lifted(float m) { return m == -INFINITY ? 0.0f : __fsub_ru(m, kLift); }
 
 __host__ __device__ constexpr size_t whole256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 

@@ -23,8 +23,8 @@
 // Heads of 128 channels.  1024 rows of each of 64 heads over 32768 tokens: 1.09 ms, 1.03 PFLOP/s, 0.62 of cuBLAS's rate; 4096 tokens of 32
 // heads over themselves: 208 us, of which 27 are the join's and about 15 the start and the ends of units.  What bounds the loop is a
 // tile's chain of scores, softmax and weights: a chunk takes both tiles 2.2 us, of which 1.1 are exponentials; the tensor pipe is busy for
-// half of the time, issue slots for 45 %.  16 requests of five drafted tokens (40 rows a unit) over up to 8192: 82 us, there bound by the unpacking
-// warps.
+// half of the time, issue slots for 45 %.  16 requests of five drafted tokens (40 rows a unit) over up to 8192: 83 us, there bound by the unpacking
+// warps.  These are replays of a graph; passes launched one after another take 2 to 3 % more.
 #include "kv4_line.cuh"
 
 namespace adadim {
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       const int first_row = x.tile * kRows + tile_row, ta = token_of(p, first_row), tb = token_of(p, first_row + rows - 1);
       const int all_hi = p.causal ? min(x.length, own + ta + 1) : x.length, all_lo = p.window > 0 ? own + tb - p.window + 1 : 0;
       // the row of queries as fp16 into shared memory
-      float factor;
+      float factor, most_score;                                      // no score of the row is larger
       bool fine;                                                     // the row's query and the scale are finite
       {
         // A warp copies its 32 rows to shared memory as they are, neighbouring lanes a row's neighbouring channels; then each thread
@@ -308,7 +308,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         // Neither zero nor NaN, so that what is hidden stays at minus infinity.  A row that is not fine has scores of zero, and so a maximum if
         // it sees anything; then it is NaN.
         factor = fine ? fmaxf(ldexpf(fabsf(p.scale) * kLog2e, t_k - e), 1.2e-38f) : 1.2e-38f;
+        const float most_q = std::is_same<T, __half>::value ? __half2float(__ushort_as_half(static_cast<unsigned short>(most))) : __uint_as_float(most << 16) * f;
+        most_score = fine ? most_q * (2688.0f * cache.dim) * factor : 0.0f;
       }
+      // Where scores may lie beyond 2^24, in steps of two and more, the weights come from the rounded product that the reference is one of, and
+      // not from the one that a fused operation keeps: it may be half a step larger.
+      const float score_factor = factor;
+      const bool large = __any_sync(0xffffffffu, most_score >= 16777216.0f);
+      if (large) factor = 1.0f;
       // the second tile's last result has been taken in
       if (i == 1 && twins > 0 && !ptx::mbar_wait_warp(&sh.twin_free, (twins - 1) & 1u, dead, status)) break;
       ptx::fence_proxy_async();
@@ -316,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       if (lane == 0) ptx::mbar_arrive(&sh.q_ready[i][jobs % kJobs]);
       taken();
 
-      float m = -INFINITY, l = 0.0f;
+      float m = -INFINITY, l = 0.0f, base = 0.0f;
       uint32_t nans = 0;                                             // blocks of the row's result that are NaN
       const int c1 = i == 0 ? x.c1_of[0] : x.c1_of[1];
       // what was noted about the values of chunk ch: a row has the NaN of the tokens that it sees
@@ -343,6 +350,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
           ptx::tc_fence_after_sync();
           const uint32_t at_half = s_at + h * kHalf;
           uint32_t va[32], vb[32];
+          if (large) {                                               // scores times their factor, in place
+#pragma unroll 1
+            for (int k = 0; k < kHalf / 16; ++k) {
+              uint32_t v[16];
+              ld16(at_half + 16 * k, v);
+              ld16_wait(v);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * score_factor);
+              st16(at_half + 16 * k, v);
+            }
+            st_wait();
+          }
           ld32(at_half, va);
           ld32(at_half + 32, vb);
           const int tok = x.key_lo() + ch * kChunk + h * kHalf;
@@ -377,10 +396,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
             top = fmaxf(max3(t0, t1, t2), t3);
           }
           const float high = top == -INFINITY ? -INFINITY : top * factor;
-          if (__any_sync(0xffffffffu, high > m + kGrowth)) {
+          if (__any_sync(0xffffffffu, high - m > kGrowth)) {
             const float now = high > m ? high : m, g = m == -INFINITY || now == m ? 1.0f : exp2_fast(m - now);
             m = now;
             l *= g;
+            base = lifted(m);
             if (last >= 0 || h > 0) {
               // once the last product of values is done, that of the other half
               ok = ptx::mbar_wait_warp(&sh.o_done[i][h ^ 1], (turn + h + 1) & 1u, dead, status);
@@ -398,7 +418,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
               st_wait();
             }
           }
-          const float base = m == -INFINITY ? 0.0f : m - kLift;
           uint64_t sum[2] = {0, 0};                                  // pairs of binary32 zeros
           const uint64_t mul = fp4::pack2(factor, factor), sub = fp4::pack2(-base, -base);
           // the sum is that of the weights before they are rounded (of the rounded ones: the prompt 227 us against 208, errors the same)
@@ -534,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
       }
     }
   } else if (warp < kUnpackWarp + kUnpackWarps) {
-    // ---- codes to fp16 tiles: a thread has half of a token's channels
+    // ---- codes to fp16 tiles: a thread has a token, all of its channels
     constexpr int kWords = HELD / 8;                                 // words of codes of a thread's token
     const int t = tid - kUnpackWarp * 32, sub = warp - kUnpackWarp;
     char* const row_at = smem + t * 128;
