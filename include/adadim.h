@@ -526,7 +526,11 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
  *   window     > 0: of those only positions above lengths - n + j - window
  *   A row that sees nothing (a length of zero, more rows than tokens) gets zeros.  What a row does not see
  *   does not reach it, NaN included.
- *   max_new    no request has more query rows than this: picks the kernels and has no part in the result.  0: not known.
+ *   max_new    no request has more query rows than this.  0: not known.
+ * max_new and width pick the kernels, which differ in the last bits of a result and in time; neither has another part in it.  A call cannot know
+ * the lengths, so that width * page stands for each of them: a call with little to read is done by one launch of its own only if the
+ * table has no room for more (one token over 4096: 11.4 us, 18.5 with a table for 131072; a prompt of 40 tokens 9.9 and 38).  Without max_new a
+ * batch that generates starts the kernel for many rows in vain (64 requests 139 and 149 us, 50 short windows 11.8 and 23.6).
  *   workspace  adadim_kv4_workspace_bytes(n_requests, n_rows, q_heads, kv_heads, head_dim), 256-byte aligned.
  * The values that the codes stand for are used as they are (exact in fp16); queries too (bf16 ones times a power of
  * two in fp16), weights are rounded to fp16, sums are binary32, and results are rounded once.  A table entry outside the
