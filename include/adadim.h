@@ -505,7 +505,7 @@ typedef struct {
  *              dtype: fp32 from binary64, fp16 and bf16 from binary32 (2^-22 of the pair).  Q, K, V may lie side by side in one matrix.
  *   heads[4], heads[5]   optional: the values of keys and of values that the cache then stands for, [n_tokens][kv_heads][head_dim],
  *              vdtype ADADIM_BF16 or ADADIM_F32 (both hold them exactly, up to their own range)
- * What is written (heads[3 .. 5]) shares no memory with what is read or written beside it, except that heads[3] may be Q, heads[5]
+ * heads[3 .. 5], which are written, share no memory with one another and the other heads, except that heads[3] may be Q, heads[5]
  * may be V, and heads[4] may be K unless pairs of channels dim / 2 apart are rotated, each the very place in the same size of element;
  * else ADADIM_ERR_PARAM (also for strides that put heads on top of one another, and for orders that columns of one matrix, heads side by
  * side and parts of every head do not cover).
@@ -536,7 +536,7 @@ ADADIM_API int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dty
  * two in fp16), weights are rounded to fp16, sums are binary32, and results are rounded once.  A table entry outside the
  * cache: its tokens are left out, (device) ADADIM_ERR_PAGES.  Entries for pages that lie behind every row's window may be anything.  Offsets that fall or leave 0 .. n_rows, lengths outside
  * 0 .. width * page: clamped, (device) ADADIM_ERR_SHAPE.  n_requests up to 8192, n_rows * q_heads and width * page up to
- * 2^31 - 4096, and n_rows + window with a window that is not causal.
+ * 2^31 - 4096, and so n_rows + window where it is not causal.
  */
 ADADIM_API int adadim_kv4_attention(const adadim_heads* qo, int dtype, int64_t n_rows, int q_heads, const int32_t* offsets,
                         const int32_t* lengths, int64_t n_requests, const int32_t* table, int64_t ldt, int64_t width,

@@ -20,10 +20,10 @@
 // the two results together from TMEM.
 // The line of work is cut into one part a CTA as for few rows.
 //
-// Heads of 128 channels.  1024 rows of each of 64 heads over 32768 tokens: 1.09 ms, 1.03 PFLOP/s, 0.62 of cuBLAS's rate; 4096 tokens of 32
-// heads over themselves: 208 us, of which 27 are the join's and about 15 the start and the ends of units.  What bounds the loop is a
+// Heads of 128 channels.  1024 rows of each of 64 heads over 32768 tokens: 1.10 ms, 1.02 PFLOP/s, 0.61 of cuBLAS's rate; 4096 tokens of 32
+// heads over themselves: 210 us, of which 27 are the join's and about 15 the start and the ends of units.  What bounds the loop is a
 // tile's chain of scores, softmax and weights: a chunk takes both tiles 2.2 us, of which 1.1 are exponentials; the tensor pipe is busy for
-// half of the time, issue slots for 45 %.  16 requests of five drafted tokens (40 rows a unit) over up to 8192: 83 us, there bound by the unpacking
+// half of the time, issue slots for 45 %.  16 requests of five drafted tokens (40 rows a unit) over up to 8192: 81 us, there bound by the unpacking
 // warps.  These are replays of a graph; passes launched one after another take 2 to 3 % more.
 #include "kv4_line.cuh"
 

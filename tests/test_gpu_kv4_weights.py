@@ -24,7 +24,7 @@ def test_many_small_weights_beside_large_ones(monkeypatch, n, new, heads, kv_hea
     """Every 32nd token has the keys' only numbers: the others' weights are 2^-tail of its own.
 
     The bound, with u half a step of the result's type: u |o|; a weight is rounded to fp16 as 2^7 times what it is to the row's reference,
-    which is some score of the row: 2^-11 relative, and where it is below 2^-14 half of fp16's least step, 2^-25.  The sum of weights is
+    which is some score of the row: 2^-11 relative, and where that is below 2^-14 half of fp16's least step, 2^-25.  The sum of weights is
     2^7 at least for every 32 tokens, so that this is 32 * 2^-32 of the largest value; a score's error as in kv4_helpers; sums 2^-22
     for every 16 tokens; results below 2^-14 have fp16's least step."""
     monkeypatch.setattr(Batch, "more_tokens", more_tokens)
