@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
 
     // the warp's steps: 32 tokens of every chunk, in a ring
     const int first = x.key_lo + (x.c0 + rank) * kChunk + warp * kStep;
-    const int steps = first >= key_hi || *dead ? 0 : min(x.c1 - x.c0, (key_hi - first + stride - 1) / stride);
+    const bool stopped = __any_sync(0xffffffffu, *dead != 0);
+    const int steps = first >= key_hi || stopped ? 0 : min(x.c1 - x.c0, (key_hi - first + stride - 1) / stride);
     int pages = -1;                                                  // of the sixteens of tokens of the next 16 steps, one a lane
     uint32_t usable = 0;                                             // two bits a stage: whether its sixteens lie in the cache
     auto fetch = [&](int it, int to) {
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kFewThreads, few_per_sm(HELD, NT)) kv4_few_ker
 #pragma unroll 1
     for (int it = 0; it < steps; ++it) {
       const char* const from = ring + stage * St::kBytes;
-      if (!ptx::mbar_wait(&bar[stage], parity, dead, p.status_dev)) break;
+      if (!ptx::mbar_wait_warp(&bar[stage], parity, dead, p.status_dev)) break;       // (one answer for all lanes: they work together behind it)
       const uint32_t use = usable >> 2 * stage & 3u;
       const int tok = first + it * stride;
       // scores of tokens tok + place and rows 2 c, 2 c + 1 of every eight

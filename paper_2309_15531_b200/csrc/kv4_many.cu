@@ -749,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_many_kernel(Kv4Attention p) {
         __syncwarp();
       }
     }
-    if (*dead) {
+    if (__any_sync(0xffffffffu, *dead != 0)) {
       if (ptx::elect_one()) ptx::mma_commit(&sh.drain);
       __syncwarp();
       const long long t = clock64();
