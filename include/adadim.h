@@ -481,7 +481,7 @@ ADADIM_API int adadim_page_tables(const int32_t* past, const int32_t* fresh, int
  * a' = a cos - b sin, b' = b cos + a sin, with (a, b) channels (j, j + dim / 2), or (2 j, 2 j + 1) where `adjacent`.
  * Channels from dim on stay as they are.  One axis for text, three for images and video (time, row, column).
  *   positions  int32 [axes][ld];  freq  double [dim / 2];  axis  uint8 [dim / 2], values below axes (others
- *              count as axes - 1), NULL: all 0;  dim a multiple of 16, up to head_dim
+ *              count as axes - 1), NULL: all 0;  dim a multiple of 8, 8 .. head_dim
  */
 typedef struct {
   const int32_t* positions;

@@ -825,12 +825,12 @@ class Kv4Cache:
 class Rotary:
     """Rotary positions: pair j of a head turns by position * freq[j] on axis axis[j] (None: one axis).  freq [dim / 2] in
     radians a position (kept in binary64), axis [dim / 2] whole numbers; the pair is channels (j, j + dim / 2), or (2 j, 2 j + 1)
-    where `adjacent`.  dim is a multiple of 16; further channels of a head are not turned.  freq and axis may be replaced by
+    where `adjacent`.  dim is a multiple of 8; further channels of a head are not turned.  freq and axis may be replaced by
     others of the same length; their values are copied."""
 
     def __init__(self, freq: torch.Tensor, axis: Optional[torch.Tensor] = None, adjacent: bool = False):
-        if freq.dim() != 1 or freq.numel() % 8 or not 8 <= freq.numel() <= 128 or not freq.is_cuda:
-            raise ValueError("Rotary: freq [dim / 2] on the device, dim a multiple of 16 up to 256")
+        if freq.dim() != 1 or freq.numel() % 4 or not 4 <= freq.numel() <= 128 or not freq.is_cuda:
+            raise ValueError("Rotary: freq [dim / 2] on the device, dim a multiple of 8 up to 256")
         self.dim, self.adjacent, self.dev = 2 * freq.numel(), bool(adjacent), freq.get_device()
         self.freq, self.axis = freq, axis
 

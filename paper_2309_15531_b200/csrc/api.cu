@@ -600,7 +600,7 @@ int adadim_kv4_append(const adadim_heads* heads, int q_heads, int dtype, int64_t
   if ((heads[4].p != nullptr || heads[5].p != nullptr) && vdtype != ADADIM_F32 && vdtype != ADADIM_BF16) return ADADIM_ERR_DTYPE;
   if (n_tokens < 0 || n_tokens > kInt32Max || q_heads < 0 || q_heads > (1 << 16)) return ADADIM_ERR_SHAPE;
   if (rotary != nullptr) {
-    if (rotary->axes < 1 || rotary->dim < 16 || rotary->dim > cache->head_dim || rotary->dim % 16 != 0) return ADADIM_ERR_PARAM;
+    if (rotary->axes < 1 || rotary->dim < 8 || rotary->dim > cache->head_dim || rotary->dim % 8 != 0) return ADADIM_ERR_PARAM;
     if (n_tokens > 0 && (rotary->positions == nullptr || rotary->freq == nullptr)) return ADADIM_ERR_NULL;
     if (rotary->axes > 1 && rotary->axis == nullptr) return ADADIM_ERR_NULL;
   }

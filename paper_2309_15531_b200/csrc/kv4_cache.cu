@@ -254,7 +254,9 @@ __device__ __forceinline__ uint32_t quantize_exact(const double (&z)[8], uint64_
   return codes;
 }
 
-template <typename T, typename V>
+// ODD: a half of the rotated part is an odd number of fours of channels, so that an eight may lie in both halves and
+// its partners are loaded one by one.
+template <typename T, typename V, bool ODD>
 __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams p) {
   __shared__ double turns_c[kMostTokens][kMaxPairs], turns_s[kMostTokens][kMaxPairs];
   __shared__ float2 turns[kMostTokens][kMaxPairs];
@@ -307,6 +309,14 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
               const double c = turn_c[(c0 + k) >> 1], sn = turn_s[(c0 + k) >> 1], a = x[k], b = x[k + 1];
               z[k] = a * c - b * sn;
               z[k + 1] = b * c + a * sn;
+            }
+          } else if constexpr (ODD) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const bool second = c0 + k >= half;
+              const int j = second ? c0 + k - half : c0 + k;
+              const double c = turn_c[j], sn = second ? turn_s[j] : -turn_s[j];
+              z[k] = static_cast<double>(x[k]) * c + static_cast<double>(widened(row[second ? j : j + half])) * sn;
             }
           } else {
             const bool second = c0 >= half;
@@ -368,7 +378,21 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
           for (int k = 0; k < 8; k += 2) turn_query<T>(a[k], a[k + 1], (c0 + k) >> 1, turn, turn_c, turn_s);
         }
         store_chunk(out + c0, p.wide_qr, a);
-      } else if (chunk * 8 < half) {
+      } else if (ODD && chunk * 8 < half) {                        // pairs whose second channels lie at odd fours; four of them at the end
+        const int j0 = chunk * 8, n = min(8, half - j0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          a[k] = k < n ? widened(row[j0 + k]) : 0.0f;
+          b[k] = k < n ? widened(row[j0 + half + k]) : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (k >= n) continue;
+          turn_query<T>(a[k], b[k], j0 + k, turn, turn_c, turn_s);
+          out[j0 + k] = narrowed<T>(a[k]);
+          out[j0 + half + k] = narrowed<T>(b[k]);
+        }
+      } else if (!ODD && chunk * 8 < half) {
         const int j0 = chunk * 8;
         load_chunk(row + j0, p.wide_q, a);
         load_chunk(row + j0 + half, p.wide_q, b);
@@ -377,7 +401,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(AppendParams
         store_chunk(out + j0, p.wide_qr, a);
         store_chunk(out + j0 + half, p.wide_qr, b);
       } else {
-        const int c0 = chunk * 8 + half;                             // behind the rotated channels
+        const int c0 = chunk * 8 + (ODD ? half - 4 : half);          // behind the rotated channels
         load_chunk(row + c0, p.wide_q, a);
         store_chunk(out + c0, p.wide_qr, a);
       }
@@ -392,8 +416,11 @@ int wide_heads(const Kv4Heads& h, int64_t esz) {
 
 template <typename T>
 int append_types(const AppendParams& p, int vdtype, dim3 grid, cudaStream_t st) {
-  if (vdtype == ADADIM_F32) kv4_append_kernel<T, float><<<grid, kAppendThreads, 0, st>>>(p);
-  else kv4_append_kernel<T, __nv_bfloat16><<<grid, kAppendThreads, 0, st>>>(p);
+  const bool odd = !p.rotary.adjacent && p.rotary.dim % 16 != 0;
+  if (vdtype == ADADIM_F32 && odd) kv4_append_kernel<T, float, true><<<grid, kAppendThreads, 0, st>>>(p);
+  else if (vdtype == ADADIM_F32) kv4_append_kernel<T, float, false><<<grid, kAppendThreads, 0, st>>>(p);
+  else if (odd) kv4_append_kernel<T, __nv_bfloat16, true><<<grid, kAppendThreads, 0, st>>>(p);
+  else kv4_append_kernel<T, __nv_bfloat16, false><<<grid, kAppendThreads, 0, st>>>(p);
   return cudaGetLastError() == cudaSuccess ? ADADIM_OK : ADADIM_ERR_CUDA;
 }
 
@@ -432,7 +459,7 @@ int kv4_append_launch(const Kv4Heads& q, const Kv4Heads& qr, int q_heads, const 
   p.wide_v = wide_heads(v, esz);
   p.wide_kv = wide_heads(k_values, vsz);
   p.wide_vv = wide_heads(v_values, vsz);
-  p.q_chunks = rotary.adjacent ? cache.dim / 8 : rotary.dim / 16 + (cache.dim - rotary.dim) / 8;
+  p.q_chunks = rotary.adjacent ? cache.dim / 8 : (rotary.dim + 15) / 16 + (cache.dim - rotary.dim) / 8;
   const int64_t tasks = static_cast<int64_t>(cache.kv_heads) * (cache.held / 8) * 2 + static_cast<int64_t>(q_heads) * p.q_chunks;
   p.q_rcp = static_cast<uint32_t>((uint64_t{1} << 32) / p.q_chunks + 1);
   p.chunk_log2 = kv4::log2_of(cache.held / 8);
