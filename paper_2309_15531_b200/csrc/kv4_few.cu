@@ -22,7 +22,7 @@
 //
 // 64 requests of up to 16384 tokens, 8 key heads of 128 channels with 8 query heads each: 141 us in replays of a graph, 649 MB, 4.6 TB/s, 0.70 of
 // a copy's rate (passes launched one after another 145 to 155 us, 0.64 to 0.68); two thirds of the issue slots are taken, half of the ALU's, and
-// a CTA's last piece and the join come on top.  One token over 4096: 11.4 us.
+// a CTA's last piece and the join come on top.  One token over 4096: 11.3 us.
 #include "kv4_line.cuh"
 
 namespace adadim {
